@@ -5,3 +5,4 @@ include/mlkv_gpu.h); this package is its thin binding.
 """
 from ._lib import STALENESS_ASYNC, load  # noqa: F401
 from .store import EmbeddingStore, MLKVError  # noqa: F401
+from . import dense  # noqa: F401

@@ -1,4 +1,4 @@
-"""ctypes binding of libmlkv_gb300.so (the C ABI of include/mlkv_gpu.h).
+"""ctypes binding of libmlkv_gb300.so (the C ABI of include/mlkv_gpu.h and include/mlkv_dense.h).
 
 Argument marshalling only: every step of the store runs in the CUDA library.
 PyTorch supplies device memory and the current stream.  There is no fallback:
@@ -52,6 +52,22 @@ FAULT_COPY = 2
 FAULT_WAIT = 3
 STATIC_MAX_KEYS = 65536
 
+# include/mlkv_dense.h
+TYPE_FLOAT = 0
+TYPE_BFLOAT = 1
+TYPE_HALF = 2
+ACT_NONE = 0
+ACT_RELU = 1
+ACT_GELU_TANH = 2
+ACT_SILU = 3
+MAX_TOP = 32
+
+EXPORTED_DENSE = [
+    "mlkv_layer_norm", "mlkv_layer_norm_backward_workspace", "mlkv_layer_norm_backward", "mlkv_linear_workspace",
+    "mlkv_linear_backward_workspace", "mlkv_linear", "mlkv_linear_backward", "mlkv_dense_sync",
+    "mlkv_token_logprobs_workspace", "mlkv_token_logprobs", "mlkv_token_logprobs_backward",
+]
+
 
 class Config(ctypes.Structure):
     _fields_ = [
@@ -69,6 +85,36 @@ class Config(ctypes.Structure):
         ("hbm_cache_rows", ctypes.c_int64),
         ("flags", ctypes.c_uint32),
         ("reserved", ctypes.c_uint32),
+    ]
+
+
+class LinearArgs(ctypes.Structure):
+    _fields_ = [
+        ("m", ctypes.c_int64),
+        ("n", ctypes.c_int64),
+        ("k", ctypes.c_int64),
+        ("d_x", ctypes.c_void_p),
+        ("x_stride", ctypes.c_int64),
+        ("d_weight", ctypes.c_void_p),
+        ("weight_stride", ctypes.c_int64),
+        ("d_bias", ctypes.c_void_p),
+        ("d_residual", ctypes.c_void_p),
+        ("residual_stride", ctypes.c_int64),
+        ("d_y", ctypes.c_void_p),
+        ("y_stride", ctypes.c_int64),
+        ("d_pre", ctypes.c_void_p),
+        ("pre_stride", ctypes.c_int64),
+        ("d_dy", ctypes.c_void_p),
+        ("dy_stride", ctypes.c_int64),
+        ("d_dx", ctypes.c_void_p),
+        ("dx_stride", ctypes.c_int64),
+        ("d_dweight", ctypes.c_void_p),
+        ("dweight_stride", ctypes.c_int64),
+        ("d_dbias", ctypes.c_void_p),
+        ("d_workspace", ctypes.c_void_p),
+        ("workspace_bytes", ctypes.c_int64),
+        ("type", ctypes.c_int32),
+        ("activation", ctypes.c_int32),
     ]
 
 
@@ -115,6 +161,20 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.mlkv_last_error.restype = ctypes.c_char_p
     lib.mlkv_status_string.argtypes = [i32]
     lib.mlkv_status_string.restype = ctypes.c_char_p
+    f32 = ctypes.c_float
+    lib.mlkv_layer_norm.argtypes = [vp, i64, i32, i64, i64, vp, vp, i32, f32, vp, i64, i32, vp, vp]
+    lib.mlkv_layer_norm_backward_workspace.argtypes = [i64, i64]
+    lib.mlkv_layer_norm_backward.argtypes = [vp, i64, i32, vp, i64, i32, i64, i64, vp, i32, vp, vp, i64, vp, vp, vp, i64, vp]
+    lib.mlkv_linear_workspace.argtypes = [ctypes.POINTER(LinearArgs)]
+    lib.mlkv_linear_backward_workspace.argtypes = [ctypes.POINTER(LinearArgs)]
+    lib.mlkv_linear.argtypes = [ctypes.POINTER(LinearArgs), vp]
+    lib.mlkv_linear_backward.argtypes = [ctypes.POINTER(LinearArgs), vp]
+    lib.mlkv_dense_sync.argtypes = [vp]
+    lib.mlkv_token_logprobs_workspace.argtypes = [i64, i64, i32, i32]
+    lib.mlkv_token_logprobs.argtypes = [vp, i64, i32, i64, i64, vp, f32, i32, vp, vp, vp, vp, vp, vp, i64, vp]
+    lib.mlkv_token_logprobs_backward.argtypes = [vp, i64, i32, i64, i64, vp, f32, vp, vp, vp, vp, vp, i64, vp]
+    for name in EXPORTED_DENSE:
+        getattr(lib, name).restype = i64 if name.endswith("_workspace") else i32
     for name in ("mlkv_open", "mlkv_close", "mlkv_get", "mlkv_put", "mlkv_insert", "mlkv_apply_grad",
                  "mlkv_lookahead", "mlkv_find", "mlkv_export", "mlkv_dedup", "mlkv_get_host",
                  "mlkv_apply_grad_host", "mlkv_sync", "mlkv_clear_status", "mlkv_time_kernel",

@@ -1,9 +1,11 @@
 """Builds libmlkv_gb300.so in-tree with nvcc for sm_103a.
 
 Each .cu is compiled in parallel to an object, then linked into one shared
-library that exports the C ABI of include/mlkv_gpu.h.  No fast-math: every
-floating-point operation of the kernels is an explicitly rounded intrinsic,
-and --fmad=false keeps the compiler from contracting any other.
+library that exports the C ABI of include/mlkv_gpu.h and include/mlkv_dense.h.
+No fast-math: every floating-point operation of the store's kernels is an
+explicitly rounded intrinsic, and --fmad=false keeps the compiler from
+contracting any other.  The dense operators are held to a tolerance, not to an
+order of operations, and may contract.
 """
 import concurrent.futures as cf
 import os
@@ -17,8 +19,9 @@ ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libmlkv_gb300.so")
 BUILD = os.path.join(ROOT, "_build")
 SOURCES = ["mlkv_index.cu", "mlkv_sort.cu", "mlkv_apply.cu", "mlkv_plan.cu", "mlkv_table.cu", "mlkv_tier.cu", "mlkv_static.cu"]
+DENSE = ["dense_norm.cu", "dense_norm_backward.cu", "dense_linear.cu", "dense_logprobs.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
-FLAGS = ["-O3", "-std=c++17", "-lineinfo", "--fmad=false", "-Xcompiler", "-fPIC",
+FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC",
          "-Xcompiler", "-ffp-contract=off", f"-I{os.path.join(ROOT, 'include')}"]
 
 
@@ -31,7 +34,7 @@ def nvcc() -> str:
 
 def _deps():
     files = [os.path.join(CSRC, f) for f in os.listdir(CSRC)]
-    files.append(os.path.join(ROOT, "include", "mlkv_gpu.h"))
+    files += [os.path.join(ROOT, "include", f) for f in ("mlkv_gpu.h", "mlkv_dense.h")]
     files.append(os.path.abspath(__file__))
     return files
 
@@ -55,7 +58,8 @@ def build(force: bool = False, verbose: bool = False, extra=()) -> str:
 
     def compile_one(src):
         obj = os.path.join(BUILD, src.replace(".cu", ".o"))
-        cmd = [cc, *ARCH, *FLAGS, *extra, "-c", os.path.join(CSRC, src), "-o", obj]
+        exact = [] if src in DENSE else ["--fmad=false"]
+        cmd = [cc, *ARCH, *FLAGS, *exact, *extra, "-c", os.path.join(CSRC, src), "-o", obj]
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode != 0:
             raise RuntimeError(f"nvcc failed on {src}:\n{r.stderr}")
@@ -63,8 +67,8 @@ def build(force: bool = False, verbose: bool = False, extra=()) -> str:
             sys.stderr.write(r.stderr)
         return obj
 
-    with cf.ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
-        objs = list(ex.map(compile_one, SOURCES))
+    with cf.ThreadPoolExecutor(max_workers=len(SOURCES) + len(DENSE)) as ex:
+        objs = list(ex.map(compile_one, [*DENSE, *SOURCES]))
     tmp = LIB + f".tmp{os.getpid()}"
     r = subprocess.run([cc, *ARCH, "-shared", "-o", tmp, *objs], capture_output=True, text=True)
     if r.returncode != 0:
