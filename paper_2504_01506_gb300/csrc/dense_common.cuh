@@ -7,6 +7,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "../../include/mlkv_dense.h"
 #include "mlkv_internal.cuh"
 
@@ -33,12 +35,45 @@ namespace mlkv {
 inline bool dense_type_ok(int32_t type) { return type >= MLKV_TYPE_FLOAT && type <= MLKV_TYPE_HALF; }
 inline int dense_type_size(int32_t type) { return type == MLKV_TYPE_FLOAT ? 4 : 2; }
 
-// SMs of the current device (0: the call failed).
+// Most dynamic shared memory that any kernel here asks for (of 227 KB, less what they declare).
+constexpr int kDenseSmem = 216 << 10;
+
+// SMs of the current device (0: the call failed); asked once per device.
 inline int dense_sms() {
+    constexpr int kDevices = 64;
+    static std::atomic<int> known[kDevices];
     int dev = 0, sms = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kDevices) return 0;
+    if ((sms = known[dev].load(std::memory_order_relaxed)) != 0) return sms;
     if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+    known[dev].store(sms, std::memory_order_relaxed);
     return sms;
+}
+
+// Room for `bytes` of dynamic shared memory, asked for once per kernel and device.
+template <class K>
+inline bool dense_smem(K* kernel, size_t bytes) {
+    if (bytes <= 32 << 10) return true;  // (what the kernel declares itself counts towards the 48 KB too)
+    constexpr int kDevices = 64, kKernels = 256;
+    static std::atomic<const void*> known[kDevices][kKernels];
+    const void* id = reinterpret_cast<const void*>(kernel);
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kDevices) return false;
+    for (int i = 0; i < kKernels; ++i) {
+        const void* k = known[dev][i].load(std::memory_order_acquire);
+        if (k == id) return true;
+        if (k) continue;
+        // (whatever a launch may ask for, at once: a later one may ask for more)
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kDenseSmem) != cudaSuccess) return false;
+        known[dev][i].compare_exchange_strong(k, id);
+        return true;
+    }
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kDenseSmem) == cudaSuccess;
+}
+
+// Working memory as the calls take it.
+inline bool workspace_ok(const void* p, int64_t given, int64_t need) {
+    return need == 0 || (p && given >= need && reinterpret_cast<uintptr_t>(p) % 256 == 0);
 }
 
 // V consecutive elements of T, moved by one load or store of V * sizeof(T) bytes.
@@ -68,6 +103,42 @@ __device__ __forceinline__ void store_as(void* p, int32_t type, int64_t i, float
     else static_cast<__half*>(p)[i] = __float2half_rn(x);
 }
 
+// Two 16-bit values in a word.
+template <class T> __device__ __forceinline__ float2 pair_of_word(uint32_t w);
+template <> __device__ __forceinline__ float2 pair_of_word<__nv_bfloat16>(uint32_t w) {
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+}
+template <> __device__ __forceinline__ float2 pair_of_word<__half>(uint32_t w) {
+    return __half22float2(*reinterpret_cast<__half2*>(&w));
+}
+template <class T> __device__ __forceinline__ uint32_t word_of_pair(float2 x);
+template <> __device__ __forceinline__ uint32_t word_of_pair<__nv_bfloat16>(float2 x) {
+    const __nv_bfloat162 r = __float22bfloat162_rn(x);
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+template <> __device__ __forceinline__ uint32_t word_of_pair<__half>(float2 x) {
+    const __half2 r = __float22half2_rn(x);
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+
+// Two fp32 operations at once.
+__device__ __forceinline__ uint64_t as_x2(float2 v) { return *reinterpret_cast<uint64_t*>(&v); }
+__device__ __forceinline__ float2 of_x2(uint64_t v) { return *reinterpret_cast<float2*>(&v); }
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(as_x2(a)), "l"(as_x2(b)));
+    return of_x2(r);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(as_x2(a)), "l"(as_x2(b)));
+    return of_x2(r);
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(as_x2(a)), "l"(as_x2(b)), "l"(as_x2(c)));
+    return of_x2(r);
+}
 // Sum over groups of G lanes (a power of two): every lane gets its group's.
 __device__ __forceinline__ float group_sum(float x, int G) {
     for (int o = G >> 1; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);

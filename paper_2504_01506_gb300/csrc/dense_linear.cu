@@ -582,7 +582,7 @@ int64_t working_memory(const mlkv_linear_args* g, bool backward) {
 int run_linear(const mlkv_linear_args* g, bool backward, void* stream) {
     const int64_t need = working_memory(g, backward);
     if (need < 0) return need == -2 ? MLKV_ERR_UNSUPPORTED : MLKV_ERR_CUDA;
-    if (need > 0 && (!g->d_workspace || g->workspace_bytes < need || reinterpret_cast<uintptr_t>(g->d_workspace) % kAlign)) return MLKV_ERR_INVALID;
+    if (!workspace_ok(g->d_workspace, g->workspace_bytes, need)) return MLKV_ERR_INVALID;
     Caller c = {(cudaStream_t)stream, dense_sms(), true, g->type, {static_cast<char*>(g->d_workspace)}};
     if (backward) c.backward(*g);
     else c.forward(*g);

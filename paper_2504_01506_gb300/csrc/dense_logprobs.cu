@@ -7,12 +7,23 @@
 //   dx_i = c (g [i = t] - p_i (g + h (log p_i + H)))      (g, h: gradients of log p_t and H)
 //
 // Bound by HBM: the logits are read once (the backward pass reads and writes
-// them once).  A block holds a chunk of a row in registers, finds its maximum,
-// then its sums; a row of several chunks is joined by a second kernel.  The
-// alternatives come out of the same registers: the k-th largest of the maxima
-// of 32 disjoint parts of the chunk is at most the chunk's k-th largest value,
-// and few other values reach it (about 30 for k = 20 where order and value have
-// nothing to do with each other), so only those are sorted.
+// them once).  A block streams a row, or a span of one where rows are few (a
+// second kernel joins the spans).  At 16 bits the stream is as near to the rate
+// of instructions as to that of memory, so it is kept short: every thread has
+// sums of its own against a reference of its own, which it moves only when a
+// value is 2^8 above it (nothing is rescaled, no barrier), and the exponent is
+// one fused multiply-add, c x - reference.  Values that far below that their
+// exponential is 0 are raised to a floor first, so that -inf times 0 cannot be.
+//
+// The alternatives come out of the same stream.  Every thread knows the largest
+// value it has seen, and in which batch first.  Of 32 disjoint parts of the
+// block, take the k-th largest of the parts' largest values: a thread's batch
+// whose largest value is below this bar holds none of the k best (nor one that
+// equals it, in a later batch than those k).  The few batches that reach the bar
+// (of a thread: about 30 while the values seen double, for k = 20) are listed in
+// shared memory; at the end the block reads them again and sorts what of them
+// reaches the last bar.  The bar is raised after 1, 3, 5, 9, 17 ... batches, by one
+// warp and without a barrier but for the first time.
 #include <math_constants.h>
 
 #include <algorithm>
@@ -25,7 +36,10 @@ using namespace mlkv;
 namespace {
 
 constexpr int kMostThreads = 256;
-constexpr int kCandidates = 512;       // values a chunk's alternatives are sorted from
+constexpr int kBatch = 4;              // 16-byte pieces a thread works on at a time ...
+constexpr int kStages = 2;             // ... of a ring of so many batches
+constexpr int kMostSpans = 64;         // of a row
+constexpr int kListed = 8;             // batches, of a thread each, that the list has room for: so many a thread
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kLeast = -200.f;       // 2^kLeast is 0 in fp32: what lies below (-inf too) need not be told apart
 
@@ -34,14 +48,14 @@ struct ProbArgs {
     int64_t stride, n;
     const int64_t* targets;
     float scale;
-    int32_t vocab, top, chunks, per_chunk;  // 16-byte pieces of a chunk
+    int32_t vocab, top, spans, per_span;  // 16-byte pieces of a span
     float* logprob;
     float* entropy;
     float* stats;
     float* top_logprobs;
     int64_t* top_ids;
-    float4* part;                // [n][chunks]: m, S, P of each chunk
-    unsigned long long* keys;    // [n][chunks][top]
+    float4* part;                // [n][spans]: m, S, P of each
+    unsigned long long* keys;    // [n][spans][top]
 };
 
 // A 16-byte piece of a row, which holds N values.
@@ -58,9 +72,17 @@ template <> struct Piece<float> {
         asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
         return r;
     }
-    static __device__ __forceinline__ float most(const uint4& q) {
-        return max2(max2(__uint_as_float(q.x), __uint_as_float(q.y)), max2(__uint_as_float(q.z), __uint_as_float(q.w)));
+    template <int B> static __device__ __forceinline__ float most(const uint4 (&q)[B]) {
+        float m = __uint_as_float(q[0].x);
+#pragma unroll
+        for (int i = 0; i < B; ++i) m = max2(max2(max2(m, __uint_as_float(q[i].x)), max2(__uint_as_float(q[i].y), __uint_as_float(q[i].z))), __uint_as_float(q[i].w));
+        return m;
     }
+    // The floor, as the exponent has it.
+    struct Floor {};
+    static __device__ __forceinline__ Floor floor_of(float, float) { return {}; }
+    static __device__ __forceinline__ float2 raised(const uint4& q, int i, Floor) { return pair(q, i); }
+    static __device__ __forceinline__ float2 clamp(float2 d) { return make_float2(fmaxf(d.x, kLeast), fmaxf(d.y, kLeast)); }
 };
 template <> struct Piece<__nv_bfloat16> {
     static constexpr int N = 8;
@@ -71,10 +93,25 @@ template <> struct Piece<__nv_bfloat16> {
         return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
     }
     static __device__ __forceinline__ __nv_bfloat162 as2(uint32_t w) { return *reinterpret_cast<__nv_bfloat162*>(&w); }
-    static __device__ __forceinline__ float most(const uint4& q) {
-        const __nv_bfloat162 m = __hmax2_nan(__hmax2_nan(as2(q.x), as2(q.y)), __hmax2_nan(as2(q.z), as2(q.w)));
+    template <int B> static __device__ __forceinline__ float most(const uint4 (&q)[B]) {
+        __nv_bfloat162 m = as2(q[0].x);
+#pragma unroll
+        for (int i = 0; i < B; ++i) m = __hmax2_nan(__hmax2_nan(__hmax2_nan(m, as2(q[i].x)), __hmax2_nan(as2(q[i].y), as2(q[i].z))), as2(q[i].w));
         return __bfloat162float(__hmax_nan(m.x, m.y));
     }
+    // The floor, on the values themselves, two at a time: so far below `at` that the exponential is 0, whatever
+    // bf16 makes of it (its range is fp32's, so there is such a value).
+    using Floor = __nv_bfloat162;
+    static __device__ __forceinline__ Floor floor_of(float at, float c) {
+        const __nv_bfloat16 v = __float2bfloat16_rd(at - fmaxf(-kLeast / c, fabsf(at) * 0x1p-6f));
+        return __nv_bfloat162(v, v);
+    }
+    static __device__ __forceinline__ float2 raised(const uint4& q, int i, Floor f) {
+        const __nv_bfloat162 v = __hmax2(as2(word(q, i)), f);
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(&v);
+        return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+    }
+    static __device__ __forceinline__ float2 clamp(float2 d) { return d; }
 };
 template <> struct Piece<__half> {
     static constexpr int N = 8;
@@ -82,36 +119,29 @@ template <> struct Piece<__half> {
     static __device__ __forceinline__ uint32_t word(const uint4& q, int i) { return i == 0 ? q.x : i == 1 ? q.y : i == 2 ? q.z : q.w; }
     static __device__ __forceinline__ __half2 as2(uint32_t w) { return *reinterpret_cast<__half2*>(&w); }
     static __device__ __forceinline__ float2 pair(const uint4& q, int i) { return __half22float2(as2(word(q, i))); }
-    static __device__ __forceinline__ float most(const uint4& q) {
-        const __half2 m = __hmax2_nan(__hmax2_nan(as2(q.x), as2(q.y)), __hmax2_nan(as2(q.z), as2(q.w)));
+    template <int B> static __device__ __forceinline__ float most(const uint4 (&q)[B]) {
+        __half2 m = as2(q[0].x);
+#pragma unroll
+        for (int i = 0; i < B; ++i) m = __hmax2_nan(__hmax2_nan(__hmax2_nan(m, as2(q[i].x)), __hmax2_nan(as2(q[i].y), as2(q[i].z))), as2(q[i].w));
         return __half2float(__hmax_nan(m.x, m.y));
     }
+    // The floor, as the exponent has it (fp16 need not have a value that low).
+    struct Floor {};
+    static __device__ __forceinline__ Floor floor_of(float, float) { return {}; }
+    static __device__ __forceinline__ float2 raised(const uint4& q, int i, Floor) { return pair(q, i); }
+    static __device__ __forceinline__ float2 clamp(float2 d) { return make_float2(fmaxf(d.x, kLeast), fmaxf(d.y, kLeast)); }
 };
 
 __device__ __forceinline__ float max_nan(float a, float b) { return Piece<float>::max2(a, b); }
 
-// Two fp32 operations at once.
-__device__ __forceinline__ uint64_t as_x2(float2 v) { return *reinterpret_cast<uint64_t*>(&v); }
-__device__ __forceinline__ float2 of_x2(uint64_t v) { return *reinterpret_cast<float2*>(&v); }
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(as_x2(a)), "l"(as_x2(b)));
-    return of_x2(r);
-}
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(as_x2(a)), "l"(as_x2(b)));
-    return of_x2(r);
-}
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(as_x2(a)), "l"(as_x2(b)), "l"(as_x2(c)));
-    return of_x2(r);
-}
 __device__ __forceinline__ float exp2_fast(float x) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
+}
+
+__device__ __forceinline__ void copy_async16(void* to, const void* from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
 }
 
 // A row's values in 16-byte pieces: the first begins at or before the row's
@@ -166,7 +196,9 @@ __device__ __forceinline__ Key key_of(float x, int index) { return (Key)order_of
 // The 32 lanes' values in falling order (bitonic sort; `from` = 32: of a bitonic sequence).
 template <class K>
 __device__ __forceinline__ K sort_lanes(K x, int lane, int from = 2) {
+#pragma unroll 1
     for (int size = from; size <= 32; size <<= 1)
+#pragma unroll 1
         for (int o = size >> 1; o; o >>= 1) {
             const K y = __shfl_xor_sync(0xffffffffu, x, o);
             const bool want_max = ((lane & o) == 0) == ((lane & size) == 0 || size == 32);
@@ -176,16 +208,41 @@ __device__ __forceinline__ K sort_lanes(K x, int lane, int from = 2) {
 }
 // The 32 largest of `count` keys, lane i holding the i-th (the warp).
 __device__ __forceinline__ Key best_of(const Key* keys, int count, int lane) {
-    Key best = sort_lanes<Key>(lane < count ? keys[lane] : 0ull, lane);
-    for (int b = 32; b < count; b += 32) {
+    Key best = 0;
+    for (int b = 0; b < count; b += 32) {
         const Key k = sort_lanes<Key>(b + lane < count ? keys[b + lane] : 0ull, lane);
         const Key other = __shfl_sync(0xffffffffu, k, 31 - lane);
         best = sort_lanes<Key>(best > other ? best : other, lane, 32);
     }
     return best;
 }
+// Leaves the `top` best of list[0 .. count) in list[0 .. top), in order, 0 where
+// there are fewer (the block; keys are distinct).  Each warp cuts its share of a
+// long list to 32; what is left is placed by counting the better ones.
+template <int THREADS>
+__device__ __noinline__ void select(Key* list, int count, int top) {
+    constexpr int kWarps = THREADS / 32;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (count > THREADS) {
+        const int share = (count + kWarps - 1) / kWarps, from = warp * share;
+        const Key k = best_of(list + from, max(0, min(share, count - from)), lane);
+        __syncthreads();
+        list[threadIdx.x] = k;
+        count = THREADS;
+    }
+    __syncthreads();
+    const Key mine = (int)threadIdx.x < count ? list[threadIdx.x] : 0;
+    int rank = 0;
+#pragma unroll 4
+    for (int i = 0; i < count; ++i) rank += list[i] > mine;
+    __syncthreads();
+    if ((int)threadIdx.x < top) list[threadIdx.x] = 0;
+    __syncthreads();
+    if (mine && rank < top) list[rank] = mine;
+    __syncthreads();
+}
 
-// A row's results from its sums (the warp; lane i with its i-th alternative).
+// A row's results from its sums (a warp; lane i with its i-th alternative).
 template <class T>
 __device__ __forceinline__ void finish_row(const ProbArgs& a, int64_t r, float m, float s, float p, Key best, int lane) {
     const bool empty = m == -CUDART_INF_F, bad = isnan(m) || m == CUDART_INF_F;
@@ -209,98 +266,222 @@ __device__ __forceinline__ void finish_row(const ProbArgs& a, int64_t r, float m
     }
 }
 
-template <class T, int NV, bool TOP>
-__global__ void __launch_bounds__(kMostThreads) k_logprobs(ProbArgs a) {
+// Sums of what a thread has seen: s = sum 2^(c x - at), p = sum (c x - at) 2^(c x - at).
+struct Sums {
+    float at, s, p;
+    // Against a reference lower by d.
+    __device__ __forceinline__ void move(float to, float d) {
+        at = to;
+        if (s == 0.f) return;  // of nothing that counts
+        d = fmaxf(d, kLeast);
+        const float e = exp2f(d);
+        p = (p + d * s) * e;
+        s *= e;
+    }
+};
+// Whether c x - c max can be formed as c x - reference: neither overflows, and a
+// floor lies below the maximum.  (Not with a row of nothing but the lowest fp32.)
+__device__ __forceinline__ bool fused_ok(float most, float c) {
+    return most == -CUDART_INF_F || (fabsf(most) <= 1e30f && fabsf(most) * c <= 1e30f && c <= 1e30f && c >= 1e-30f);
+}
+
+template <class T, bool TOP, int THREADS>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprobs(ProbArgs a) {
     pdl_enter();
     using P = Piece<T>;
-    __shared__ float maxima[32];
-    __shared__ float2 sums[kMostThreads / 32];
-    __shared__ Key found[TOP ? kCandidates : 1];
-    __shared__ int count;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    const int64_t r = blockIdx.x / (unsigned)a.chunks;
-    const int chunk = (int)(blockIdx.x % (unsigned)a.chunks);
+    constexpr uint32_t f = P::kMinusInf;
+    constexpr int kWarps = THREADS / 32, kRoom = kListed * THREADS, kStep = kBatch * THREADS;
+    extern __shared__ __align__(16) uint8_t shared[];  // the ring; then [kRoom] listed batches
+    __shared__ float2 sums[kWarps];
+    __shared__ Key parts[32];        // the parts' largest values, with the batch that has it first
+    __shared__ volatile unsigned long long bar;  // (value, last batch), raised by one warp or another
+    __shared__ int count, values;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    uint4* ring = reinterpret_cast<uint4*>(shared) + threadIdx.x;  // (a thread reads what it copied itself)
+    int* listed = reinterpret_cast<int*>(shared + kStages * kStep * sizeof(uint4));
+    Key* list = reinterpret_cast<Key*>(shared);  // at the end, where the ring was
+    static_assert(kStages * kBatch * sizeof(uint4) >= (kListed + 2) * sizeof(Key), "the list fits the ring");
+    const int64_t r = blockIdx.x / (unsigned)a.spans;
+    const int span = (int)(blockIdx.x % (unsigned)a.spans);
     const RowPieces<T> row(a.x, r * a.stride, a.vocab);
-    const int p0 = chunk * a.per_chunk, p1 = min(row.count, p0 + a.per_chunk);
-    uint4 q[NV];
+    const int p0 = span * a.per_span, p1 = min(row.count, p0 + a.per_span);
+    const float c = a.scale * kLog2e;
+    const float2 c2 = make_float2(c, c);
+    auto fetch = [&](int base, int stage) {
+        uint4* to = ring + stage * kStep;
+        if (base > 0 && base + kStep <= min(p1, row.count - 1)) {
+            const uint4* from = reinterpret_cast<const uint4*>(row.first) + base + threadIdx.x;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int p = p0 + i * (int)blockDim.x + (int)threadIdx.x;
-        constexpr uint32_t f = P::kMinusInf;
-        q[i] = p < p1 ? row.load(p) : make_uint4(f, f, f, f);
-    }
-    if (TOP && threadIdx.x == 0) count = 0;
-    float m = P::most(q[0]);
-#pragma unroll
-    for (int i = 1; i < NV; ++i) m = max_nan(m, P::most(q[i]));
-    // the 32 parts' maxima: each that of as many lanes as there are warps
-    for (int o = warps >> 1; o; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
-    if (lane % warps == 0) maxima[warp * (32 / warps) + lane / warps] = m;
-    __syncthreads();
-    m = maxima[lane];
-    float least = 0.f;  // the smallest value that may be an alternative
-    if (TOP) {
-        const uint32_t sorted = sort_lanes<uint32_t>(order_of(m), lane);
-        m = value_of(__shfl_sync(0xffffffffu, sorted, 0));
-        least = value_of(__shfl_sync(0xffffffffu, sorted, a.top - 1));
-        least = fmaxf(least, -3.4028234663852886e38f);  // (also where it is NaN: -inf is no alternative)
-    } else {
-        for (int o = 16; o; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
-    }
-    const float base = m == -CUDART_INF_F ? 0.f : m, c = a.scale * kLog2e;
-    const float2 minus = make_float2(-base, -base), c2 = make_float2(c, c);
-    float2 s2 = make_float2(0.f, 0.f), t2 = make_float2(0.f, 0.f);
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-#pragma unroll
-        for (int k = 0; k < P::N / 2; ++k) {
-            float2 d = mul2(add2(P::pair(q[i], k), minus), c2);
-            d = make_float2(fmaxf(d.x, kLeast), fmaxf(d.y, kLeast));
-            const float2 e = make_float2(exp2_fast(d.x), exp2_fast(d.y));
-            s2 = add2(s2, e);
-            t2 = fma2(d, e, t2);
+            for (int i = 0; i < kBatch; ++i) copy_async16(to + i * THREADS, from + i * THREADS);
+        } else {
+#pragma unroll 1
+            for (int i = 0; i < kBatch; ++i) {
+                const int p = base + i * THREADS + (int)threadIdx.x;
+                if (p < p1 && row.whole(p)) copy_async16(to + i * THREADS, reinterpret_cast<const uint4*>(row.first) + p);
+                else to[i * THREADS] = p < p1 ? row.load(p) : make_uint4(f, f, f, f);
+            }
         }
-        if (TOP && P::most(q[i]) >= least) {
-            const int at = row.index(p0 + i * (int)blockDim.x + (int)threadIdx.x);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int i = 0; i < kStages - 1; ++i) fetch(p0 + i * kStep, i);
+    if (TOP && threadIdx.x == 0) {
+        count = values = 0;
+        bar = 0xFF7FFFFF7FFFFFFFull;  // everything
+    }
+    Sums sum = {0.f, 0.f, 0.f};
+    typename P::Floor floor = P::floor_of(0.f, c);
+    float most = -CUDART_INF_F;  // the largest value this thread has seen (NaN where there is one) ...
+    int first = 0;               // ... and the first batch that holds it
+    float least = 0.f;           // the bar: batches whose largest value is above this, or equal up to batch `last`
+    int last = 0;
+    auto tell = [&] {  // the best of this warp's parts
+        Key mine = most == -CUDART_INF_F ? 0ull : key_of(most, first);
+#pragma unroll
+        for (int o = kWarps >> 1; o; o >>= 1) {
+            const Key y = __shfl_xor_sync(0xffffffffu, mine, o);
+            mine = mine > y ? mine : y;
+        }
+        if (lane % kWarps == 0) *const_cast<volatile Key*>(&parts[warp * (32 / kWarps) + lane / kWarps]) = mine;
+    };
+    // The bar of what the parts have told (a warp): of the k-th largest value the last batch that has it.  What
+    // other warps have seen since, or tell meanwhile, makes the bar lower than it could be, and as good.
+    auto raise = [&] {
+        const Key mine = *const_cast<volatile Key*>(&parts[lane]);
+        const uint32_t value = (uint32_t)(mine >> 32);
+        int above = 0;
+#pragma unroll 8
+        for (int i = 0; i < 32; ++i) above += __shfl_sync(0xffffffffu, value, i) > value;
+        const uint32_t kth = __reduce_min_sync(0xffffffffu, above < a.top ? value : 0xFFFFFFFFu);
+        const uint32_t batch = __reduce_min_sync(0xffffffffu, value == kth ? (uint32_t)mine : 0xFFFFFFFFu);
+        least = kth ? value_of(kth) : -3.4028234663852886e38f;  // (0: fewer parts with a value than k)
+        last = kth ? (int)(0xFFFFFFFEu - batch) : 0x7FFFFFFF;
+        return __reduce_max_sync(0xffffffffu, value);
+    };
+    int batch = 0, stage = 0;
+    for (int base = p0; base < p1; base += kStep, ++batch) {
+        fetch(base + (kStages - 1) * kStep, stage == 0 ? kStages - 1 : stage - 1);
+        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+        uint4 q[kBatch];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) q[i] = ring[stage * kStep + i * THREADS];
+        stage = stage == kStages - 1 ? 0 : stage + 1;
+        const float now = P::most(q);
+        if (now > most) first = batch;
+        most = max_nan(most, now);
+        if (TOP) {
+            if ((batch & (batch - 1)) == 0) {
+                tell();
+                if (batch == 0) {
+                    __syncthreads();
+                    raise();
+                }
+            } else if ((batch & (batch - 2)) == 1 && warp == __popc(batch) % kWarps) {
+                raise();  // (a batch later, when the other warps have told too, as a rule)
+                if (lane == 0) bar = (unsigned long long)__float_as_uint(least) << 32 | (uint32_t)last;
+            } else {
+                const unsigned long long told = bar;
+                const float value = __uint_as_float((uint32_t)(told >> 32));
+                const int since = (int)(uint32_t)told;
+                if (value > least || (value == least && since < last)) least = value, last = since;
+            }
+            if (now >= least && (now > least || batch <= last)) {
+                const int to = atomicAdd(&count, 1);
+                if (to < kRoom) listed[to] = base + (int)threadIdx.x;
+            }
+        }
+        const float to = now * c;
+        if (to - sum.at > 8.f || (sum.s == 0.f && to > -1e30f)) {  // (what is lower counts nothing against 0 either)
+            sum.move(to, sum.at - to);
+            floor = P::floor_of(now, c);
+        }
+        const float2 minus = make_float2(-sum.at, -sum.at);
+        float2 s2 = make_float2(sum.s, 0.f), t2 = make_float2(sum.p, 0.f);
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i)
 #pragma unroll
             for (int k = 0; k < P::N / 2; ++k) {
-                const float2 x = P::pair(q[i], k);
-                if (x.x >= least) {
-                    const int to = atomicAdd(&count, 1);
-                    if (to < kCandidates) found[to] = key_of(x.x, at + 2 * k);
-                }
-                if (x.y >= least) {
-                    const int to = atomicAdd(&count, 1);
-                    if (to < kCandidates) found[to] = key_of(x.y, at + 2 * k + 1);
-                }
+                const float2 d = P::clamp(fma2(P::raised(q[i], k, floor), c2, minus));
+                const float2 e = make_float2(exp2_fast(d.x), exp2_fast(d.y));
+                s2 = add2(s2, e);
+                t2 = fma2(d, e, t2);
+            }
+        sum.s = s2.x + s2.y;
+        sum.p = t2.x + t2.y;
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    // the block's largest value, and its sums against it
+    tell();
+    __syncthreads();
+    {
+        const uint32_t top = TOP ? raise() : __reduce_max_sync(0xffffffffu, (uint32_t)(parts[lane] >> 32));
+        most = top ? value_of(top) : -CUDART_INF_F;
+    }
+    if (fused_ok(most, c)) {
+        sum.move(0.f, most == -CUDART_INF_F ? 0.f : fmaf(-most, c, sum.at));
+    } else {
+        sum.s = sum.p = 0.f;
+        for (int p = p0 + (int)threadIdx.x; p < p1; p += THREADS) {
+            const uint4 w = row.load(p);
+#pragma unroll 1
+            for (int e = 0; e < P::N / 2; ++e) {
+                const float2 x = P::pair(w, e);
+                const float d0 = fmaxf((x.x - most) * c, kLeast), d1 = fmaxf((x.y - most) * c, kLeast);
+                sum.s += exp2_fast(d0) + exp2_fast(d1);
+                sum.p += d0 * exp2_fast(d0) + d1 * exp2_fast(d1);
             }
         }
     }
-    float s = group_sum(s2.x + s2.y, 32), t = group_sum(t2.x + t2.y, 32);
+    const float s = group_sum(sum.s, 32), t = group_sum(sum.p, 32);
     if (lane == 0) sums[warp] = make_float2(s, t);
-    __syncthreads();
-    int n = 0;
     if (TOP) {
-        n = count;
-        // More values than there is room for reach the bound (equal ones, as a rule), or NaN is among them: the
-        // alternatives one by one.
-        if (n > kCandidates || isnan(m)) {
-            __syncthreads();
-            n = a.top;
-            Key mine = 0, last = ~0ull;
+        if (count <= kRoom && !isnan(most)) {
+            // the listed batches' pieces, a thread one at a time; what reaches the bar is cut to the k best when
+            // there is much of it
+            const int n = count * kBatch;
+            Key least_key = 0;
+            for (int i0 = 0; i0 < n; i0 += THREADS) {
+                const int i = i0 + (int)threadIdx.x, p = i < n ? listed[i / kBatch] + (i % kBatch) * THREADS : p1;
+                if (p < p1) {
+                    const int at = row.index(p);
+                    const uint4 w = row.load(p);
+#pragma unroll
+                    for (int e = 0; e < P::N; ++e) {
+                        const float2 two = P::pair(w, e / 2);
+                        const float x = e & 1 ? two.y : two.x;
+                        if (!(x >= least)) continue;
+                        const Key key = key_of(x, at + e);
+                        if (key > least_key) list[atomicAdd(&values, 1)] = key;
+                    }
+                }
+                __syncthreads();
+                const int have = values;
+                __syncthreads();
+                if (have > THREADS) {
+                    select<THREADS>(list, have, a.top);
+                    least_key = list[a.top - 1];
+                    if (threadIdx.x == 0) values = a.top;
+                    __syncthreads();
+                }
+            }
+            select<THREADS>(list, values, a.top);
+        } else {
+            // The list ran over, or NaN is among the values: one alternative after another, from the row itself.
+            Key mine = 0, below = ~0ull;
             bool look = true;
+            __syncthreads();
             for (int k = 0; k < a.top; ++k) {
                 if (look) {
                     mine = 0;
-#pragma unroll
-                    for (int i = 0; i < NV; ++i) {
-                        const int at = row.index(p0 + i * (int)blockDim.x + (int)threadIdx.x);
-#pragma unroll
+                    for (int p = p0 + (int)threadIdx.x; p < p1; p += THREADS) {
+                        const uint4 w = row.load(p);
+                        const int at = row.index(p);
+#pragma unroll 1
                         for (int e = 0; e < P::N / 2; ++e) {
-                            const float2 x = P::pair(q[i], e);
+                            const float2 x = P::pair(w, e);
                             const Key k0 = key_of(x.x, at + 2 * e), k1 = key_of(x.y, at + 2 * e + 1);
-                            if (x.x != -CUDART_INF_F && k0 < last && k0 > mine) mine = k0;
-                            if (x.y != -CUDART_INF_F && k1 < last && k1 > mine) mine = k1;
+                            if (x.x != -CUDART_INF_F && k0 < below && k0 > mine) mine = k0;
+                            if (x.y != -CUDART_INF_F && k1 < below && k1 > mine) mine = k1;
                         }
                     }
                 }
@@ -309,56 +490,77 @@ __global__ void __launch_bounds__(kMostThreads) k_logprobs(ProbArgs a) {
                     const Key y = __shfl_xor_sync(0xffffffffu, b, o);
                     b = b > y ? b : y;
                 }
-                if (lane == 0) found[32 + 8 * (k & 1) + warp] = b;
+                if (lane == 0) parts[8 * (k & 1) + warp] = b;
                 __syncthreads();
-                for (int w = 0; w < warps; ++w) {
-                    const Key y = found[32 + 8 * (k & 1) + w];
+                for (int w = 0; w < kWarps; ++w) {
+                    const Key y = parts[8 * (k & 1) + w];
                     b = b > y ? b : y;
                 }
-                if (threadIdx.x == 0) found[k] = b;
+                if (threadIdx.x == 0) list[k] = b;
                 look = b == mine;
-                last = b;
+                below = b;
             }
             __syncthreads();
         }
+    } else {
+        __syncthreads();
     }
     if (warp != 0) return;
-    const float2 w = lane < warps ? sums[lane] : make_float2(0.f, 0.f);
-    s = group_sum(w.x, 32);
-    t = group_sum(w.y, 32);
-    const Key best = TOP ? best_of(found, n, lane) : 0ull;
-    if (a.chunks == 1) {
-        finish_row<T>(a, r, m, s, t, best, lane);
+    const float2 w = lane < kWarps ? sums[lane] : make_float2(0.f, 0.f);
+    sum.s = group_sum(w.x, 32);
+    sum.p = group_sum(w.y, 32);
+    const Key mine = TOP && lane < a.top ? list[lane] : 0ull;
+    if (a.spans == 1) {
+        finish_row<T>(a, r, most, sum.s, sum.p, mine, lane);
         return;
     }
-    if (lane == 0) a.part[blockIdx.x] = make_float4(m, s, t, 0.f);
-    if (TOP && lane < a.top) a.keys[(int64_t)blockIdx.x * a.top + lane] = best;
+    if (lane == 0) a.part[blockIdx.x] = make_float4(most, sum.s, sum.p, 0.f);
+    if (TOP && lane < a.top) a.keys[(int64_t)blockIdx.x * a.top + lane] = mine;
 }
 
-// A row's chunks joined (a warp a row).
+// A row's spans joined (a block a row).
 template <class T>
-__global__ void __launch_bounds__(128) k_logprobs_join(ProbArgs a) {
+__global__ void __launch_bounds__(kMostThreads) k_logprobs_join(ProbArgs a) {
     pdl_enter();
-    const int lane = threadIdx.x & 31;
-    const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-    if (r >= a.n) return;
-    const float4* part = a.part + r * a.chunks;
+    __shared__ Key list[kMostSpans * MLKV_MAX_TOP];
+    __shared__ Key bars[kMostThreads / 32];
+    __shared__ int count;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t r = blockIdx.x;
+    const float4* part = a.part + r * a.spans;
+    if (a.top) {
+        // no alternative is below any span's last, and few others are not
+        const Key* keys = a.keys + r * a.spans * a.top;
+        Key bar = 0;
+        for (int i = threadIdx.x; i < a.spans; i += kMostThreads) bar = max(bar, keys[i * a.top + a.top - 1]);
+        for (int o = 16; o; o >>= 1) bar = max(bar, __shfl_xor_sync(0xffffffffu, bar, o));
+        if (lane == 0) bars[warp] = bar;
+        if (threadIdx.x == 0) count = 0;
+        __syncthreads();
+        for (int w = 0; w < kMostThreads / 32; ++w) bar = max(bar, bars[w]);
+        for (int i = threadIdx.x; i < a.spans * a.top; i += kMostThreads) {
+            const Key k = keys[i];
+            if (k && k >= bar) list[atomicAdd(&count, 1)] = k;
+        }
+        __syncthreads();
+        select<kMostThreads>(list, count, a.top);
+    }
+    if (warp != 0) return;
     const float c = a.scale * kLog2e;
     float m = -CUDART_INF_F;
-    for (int i = lane; i < a.chunks; i += 32) m = max_nan(m, part[i].x);
+    for (int i = lane; i < a.spans; i += 32) m = max_nan(m, part[i].x);
     for (int o = 16; o; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
     float s = 0.f, t = 0.f;
-    for (int i = lane; i < a.chunks; i += 32) {
+    for (int i = lane; i < a.spans; i += 32) {
         const float4 q = part[i];
-        if (q.x == -CUDART_INF_F) continue;  // (its sums are of nothing)
-        const float d = fmaxf((q.x - m) * c, kLeast), e = exp2f(d);
-        s += q.y * e;
-        t += (q.z + d * q.y) * e;
+        Sums one = {0.f, q.y, q.z};
+        if (q.x != -CUDART_INF_F) one.move(0.f, (q.x - m) * c);
+        s += one.s;
+        t += one.p;
     }
     s = group_sum(s, 32);
     t = group_sum(t, 32);
-    const Key best = a.top ? best_of(a.keys + r * a.chunks * a.top, a.chunks * a.top, lane) : 0ull;
-    finish_row<T>(a, r, m, s, t, best, lane);
+    finish_row<T>(a, r, m, s, t, a.top && lane < a.top ? list[lane] : 0ull, lane);
 }
 
 struct GradArgs {
@@ -382,7 +584,7 @@ __device__ __forceinline__ uint32_t pack2(float2 v) {
 }
 
 template <class T, int NV>
-__global__ void __launch_bounds__(kMostThreads) k_logprobs_backward(GradArgs a) {
+__global__ void __launch_bounds__(kMostThreads, 4) k_logprobs_backward(GradArgs a) {
     pdl_enter();
     using P = Piece<T>;
     constexpr int N = P::N;
@@ -445,21 +647,45 @@ __global__ void __launch_bounds__(kMostThreads) k_logprobs_backward(GradArgs a) 
 }
 
 struct Split {
-    int threads, NV, chunks, per_chunk;
+    int threads, NV, parts, per_part;
 };
 
-// How a row of so many 16-byte pieces is cut: one chunk where a block's
-// registers hold it, in as few threads as hold 4 pieces each; longer rows in
-// equal chunks, smaller ones where there are too few rows to fill the GPU.
-Split split_of(int64_t n, int64_t vocab, int size, int sms) {
-    const int64_t pieces = (vocab * size + 15 + 15) / 16;  // wherever the row begins
+// 16-byte pieces of the longest row: one more where rows may begin within one.
+int64_t pieces_of(int64_t vocab, int size, bool aligned) { return (vocab * size + (aligned ? 15 : 30)) / 16; }
+bool pieces_aligned(const void* p, int64_t stride, int size) {
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * size % 16 == 0;
+}
+
+// The forward pass: threads a block, and spans a row.  As many blocks run at a
+// time as hold 1,024 threads an SM; the spans are what makes the last of these
+// waves end soonest, a block costing about 1,700 pieces beside its own (2.4 us
+// of latencies at 1.4 ns a piece).
+Split spans_of(int64_t n, int64_t pieces, int sms) {
+    int threads = kMostThreads;
+    for (int t = 32; t < kMostThreads; t *= 2)
+        if (pieces <= (int64_t)t * (t < 128 ? 8 : 16)) {
+            threads = t;
+            break;
+        }
+    const int64_t wave = (int64_t)sms * (1024 / threads);
+    int64_t best = 1, cost = INT64_MAX;
+    for (int64_t s = 1; s <= kMostSpans && (s == 1 || pieces / s >= 256); ++s) {
+        const int64_t now = (n * s + wave - 1) / wave * (pieces / s + 1700);
+        if (now < cost) cost = now, best = s;
+        if (n > 4 * wave) break;
+    }
+    return {threads, 0, (int)best, (int)((pieces + best - 1) / best)};
+}
+
+// The backward pass: a block holds what it loads at once, up to 8 pieces a thread.
+Split parts_of(int64_t n, int64_t pieces, int sms) {
     for (int t = 32; t <= kMostThreads; t *= 2)
         for (int nv = 1; nv <= 4; nv *= 2)
             if (pieces <= (int64_t)t * nv) return {t, nv, 1, (int)pieces};
     int nv = 8;
     while (nv > 2 && n * ((pieces + kMostThreads * nv - 1) / (kMostThreads * nv)) < 2 * sms) nv /= 2;
-    const int64_t chunks = (pieces + kMostThreads * nv - 1) / (kMostThreads * nv);
-    return {kMostThreads, nv, (int)chunks, (int)((pieces + chunks - 1) / chunks)};
+    const int64_t parts = (pieces + kMostThreads * nv - 1) / (kMostThreads * nv);
+    return {kMostThreads, nv, (int)parts, (int)((pieces + parts - 1) / parts)};
 }
 
 template <class F>
@@ -478,12 +704,20 @@ void by_pieces(int nv, F f) {
     else f(Int<8>{});
 }
 
+template <class F>
+void by_threads(int threads, F f) {
+    if (threads == 32) f(Int<32>{});
+    else if (threads == 64) f(Int<64>{});
+    else if (threads == 128) f(Int<128>{});
+    else f(Int<256>{});
+}
+
 bool probs_ok(int64_t n, int64_t vocab, int32_t type, float scale) {
     return n >= 0 && n < (int64_t)1 << 31 && vocab >= 1 && vocab < (int64_t)1 << 30 && dense_type_ok(type) && scale > 0.f && std::isfinite(scale);
 }
 
 // Blocks of a launch, at most 2^31 - 1 of them.
-bool grid_ok(int64_t n, const Split& s) { return n * s.chunks < (int64_t)1 << 31; }
+bool grid_ok(int64_t n, const Split& s) { return n * s.parts < (int64_t)1 << 31; }
 
 }  // namespace
 
@@ -492,8 +726,12 @@ extern "C" int64_t mlkv_token_logprobs_workspace(int64_t n, int64_t vocab, int32
     if (n == 0) return 0;
     const int sms = dense_sms();
     if (!sms) return -1;
-    const Split s = split_of(n, vocab, dense_type_size(type), sms);
-    return s.chunks == 1 ? 0 : n * s.chunks * (16 + 8 * (int64_t)top);
+    int64_t most = 0;  // wherever the rows begin
+    for (bool aligned : {false, true}) {
+        const Split s = spans_of(n, pieces_of(vocab, dense_type_size(type), aligned), sms);
+        if (s.parts > 1) most = std::max(most, n * s.parts * (16 + 8 * (int64_t)top));
+    }
+    return most;
 }
 
 extern "C" int mlkv_token_logprobs(const void* d_logits, int64_t stride, int32_t type, int64_t n, int64_t vocab,
@@ -507,27 +745,34 @@ extern "C" int mlkv_token_logprobs(const void* d_logits, int64_t stride, int32_t
     if (top > 0 && (!d_top_logprobs || !d_top_ids)) return MLKV_ERR_INVALID;
     const int sms = dense_sms();
     if (!sms) return MLKV_ERR_CUDA;
-    const Split s = split_of(n, vocab, dense_type_size(type), sms);
+    const int size = dense_type_size(type);
+    const Split s = spans_of(n, pieces_of(vocab, size, pieces_aligned(d_logits, stride, size)), sms);
     if (!grid_ok(n, s)) return MLKV_ERR_UNSUPPORTED;
-    if (s.chunks > 1 && (!d_workspace || workspace_bytes < n * s.chunks * (16 + 8 * (int64_t)top))) return MLKV_ERR_INVALID;
+    if (!workspace_ok(d_workspace, workspace_bytes, s.parts > 1 ? n * s.parts * (16 + 8 * (int64_t)top) : 0)) return MLKV_ERR_INVALID;
     ProbArgs a = {};
     a.x = d_logits; a.stride = stride; a.n = n; a.targets = d_targets; a.scale = scale; a.vocab = (int32_t)vocab;
-    a.top = top; a.chunks = s.chunks; a.per_chunk = s.per_chunk; a.logprob = d_logprob; a.entropy = d_entropy;
+    a.top = top; a.spans = s.parts; a.per_span = s.per_part; a.logprob = d_logprob; a.entropy = d_entropy;
     a.stats = d_stats; a.top_logprobs = d_top_logprobs; a.top_ids = d_top_ids;
     a.part = static_cast<float4*>(d_workspace);
-    a.keys = reinterpret_cast<Key*>(a.part + n * s.chunks);
+    a.keys = reinterpret_cast<Key*>(a.part + n * s.parts);
     cudaStream_t st = (cudaStream_t)stream;
+    bool ok = true;
     by_type(type, [&](auto t) {
         using T = decltype(t);
-        by_pieces(s.NV, [&](auto nv) {
-            constexpr int NV = decltype(nv)::value;
-            const dim3 grid((unsigned)(n * s.chunks)), block(s.threads);
-            if (top) launch_kernel(true, k_logprobs<T, NV, true>, grid, block, 0, st, a);
-            else launch_kernel(true, k_logprobs<T, NV, false>, grid, block, 0, st, a);
+        const dim3 grid((unsigned)(n * s.parts)), block(s.threads);
+        auto launch = [&](auto kernel, bool listed) {
+            const size_t bytes = (size_t)s.threads * (kStages * kBatch * sizeof(uint4) + (listed ? kListed * sizeof(int) : 0));
+            ok = dense_smem(kernel, bytes);
+            if (ok) launch_kernel(true, kernel, grid, block, bytes, st, a);
+        };
+        by_threads(s.threads, [&](auto n) {
+            constexpr int N = decltype(n)::value;
+            if (top) launch(k_logprobs<T, true, N>, true);
+            else launch(k_logprobs<T, false, N>, false);
         });
-        if (s.chunks > 1) launch_kernel(true, k_logprobs_join<T>, dim3((unsigned)((n + 3) / 4)), dim3(128), 0, st, a);
+        if (ok && s.parts > 1) launch_kernel(true, k_logprobs_join<T>, dim3((unsigned)n), dim3(kMostThreads), 0, st, a);
     });
-    return cudaGetLastError() == cudaSuccess ? MLKV_OK : MLKV_ERR_CUDA;
+    return ok && cudaGetLastError() == cudaSuccess ? MLKV_OK : MLKV_ERR_CUDA;
 }
 
 extern "C" int mlkv_token_logprobs_backward(const void* d_logits, int64_t stride, int32_t type, int64_t n, int64_t vocab,
@@ -541,17 +786,18 @@ extern "C" int mlkv_token_logprobs_backward(const void* d_logits, int64_t stride
         dlogits_stride < vocab || (d_dlogits == d_logits && dlogits_stride != stride)) return MLKV_ERR_INVALID;
     const int sms = dense_sms();
     if (!sms) return MLKV_ERR_CUDA;
-    const Split s = split_of(n, vocab, dense_type_size(type), sms);
+    const int size = dense_type_size(type);
+    const Split s = parts_of(n, pieces_of(vocab, size, pieces_aligned(d_logits, stride, size)), sms);
     if (!grid_ok(n, s)) return MLKV_ERR_UNSUPPORTED;
     GradArgs a = {};
     a.x = d_logits; a.dx = d_dlogits; a.stride = stride; a.dx_stride = dlogits_stride; a.targets = d_targets;
     a.entropy = d_entropy; a.stats = d_stats; a.dlogprob = d_dlogprob; a.dentropy = d_dentropy; a.scale = scale;
-    a.vocab = (int32_t)vocab; a.chunks = s.chunks; a.per_chunk = s.per_chunk;
+    a.vocab = (int32_t)vocab; a.chunks = s.parts; a.per_chunk = s.per_part;
     cudaStream_t st = (cudaStream_t)stream;
     by_type(type, [&](auto t) {
         using T = decltype(t);
         by_pieces(s.NV, [&](auto nv) {
-            launch_kernel(true, k_logprobs_backward<T, decltype(nv)::value>, dim3((unsigned)(n * s.chunks)), dim3(s.threads), 0, st, a);
+            launch_kernel(true, k_logprobs_backward<T, decltype(nv)::value>, dim3((unsigned)(n * s.parts)), dim3(s.threads), 0, st, a);
         });
     });
     return cudaGetLastError() == cudaSuccess ? MLKV_OK : MLKV_ERR_CUDA;

@@ -32,27 +32,70 @@ struct NormArgs {
     int32_t lanes;   // L: lanes per row, a power of two below 32 or a multiple of 32
 };
 
-// V values of a weight vector from index i on, which V divides.
+// Weights, held as fp32 in shared memory: in order, or, for vectors of 8, the
+// first four values of every vector, then the last four (16-byte reads of
+// neighbouring lanes then lie side by side).
 template <int V>
-__device__ __forceinline__ void load_weights(const void* p, int32_t type, int i, float (&o)[V]) {
-    if (type == MLKV_TYPE_FLOAT) {
+__device__ __forceinline__ int weight_place(int c, int dim) {
+    return V == 8 ? (((c >> 2) & 1) * (dim / 8) + (c >> 3)) * 4 + (c & 3) : c;
+}
+template <int V>
+__device__ __forceinline__ void stage_weights(float* to, const void* p, int32_t type, int dim) {
+    for (int c = threadIdx.x; c < dim; c += blockDim.x) to[weight_place<V>(c, dim)] = load_as_float(p, type, c);
+}
+
+// A vector of V values as it lies in memory, read and written in pairs (of one
+// value: it and 0).  Kept in 32-bit words: 16-bit values apart would take a
+// register each.
+template <int V> constexpr int kPairs = (V + 1) / 2;
+template <class T, int V> struct Values {
+    static constexpr int kWords = sizeof(T) * V / 4;
+    Pack<uint32_t, kWords> q;
+    __device__ __forceinline__ void load(const T* p) { q = *reinterpret_cast<const Pack<uint32_t, kWords>*>(p); }
+    __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<Pack<uint32_t, kWords>*>(p) = q; }
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) q.v[i] = 0;
+    }
+    __device__ __forceinline__ float2 pair(int k) const {
+        if constexpr (sizeof(T) == 4) return make_float2(__uint_as_float(q.v[2 * k]), V > 1 ? __uint_as_float(q.v[V > 1 ? 2 * k + 1 : 0]) : 0.f);
+        else return pair_of_word<T>(q.v[k]);
+    }
+    __device__ __forceinline__ void set(int k, float2 x) {
+        if constexpr (sizeof(T) == 4) {
+            q.v[2 * k] = __float_as_uint(x.x);
+            if (V > 1) q.v[V > 1 ? 2 * k + 1 : 0] = __float_as_uint(x.y);
+        } else {
+            q.v[k] = word_of_pair<T>(x);
+        }
+    }
+};
+template <class T> struct Half1 {
+    uint16_t q;
+    __device__ __forceinline__ void load(const T* p) { q = *reinterpret_cast<const uint16_t*>(p); }
+    __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<uint16_t*>(p) = q; }
+    __device__ __forceinline__ void zero() { q = 0; }
+    __device__ __forceinline__ float2 pair(int) const { return make_float2(pair_of_word<T>(q).x, 0.f); }
+    __device__ __forceinline__ void set(int, float2 x) { q = (uint16_t)word_of_pair<T>(make_float2(x.x, 0.f)); }
+};
+template <> struct Values<__nv_bfloat16, 1> : Half1<__nv_bfloat16> {};
+template <> struct Values<__half, 1> : Half1<__half> {};
+
+template <int V>
+__device__ __forceinline__ void weight_pairs(const float* w, int j, int dim, float2 (&o)[kPairs<V>]) {
+    if constexpr (V == 1) {
+        o[0] = make_float2(w[j], 0.f);
+    } else {
         constexpr int H = V > 4 ? 4 : V;
 #pragma unroll
         for (int c = 0; c < V; c += H) {
-            const Pack<float, H> q = *reinterpret_cast<const Pack<float, H>*>(static_cast<const float*>(p) + i + c);
+            const Pack<float, H> q = *reinterpret_cast<const Pack<float, H>*>(w + weight_place<V>(j * V + c, dim));
 #pragma unroll
-            for (int e = 0; e < H; ++e) o[c + e] = q.v[e];
+            for (int k = 0; k < H / 2; ++k) o[c / 2 + k] = make_float2(q.v[2 * k], q.v[2 * k + 1]);
         }
-    } else if (type == MLKV_TYPE_BFLOAT) {
-        const auto q = *reinterpret_cast<const Pack<__nv_bfloat16, V>*>(static_cast<const __nv_bfloat16*>(p) + i);
-#pragma unroll
-        for (int e = 0; e < V; ++e) o[e] = to_float(q.v[e]);
-    } else {
-        const auto q = *reinterpret_cast<const Pack<__half, V>*>(static_cast<const __half*>(p) + i);
-#pragma unroll
-        for (int e = 0; e < V; ++e) o[e] = to_float(q.v[e]);
     }
 }
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 
 // Where a thread stands in its block's teams.
 struct Team {
@@ -60,8 +103,8 @@ struct Team {
     __device__ explicit Team(int lanes)
         : L(lanes), lane(threadIdx.x % lanes), index(threadIdx.x / lanes), count(blockDim.x / lanes),
           warps(lanes / 32), warp((threadIdx.x % lanes) / 32) {}
-    // The sums of a and b over the team.  buf: 2 x 2 x 32 floats of the block, used in turn (turn: 0, 1, 0, ...),
-    // so one barrier a sum is enough.  The teams of a block call it equally often.
+    // The sums of a and b over the team.  buf: 2 x 32 pairs of the block, used in turn (turn: 0, 1, 0, ...), so
+    // that one barrier a sum is enough: who writes a buffer again has seen all of its team past the next sum.
     __device__ __forceinline__ void sum(float& a, float& b, float2* buf, int turn) const {
         const int G = L < 32 ? L : 32;
         for (int o = G >> 1; o; o >>= 1) {
@@ -71,7 +114,7 @@ struct Team {
         if (L <= 32) return;
         float2* mine = buf + turn * 32 + index * warps;
         if ((threadIdx.x & 31) == 0) mine[warp] = make_float2(a, b);
-        __syncthreads();
+        asm volatile("bar.sync %0, %1;" ::"r"(index + 1), "r"(L) : "memory");  // (at most 4 teams of several warps)
         a = b = 0.f;
         for (int i = 0; i < warps; ++i) {
             const float2 q = mine[i];
@@ -79,17 +122,12 @@ struct Team {
             b += q.y;
         }
     }
+    __device__ __forceinline__ float sum(float a, float2* buf, int turn) const {
+        float none = 0.f;
+        sum(a, none, buf, turn);
+        return a;
+    }
 };
-
-template <class T, int V>
-__device__ __forceinline__ Pack<T, V> load_pack(const T* p) { return *reinterpret_cast<const Pack<T, V>*>(p); }
-template <class T, int V>
-__device__ __forceinline__ Pack<T, V> zero_pack() {
-    Pack<T, V> q;
-#pragma unroll
-    for (int e = 0; e < V; ++e) q.v[e] = from_float<T>(0.f);
-    return q;
-}
 
 // Values per vector: 16 bytes of the wider type, or as many as every row and
 // weight vector is aligned to.

@@ -15,75 +15,92 @@ namespace {
 constexpr int kBackwardValues = 16;  // most values of x and dy each that a lane holds, beside their columns' sums
 
 // The rows' gradients, and the sums over this block's rows of dy xh and dy.
+// A team has the next row on its way while it works on one.
 template <class TX, class TY, int V, int NV>
 __global__ void __launch_bounds__(kNormLanes) k_norm_backward(NormArgs a) {
     pdl_enter();
-    extern __shared__ float cols[];  // [2][dim], where a block has several teams
+    extern __shared__ float shared[];  // the weight, [dim]; then the teams' sums, [2][dim]
     __shared__ float2 buf[64];
+    constexpr int H = kPairs<V>;
     const Team tm(a.lanes);
     const int nvec = a.dim / V;
-    float dw[NV][V], db[NV][V];
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int e = 0; e < V; ++e) dw[i][e] = db[i][e] = 0.f;
     const int64_t step = (int64_t)gridDim.x * tm.count;
-    Pack<TX, V> x[NV];
-    Pack<TY, V> dy[NV];
-    float mu = 0.f, rs = 0.f;
-    auto load = [&](int64_t r) {
+    float2 dw[NV][H], db[NV][H];
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int k = 0; k < H; ++k) dw[i][k] = db[i][k] = both(0.f);
+    struct Row {
+        Values<TX, V> x[NV];
+        Values<TY, V> dy[NV];
+        float2 stats;
+    };
+    auto load = [&](int64_t r, Row& q) {
         const bool live = r < a.rows;
         const TX* xr = static_cast<const TX*>(a.x) + r * a.x_stride;
         const TY* dr = static_cast<const TY*>(a.dy) + r * a.dy_stride;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int j = tm.lane + i * tm.L;
-            x[i] = live && j < nvec ? load_pack<TX, V>(xr + j * V) : zero_pack<TX, V>();
-            dy[i] = live && j < nvec ? load_pack<TY, V>(dr + j * V) : zero_pack<TY, V>();
-        }
-        mu = live ? a.stats[2 * r] : 0.f;
-        rs = live ? a.stats[2 * r + 1] : 0.f;
-    };
-    int64_t r = (int64_t)blockIdx.x * tm.count + tm.index;
-    load(r);
-    int turn = 0;
-    // every team of the block takes as many turns (the sums' barriers)
-    for (int64_t first = (int64_t)blockIdx.x * tm.count; first < a.rows; first += step, r += step, turn ^= 1) {
-        float c1 = 0.f, c2 = 0.f;
-        float xh[NV][V], g[NV][V];
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int j = tm.lane + i * tm.L;
-            float w[V];
-            if (a.w && j < nvec) load_weights<V>(a.w, a.w_type, j * V, w);
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                const float d = to_float(dy[i].v[e]);
-                xh[i][e] = (to_float(x[i].v[e]) - mu) * rs;
-                g[i][e] = a.w && j < nvec ? d * w[e] : d;
-                c1 += g[i][e];
-                c2 += g[i][e] * xh[i][e];
-                dw[i][e] += d * xh[i][e];
-                db[i][e] += d;
+            q.x[i].zero();
+            q.dy[i].zero();
+            if (live && j < nvec) {
+                q.x[i].load(xr + j * V);
+                q.dy[i].load(dr + j * V);
             }
         }
-        const float rs_now = rs;
-        load(r + step);
-        if (!a.out) continue;
-        tm.sum(c1, c2, buf, turn);
-        c1 /= (float)a.dim;
-        c2 /= (float)a.dim;
-        if (r >= a.rows) continue;
-        TX* o = static_cast<TX*>(a.out) + r * a.out_stride;
+        q.stats = live ? *reinterpret_cast<const float2*>(a.stats + 2 * r) : both(0.f);
+    };
+    int64_t r = (int64_t)blockIdx.x * tm.count + tm.index;
+    Row q, next;
+    load(r, q);
+    if (a.w) {
+        stage_weights<V>(shared, a.w, a.w_type, a.dim);
+        __syncthreads();
+    }
+    int turn = 0;
+    // the lanes of a warp take as many turns as its first team does
+    for (int64_t first = tm.L < 32 ? r - (threadIdx.x & 31) / tm.L : r; first < a.rows; first += step, r += step, turn ^= 1) {
+        load(r + step, next);
+        const float2 minus = both(-q.stats.x), rs = both(q.stats.y);
+        float2 c1 = both(0.f), c2 = both(0.f);
+        auto row = [&](auto f) {  // f(i, k, g, xh, dy) of every pair
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int j = tm.lane + i * tm.L;
-            if (j >= nvec) continue;
-            Pack<TX, V> q;
+            for (int i = 0; i < NV; ++i) {
+                const int j = tm.lane + i * tm.L;
+                float2 w[H];
+                if (a.w && j < nvec) weight_pairs<V>(shared, j, a.dim, w);
 #pragma unroll
-            for (int e = 0; e < V; ++e) q.v[e] = from_float<TX>(rs_now * (g[i][e] - c1 - xh[i][e] * c2));
-            *reinterpret_cast<Pack<TX, V>*>(o + j * V) = q;
+                for (int k = 0; k < H; ++k) {
+                    const float2 d = q.dy[i].pair(k), xh = mul2(add2(q.x[i].pair(k), minus), rs);
+                    f(i, k, a.w && j < nvec ? mul2(d, w[k]) : d, xh, d);
+                }
+            }
+        };
+        row([&](int i, int k, float2 g, float2 xh, float2 d) {
+            c1 = add2(c1, g);
+            c2 = fma2(g, xh, c2);
+            dw[i][k] = fma2(d, xh, dw[i][k]);
+            db[i][k] = add2(db[i][k], d);
+        });
+        if (a.out) {
+            float s1 = c1.x + c1.y, s2 = c2.x + c2.y;
+            tm.sum(s1, s2, buf, turn);
+            const float2 m1 = both(-s1 / (float)a.dim), m2 = both(-s2 / (float)a.dim);
+            if (r < a.rows) {
+                TX* o = static_cast<TX*>(a.out) + r * a.out_stride;
+                Values<TX, V> p[NV];
+                row([&](int i, int k, float2 g, float2 xh, float2) {
+                    p[i].set(k, mul2(fma2(xh, m2, add2(g, m1)), rs));
+                });
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    const int j = tm.lane + i * tm.L;
+                    if (j < nvec) p[i].store(o + j * V);
+                }
+            }
         }
+        q = next;
     }
     if (!a.part && !a.dweight && !a.dbias) return;
     // the lanes of a warp that hold the same columns
@@ -91,46 +108,50 @@ __global__ void __launch_bounds__(kNormLanes) k_norm_backward(NormArgs a) {
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                dw[i][e] += __shfl_xor_sync(0xffffffffu, dw[i][e], o);
-                db[i][e] += __shfl_xor_sync(0xffffffffu, db[i][e], o);
+            for (int k = 0; k < H; ++k) {
+                dw[i][k].x += __shfl_xor_sync(0xffffffffu, dw[i][k].x, o);
+                db[i][k].x += __shfl_xor_sync(0xffffffffu, db[i][k].x, o);
+                dw[i][k].y += __shfl_xor_sync(0xffffffffu, dw[i][k].y, o);
+                db[i][k].y += __shfl_xor_sync(0xffffffffu, db[i][k].y, o);
             }
     // ... then the block's teams (a warp's, where it holds several), one after another
+    float* cols = shared + (a.w ? a.dim : 0);
     const int teams = tm.L < 32 ? blockDim.x / 32 : tm.count, mine = tm.L < 32 ? threadIdx.x / 32 : tm.index;
     const bool holds = tm.L >= 32 || (threadIdx.x & 31) < tm.L;
+    auto each = [&](auto f) {  // f(column, dw, db)
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int j = tm.lane + i * tm.L;
+            if (j >= nvec) continue;
+#pragma unroll
+            for (int k = 0; k < H; ++k) {
+                f(j * V + 2 * k, dw[i][k].x, db[i][k].x);
+                if (2 * k + 1 < V) f(j * V + 2 * k + 1, dw[i][k].y, db[i][k].y);
+            }
+        }
+    };
     for (int t = 0; t < teams - 1; ++t) {
         if (mine == t && holds)
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int j = tm.lane + i * tm.L;
-                if (j >= nvec) continue;
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    const float before_w = t ? cols[j * V + e] : 0.f, before_b = t ? cols[a.dim + j * V + e] : 0.f;
-                    cols[j * V + e] = before_w + dw[i][e];
-                    cols[a.dim + j * V + e] = before_b + db[i][e];
-                }
-            }
+            each([&](int c, float w, float b) {
+                cols[c] = (t ? cols[c] : 0.f) + w;
+                cols[a.dim + c] = (t ? cols[a.dim + c] : 0.f) + b;
+            });
         __syncthreads();
     }
     if (mine != teams - 1 || !holds) return;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int j = tm.lane + i * tm.L;
-        if (j >= nvec) continue;
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-            const int c = j * V + e;
-            const float sw = dw[i][e] + (teams > 1 ? cols[c] : 0.f), sb = db[i][e] + (teams > 1 ? cols[a.dim + c] : 0.f);
-            if (a.part) {
-                a.part[(int64_t)blockIdx.x * 2 * a.dim + c] = sw;
-                a.part[(int64_t)blockIdx.x * 2 * a.dim + a.dim + c] = sb;
-            } else {
-                if (a.dweight) store_as(a.dweight, a.w_type, c, sw);
-                if (a.dbias) store_as(a.dbias, a.w_type, c, sb);
-            }
+    each([&](int c, float w, float b) {
+        if (teams > 1) {
+            w += cols[c];
+            b += cols[a.dim + c];
         }
-    }
+        if (a.part) {
+            a.part[(int64_t)blockIdx.x * 2 * a.dim + c] = w;
+            a.part[(int64_t)blockIdx.x * 2 * a.dim + a.dim + c] = b;
+        } else {
+            if (a.dweight) store_as(a.dweight, a.w_type, c, w);
+            if (a.dbias) store_as(a.dbias, a.w_type, c, b);
+        }
+    });
 }
 
 // Rows too long for registers: a block a row ...
@@ -232,16 +253,17 @@ extern "C" int mlkv_layer_norm_backward(const void* d_dy, int64_t dy_stride, int
     a.x = d_x; a.dy = d_dy; a.out = d_dx; a.w = d_weight; a.stats = const_cast<float*>(d_stats);
     a.x_stride = x_stride; a.dy_stride = dy_stride; a.out_stride = dx_stride; a.rows = rows;
     a.dim = (int32_t)dim; a.w_type = w_type; a.dweight = d_dweight; a.dbias = d_dbias;
-    const int xs = dense_type_size(x_type), ys = dense_type_size(dy_type), ws = dense_type_size(w_type);
-    const int V = norm_vector_width(dim, {{d_x, xs}, {d_dy, ys}, {d_dx, xs}, {d_weight, ws}},
+    const int xs = dense_type_size(x_type), ys = dense_type_size(dy_type);
+    const int V = norm_vector_width(dim, {{d_x, xs}, {d_dy, ys}, {d_dx, xs}},
                                {x_stride, dy_stride, d_dx ? dx_stride : 0}, 16 / xs);
     const NormShape sh = norm_shape(dim, V, kBackwardValues);
     const int threads = sh.lanes ? norm_team_threads(sh.lanes) : kNormLongLanes, teams = sh.lanes ? threads / sh.lanes : 1;
     int64_t blocks = std::min(kMostBlocks, backward_blocks(rows, teams, sms, threads));
     if (!sh.lanes) blocks = std::max<int64_t>(1, std::min<int64_t>(rows, (2 * sms * 128 + dim - 1) / dim));
     const bool parts = want_cols && (blocks > 1 || !sh.lanes);
-    if (parts && (!d_workspace || workspace_bytes < blocks * 2 * dim * (int64_t)sizeof(float))) return MLKV_ERR_INVALID;
+    if (!workspace_ok(d_workspace, workspace_bytes, parts ? blocks * 2 * dim * (int64_t)sizeof(float) : 0)) return MLKV_ERR_INVALID;
     a.part = parts ? static_cast<float*>(d_workspace) : nullptr;
+    bool ok = true;
     by_types(x_type, dy_type, [&](auto tx, auto ty) {
         using TX = decltype(tx);
         using TY = decltype(ty);
@@ -258,12 +280,13 @@ extern "C" int mlkv_layer_norm_backward(const void* d_dy, int64_t dy_stride, int
         a.lanes = sh.lanes;
         by_width<TX, kBackwardValues>(V, sh.NV, [&](auto v, auto nv) {
             auto kernel = k_norm_backward<TX, TY, decltype(v)::value, decltype(nv)::value>;
-            const size_t smem = sh.lanes < threads ? 2 * (size_t)dim * sizeof(float) : 0;
-            launch_kernel(true, kernel, dim3((unsigned)blocks), dim3(threads), smem, st, a);
+            const size_t smem = ((d_weight ? 1 : 0) + (sh.lanes < threads ? 2 : 0)) * (size_t)dim * sizeof(float);
+            ok = dense_smem(kernel, smem);
+            if (ok) launch_kernel(true, kernel, dim3((unsigned)blocks), dim3(threads), smem, st, a);
         });
     });
-    if (parts)
+    if (parts && ok)
         launch_kernel(true, k_norm_cols, dim3((unsigned)((2 * dim + 31) / 32)), dim3(1024), 0, st,
                       (const float*)d_workspace, (int)blocks, (int)dim, d_dweight, d_dbias, w_type);
-    return cudaGetLastError() == cudaSuccess ? MLKV_OK : MLKV_ERR_CUDA;
+    return ok && cudaGetLastError() == cudaSuccess ? MLKV_OK : MLKV_ERR_CUDA;
 }

@@ -18,7 +18,7 @@ memory comes from torch's allocator for the length of the call.  This module
 only checks arguments (TypeError, ValueError) and passes pointers.  Formulas and
 the treatment of masked and invalid values: include/mlkv_dense.h.
 """
-import ctypes
+import contextlib
 import typing
 
 import torch
@@ -78,6 +78,14 @@ def _on_gpu(x: torch.Tensor, name: str):
         raise TypeError(f"{name} must be a CUDA tensor")
 
 
+_HERE = contextlib.nullcontext()
+
+
+def _current(device):
+    """Makes the device current for a library call (nothing to do, as a rule)."""
+    return _HERE if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+
 def _ptr(x) -> int | None:
     return None if x is None else x.data_ptr()
 
@@ -112,7 +120,7 @@ def layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.
     w, b, kind = _norm_weights(weight, bias, dim, x.device)
     y = torch.empty((rows, dim), dtype=out_dtype, device=x.device)
     stats = torch.empty((rows, 2), dtype=torch.float32, device=x.device) if save_stats else None
-    with torch.cuda.device(x.device):
+    with _current(x.device):
         _check(L.load().mlkv_layer_norm(x.data_ptr(), _row_stride(x), _TYPES[x.dtype], rows, dim, _ptr(w), _ptr(b), kind,
                                         eps, y.data_ptr(), dim, _TYPES[out_dtype], _ptr(stats), _stream(x.device)))
     return (y, stats) if save_stats else y
@@ -134,7 +142,7 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor 
     dw = None if w is None else torch.empty(dim, dtype=wt, device=x.device)
     db = torch.empty(dim, dtype=wt, device=x.device) if bias else None
     lib = L.load()
-    with torch.cuda.device(x.device):
+    with _current(x.device):
         ws = _workspace(lib.mlkv_layer_norm_backward_workspace(rows, dim), x.device)
         _check(lib.mlkv_layer_norm_backward(dy.data_ptr(), _row_stride(dy), _TYPES[dy.dtype], x.data_ptr(), _row_stride(x),
                                             _TYPES[x.dtype], rows, dim, _ptr(w), kind, stats.data_ptr(), dx.data_ptr(), dim,
@@ -183,7 +191,7 @@ def linear(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None = No
         pre = torch.empty((m, n), dtype=x.dtype, device=x.device)
         a.d_pre, a.pre_stride = pre.data_ptr(), n
     lib = L.load()
-    with torch.cuda.device(x.device):
+    with _current(x.device):
         ws = _workspace(lib.mlkv_linear_workspace(a), x.device)
         if ws is not None:
             a.d_workspace, a.workspace_bytes = ws.data_ptr(), ws.numel()
@@ -210,7 +218,7 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, pre
     db = torch.empty(n, dtype=x.dtype, device=x.device) if bias else None
     a.d_dx, a.dx_stride, a.d_dweight, a.dweight_stride, a.d_dbias = _ptr(dx), k, _ptr(dw), k, _ptr(db)
     lib = L.load()
-    with torch.cuda.device(x.device):
+    with _current(x.device):
         ws = _workspace(lib.mlkv_linear_backward_workspace(a), x.device)
         if ws is not None:
             a.d_workspace, a.workspace_bytes = ws.data_ptr(), ws.numel()
@@ -253,7 +261,7 @@ def token_logprobs(logits: torch.Tensor, targets: torch.Tensor, *, top: int = 0,
     ids = torch.empty((n, top), dtype=torch.int64, device=dev) if top else None
     lib = L.load()
     kind = _TYPES[logits.dtype]
-    with torch.cuda.device(dev):
+    with _current(dev):
         ws = _workspace(lib.mlkv_token_logprobs_workspace(n, vocab, kind, top), dev)
         _check(lib.mlkv_token_logprobs(logits.data_ptr(), _row_stride(logits), kind, n, vocab, targets.data_ptr(), scale,
                                        top, logprob.data_ptr(), entropy.data_ptr(), stats.data_ptr(), _ptr(tops),
@@ -278,7 +286,7 @@ def token_logprobs_backward(logits: torch.Tensor, targets: torch.Tensor, result:
     if in_place and logits is not given:
         raise TypeError("logits written in place must have contiguous rows")
     out = logits if in_place else torch.empty((n, vocab), dtype=logits.dtype, device=dev)
-    with torch.cuda.device(dev):
+    with _current(dev):
         _check(L.load().mlkv_token_logprobs_backward(logits.data_ptr(), _row_stride(logits), _TYPES[logits.dtype], n, vocab,
                                                      targets.data_ptr(), scale, entropy.data_ptr(), stats.data_ptr(),
                                                      _ptr(g), _ptr(h), out.data_ptr(), _row_stride(out), _stream(dev)))
