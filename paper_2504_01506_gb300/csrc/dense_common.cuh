@@ -35,8 +35,8 @@ namespace mlkv {
 inline bool dense_type_ok(int32_t type) { return type >= MLKV_TYPE_FLOAT && type <= MLKV_TYPE_HALF; }
 inline int dense_type_size(int32_t type) { return type == MLKV_TYPE_FLOAT ? 4 : 2; }
 
-// Most dynamic shared memory that any kernel here asks for (of 227 KB, less what they declare).
-constexpr int kDenseSmem = 216 << 10;
+// Most dynamic shared memory that any kernel here asks for (of 227 KB with what they declare).
+constexpr int kDenseSmem = 226 << 10;
 
 // SMs of the current device (0: the call failed); asked once per device.
 inline int dense_sms() {

@@ -22,7 +22,6 @@ namespace {
 
 constexpr int kBM = 128;      // rows (i) of a tile
 constexpr int kBK = 64;       // values along k of a stage: 128 bytes
-constexpr int kThreads = 192; // four epilogue warps, a TMA warp, an MMA warp
 
 __device__ uint32_t g_status;  // MLKV_ERR_TIMEOUT: a wait ran out
 
@@ -50,38 +49,65 @@ __device__ __forceinline__ float widen(int32_t type, uint16_t v) {
 __device__ __forceinline__ uint16_t narrow(int32_t type, float v) {
     return type == MLKV_TYPE_BFLOAT ? __bfloat16_as_ushort(__float2bfloat16_rn(v)) : __half_as_ushort(__float2half_rn(v));
 }
-__device__ __forceinline__ uint32_t narrow2(int32_t type, float lo, float hi) {
-    return (uint32_t)narrow(type, lo) | (uint32_t)narrow(type, hi) << 16;
-}
 
-__device__ __forceinline__ float sigmoid_fast(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
-constexpr float kGelu = 1.5957691216057308f, kGelu3 = 0.044715f;  // 2 sqrt(2/pi): (1 + tanh u) / 2 = sigmoid(2u)
-__device__ __forceinline__ float activate(int32_t act, float z) {
-    if (act == MLKV_ACT_RELU) return z > 0.f ? z : (z != z ? z : 0.f);
-    if (act == MLKV_ACT_SILU) return z == -INFINITY ? 0.f : z * sigmoid_fast(z);
-    if (act == MLKV_ACT_GELU_TANH) return z == -INFINITY ? 0.f : z * sigmoid_fast(kGelu * (z + kGelu3 * z * z * z));
-    return z;
+// 1 / (1 + 2^u), two at a time, to a few units of 2^-22: what follows is rounded to 16 bits.
+__device__ __forceinline__ float2 squash(float2 u) {
+    float2 e, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.x) : "f"(u.x));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.y) : "f"(u.y));
+    e = add2(e, make_float2(1.f, 1.f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.x) : "f"(e.x));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(e.y));
+    return r;
 }
-__device__ __forceinline__ float slope(int32_t act, float z) {
-    if (act == MLKV_ACT_RELU) return z > 0.f ? 1.f : (z != z ? z : 0.f);
-    // far from 0 the slopes are 0 and 1; the bound keeps products of a vanished and an infinite factor out
-    z = fminf(fmaxf(z, -100.f), 100.f) + (z != z ? z : 0.f);
-    if (act == MLKV_ACT_SILU) {
-        const float q = sigmoid_fast(z);
-        return q * (1.f + z * (1.f - q));
-    }
-    if (act == MLKV_ACT_GELU_TANH) {
-        const float q = sigmoid_fast(kGelu * (z + kGelu3 * z * z * z));
-        return q + z * q * (1.f - q) * kGelu * (1.f + 3.f * kGelu3 * z * z);
-    }
-    return 1.f;
+__device__ __forceinline__ float2 splat2(float x) { return make_float2(x, x); }
+__device__ __forceinline__ float at_least(float x, float least) {  // NaN stays NaN
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(least));
+    return r;
+}
+__device__ __forceinline__ float at_most(float x, float most) {
+    float r;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(most));
+    return r;
+}
+// sigmoid(z) = squash(kSilu z);  (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2 = squash(z (kGelu + kGelu3 z^2))
+constexpr float kLog2e = 1.4426950408889634f, kSilu = -kLog2e, kGeluSlope = 1.5957691216057308f, kCube = 0.044715f;
+constexpr float kGelu = -kLog2e * kGeluSlope, kGelu3 = kGelu * kCube;
+// Of two values.  (Far below 0 the value is 0, not the product of -inf and 0.)
+template <int ACT>
+__device__ __forceinline__ float2 activate(float2 z) {
+    if (ACT == MLKV_ACT_NONE) return z;
+    if (ACT == MLKV_ACT_RELU) return make_float2(at_least(z.x, 0.f), at_least(z.y, 0.f));
+    const float2 low = make_float2(at_least(z.x, -1e4f), at_least(z.y, -1e4f));
+    if (ACT == MLKV_ACT_SILU) return mul2(low, squash(mul2(low, splat2(kSilu))));
+    return mul2(low, squash(mul2(low, fma2(mul2(low, low), splat2(kGelu3), splat2(kGelu)))));
+}
+// The slope there.  (Far from 0 it is 0 or 1, not a product with an infinite factor.)
+template <int ACT>
+__device__ __forceinline__ float2 slope(float2 z) {
+    if (ACT == MLKV_ACT_NONE) return splat2(1.f);
+    if (ACT == MLKV_ACT_RELU) return make_float2(z.x > 0.f ? 1.f : z.x != z.x ? z.x : 0.f, z.y > 0.f ? 1.f : z.y != z.y ? z.y : 0.f);
+    z = make_float2(at_most(at_least(z.x, -100.f), 100.f), at_most(at_least(z.y, -100.f), 100.f));
+    const float2 one = splat2(1.f), z2 = mul2(z, z);
+    // q + z q (1 - q) u', u the argument of the sigmoid
+    const float2 q = squash(ACT == MLKV_ACT_SILU ? mul2(z, splat2(kSilu)) : mul2(z, fma2(z2, splat2(kGelu3), splat2(kGelu))));
+    const float2 rest = mul2(mul2(z, q), fma2(q, splat2(-1.f), one));
+    return ACT == MLKV_ACT_SILU ? add2(rest, q) : fma2(rest, fma2(z2, splat2(3.f * kGeluSlope * kCube), splat2(kGeluSlope)), q);
+}
+template <int N> struct Act { static constexpr int value = N; };
+template <class F>
+__device__ __forceinline__ void by_act(int32_t act, F f) {
+    if (act == MLKV_ACT_RELU) f(Act<MLKV_ACT_RELU>{});
+    else if (act == MLKV_ACT_GELU_TANH) f(Act<MLKV_ACT_GELU_TANH>{});
+    else if (act == MLKV_ACT_SILU) f(Act<MLKV_ACT_SILU>{});
 }
 
 // What becomes of the sum at (row, col) of the output.
 __device__ __forceinline__ float finish(const Epilogue& e, float v, int64_t row, int64_t col) {
     if (e.bias) v += widen(e.type, static_cast<const uint16_t*>(e.bias)[col]);
     if (e.pre) static_cast<uint16_t*>(e.pre)[row * e.pre_stride + col] = narrow(e.type, v);
-    v = activate(e.act, v);
+    by_act(e.act, [&](auto act) { v = activate<decltype(act)::value>(splat2(v)).x; });
     if (e.residual) v += widen(e.type, static_cast<const uint16_t*>(e.residual)[row * e.residual_stride + col]);
     return v;
 }
@@ -98,79 +124,194 @@ __device__ __forceinline__ void tile_at(const Product& p, int t, int& i, int& j,
     j = t / size;
 }
 
-// 16 sums of row i of the product, from column j0 on.
-template <bool SWAP>
-__device__ __forceinline__ void put16(const Product& p, const uint32_t (&r)[16], int64_t row_i, int64_t j0, int share) {
+// 16 sums of a tile whose rows run along the output's columns: this lane's
+// column i of the output, from row j0 on.  A warp writes 32 columns of a row at a time.
+template <class T>
+__device__ __forceinline__ void put_columns(const Product& p, const uint32_t (&r)[16], int64_t i, int64_t j0, int share) {
     const Epilogue& e = p.e;
-    if (e.part) {
-        float* o = e.part + share * e.part_size;
 #pragma unroll
-        for (int q = 0; q < 16; ++q)
-            if (j0 + q < p.J) o[SWAP ? (j0 + q) * e.part_stride + row_i : row_i * e.part_stride + j0 + q] = __uint_as_float(r[q]);
-    } else if (SWAP) {
-#pragma unroll
-        for (int q = 0; q < 16; ++q)
-            if (j0 + q < p.J)
-                static_cast<uint16_t*>(e.out)[(j0 + q) * e.out_stride + row_i] =
-                    narrow(e.type, finish(e, __uint_as_float(r[q]), j0 + q, row_i));
-    } else if (e.wide && j0 + 16 <= p.J) {
-        float v[16];
-#pragma unroll
-        for (int q = 0; q < 16; ++q) v[q] = __uint_as_float(r[q]);
-        if (e.bias)
-#pragma unroll
-            for (int q = 0; q < 16; ++q) v[q] += widen(e.type, static_cast<const uint16_t*>(e.bias)[j0 + q]);
-        if (e.pre) {
-            uint4* o = reinterpret_cast<uint4*>(static_cast<uint16_t*>(e.pre) + row_i * e.pre_stride + j0);
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-                o[h] = make_uint4(narrow2(e.type, v[8 * h], v[8 * h + 1]), narrow2(e.type, v[8 * h + 2], v[8 * h + 3]),
-                                  narrow2(e.type, v[8 * h + 4], v[8 * h + 5]), narrow2(e.type, v[8 * h + 6], v[8 * h + 7]));
-        }
-        if (e.act != MLKV_ACT_NONE)
-#pragma unroll
-            for (int q = 0; q < 16; ++q) v[q] = activate(e.act, v[q]);
-        if (e.residual) {
-            const uint4* o = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(e.residual) + row_i * e.residual_stride + j0);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const uint4 x = o[h];
-                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    v[8 * h + 2 * q] += widen(e.type, (uint16_t)w[q]);
-                    v[8 * h + 2 * q + 1] += widen(e.type, (uint16_t)(w[q] >> 16));
-                }
-            }
-        }
-        uint4* o = reinterpret_cast<uint4*>(static_cast<uint16_t*>(e.out) + row_i * e.out_stride + j0);
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-            o[h] = make_uint4(narrow2(e.type, v[8 * h], v[8 * h + 1]), narrow2(e.type, v[8 * h + 2], v[8 * h + 3]),
-                              narrow2(e.type, v[8 * h + 4], v[8 * h + 5]), narrow2(e.type, v[8 * h + 6], v[8 * h + 7]));
-    } else {
-#pragma unroll
-        for (int q = 0; q < 16; ++q)
-            if (j0 + q < p.J)
-                static_cast<uint16_t*>(e.out)[row_i * e.out_stride + j0 + q] =
-                    narrow(e.type, finish(e, __uint_as_float(r[q]), row_i, j0 + q));
+    for (int q = 0; q < 16; ++q) {
+        if (j0 + q >= p.J) break;
+        const float v = __uint_as_float(r[q]);
+        if (e.part) e.part[share * e.part_size + (j0 + q) * e.part_stride + i] = v;
+        else static_cast<T*>(e.out)[(j0 + q) * e.out_stride + i] = from_float<T>(finish(e, v, j0 + q, i));
     }
 }
 
-template <int BN> struct Ring {
-    static constexpr int kA = kBM * kBK * 2, kB = BN * kBK * 2, kStage = kA + kB;
-    static constexpr int kStages = (200 * 1024) / kStage < 12 ? (200 * 1024) / kStage : 12;
-    static constexpr int kBytes = kStages * kStage + 1024;  // (aligned to 1,024 within)
+// A warp's corner of shared memory.  The lane that has a row writes and reads it
+// here; memory is written and read rows side by side.  16-byte pieces are placed
+// so that neither a lane's going along its row nor the lanes' going along one
+// meets a bank twice: 32 rows of 64 bytes (32 values; room for two of these) have
+// piece c at c ^ (row / 2 & 3), 32 rows of 128 bytes (32 sums) at c ^ (row & 7).
+struct Corner {
+    uint8_t* at;
+    __device__ __forceinline__ uint4& piece(int row, int c) const { return *reinterpret_cast<uint4*>(at + row * 64 + ((c ^ (row >> 1 & 3)) << 4)); }
+    __device__ __forceinline__ uint16_t& value(int row, int c) const {
+        return *reinterpret_cast<uint16_t*>(at + row * 64 + (((c >> 3) ^ (row >> 1 & 3)) << 4) + (c & 7) * 2);
+    }
+    __device__ __forceinline__ uint4& sums(int row, int c) const { return *reinterpret_cast<uint4*>(at + row * 128 + ((c ^ (row & 7)) << 4)); }
+};
+
+// Where a block of 32 rows by 32 columns lies in a matrix of 16-bit values, and how it is moved.
+struct Place {
+    int64_t r0, c0, rows, cols;
+    int lane;
+    bool wide;  // all its columns are there, and 16 bytes of a row can be moved at a time
+    __device__ __forceinline__ int row(int i) const { return i * 8 + (lane >> 2); }  // of the i-th piece that this lane moves
+    template <class T> __device__ __forceinline__ T* at(T* m, int64_t stride, int i) const { return m + (r0 + row(i)) * stride + c0 + (lane & 3) * 8; }
+};
+template <class T>
+__device__ __forceinline__ void put_corner(Corner s, T* m, int64_t stride, const Place& q) {
+    if (q.wide) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (q.r0 + q.row(i) < q.rows) *reinterpret_cast<uint4*>(q.at(m, stride, i)) = s.piece(q.row(i), q.lane & 3);
+    } else if (q.c0 + q.lane < q.cols) {
+#pragma unroll 8
+        for (int r = 0; r < 32; ++r)
+            if (q.r0 + r < q.rows) reinterpret_cast<uint16_t*>(m)[(q.r0 + r) * stride + q.c0 + q.lane] = s.value(r, q.lane);
+    }
+}
+// A block of the residual: loaded ahead of its use, then put into the corner.
+template <class T>
+struct Ahead {
+    uint4 v[4];
+    __device__ __forceinline__ void load(const T* m, int64_t stride, const Place& q) {
+        if (!q.wide) return;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (q.r0 + q.row(i) < q.rows) v[i] = *reinterpret_cast<const uint4*>(q.at(m, stride, i));
+    }
+    __device__ __forceinline__ void settle(Corner s, const T* m, int64_t stride, const Place& q) const {
+        if (q.wide) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s.piece(q.row(i), q.lane & 3) = v[i];
+        } else if (q.c0 + q.lane < q.cols) {
+#pragma unroll 8
+            for (int r = 0; r < 32; ++r)
+                if (q.r0 + r < q.rows) s.value(r, q.lane) = reinterpret_cast<const uint16_t*>(m)[(q.r0 + r) * stride + q.c0 + q.lane];
+        }
+    }
+};
+
+// A warp's 32 rows of a tile's sums, from column c0 on, 32 columns at a time: out
+// of tensor memory and through the epilogue.  `wait` returns when the sums are
+// there; the residual's first block is on its way before that, each other while
+// the one before it is worked on.
+template <class T, class W>
+__device__ __forceinline__ bool put_blocks(const Product& p, uint32_t tmem, Corner corner, int64_t r0, int64_t c0, int blocks, int share, int lane, W wait) {
+    const Epilogue& e = p.e;
+    const Corner other = {corner.at + 2048};
+    const T* residual = static_cast<const T*>(e.residual);
+    auto place = [&](int b) { return Place{r0, c0 + b * 32, p.I, p.J, lane, e.wide && c0 + b * 32 + 32 <= p.J}; };
+    auto bias_of = [&](int b) {
+        const int64_t c = c0 + b * 32 + lane;
+        return c < p.J ? to_float(static_cast<const T*>(e.bias)[c]) : 0.f;
+    };
+    Ahead<T> ahead;
+    float bias = 0.f;
+    if (e.bias) bias = bias_of(0);
+    if (residual) ahead.load(residual, e.residual_stride, place(0));
+    if (!wait()) return false;
+#pragma unroll 1
+    for (int b = 0; b < blocks && c0 + b * 32 < p.J; ++b) {
+        const Place q = place(b);
+        uint32_t acc[32];
+        __syncwarp();
+        tmem_ld32(tmem + b * 32, acc);
+        if (e.part) {
+            tmem_wait_ld();
+            float* part = e.part + share * e.part_size;  // (rows of whole 16-byte pieces)
+#pragma unroll
+            for (int c = 0; c < 8; ++c) corner.sums(lane, c) = make_uint4(acc[4 * c], acc[4 * c + 1], acc[4 * c + 2], acc[4 * c + 3]);
+            __syncwarp();
+            const int c = lane & 7;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int r = i * 4 + (lane >> 3);
+                if (r0 + r < p.I && q.c0 + c * 4 < e.part_stride)
+                    *reinterpret_cast<uint4*>(part + (r0 + r) * e.part_stride + q.c0 + c * 4) = corner.sums(r, c);
+            }
+            __syncwarp();
+            continue;
+        }
+        if (e.bias) {
+            reinterpret_cast<float*>(corner.at)[lane] = bias;
+            if (b + 1 < blocks) bias = bias_of(b + 1);
+            __syncwarp();
+        }
+        tmem_wait_ld();
+        float2 v[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) v[k] = make_float2(__uint_as_float(acc[2 * k]), __uint_as_float(acc[2 * k + 1]));
+        if (e.bias) {
+#pragma unroll
+            for (int k = 0; k < 16; k += 2) {
+                const float4 x = reinterpret_cast<const float4*>(corner.at)[k / 2];
+                v[k] = add2(v[k], make_float2(x.x, x.y));
+                v[k + 1] = add2(v[k + 1], make_float2(x.z, x.w));
+            }
+            __syncwarp();
+        }
+        auto stage = [&] {
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                corner.piece(lane, c) = make_uint4(word_of_pair<T>(v[4 * c]), word_of_pair<T>(v[4 * c + 1]), word_of_pair<T>(v[4 * c + 2]), word_of_pair<T>(v[4 * c + 3]));
+            __syncwarp();
+        };
+        if (e.pre) {
+            stage();
+            put_corner(corner, static_cast<T*>(e.pre), e.pre_stride, q);
+        }
+        if (residual) {
+            ahead.settle(other, residual, e.residual_stride, q);
+            if (b + 1 < blocks) ahead.load(residual, e.residual_stride, place(b + 1));
+        }
+        by_act(e.act, [&](auto act) {
+#pragma unroll
+            for (int k = 0; k < 16; ++k) v[k] = activate<decltype(act)::value>(v[k]);
+        });
+        __syncwarp();
+        if (residual) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const uint4 x = other.piece(lane, c);
+                v[4 * c] = add2(v[4 * c], pair_of_word<T>(x.x));
+                v[4 * c + 1] = add2(v[4 * c + 1], pair_of_word<T>(x.y));
+                v[4 * c + 2] = add2(v[4 * c + 2], pair_of_word<T>(x.z));
+                v[4 * c + 3] = add2(v[4 * c + 3], pair_of_word<T>(x.w));
+            }
+        }
+        stage();
+        put_corner(corner, static_cast<T*>(e.out), e.out_stride, q);
+    }
+    return true;
+}
+
+// The shared memory of a block: the ring of operand tiles, and a corner for every
+// epilogue warp.
+// A pair of blocks has a tile of 256 rows between them, and half of its columns' operand each.
+template <int BN, bool SWAP, bool PAIR> struct Ring {
+    static constexpr int kEpilogue = SWAP || BN < 128 ? 4 : 8;  // warps
+    static constexpr int kThreads = (kEpilogue + 2) * 32;       // ... and the TMA warp, and the MMA warp
+    static constexpr int kA = kBM * kBK * 2, kB = (PAIR ? BN / 2 : BN) * kBK * 2, kStage = kA + kB;
+    static constexpr int kCorners = SWAP ? 0 : kEpilogue * 4096;
+    static constexpr int kFit = (kDenseSmem - 1024 - kCorners) / kStage;
+    static constexpr int kStages = kFit < 12 ? kFit : 12;
+    static constexpr int kBytes = kStages * kStage + kCorners + 1024;  // (aligned to 1,024 within)
     static constexpr uint32_t kColumns = 2 * BN < 32 ? 32 : 2 * BN;
 };
 
 // A_MN, B_MN: the operand's rows run along i (j), not k.  SWAP: i runs along
 // the output's columns (few rows: the weight is the operand of 128 rows a tile).
-template <int BN, bool A_MN, bool B_MN, bool SWAP>
-__global__ void __launch_bounds__(kThreads, 1)
+// PAIR: two blocks on neighbouring SMs share a tile of 256 rows.  Each holds its
+// own 128 rows of A, half of B's and its rows' sums; the first issues the
+// products of both, so that B crosses each SM's shared memory half as often.
+template <int BN, bool A_MN, bool B_MN, bool SWAP, bool PAIR, class T>
+__global__ void __launch_bounds__(Ring<BN, SWAP, PAIR>::kThreads, 1)
     k_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mb, const Product p) {
-    using R = Ring<BN>;
-    constexpr int S = R::kStages;
+    using R = Ring<BN, SWAP, PAIR>;
+    constexpr int S = R::kStages, kTma = R::kEpilogue, kMma = kTma + 1, kBlocks = PAIR ? 2 : 1, kCols = BN / kBlocks;
     extern __shared__ uint8_t raw[];
     __shared__ __align__(8) uint64_t bars[2 * S + 4];
     __shared__ uint32_t tmem_at;
@@ -178,6 +319,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t ring = (smem_of(raw) + 1023u) & ~1023u;
     const uint32_t full = smem_of(bars), empty = full + 8 * S, done = empty + 8 * S, drained = done + 16;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = PAIR ? cluster_rank() : 0;
     if (threadIdx.x == 0) {
         for (int s = 0; s < S; ++s) {
             mbar_init(full + 8 * s, 1);
@@ -185,53 +327,60 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         for (int s = 0; s < 2; ++s) {
             mbar_init(done + 8 * s, 1);
-            mbar_init(drained + 8 * s, 128);
+            mbar_init(drained + 8 * s, kBlocks * R::kEpilogue);
         }
         stop = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         tma_prefetch(&ma);
         tma_prefetch(&mb);
     }
-    if (warp == 5) tmem_alloc(smem_of(&tmem_at), R::kColumns);
+    if (warp == kMma) tmem_alloc<PAIR>(smem_of(&tmem_at), R::kColumns);
     tc_fence_before();
     __syncthreads();
+    if (PAIR) cluster_sync();
     tc_fence_after();
     const uint32_t tmem = tmem_at;
     pdl_enter();
 
-    const int total = p.tiles_i * p.tiles_j * p.shares;
-    if (warp == 4) {
+    const int total = p.tiles_i * p.tiles_j * p.shares, first = blockIdx.x / kBlocks, step = gridDim.x / kBlocks;
+    if (warp == kTma) {
         if (lane == 0) {
             uint32_t n = 0;  // stages filled
             bool ok = true;
-            for (int t = blockIdx.x; t < total && ok; t += gridDim.x) {
+            for (int t = first; t < total && ok; t += step) {
                 int i, j, share;
                 tile_at(p, t, i, j, share);
                 const int k0 = share * p.blocks_per_share, k1 = min(p.blocks, k0 + p.blocks_per_share);
+                const int row = (i * kBlocks + (int)rank) * kBM, col = j * BN + (int)rank * kCols;
                 for (int k = k0; k < k1; ++k, ++n) {
-                    const uint32_t s = n % S, at = ring + s * R::kStage, bar = full + 8 * s;
+                    const uint32_t s = n % S, at = ring + s * R::kStage;
                     if (n >= S && !(ok = mbar_wait(empty + 8 * s, (n / S - 1) & 1, &stop))) break;
-                    mbar_expect(bar, R::kStage);
+                    if (rank == 0) mbar_expect(full + 8 * s, kBlocks * R::kStage);
+                    const uint32_t bar = PAIR ? place_in(full + 8 * s, 0) : full + 8 * s;
+                    auto load = [&](uint32_t to, const CUtensorMap* m, int x, int y) {
+                        if (PAIR) tma_load_pair(to, m, x, y, bar);
+                        else tma_load(to, m, x, y, bar);
+                    };
                     if (A_MN)
-                        for (int b = 0; b < kBM / 64; ++b) tma_load(at + b * 8192, &ma, i * kBM + b * 64, k * kBK, bar);
+                        for (int b = 0; b < kBM / 64; ++b) load(at + b * 8192, &ma, row + b * 64, k * kBK);
                     else
-                        tma_load(at, &ma, k * kBK, i * kBM, bar);
+                        load(at, &ma, k * kBK, row);
                     if (B_MN)
-                        for (int b = 0; b < BN / 64; ++b) tma_load(at + R::kA + b * 8192, &mb, j * BN + b * 64, k * kBK, bar);
+                        for (int b = 0; b < kCols / 64; ++b) load(at + R::kA + b * 8192, &mb, col + b * 64, k * kBK);
                     else
-                        tma_load(at + R::kA, &mb, k * kBK, j * BN, bar);
+                        load(at + R::kA, &mb, k * kBK, col);
                 }
             }
-            if (!ok) {  // given up: the copies in flight still write into this block's shared memory
+            if (!ok && rank == 0) {  // given up: the copies in flight still write into shared memory
                 for (uint32_t b = n > S ? n - S : 0; b < n; ++b)
                     for (uint32_t tries = 0; tries < 1u << 20 && !mbar_try(full + 8 * (b % S), (b / S) & 1); ++tries) {}
             }
         }
-    } else if (warp == 5) {
-        if (lane == 0) {
+    } else if (warp == kMma) {
+        if (lane == 0 && rank == 0) {
             uint32_t n = 0, u = 0;  // stages read, accumulators used
             bool ok = true;
-            for (int t = blockIdx.x; t < total && ok; t += gridDim.x, ++u) {
+            for (int t = first; t < total && ok; t += step, ++u) {
                 int i, j, share;
                 tile_at(p, t, i, j, share);
                 const int k0 = share * p.blocks_per_share, k1 = min(p.blocks, k0 + p.blocks_per_share);
@@ -245,38 +394,55 @@ __global__ void __launch_bounds__(kThreads, 1)
                     const uint64_t da = smem_desc(at, A_MN ? 8192 : 16), db = smem_desc(at + R::kA, B_MN ? 8192 : 16);
 #pragma unroll
                     for (int q = 0; q < kBK / 16; ++q)  // 16 values along k: 32 bytes of a row, or 16 rows
-                        tc_mma(d, da + q * (A_MN ? 128 : 2), db + q * (B_MN ? 128 : 2), p.idesc, k > k0 || q > 0);
-                    tc_commit(empty + 8 * s);
+                        tc_mma<PAIR>(d, da + q * (A_MN ? 128 : 2), db + q * (B_MN ? 128 : 2), p.idesc, k > k0 || q > 0);
+                    tc_commit<PAIR>(empty + 8 * s);
                 }
-                if (ok) tc_commit(done + 8 * acc);
+                if (ok) tc_commit<PAIR>(done + 8 * acc);
             }
         }
     } else {
         uint32_t u = 0;
-        for (int t = blockIdx.x; t < total; t += gridDim.x, ++u) {
+        const uint32_t told = PAIR ? place_in(drained, 0) : drained;
+        for (int t = first; t < total; t += step, ++u) {
             int i, j, share;
             tile_at(p, t, i, j, share);
-            const uint32_t acc = u & 1, at = tmem + acc * BN + ((uint32_t)warp << 21);
-            if (!__all_sync(0xffffffffu, mbar_wait(done + 8 * acc, (u / 2) & 1, &stop))) break;
-            tc_fence_after();
-            const int64_t row_i = (int64_t)i * kBM + warp * 32 + lane;
-            for (int c = 0; c < BN; c += 16) {
-                uint32_t r[16];
-                __syncwarp();
-                tmem_ld16(at + c, r);
-                tmem_wait_ld();
-                if (row_i < p.I) put16<SWAP>(p, r, row_i, (int64_t)j * BN + c, share);
+            const uint32_t acc = u & 1, at = tmem + acc * BN + ((uint32_t)(warp & 3) << 21);
+            auto wait = [&] {
+                const bool ok = __all_sync(0xffffffffu, mbar_wait(done + 8 * acc, (u / 2) & 1, &stop));
+                tc_fence_after();
+                return ok;
+            };
+            const int64_t r0 = ((int64_t)i * kBlocks + rank) * kBM + (warp & 3) * 32;
+            if constexpr (SWAP) {
+                if (!wait()) break;
+#pragma unroll 1
+                for (int c = 0; c < BN; c += 16) {
+                    uint32_t r[16];
+                    __syncwarp();
+                    tmem_ld16(at + c, r);
+                    tmem_wait_ld();
+                    if (r0 + lane < p.I) put_columns<T>(p, r, r0 + lane, (int64_t)j * BN + c, share);
+                }
+            } else {
+                const int cols = BN * 4 / R::kEpilogue, c = (warp >> 2) * cols;  // this warp's
+                const Corner corner = {reinterpret_cast<uint8_t*>(raw) + (ring - smem_of(raw)) + S * R::kStage + warp * 4096};
+                if (!put_blocks<T>(p, at + c, corner, r0, (int64_t)j * BN + c, r0 < p.I ? cols / 32 : 0, share, lane, wait)) break;
             }
             __syncwarp();
             tc_fence_before();
-            mbar_arrive(drained + 8 * acc);
+            __syncwarp();
+            if (lane == 0) {
+                if (PAIR) mbar_arrive_in(told + 8 * acc);
+                else mbar_arrive(told + 8 * acc);
+            }
         }
     }
     tc_fence_before();
     __syncthreads();
+    if (PAIR) cluster_sync();  // nothing of the other block's is on its way here any more
     tc_fence_after();
     if (threadIdx.x == 0 && stop) atomicMax(&g_status, (uint32_t)MLKV_ERR_TIMEOUT);
-    if (warp == 5) tmem_free(tmem, R::kColumns);
+    if (warp == kMma) tmem_free<PAIR>(tmem, R::kColumns);
 }
 
 // The shares of k added up in order, and the epilogue (shares == 0: of zeros).
@@ -308,45 +474,67 @@ __global__ void __launch_bounds__(256) k_align(const uint16_t* __restrict__ in, 
 // p = dy act'(z), and the sums of its columns over a block's rows.  A thread
 // takes V columns, a block 32 V columns of a share of the rows.
 struct Slope {
-    const uint16_t* dy;
-    const uint16_t* pre;
-    uint16_t* p;       // null: not wanted (p is dy)
+    const void* dy;
+    const void* pre;
+    void* p;           // null: not wanted (p is dy)
     float* part;       // [shares][cols], null with one share or no sums
     void* dbias;
     int64_t dy_stride, pre_stride, p_stride, rows, cols, share;
-    int32_t type, act;
+    int32_t act;
 };
-template <int V>
+template <int V, class T>
 __global__ void __launch_bounds__(256) k_slope(Slope a) {
     pdl_enter();
     __shared__ float sums[8][32 * V];
+    constexpr int H = (V + 1) / 2;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t c = (blockIdx.x * 32ll + lane) * V;
     const int64_t r0 = blockIdx.y * a.share, r1 = min(a.rows, r0 + a.share);
-    float s[V];
+    float2 s[H];
 #pragma unroll
-    for (int q = 0; q < V; ++q) s[q] = 0.f;
+    for (int q = 0; q < H; ++q) s[q] = splat2(0.f);
+    using Row = Pack<uint16_t, V>;
+    const T* dy = static_cast<const T*>(a.dy) + c;
+    const T* pre = static_cast<const T*>(a.pre) + c;
+    auto pair = [](const Row& x, int q) {
+        if constexpr (V == 1) return make_float2(pair_of_word<T>(x.v[0]).x, 0.f);
+        else return pair_of_word<T>(reinterpret_cast<const uint32_t*>(&x)[q]);
+    };
+    constexpr int kRows = 4;  // on their way at a time
     if (c < a.cols)
-        for (int64_t r = r0 + warp; r < r1; r += 8) {
-            const Pack<uint16_t, V> d = *reinterpret_cast<const Pack<uint16_t, V>*>(a.dy + r * a.dy_stride + c);
-            Pack<uint16_t, V> o = d;
-            if (a.act != MLKV_ACT_NONE) {
-                const Pack<uint16_t, V> z = *reinterpret_cast<const Pack<uint16_t, V>*>(a.pre + r * a.pre_stride + c);
+        for (int64_t r = r0 + warp; r < r1; r += 8 * kRows) {
+            Row d[kRows], z[kRows];
 #pragma unroll
-                for (int q = 0; q < V; ++q) {
-                    const float v = widen(a.type, d.v[q]) * slope(a.act, widen(a.type, z.v[q]));
-                    o.v[q] = narrow(a.type, v);
-                    s[q] += v;
-                }
-            } else {
-#pragma unroll
-                for (int q = 0; q < V; ++q) s[q] += widen(a.type, d.v[q]);
+            for (int i = 0; i < kRows; ++i) {
+                if (r + 8 * i >= r1) continue;
+                d[i] = *reinterpret_cast<const Row*>(dy + (r + 8 * i) * a.dy_stride);
+                if (a.act != MLKV_ACT_NONE) z[i] = *reinterpret_cast<const Row*>(pre + (r + 8 * i) * a.pre_stride);
             }
-            if (a.p) *reinterpret_cast<Pack<uint16_t, V>*>(a.p + r * a.p_stride + c) = o;
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) {
+                if (r + 8 * i >= r1) continue;
+                if (a.act == MLKV_ACT_NONE) {
+#pragma unroll
+                    for (int q = 0; q < H; ++q) s[q] = add2(s[q], pair(d[i], q));
+                }
+                by_act(a.act, [&](auto act) {
+#pragma unroll
+                    for (int q = 0; q < H; ++q) {
+                        const float2 v = mul2(pair(d[i], q), slope<decltype(act)::value>(pair(z[i], q)));
+                        s[q] = add2(s[q], v);
+                        if constexpr (V == 1) d[i].v[0] = (uint16_t)word_of_pair<T>(v);
+                        else reinterpret_cast<uint32_t*>(&d[i])[q] = word_of_pair<T>(v);
+                    }
+                });
+                if (a.p) *reinterpret_cast<Row*>(static_cast<T*>(a.p) + (r + 8 * i) * a.p_stride + c) = d[i];
+            }
         }
     if (!a.dbias) return;
 #pragma unroll
-    for (int q = 0; q < V; ++q) sums[warp][lane * V + q] = s[q];
+    for (int q = 0; q < H; ++q) {
+        sums[warp][lane * V + 2 * q] = s[q].x;
+        if (2 * q + 1 < V) sums[warp][lane * V + 2 * q + 1] = s[q].y;
+    }
     __syncthreads();
     for (int q = threadIdx.x; q < 32 * V; q += 256) {
         const int64_t col = blockIdx.x * 32ll * V + q;
@@ -355,16 +543,23 @@ __global__ void __launch_bounds__(256) k_slope(Slope a) {
 #pragma unroll
         for (int w = 0; w < 8; ++w) t += sums[w][q];
         if (a.part) a.part[blockIdx.y * a.cols + col] = t;
-        else static_cast<uint16_t*>(a.dbias)[col] = narrow(a.type, t);
+        else static_cast<T*>(a.dbias)[col] = from_float<T>(t);
     }
 }
-__global__ void __launch_bounds__(256) k_column_sums(const float* __restrict__ part, int shares, int64_t cols, void* out, int32_t type) {
+// The shares' sums of 32 columns, added up by 32 warps of which each takes every 32nd share, then over the warps.
+__global__ void __launch_bounds__(1024) k_column_sums(const float* __restrict__ part, int shares, int64_t cols, void* out, int32_t type) {
     pdl_enter();
-    const int64_t c = blockIdx.x * 256ll + threadIdx.x;
-    if (c >= cols) return;
+    __shared__ float s[32][33];
+    const int64_t c = blockIdx.x * 32ll + (threadIdx.x & 31);
+    const int w = threadIdx.x >> 5;
     float t = 0.f;
-    for (int s = 0; s < shares; ++s) t += part[s * cols + c];
-    static_cast<uint16_t*>(out)[c] = narrow(type, t);
+    if (c < cols)
+        for (int b = w; b < shares; b += 32) t += part[b * cols + c];
+    s[w][threadIdx.x & 31] = t;
+    __syncthreads();
+    t = group_sum(s[threadIdx.x & 31][w], 32);  // warp w: column w of the block's
+    const int64_t o = blockIdx.x * 32ll + w;
+    if ((threadIdx.x & 31) == 0 && o < cols) static_cast<uint16_t*>(out)[o] = narrow(type, t);
 }
 
 // --- host ----------------------------------------------------------------------
@@ -430,18 +625,47 @@ struct Caller {
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
     }
 
-    template <int BN, bool A_MN, bool B_MN, bool SWAP>
+    template <int BN, bool A_MN, bool B_MN, bool SWAP, bool PAIR = false>
     void launch(const Matrix& a, const Matrix& b, Product p) {
+        using R = Ring<BN, SWAP, PAIR>;
         CUtensorMap ma, mb;
-        auto kernel = k_product<BN, A_MN, B_MN, SWAP>;
-        if (!encode(&ma, a, A_MN, kBM) || !encode(&mb, b, B_MN, BN) ||
-            cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Ring<BN>::kBytes) != cudaSuccess) {
+        if (!encode(&ma, a, A_MN, kBM) || !encode(&mb, b, B_MN, PAIR ? BN / 2 : BN)) {
             rc = MLKV_ERR_CUDA;
             return;
         }
-        p.idesc = mma_desc(type == MLKV_TYPE_BFLOAT, A_MN, B_MN, kBM, BN);
+        p.idesc = mma_desc(type == MLKV_TYPE_BFLOAT, A_MN, B_MN, PAIR ? 2 * kBM : kBM, BN);
         const int64_t tiles = (int64_t)p.tiles_i * p.tiles_j * p.shares;
-        launch_kernel(true, kernel, dim3((unsigned)std::min<int64_t>(tiles, sms)), dim3(kThreads), Ring<BN>::kBytes, st, ma, mb, p);
+        auto go = [&](auto kernel) {
+            if (!dense_smem(kernel, R::kBytes)) rc = MLKV_ERR_CUDA;
+            else if (PAIR) launch_pairs(kernel, std::min<int64_t>(tiles, sms / 2), R::kThreads, R::kBytes, ma, mb, p);
+            else launch_kernel(true, kernel, dim3((unsigned)std::min<int64_t>(tiles, sms)), dim3(R::kThreads), R::kBytes, st, ma, mb, p);
+        };
+        if (type == MLKV_TYPE_BFLOAT) go(k_product<BN, A_MN, B_MN, SWAP, PAIR, __nv_bfloat16>);
+        else go(k_product<BN, A_MN, B_MN, SWAP, PAIR, __half>);
+    }
+    template <class K>
+    void launch_pairs(K kernel, int64_t pairs, int threads, size_t smem, const CUtensorMap& ma, const CUtensorMap& mb, const Product& p) {
+        cudaLaunchAttribute attr[2];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = 2;
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[1].val.programmaticStreamSerializationAllowed = 1;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)(2 * pairs));
+        cfg.blockDim = dim3(threads);
+        cfg.dynamicSmemBytes = smem;
+        cfg.stream = st;
+        cfg.attrs = attr;
+        cfg.numAttrs = MLKV_PDL ? 2 : 1;
+        cudaLaunchKernelEx(&cfg, kernel, ma, mb, p);  // an error stays in cudaGetLastError()
+    }
+
+    // Whether pairs of blocks take the tiles of 256 columns: where there are enough for every pair, and k is long
+    // enough for the products to count beside the epilogue.  (Single blocks / pairs, us: 16,384 x 4,096 by k = 4,096
+    // 331 / 298; 8,192 x 1,024 by 8,192 102 / 86; 4,096 x 4,096 by 1,024 32 / 29; 65,536 x 512 by 416 37 / 42.)
+    bool pair_pays(int64_t tiles_i, int64_t tiles_j, int64_t blocks) const {
+        return (tiles_i + 1) / 2 * tiles_j >= sms / 2 && blocks >= 12;
     }
 
     // out = epilogue(A B^T): A [rows][k], B [cols][k]; *_mn: held as [k][rows], [k][cols].
@@ -464,21 +688,22 @@ struct Caller {
         p.I = (int32_t)(swap ? cols : rows);
         p.J = (int32_t)(swap ? rows : cols);
         p.blocks = (int32_t)((k + kBK - 1) / kBK);
-        p.tiles_i = (p.I + kBM - 1) / kBM;
         p.tiles_j = (p.J + bn - 1) / bn;
+        const bool pair = !swap && bn == 256 && pair_pays((p.I + kBM - 1) / kBM, p.tiles_j, p.blocks);
+        p.tiles_i = (p.I + (pair ? 2 * kBM : kBM) - 1) / (pair ? 2 * kBM : kBM);
         if ((int64_t)p.tiles_i * p.tiles_j >= (int64_t)1 << 30) {
             rc = MLKV_ERR_UNSUPPORTED;
             return;
         }
         // too few tiles for the GPU: k in shares of at least 4 blocks
         const int64_t tiles = (int64_t)p.tiles_i * p.tiles_j;
-        int64_t shares = std::max<int64_t>(1, std::min<int64_t>(sms / tiles, p.blocks / 4));
+        int64_t shares = std::max<int64_t>(1, std::min<int64_t>((pair ? sms / 2 : sms) / tiles, p.blocks / 4));
         p.blocks_per_share = (int32_t)((p.blocks + shares - 1) / shares);
         p.shares = (p.blocks + p.blocks_per_share - 1) / p.blocks_per_share;
         p.e = e;
         if (p.shares > 1) {
-            p.e.part_stride = cols;
-            p.e.part_size = rows * cols;
+            p.e.part_stride = round_up(cols, 4);
+            p.e.part_size = rows * p.e.part_stride;
             p.e.part = static_cast<float*>(arena.take(p.shares * p.e.part_size * 4));
         }
         if (!run) return;
@@ -492,6 +717,7 @@ struct Caller {
         if (!swap) {
             if (bn == 64) launch<64, A_MN, B_MN, false>(a, b, p);
             else if (bn == 128) launch<128, A_MN, B_MN, false>(a, b, p);
+            else if (pair) launch<256, A_MN, B_MN, false, true>(a, b, p);
             else launch<256, A_MN, B_MN, false>(a, b, p);
         }
         if (p.shares > 1) {
@@ -514,14 +740,14 @@ struct Caller {
         const bool copy = products && (act || !p.aligned());
         if (g.m && g.n && (copy || g.d_dbias)) {
             Slope s = {};
-            s.dy = p.p; s.dy_stride = g.dy_stride; s.pre = (const uint16_t*)g.d_pre; s.pre_stride = g.pre_stride;
-            s.rows = g.m; s.cols = g.n; s.type = type; s.act = g.activation; s.dbias = g.d_dbias;
+            s.dy = p.p; s.dy_stride = g.dy_stride; s.pre = g.d_pre; s.pre_stride = g.pre_stride;
+            s.rows = g.m; s.cols = g.n; s.act = g.activation; s.dbias = g.d_dbias;
             if (copy) {
                 s.p_stride = round_up(g.n, 8);
-                s.p = static_cast<uint16_t*>(arena.take(g.m * s.p_stride * 2));
-                p = {s.p, s.p_stride, g.m, g.n};
+                s.p = arena.take(g.m * s.p_stride * 2);
+                p = {static_cast<const uint16_t*>(s.p), s.p_stride, g.m, g.n};
             }
-            const Matrix dy = {s.dy, s.dy_stride, 0, 0}, pre = {s.pre, s.pre_stride, 0, 0};
+            const Matrix dy = {(const uint16_t*)s.dy, s.dy_stride, 0, 0}, pre = {(const uint16_t*)s.pre, s.pre_stride, 0, 0};
             const int V = g.n % 8 == 0 && dy.aligned() && (!act || pre.aligned()) ? 8 : 1;
             const int64_t across = (g.n + 32 * V - 1) / (32 * V);
             const int64_t shares = std::max<int64_t>(1, std::min<int64_t>((g.m + 31) / 32, 8ll * sms / across));
@@ -530,9 +756,10 @@ struct Caller {
             if (g.d_dbias && down > 1) s.part = static_cast<float*>(arena.take((int64_t)down * g.n * 4));
             if (run) {
                 const dim3 grid((unsigned)across, down);
-                if (V == 8) launch_kernel(true, k_slope<8>, grid, dim3(256), 0, st, s);
-                else launch_kernel(true, k_slope<1>, grid, dim3(256), 0, st, s);
-                if (s.part) launch_kernel(true, k_column_sums, dim3((unsigned)((g.n + 255) / 256)), dim3(256), 0, st,
+                const bool b = type == MLKV_TYPE_BFLOAT;
+                if (V == 8) launch_kernel(true, b ? k_slope<8, __nv_bfloat16> : k_slope<8, __half>, grid, dim3(256), 0, st, s);
+                else launch_kernel(true, b ? k_slope<1, __nv_bfloat16> : k_slope<1, __half>, grid, dim3(256), 0, st, s);
+                if (s.part) launch_kernel(true, k_column_sums, dim3((unsigned)((g.n + 31) / 32)), dim3(1024), 0, st,
                                           (const float*)s.part, (int)down, g.n, g.d_dbias, type);
             }
         } else if (run && g.d_dbias && g.n) {
