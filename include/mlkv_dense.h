@@ -61,7 +61,7 @@ extern "C" {
  * x_type: any; y_type: x_type, or any when x_type is MLKV_TYPE_FLOAT (the
  * store's rows enter 16-bit arithmetic here).  d_weight, d_bias: [dim] of
  * w_type, either may be null (1, 0).  d_stats: null, or fp32 [rows][2], which
- * takes each row's (mu, 1 / sqrt(v + eps)) for the backward pass.  rows >= 0,
+ * takes each row's (mu, 1 / sqrt(v + eps)) for the backward pass.  0 <= rows < 2^30,
  * 1 <= dim < 2^20, eps >= 0.  d_y may be d_x where types and strides agree. */
 int mlkv_layer_norm(const void* d_x, int64_t x_stride, int32_t x_type, int64_t rows, int64_t dim,
                     const void* d_weight, const void* d_bias, int32_t w_type, float eps, void* d_y,

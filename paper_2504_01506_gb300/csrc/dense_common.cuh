@@ -139,6 +139,18 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(as_x2(a)), "l"(as_x2(b)), "l"(as_x2(c)));
     return of_x2(r);
 }
+
+// N bytes (4, 8 or 16, aligned) on their way into shared memory.
+template <int N>
+__device__ __forceinline__ void copy_async(void* to, const void* from) {
+    const uint32_t at = (uint32_t)__cvta_generic_to_shared(to);
+    if constexpr (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at), "l"(from) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(at), "l"(from), "n"(N) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
 // Sum over groups of G lanes (a power of two): every lane gets its group's.
 __device__ __forceinline__ float group_sum(float x, int G) {
     for (int o = G >> 1; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);

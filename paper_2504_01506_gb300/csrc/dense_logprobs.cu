@@ -140,10 +140,6 @@ __device__ __forceinline__ float exp2_fast(float x) {
     return r;
 }
 
-__device__ __forceinline__ void copy_async16(void* to, const void* from) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
-}
-
 // A row's values in 16-byte pieces: the first begins at or before the row's
 // first value, on a 16-byte boundary; the values outside the row are not read.
 template <class T>
@@ -312,16 +308,16 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprobs(ProbArgs a
         if (base > 0 && base + kStep <= min(p1, row.count - 1)) {
             const uint4* from = reinterpret_cast<const uint4*>(row.first) + base + threadIdx.x;
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i) copy_async16(to + i * THREADS, from + i * THREADS);
+            for (int i = 0; i < kBatch; ++i) copy_async<16>(to + i * THREADS, from + i * THREADS);
         } else {
 #pragma unroll 1
             for (int i = 0; i < kBatch; ++i) {
                 const int p = base + i * THREADS + (int)threadIdx.x;
-                if (p < p1 && row.whole(p)) copy_async16(to + i * THREADS, reinterpret_cast<const uint4*>(row.first) + p);
+                if (p < p1 && row.whole(p)) copy_async<16>(to + i * THREADS, reinterpret_cast<const uint4*>(row.first) + p);
                 else to[i * THREADS] = p < p1 ? row.load(p) : make_uint4(f, f, f, f);
             }
         }
-        asm volatile("cp.async.commit_group;" ::: "memory");
+        copy_commit();
     };
 #pragma unroll
     for (int i = 0; i < kStages - 1; ++i) fetch(p0 + i * kStep, i);
@@ -361,7 +357,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprobs(ProbArgs a
     int batch = 0, stage = 0;
     for (int base = p0; base < p1; base += kStep, ++batch) {
         fetch(base + (kStages - 1) * kStep, stage == 0 ? kStages - 1 : stage - 1);
-        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+        copy_wait<kStages - 1>();
         uint4 q[kBatch];
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) q[i] = ring[stage * kStep + i * THREADS];
@@ -409,7 +405,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprobs(ProbArgs a
         sum.s = s2.x + s2.y;
         sum.p = t2.x + t2.y;
     }
-    asm volatile("cp.async.wait_all;" ::: "memory");
+    copy_wait<0>();
     // the block's largest value, and its sums against it
     tell();
     __syncthreads();

@@ -10,79 +10,100 @@ using namespace mlkv;
 
 namespace {
 
-// Most values a lane holds.  (65,536 rows of 2,048 in bf16: as fast with 64, which spills.)
-constexpr int kForwardValues = 32;
+constexpr int kForwardValues = 32;  // most values a lane holds
+constexpr int kForwardLanes = 256;   // a block's threads
+constexpr int kForwardBlocks = 3;    // blocks an SM: 80 registers a thread
 
-// A block's teams take rows in turn; the weights are staged once a block.
-template <class TX, class TY, int V, int NV>
-__global__ void __launch_bounds__(kNormLanes, 2) k_norm(NormArgs a) {
+// A block's teams take rows in turn; the weights are staged once a block.  Rows
+// that are aligned come through shared memory, two of each team on their way (a
+// thread reads what it copied itself).  What a lane holds beyond the row's end is
+// a copy of its last vector, or 0, left out of the sums.
+template <class TX, class TY, int NV, bool ALIGNED>
+__global__ void __launch_bounds__(kForwardLanes, kForwardBlocks) k_norm(NormArgs a) {
     pdl_enter();
-    extern __shared__ float weights[];  // [2][dim]
-    __shared__ float2 buf[64];
-    constexpr int H = kPairs<V>;
-    const Team tm(a.lanes);
-    const int64_t step = (int64_t)gridDim.x * tm.count;
-    const int nvec = a.dim / V;
-    Values<TX, V> q[NV];
-    auto load = [&](int64_t r) {
-        const TX* x = static_cast<const TX*>(a.x) + r * a.x_stride;
+    extern __shared__ __align__(16) float weights[];  // [2][room]; then the rows on their way
+    __shared__ __align__(16) float2 buf[64];
+    constexpr int V = 16 / sizeof(TX), H = V / 2;
+    const Team tm(a.lanes, buf);
+    const int rows = (int)a.rows, step = (int)gridDim.x * tm.count;
+    const int nvec = (a.dim + V - 1) / V, room = tm.L * NV * V;
+    const Span span(static_cast<const TX*>(a.x), a.rows, a.x_stride, a.dim);
+    int at[NV];  // of this lane's vectors, the last one again where there are no more
+#pragma unroll
+    for (int i = 0; i < NV; ++i) at[i] = min(tm.lane + i * tm.L, nvec - 1) * V;
+    Values<TX, V, ALIGNED> q[NV];
+    uint4* ring = reinterpret_cast<uint4*>(weights + 2 * room) + threadIdx.x;
+    int r = (int)blockIdx.x * tm.count + tm.index, ahead = r;
+    const TX* x = static_cast<const TX*>(a.x) + r * a.x_stride;
+    TY* y = static_cast<TY*>(a.out) + r * a.out_stride;
+    const int64_t x_step = step * a.x_stride, y_step = step * a.out_stride;
+    // the next row not yet on its way: into slot `slot`, or (unaligned) registers
+    auto fetch = [&](int slot) {
+        if (ahead < rows) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                if constexpr (ALIGNED) copy_async<16>(ring + (slot * NV + i) * (int)blockDim.x, x + at[i]);
+                else q[i].load(x + at[i], a.dim - at[i], span);
+            }
+        }
+        if (ALIGNED) copy_commit();
+        x += x_step;
+        ahead += step;
+    };
+    fetch(0);
+    if (ALIGNED) fetch(1);
+    stage_weights<V>(weights, a.w, a.w_type, a.dim, room, 1.f);
+    stage_weights<V>(weights + room, a.b, a.w_type, a.dim, room, 0.f);
+    __syncthreads();
+    const float inverse = 1.f / (float)a.dim;
+    int slot = 0;
+    // the lanes of a warp take as many turns as its first team does
+    for (int first = tm.L < 32 ? r - (int)(threadIdx.x & 31) / tm.L : r; first < rows; first += step, r += step, y += y_step, slot ^= 1) {
+        float2 f[NV][H], s = both(0.f), v = both(0.f);
+        if constexpr (ALIGNED) copy_wait<kNormAhead - 1>();
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            if constexpr (ALIGNED) q[i].load(reinterpret_cast<const TX*>(ring + (slot * NV + i) * (int)blockDim.x), V, span);
+#pragma unroll
+            for (int k = 0; k < H; ++k) f[i][k] = q[i].pair(k);
+            if (tm.lane + i * tm.L < nvec)
+#pragma unroll
+                for (int k = 0; k < H; ++k) s = add2(s, f[i][k]);
+        }
+        const float mu = tm.sum(s.x + s.y, 0) * inverse;
+        if (ALIGNED || sizeof(TX) == 2) fetch(slot);  // (an unaligned fp32 row is too wide to have the next one beside it)
+        const float2 minus = both(-mu);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int j = tm.lane + i * tm.L;
-            q[i].zero();
-            if (r < a.rows && j < nvec) q[i].load(x + j * V);
+#pragma unroll
+            for (int k = 0; k < H; ++k) f[i][k] = add2(f[i][k], minus);
+            if (!ALIGNED && j == nvec - 1)
+#pragma unroll
+                for (int k = 0; k < H; ++k) {
+                    if (j * V + 2 * k >= a.dim) f[i][k].x = 0.f;
+                    if (j * V + 2 * k + 1 >= a.dim) f[i][k].y = 0.f;
+                }
+            if (j < nvec)
+#pragma unroll
+                for (int k = 0; k < H; ++k) v = fma2(f[i][k], f[i][k], v);
         }
-    };
-    int64_t r = (int64_t)blockIdx.x * tm.count + tm.index;
-    load(r);
-    if (a.w) stage_weights<V>(weights, a.w, a.w_type, a.dim);
-    if (a.b) stage_weights<V>(weights + a.dim, a.b, a.w_type, a.dim);
-    if (a.w || a.b) __syncthreads();
-    // the lanes of a warp take as many turns as its first team does
-    for (int64_t first = tm.L < 32 ? r - (threadIdx.x & 31) / tm.L : r; first < a.rows; first += step, r += step) {
-        const bool live = r < a.rows;
-        float2 s = both(0.f);
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int k = 0; k < H; ++k) s = add2(s, q[i].pair(k));
-        const float mu = tm.sum(s.x + s.y, buf, 0) / (float)a.dim;
-        const float2 minus = both(-mu);
-        float2 v = both(0.f);
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            if (tm.lane + i * tm.L >= nvec) continue;
-#pragma unroll
-            for (int k = 0; k < H; ++k) {
-                float2 d = add2(q[i].pair(k), minus);
-                if (V == 1) d.y = 0.f;
-                v = fma2(d, d, v);
-            }
-        }
-        const float rs = 1.f / sqrtf(tm.sum(v.x + v.y, buf, 1) / (float)a.dim + a.eps);
-        if (live) {
-            if (a.stats && tm.lane == 0) *reinterpret_cast<float2*>(a.stats + 2 * r) = make_float2(mu, rs);
-            TY* y = static_cast<TY*>(a.out) + r * a.out_stride;
+        const float rs = 1.f / sqrtf(tm.sum(v.x + v.y, 1) * inverse + a.eps);
+        if (r < rows) {
+            if (a.stats && tm.lane == 0) reinterpret_cast<float2*>(a.stats)[r] = make_float2(mu, rs);
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const int j = tm.lane + i * tm.L;
-                if (j >= nvec) continue;
                 float2 w[H], b[H];
-                if (a.w) weight_pairs<V>(weights, j, a.dim, w);
-                if (a.b) weight_pairs<V>(weights + a.dim, j, a.dim, b);
-                Values<TY, V> o;
+                weight_pairs<V>(weights, j, room, w);
+                weight_pairs<V>(weights + room, j, room, b);
+                Values<TY, V, ALIGNED> o;
 #pragma unroll
-                for (int k = 0; k < H; ++k) {
-                    float2 t = mul2(add2(q[i].pair(k), minus), both(rs));
-                    if (a.w && a.b) t = fma2(t, w[k], b[k]);
-                    else if (a.w) t = mul2(t, w[k]);
-                    else if (a.b) t = add2(t, b[k]);
-                    o.set(k, t);
-                }
-                o.store(y + j * V);
+                for (int k = 0; k < H; ++k) o.set(k, fma2(mul2(f[i][k], both(rs)), w[k], b[k]));
+                if (j < nvec) o.store(y + j * V, a.dim - j * V);
             }
         }
-        load(r + step);
+        if (!(ALIGNED || sizeof(TX) == 2)) fetch(0);
     }
 }
 
@@ -90,18 +111,19 @@ __global__ void __launch_bounds__(kNormLanes, 2) k_norm(NormArgs a) {
 template <class TX, class TY>
 __global__ void __launch_bounds__(kNormLongLanes) k_norm_long(NormArgs a) {
     pdl_enter();
-    __shared__ float2 buf[64];
-    const Team tm(kNormLongLanes);
+    __shared__ __align__(16) float2 buf[64];
+    const Team tm(kNormLongLanes, buf);
+    __syncthreads();
     const TX* x = static_cast<const TX*>(a.x) + blockIdx.x * a.x_stride;
     float s = 0.f, none = 0.f, v = 0.f;
     for (int j = tm.lane; j < a.dim; j += kNormLongLanes) s += to_float(x[j]);
-    tm.sum(s, none, buf, 0);
+    tm.sum(s, none, 0);
     const float mu = s / (float)a.dim;
     for (int j = tm.lane; j < a.dim; j += kNormLongLanes) {
         const float d = to_float(x[j]) - mu;
         v += d * d;
     }
-    tm.sum(v, none, buf, 1);
+    tm.sum(v, none, 1);
     const float rs = 1.f / sqrtf(v / (float)a.dim + a.eps);
     if (a.stats && tm.lane == 0) {
         a.stats[2 * blockIdx.x] = mu;
@@ -129,11 +151,12 @@ extern "C" int mlkv_layer_norm(const void* d_x, int64_t x_stride, int32_t x_type
     a.x = d_x; a.out = d_y; a.w = d_weight; a.b = d_bias; a.stats = d_stats;
     a.x_stride = x_stride; a.out_stride = y_stride; a.rows = rows; a.dim = (int32_t)dim; a.w_type = w_type; a.eps = eps;
     const int xs = dense_type_size(x_type), ys = dense_type_size(y_type);
-    const int V = norm_vector_width(dim, {{d_x, xs}, {d_y, ys}}, {x_stride, y_stride}, 16 / xs);
-    const NormShape sh = norm_shape(dim, V, kForwardValues);
+    const int V = 16 / xs;
+    const bool aligned = norm_aligned(d_x, x_stride, xs, dim, V) && norm_aligned(d_y, y_stride, ys, dim, V);
     cudaStream_t st = (cudaStream_t)stream;
     const int sms = dense_sms();
     if (!sms) return MLKV_ERR_CUDA;
+    const NormShape sh = norm_shape(rows, dim, V, kForwardValues, kForwardLanes, sms);
     bool ok = true;
     by_types(x_type, y_type, [&](auto tx, auto ty) {
         using TX = decltype(tx);
@@ -144,11 +167,11 @@ extern "C" int mlkv_layer_norm(const void* d_x, int64_t x_stride, int32_t x_type
         }
         a.lanes = sh.lanes;
         const int threads = norm_team_threads(sh.lanes), teams = threads / sh.lanes;
-        const size_t smem = d_weight || d_bias ? 2 * (size_t)dim * sizeof(float) : 0;
-        const int64_t resident = std::max<int64_t>(1, std::min<int64_t>(1024 / threads, (200 << 10) / (smem + 1)));
+        const size_t smem = 2 * (size_t)sh.lanes * sh.NV * V * sizeof(float) + (aligned ? (size_t)kNormAhead * sh.NV * threads * 16 : 0);
+        const int64_t resident = std::max<int64_t>(1, std::min<int64_t>(kForwardBlocks, kDenseSmem / (int64_t)(smem + 2048)));
         const unsigned blocks = (unsigned)std::min<int64_t>(sms * resident, (rows + teams - 1) / teams);
-        by_width<TX, kForwardValues>(V, sh.NV, [&](auto v, auto nv) {
-            auto kernel = k_norm<TX, TY, decltype(v)::value, decltype(nv)::value>;
+        by_shape<kForwardValues * (int)sizeof(TX) / 16>(sh.NV, aligned, [&](auto nv, auto al) {
+            auto kernel = k_norm<TX, TY, decltype(nv)::value, decltype(al)::value>;
             ok = dense_smem(kernel, smem);
             if (ok) launch_kernel(true, kernel, dim3(blocks), dim3(threads), smem, st, a);
         });

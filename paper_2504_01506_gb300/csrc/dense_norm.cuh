@@ -13,7 +13,7 @@
 namespace mlkv {
 
 constexpr int64_t kNormMaxDim = (int64_t)1 << 20;
-constexpr int kNormLanes = 512;       // most lanes of a team: 128 registers a thread
+constexpr int kNormLanes = 512;       // most lanes of a team
 constexpr int kNormLongLanes = 1024;  // lanes of the kernels of rows too long for registers
 
 struct NormArgs {
@@ -32,137 +32,234 @@ struct NormArgs {
     int32_t lanes;   // L: lanes per row, a power of two below 32 or a multiple of 32
 };
 
-// Weights, held as fp32 in shared memory: in order, or, for vectors of 8, the
-// first four values of every vector, then the last four (16-byte reads of
-// neighbouring lanes then lie side by side).
+// A lane's vectors are 16 bytes of x: V values.  Weights, held as fp32 in shared
+// memory: in order, or, for vectors of 8, the first four values of every vector,
+// then the last four (16-byte reads of neighbouring lanes then lie side by side).
+// `room` values, a multiple of V and at least dim; those past dim are 0, and
+// without a weight it is `none`.
 template <int V>
-__device__ __forceinline__ int weight_place(int c, int dim) {
-    return V == 8 ? (((c >> 2) & 1) * (dim / 8) + (c >> 3)) * 4 + (c & 3) : c;
+__device__ __forceinline__ int weight_place(int c, int room) {
+    return V == 8 ? (((c >> 2) & 1) * (room / 8) + (c >> 3)) * 4 + (c & 3) : c;
 }
 template <int V>
-__device__ __forceinline__ void stage_weights(float* to, const void* p, int32_t type, int dim) {
-    for (int c = threadIdx.x; c < dim; c += blockDim.x) to[weight_place<V>(c, dim)] = load_as_float(p, type, c);
+__device__ __forceinline__ void stage_weights(float* to, const void* p, int32_t type, int dim, int room, float none) {
+    for (int c = threadIdx.x; c < room; c += blockDim.x)
+        to[weight_place<V>(c, room)] = c >= dim ? 0.f : p ? load_as_float(p, type, c) : none;
+}
+template <int V>
+__device__ __forceinline__ void weight_pairs(const float* w, int j, int room, float2 (&o)[V / 2]) {
+#pragma unroll
+    for (int c = 0; c < V; c += 4) {
+        const float4 q = *reinterpret_cast<const float4*>(w + weight_place<V>(j * V + c, room));
+        o[c / 2] = make_float2(q.x, q.y);
+        o[c / 2 + 1] = make_float2(q.z, q.w);
+    }
 }
 
-// A vector of V values as it lies in memory, read and written in pairs (of one
-// value: it and 0).  Kept in 32-bit words: 16-bit values apart would take a
-// register each.
-template <int V> constexpr int kPairs = (V + 1) / 2;
-template <class T, int V> struct Values {
-    static constexpr int kWords = sizeof(T) * V / 4;
-    Pack<uint32_t, kWords> q;
-    __device__ __forceinline__ void load(const T* p) { q = *reinterpret_cast<const Pack<uint32_t, kWords>*>(p); }
-    __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<Pack<uint32_t, kWords>*>(p) = q; }
+// The memory that a matrix spans, from its first value to its last.
+struct Span {
+    uintptr_t from, to;
+    template <class T>
+    __device__ __forceinline__ Span(const T* p, int64_t rows, int64_t stride, int dim)
+        : from(reinterpret_cast<uintptr_t>(p)), to(reinterpret_cast<uintptr_t>(p + (rows - 1) * stride + dim)) {}
+};
+
+// V values as they lie in memory, read and written in pairs, kept in 32-bit words
+// (16-bit values apart would take a register each).  ALIGNED: on 16 bytes (of x;
+// 8 of a 16-bit y beside an fp32 x), and a row is whole vectors.  Else as wide as
+// the row's place allows (the same for all its vectors): 8 bytes, 4, or, with
+// 16-bit values off a word, the words around them, shifted.
+template <class T, int V, bool ALIGNED> struct Values {
+    static constexpr int W = sizeof(T) * V / 4, kBytes = sizeof(T) * V;
+    uint32_t w[W];
+
+    template <int N>
+    static __device__ __forceinline__ void read(const void* p, uint32_t* to) {
+        const Pack<uint32_t, N> q = *reinterpret_cast<const Pack<uint32_t, N>*>(p);
+#pragma unroll
+        for (int i = 0; i < N; ++i) to[i] = q.v[i];
+    }
+    // The first n values (the rest 0).
+    __device__ __forceinline__ void load(const T* p, int n, const Span& span) {
+        if constexpr (ALIGNED) {
+            read<W>(p, w);
+        } else {
+            const uint32_t* p32 = reinterpret_cast<const uint32_t*>(p);
+            const uint32_t by = (uint32_t)reinterpret_cast<uintptr_t>(p) & (kBytes - 1);
+            if (n < V) {
+                zero();
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    if (e >= n) continue;
+                    if constexpr (sizeof(T) == 4) w[e] = p32[e];
+                    else w[e / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[e] << (16 * (e & 1));
+                }
+            } else if (by == 0) {
+                read<W>(p, w);
+            } else if ((by & 7) == 0) {
+#pragma unroll
+                for (int i = 0; i < W; i += 2) read<2>(p32 + i, w + i);
+            } else if ((by & 3) == 0) {
+#pragma unroll
+                for (int i = 0; i < W; ++i) w[i] = p32[i];
+            } else {
+                // the words around; the values at the matrix's ends by themselves
+                const uint16_t* p16 = reinterpret_cast<const uint16_t*>(p);
+                const uint32_t* around = reinterpret_cast<const uint32_t*>(p16 - 1);
+                uint32_t v[W + 1];
+                v[0] = reinterpret_cast<uintptr_t>(p) > span.from ? around[0] : (uint32_t)p16[0] << 16;
+#pragma unroll
+                for (int i = 1; i < W; ++i) v[i] = around[i];
+                v[W] = reinterpret_cast<uintptr_t>(p + V) < span.to ? around[W] : p16[V - 1];
+#pragma unroll
+                for (int i = 0; i < W; ++i) w[i] = __funnelshift_r(v[i], v[i + 1], 16);
+            }
+        }
+    }
     __device__ __forceinline__ void zero() {
 #pragma unroll
-        for (int i = 0; i < kWords; ++i) q.v[i] = 0;
+        for (int i = 0; i < W; ++i) w[i] = 0;
+    }
+    // What was computed of the values is not to be kept for later: it takes more registers than they do.
+    __device__ __forceinline__ void forget() {
+#pragma unroll
+        for (int i = 0; i < W; ++i) asm volatile("" : "+r"(w[i]));
     }
     __device__ __forceinline__ float2 pair(int k) const {
-        if constexpr (sizeof(T) == 4) return make_float2(__uint_as_float(q.v[2 * k]), V > 1 ? __uint_as_float(q.v[V > 1 ? 2 * k + 1 : 0]) : 0.f);
-        else return pair_of_word<T>(q.v[k]);
+        if constexpr (sizeof(T) == 4) return make_float2(__uint_as_float(w[2 * k]), __uint_as_float(w[2 * k + 1]));
+        else return pair_of_word<T>(w[k]);
     }
     __device__ __forceinline__ void set(int k, float2 x) {
         if constexpr (sizeof(T) == 4) {
-            q.v[2 * k] = __float_as_uint(x.x);
-            if (V > 1) q.v[V > 1 ? 2 * k + 1 : 0] = __float_as_uint(x.y);
+            w[2 * k] = __float_as_uint(x.x);
+            w[2 * k + 1] = __float_as_uint(x.y);
         } else {
-            q.v[k] = word_of_pair<T>(x);
+            w[k] = word_of_pair<T>(x);
+        }
+    }
+    // The first n values.
+    __device__ __forceinline__ void store(T* p, int n) const {
+        if constexpr (ALIGNED) {
+            Pack<uint32_t, W> q;
+#pragma unroll
+            for (int i = 0; i < W; ++i) q.v[i] = w[i];
+            *reinterpret_cast<Pack<uint32_t, W>*>(p) = q;
+        } else {
+            const uint32_t by = (uint32_t)reinterpret_cast<uintptr_t>(p);
+            uint32_t* p32 = reinterpret_cast<uint32_t*>(p);
+            if (n >= V && !(by & (kBytes - 1))) {
+                Pack<uint32_t, W> q;
+#pragma unroll
+                for (int i = 0; i < W; ++i) q.v[i] = w[i];
+                *reinterpret_cast<Pack<uint32_t, W>*>(p) = q;
+            } else if (n >= V && !(by & 7)) {
+#pragma unroll
+                for (int i = 0; i < W; i += 2) *reinterpret_cast<uint2*>(p32 + i) = make_uint2(w[i], w[i + 1]);
+            } else if (n >= V && !(by & 3)) {
+#pragma unroll
+                for (int i = 0; i < W; ++i) p32[i] = w[i];
+            } else if constexpr (sizeof(T) == 2) {
+                uint16_t* p16 = reinterpret_cast<uint16_t*>(p);
+                if (n >= V) {  // two bytes off a word: a half, the words between, a half
+                    p16[0] = (uint16_t)w[0];
+#pragma unroll
+                    for (int i = 0; i + 1 < W; ++i) *reinterpret_cast<uint32_t*>(p16 + 1 + 2 * i) = __funnelshift_r(w[i], w[i + 1], 16);
+                    p16[V - 1] = (uint16_t)(w[W - 1] >> 16);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < V; ++e)
+                        if (e < n) p16[e] = (uint16_t)(w[e / 2] >> (16 * (e & 1)));
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < W; ++i)
+                    if (i < n) p32[i] = w[i];
+            }
         }
     }
 };
-template <class T> struct Half1 {
-    uint16_t q;
-    __device__ __forceinline__ void load(const T* p) { q = *reinterpret_cast<const uint16_t*>(p); }
-    __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<uint16_t*>(p) = q; }
-    __device__ __forceinline__ void zero() { q = 0; }
-    __device__ __forceinline__ float2 pair(int) const { return make_float2(pair_of_word<T>(q).x, 0.f); }
-    __device__ __forceinline__ void set(int, float2 x) { q = (uint16_t)word_of_pair<T>(make_float2(x.x, 0.f)); }
-};
-template <> struct Values<__nv_bfloat16, 1> : Half1<__nv_bfloat16> {};
-template <> struct Values<__half, 1> : Half1<__half> {};
-
-template <int V>
-__device__ __forceinline__ void weight_pairs(const float* w, int j, int dim, float2 (&o)[kPairs<V>]) {
-    if constexpr (V == 1) {
-        o[0] = make_float2(w[j], 0.f);
-    } else {
-        constexpr int H = V > 4 ? 4 : V;
-#pragma unroll
-        for (int c = 0; c < V; c += H) {
-            const Pack<float, H> q = *reinterpret_cast<const Pack<float, H>*>(w + weight_place<V>(j * V + c, dim));
-#pragma unroll
-            for (int k = 0; k < H / 2; ++k) o[c / 2 + k] = make_float2(q.v[2 * k], q.v[2 * k + 1]);
-        }
-    }
-}
 __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 
 // Where a thread stands in its block's teams.
 struct Team {
-    int L, lane, index, count, warps, warp;  // lanes a row; this lane; this team; teams a block; warps a team; this warp of it
-    __device__ explicit Team(int lanes)
-        : L(lanes), lane(threadIdx.x % lanes), index(threadIdx.x / lanes), count(blockDim.x / lanes),
-          warps(lanes / 32), warp((threadIdx.x % lanes) / 32) {}
-    // The sums of a and b over the team.  buf: 2 x 32 pairs of the block, used in turn (turn: 0, 1, 0, ...), so
-    // that one barrier a sum is enough: who writes a buffer again has seen all of its team past the next sum.
-    __device__ __forceinline__ void sum(float& a, float& b, float2* buf, int turn) const {
-        const int G = L < 32 ? L : 32;
-        for (int o = G >> 1; o; o >>= 1) {
+    int L, lane, index, count, warps;  // lanes a row; this lane; this team; teams a block; warps a team
+    float2* mine;                      // this team's place for its warps' sums: 2 x (8, or all 32) pairs
+    // sums: 64 pairs of the block.  (Followed by a barrier of the block before the first sum.)
+    __device__ Team(int lanes, float2* sums)
+        : L(lanes), lane(threadIdx.x % lanes), index(threadIdx.x / lanes), count(blockDim.x / lanes), warps(lanes / 32) {
+        mine = sums + (warps <= 8 ? index * 16 : 0);  // (at most 4 teams of several warps, one of more than 8)
+        for (int i = threadIdx.x; i < 64; i += blockDim.x) sums[i] = make_float2(0.f, 0.f);
+    }
+    // The sums of a and b over the team.  `turn` goes 0, 1, 0, ..., so that one barrier a sum is enough: who
+    // writes a place again has seen all of its team past the next sum.
+    __device__ __forceinline__ void sum(float& a, float& b, int turn) const {
+        if (L < 32) {
+            for (int o = L >> 1; o; o >>= 1) {
+                a += __shfl_xor_sync(0xffffffffu, a, o);
+                b += __shfl_xor_sync(0xffffffffu, b, o);
+            }
+            return;
+        }
+#pragma unroll
+        for (int o = 16; o; o >>= 1) {
             a += __shfl_xor_sync(0xffffffffu, a, o);
             b += __shfl_xor_sync(0xffffffffu, b, o);
         }
-        if (L <= 32) return;
-        float2* mine = buf + turn * 32 + index * warps;
-        if ((threadIdx.x & 31) == 0) mine[warp] = make_float2(a, b);
-        asm volatile("bar.sync %0, %1;" ::"r"(index + 1), "r"(L) : "memory");  // (at most 4 teams of several warps)
-        a = b = 0.f;
-        for (int i = 0; i < warps; ++i) {
-            const float2 q = mine[i];
-            a += q.x;
-            b += q.y;
+        if (L == 32) return;
+        float2* at = mine + turn * (warps <= 8 ? 8 : 32);
+        if ((threadIdx.x & 31) == 0) at[lane >> 5] = make_float2(a, b);
+        asm volatile("bar.sync %0, %1;" ::"r"(index + 1), "r"(L) : "memory");
+        float2 s = make_float2(0.f, 0.f);
+        if (warps <= 8) {  // (places without a warp hold 0)
+#pragma unroll
+            for (int i = 0; i < 4; i += 2) s = pair_sum(s, at + i);
+            if (warps > 4)
+#pragma unroll
+                for (int i = 4; i < 8; i += 2) s = pair_sum(s, at + i);
+        } else {
+            for (int i = 0; i < warps; ++i) s = add2(s, at[i]);
         }
+        a = s.x;
+        b = s.y;
     }
-    __device__ __forceinline__ float sum(float a, float2* buf, int turn) const {
+    static __device__ __forceinline__ float2 pair_sum(float2 s, const float2* two) {
+        const float4 q = *reinterpret_cast<const float4*>(two);
+        return add2(add2(s, make_float2(q.x, q.y)), make_float2(q.z, q.w));
+    }
+    __device__ __forceinline__ float sum(float a, int turn) const {
         float none = 0.f;
-        sum(a, none, buf, turn);
+        sum(a, none, turn);
         return a;
     }
 };
 
-// Values per vector: 16 bytes of the wider type, or as many as every row and
-// weight vector is aligned to.
-inline int norm_vector_width(int64_t dim, std::initializer_list<std::pair<const void*, int>> bases,
-                 std::initializer_list<int64_t> strides, int most) {
-    int v = most;
-    auto fits = [&](int n) {
-        if (dim % n) return false;
-        for (int64_t s : strides)
-            if (s % n) return false;
-        for (auto& b : bases)
-            if (reinterpret_cast<uintptr_t>(b.first) % (uintptr_t)std::min(16, n * b.second)) return false;
-        return true;
-    };
-    while (v > 1 && !fits(v)) v /= 2;
-    return v;
+// Whether rows are whole vectors of V values on their boundary.
+inline bool norm_aligned(const void* p, int64_t stride, int size, int64_t dim, int V) {
+    return !p || (reinterpret_cast<uintptr_t>(p) % (V * size) == 0 && stride % V == 0 && dim % V == 0);
 }
 
+constexpr int kNormAhead = 2;  // rows on their way into shared memory, where rows are aligned
+
 struct NormShape {
-    int V, NV, lanes;  // lanes == 0: the row does not fit
+    int NV, lanes;  // lanes == 0: the row does not fit
 };
-// The vectors a lane holds: as few lanes as hold the row with at most `most` values each.
-inline NormShape norm_shape(int64_t dim, int V, int most) {
-    const int64_t nvec = dim / V;
+// The vectors a lane holds: as many as `most` values allow, so that as few lanes
+// as can be share the sums over a row (their cost is per lane and row: 200,003
+// rows of 100 fp32 values take 64 us with one vector a lane, 39 with 2, 30 with
+// 4, 26 with 8); fewer where there are too few rows to fill the GPU that way.
+inline NormShape norm_shape(int64_t rows, int64_t dim, int V, int most, int most_lanes, int sms) {
+    const int64_t nvec = (dim + V - 1) / V;
+    auto lanes_of = [&](int nv) {
+        const int64_t n = (nvec + nv - 1) / nv;
+        int64_t p = 1;
+        while (p < n && p < 32) p *= 2;
+        return n <= 32 ? p : (n + 31) / 32 * 32;
+    };
     int nv = 1;
-    while (nv < 16 && nv * 2 * V <= most && nvec > (int64_t)32 * nv) nv *= 2;
-    int64_t lanes = (nvec + nv - 1) / nv;
-    if (lanes <= 32) {
-        int p = 1;
-        while (p < lanes) p *= 2;
-        lanes = p;
-    } else {
-        lanes = (lanes + 31) / 32 * 32;
-    }
-    return {V, nv, lanes > kNormLanes ? 0 : (int)lanes};
+    while (nv * 2 * V <= most && nv < nvec) nv *= 2;
+    while (nv > 1 && lanes_of(nv / 2) <= 32 && rows * lanes_of(nv) < 1024ll * sms) nv /= 2;
+    const int64_t lanes = lanes_of(nv);
+    return {nv, lanes > most_lanes ? 0 : (int)lanes};
 }
 
 template <class F>
@@ -177,30 +274,23 @@ bool by_types(int32_t x_type, int32_t y_type, F f) {
     return false;
 }
 template <int N> struct Int { static constexpr int value = N; };
-// f(values a vector, vectors a lane), of which a lane holds at most MOST values.
-template <class T, int MOST, class F>
-void by_width(int V, int NV, F f) {
-    auto nv = [&](auto v) {
-        constexpr int w = decltype(v)::value;
-        if (NV == 1) f(v, Int<1>{});
-        else if (NV == 2) f(v, Int<2>{});
-        else if constexpr (4 * w <= MOST) {
-            if (NV == 4) f(v, Int<4>{});
-            else if constexpr (8 * w <= MOST) {
-                if (NV == 8) f(v, Int<8>{});
-                else if constexpr (16 * w <= MOST) f(v, Int<16>{});
-            }
+// f(vectors a lane, whether rows are aligned).
+template <int MOST_NV, class F>
+void by_shape(int NV, bool aligned, F f) {
+    auto nv = [&](auto al) {
+        if (NV == 1) f(Int<1>{}, al);
+        else if (NV == 2) f(Int<2>{}, al);
+        else if constexpr (MOST_NV >= 4) {
+            if (NV == 4) f(Int<4>{}, al);
+            else if constexpr (MOST_NV >= 8) f(Int<8>{}, al);
         }
     };
-    if constexpr (sizeof(T) == 2)
-        if (V == 8) return nv(Int<8>{});
-    if (V >= 4) nv(Int<4>{});
-    else if (V == 2) nv(Int<2>{});
-    else nv(Int<1>{});
+    if (aligned) nv(Int<1>{});
+    else nv(Int<0>{});
 }
 
 inline bool norm_ok(const void* x, int64_t x_stride, int32_t x_type, int32_t y_type, int32_t w_type, int64_t rows, int64_t dim) {
-    if (rows < 0 || rows >= (int64_t)1 << 31 || dim < 1 || dim >= kNormMaxDim) return false;
+    if (rows < 0 || rows >= (int64_t)1 << 30 || dim < 1 || dim >= kNormMaxDim) return false;
     if (!dense_type_ok(x_type) || !dense_type_ok(y_type) || !dense_type_ok(w_type)) return false;
     if (x_type != y_type && x_type != MLKV_TYPE_FLOAT) return false;
     return rows == 0 || (x && x_stride >= dim);

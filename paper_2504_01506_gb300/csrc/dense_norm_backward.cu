@@ -13,94 +13,134 @@ using namespace mlkv;
 namespace {
 
 constexpr int kBackwardValues = 16;  // most values of x and dy each that a lane holds, beside their columns' sums
+constexpr int kBackwardLanes = 512;  // threads an SM: 128 registers each
 
-// The rows' gradients, and the sums over this block's rows of dy xh and dy.
-// A team has the next row on its way while it works on one.
-template <class TX, class TY, int V, int NV>
-__global__ void __launch_bounds__(kNormLanes) k_norm_backward(NormArgs a) {
+// The rows' gradients, and the sums over this block's rows of dy xh and dy.  Rows
+// that are aligned come through shared memory, two of each team on their way (a
+// thread reads what it copied itself).  What a lane holds beyond the row's end is a copy of its last vector, or 0, with weight 0.
+template <class TX, class TY, int NV, bool ALIGNED>
+__global__ void __launch_bounds__(kBackwardLanes, 1) k_norm_backward(NormArgs a) {
     pdl_enter();
-    extern __shared__ float shared[];  // the weight, [dim]; then the teams' sums, [2][dim]
-    __shared__ float2 buf[64];
-    constexpr int H = kPairs<V>;
-    const Team tm(a.lanes);
-    const int nvec = a.dim / V;
-    const int64_t step = (int64_t)gridDim.x * tm.count;
+    extern __shared__ __align__(16) float shared[];  // the weight, [room]; the rows on their way; the teams' sums, [2][dim]
+    __shared__ __align__(16) float2 buf[64];
+    constexpr int V = 16 / sizeof(TX), H = V / 2;
+    const Team tm(a.lanes, buf);
+    const int rows = (int)a.rows, step = (int)gridDim.x * tm.count;
+    const int nvec = (a.dim + V - 1) / V, room = tm.L * NV * V;
+    const Span x_span(static_cast<const TX*>(a.x), a.rows, a.x_stride, a.dim);
+    const Span dy_span(static_cast<const TY*>(a.dy), a.rows, a.dy_stride, a.dim);
     float2 dw[NV][H], db[NV][H];
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
         for (int k = 0; k < H; ++k) dw[i][k] = db[i][k] = both(0.f);
-    struct Row {
-        Values<TX, V> x[NV];
-        Values<TY, V> dy[NV];
-        float2 stats;
-    };
-    auto load = [&](int64_t r, Row& q) {
-        const bool live = r < a.rows;
-        const TX* xr = static_cast<const TX*>(a.x) + r * a.x_stride;
-        const TY* dr = static_cast<const TY*>(a.dy) + r * a.dy_stride;
+    int at[NV];  // of this lane's vectors, the last one again where there are no more
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int j = tm.lane + i * tm.L;
-            q.x[i].zero();
-            q.dy[i].zero();
-            if (live && j < nvec) {
-                q.x[i].load(xr + j * V);
-                q.dy[i].load(dr + j * V);
-            }
-        }
-        q.stats = live ? *reinterpret_cast<const float2*>(a.stats + 2 * r) : both(0.f);
-    };
-    int64_t r = (int64_t)blockIdx.x * tm.count + tm.index;
-    Row q, next;
-    load(r, q);
-    if (a.w) {
-        stage_weights<V>(shared, a.w, a.w_type, a.dim);
-        __syncthreads();
-    }
-    int turn = 0;
-    // the lanes of a warp take as many turns as its first team does
-    for (int64_t first = tm.L < 32 ? r - (threadIdx.x & 31) / tm.L : r; first < a.rows; first += step, r += step, turn ^= 1) {
-        load(r + step, next);
-        const float2 minus = both(-q.stats.x), rs = both(q.stats.y);
-        float2 c1 = both(0.f), c2 = both(0.f);
-        auto row = [&](auto f) {  // f(i, k, g, xh, dy) of every pair
+    for (int i = 0; i < NV; ++i) at[i] = min(tm.lane + i * tm.L, nvec - 1) * V;
+    Values<TX, V, ALIGNED> x[NV];
+    Values<TY, V, ALIGNED> dy[NV];
+    int r = (int)blockIdx.x * tm.count + tm.index;
+    const TX* x_at = static_cast<const TX*>(a.x) + r * a.x_stride;
+    const TY* dy_at = static_cast<const TY*>(a.dy) + r * a.dy_stride;
+    TX* o = static_cast<TX*>(a.out) + r * a.out_stride;
+    const int64_t x_step = step * a.x_stride, dy_step = step * a.dy_stride, o_step = step * a.out_stride;
+    constexpr int kBytes = sizeof(TY) * V;  // of a vector of dy
+    uint8_t* x_ring = reinterpret_cast<uint8_t*>(shared + room) + threadIdx.x * 16;
+    uint8_t* dy_ring = reinterpret_cast<uint8_t*>(shared + room) + (ALIGNED ? kNormAhead * NV * blockDim.x * 16 : 0) + threadIdx.x * kBytes;
+    float2 stats_ahead[2] = {both(0.f), both(0.f)};
+    int ahead = r;
+    // the next row not yet on its way: into slot `slot`, or (unaligned) registers
+    auto fetch = [&](int slot, float2& its) {
+        if (ahead < rows) {
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int j = tm.lane + i * tm.L;
-                float2 w[H];
-                if (a.w && j < nvec) weight_pairs<V>(shared, j, a.dim, w);
-#pragma unroll
-                for (int k = 0; k < H; ++k) {
-                    const float2 d = q.dy[i].pair(k), xh = mul2(add2(q.x[i].pair(k), minus), rs);
-                    f(i, k, a.w && j < nvec ? mul2(d, w[k]) : d, xh, d);
+                if constexpr (ALIGNED) {
+                    copy_async<16>(x_ring + (slot * NV + i) * (int)blockDim.x * 16, x_at + at[i]);
+                    copy_async<kBytes>(dy_ring + (slot * NV + i) * (int)blockDim.x * kBytes, dy_at + at[i]);
+                } else {
+                    x[i].load(x_at + at[i], a.dim - at[i], x_span);
+                    dy[i].load(dy_at + at[i], a.dim - at[i], dy_span);
                 }
             }
-        };
-        row([&](int i, int k, float2 g, float2 xh, float2 d) {
-            c1 = add2(c1, g);
-            c2 = fma2(g, xh, c2);
-            dw[i][k] = fma2(d, xh, dw[i][k]);
-            db[i][k] = add2(db[i][k], d);
-        });
+            its = reinterpret_cast<const float2*>(a.stats)[ahead];
+        } else if (!ALIGNED) {  // a team past the last row, beside one that is not
+#pragma unroll
+            for (int i = 0; i < NV; ++i) dy[i].zero();
+        }
+        if (ALIGNED) copy_commit();
+        x_at += x_step;
+        dy_at += dy_step;
+        ahead += step;
+    };
+    if (!ALIGNED)
+#pragma unroll
+        for (int i = 0; i < NV; ++i) x[i].zero();
+    fetch(0, stats_ahead[0]);
+    if (ALIGNED) fetch(1, stats_ahead[1]);
+    const float inverse = -1.f / (float)a.dim;
+    stage_weights<V>(shared, a.w, a.w_type, a.dim, room, 1.f);
+    __syncthreads();
+    int turn = 0;
+    // the lanes of a warp take as many turns as its first team does
+    for (int first = tm.L < 32 ? r - (int)(threadIdx.x & 31) / tm.L : r; first < rows; first += step, r += step, o += o_step, turn ^= 1) {
+        const float2 stats = stats_ahead[0];
+        if constexpr (ALIGNED) {
+            copy_wait<kNormAhead - 1>();
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                x[i].load(reinterpret_cast<const TX*>(x_ring + (turn * NV + i) * (int)blockDim.x * 16), V, x_span);
+                dy[i].load(reinterpret_cast<const TY*>(dy_ring + (turn * NV + i) * (int)blockDim.x * kBytes), V, dy_span);
+                if (r >= rows) {  // a team past the last row, beside one that is not
+                    x[i].zero();
+                    dy[i].zero();
+                }
+            }
+        }
+        const float2 minus = both(-stats.x), rs = both(stats.y);
+        float2 c1 = both(0.f), c2 = both(0.f);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            float2 w[H];
+            weight_pairs<V>(shared, tm.lane + i * tm.L, room, w);
+#pragma unroll
+            for (int k = 0; k < H; ++k) {
+                const float2 d = dy[i].pair(k), xh = mul2(add2(x[i].pair(k), minus), rs), g = mul2(d, w[k]);
+                c1 = add2(c1, g);
+                c2 = fma2(g, xh, c2);
+                dw[i][k] = fma2(d, xh, dw[i][k]);
+                db[i][k] = add2(db[i][k], d);
+            }
+        }
+        if (ALIGNED) {
+            stats_ahead[0] = stats_ahead[1];
+            fetch(turn, stats_ahead[1]);
+        }
         if (a.out) {
             float s1 = c1.x + c1.y, s2 = c2.x + c2.y;
-            tm.sum(s1, s2, buf, turn);
-            const float2 m1 = both(-s1 / (float)a.dim), m2 = both(-s2 / (float)a.dim);
-            if (r < a.rows) {
-                TX* o = static_cast<TX*>(a.out) + r * a.out_stride;
-                Values<TX, V> p[NV];
-                row([&](int i, int k, float2 g, float2 xh, float2) {
-                    p[i].set(k, mul2(fma2(xh, m2, add2(g, m1)), rs));
-                });
+            tm.sum(s1, s2, turn);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                x[i].forget();
+                dy[i].forget();
+            }
+            if (r < rows) {
+                const float2 m1 = both(s1 * inverse), m2 = both(s2 * inverse);
 #pragma unroll
                 for (int i = 0; i < NV; ++i) {
                     const int j = tm.lane + i * tm.L;
-                    if (j < nvec) p[i].store(o + j * V);
+                    float2 w[H];
+                    weight_pairs<V>(shared, j, room, w);
+                    Values<TX, V, ALIGNED> p;
+#pragma unroll
+                    for (int k = 0; k < H; ++k) {
+                        const float2 xh = mul2(add2(x[i].pair(k), minus), rs);
+                        p.set(k, mul2(fma2(xh, m2, fma2(dy[i].pair(k), w[k], m1)), rs));
+                    }
+                    if (j < nvec) p.store(o + j * V, a.dim - j * V);
                 }
             }
         }
-        q = next;
+        if (!ALIGNED) fetch(0, stats_ahead[0]);
     }
     if (!a.part && !a.dweight && !a.dbias) return;
     // the lanes of a warp that hold the same columns
@@ -115,7 +155,7 @@ __global__ void __launch_bounds__(kNormLanes) k_norm_backward(NormArgs a) {
                 db[i][k].y += __shfl_xor_sync(0xffffffffu, db[i][k].y, o);
             }
     // ... then the block's teams (a warp's, where it holds several), one after another
-    float* cols = shared + (a.w ? a.dim : 0);
+    float* cols = shared + room + (ALIGNED ? kNormAhead * NV * (int)blockDim.x * (16 + kBytes) / 4 : 0);
     const int teams = tm.L < 32 ? blockDim.x / 32 : tm.count, mine = tm.L < 32 ? threadIdx.x / 32 : tm.index;
     const bool holds = tm.L >= 32 || (threadIdx.x & 31) < tm.L;
     auto each = [&](auto f) {  // f(column, dw, db)
@@ -125,8 +165,8 @@ __global__ void __launch_bounds__(kNormLanes) k_norm_backward(NormArgs a) {
             if (j >= nvec) continue;
 #pragma unroll
             for (int k = 0; k < H; ++k) {
-                f(j * V + 2 * k, dw[i][k].x, db[i][k].x);
-                if (2 * k + 1 < V) f(j * V + 2 * k + 1, dw[i][k].y, db[i][k].y);
+                if (ALIGNED || j * V + 2 * k < a.dim) f(j * V + 2 * k, dw[i][k].x, db[i][k].x);
+                if (ALIGNED || j * V + 2 * k + 1 < a.dim) f(j * V + 2 * k + 1, dw[i][k].y, db[i][k].y);
             }
         }
     };
@@ -158,8 +198,9 @@ __global__ void __launch_bounds__(kNormLanes) k_norm_backward(NormArgs a) {
 template <class TX, class TY>
 __global__ void __launch_bounds__(kNormLongLanes) k_norm_backward_long(NormArgs a) {
     pdl_enter();
-    __shared__ float2 buf[64];
-    const Team tm(kNormLongLanes);
+    __shared__ __align__(16) float2 buf[64];
+    const Team tm(kNormLongLanes, buf);
+    __syncthreads();
     const TX* x = static_cast<const TX*>(a.x) + blockIdx.x * a.x_stride;
     const TY* dy = static_cast<const TY*>(a.dy) + blockIdx.x * a.dy_stride;
     const float mu = a.stats[2 * blockIdx.x], rs = a.stats[2 * blockIdx.x + 1];
@@ -169,7 +210,7 @@ __global__ void __launch_bounds__(kNormLongLanes) k_norm_backward_long(NormArgs 
         c1 += g;
         c2 += g * ((to_float(x[j]) - mu) * rs);
     }
-    tm.sum(c1, c2, buf, 0);
+    tm.sum(c1, c2, 0);
     c1 /= (float)a.dim;
     c2 /= (float)a.dim;
     TX* o = static_cast<TX*>(a.out) + blockIdx.x * a.out_stride;
@@ -218,7 +259,7 @@ __global__ void __launch_bounds__(1024) k_norm_cols(const float* __restrict__ pa
 
 // Blocks whose sums of columns are kept apart: as many as run at a time.
 int64_t backward_blocks(int64_t rows, int teams, int sms, int threads) {
-    const int64_t most = (int64_t)sms * std::max(1, 1024 / threads);
+    const int64_t most = (int64_t)sms * (kBackwardLanes / threads);
     return std::max<int64_t>(1, std::min(most, (rows + teams - 1) / teams));
 }
 constexpr int64_t kMostBlocks = 256 * 8;  // of any device
@@ -226,7 +267,7 @@ constexpr int64_t kMostBlocks = 256 * 8;  // of any device
 }  // namespace
 
 extern "C" int64_t mlkv_layer_norm_backward_workspace(int64_t rows, int64_t dim) {
-    if (rows < 0 || rows >= (int64_t)1 << 31 || dim < 1 || dim >= kNormMaxDim) return -1;
+    if (rows < 0 || rows >= (int64_t)1 << 30 || dim < 1 || dim >= kNormMaxDim) return -1;
     return std::min(kMostBlocks, std::max<int64_t>(rows, 1)) * 2 * dim * (int64_t)sizeof(float);
 }
 
@@ -254,11 +295,12 @@ extern "C" int mlkv_layer_norm_backward(const void* d_dy, int64_t dy_stride, int
     a.x_stride = x_stride; a.dy_stride = dy_stride; a.out_stride = dx_stride; a.rows = rows;
     a.dim = (int32_t)dim; a.w_type = w_type; a.dweight = d_dweight; a.dbias = d_dbias;
     const int xs = dense_type_size(x_type), ys = dense_type_size(dy_type);
-    const int V = norm_vector_width(dim, {{d_x, xs}, {d_dy, ys}, {d_dx, xs}},
-                               {x_stride, dy_stride, d_dx ? dx_stride : 0}, 16 / xs);
-    const NormShape sh = norm_shape(dim, V, kBackwardValues);
+    const int V = 16 / xs;
+    const bool aligned = norm_aligned(d_x, x_stride, xs, dim, V) && norm_aligned(d_dy, dy_stride, ys, dim, V) &&
+                         norm_aligned(d_dx, dx_stride, xs, dim, V);
+    const NormShape sh = norm_shape(rows, dim, V, kBackwardValues, kBackwardLanes, sms);
     const int threads = sh.lanes ? norm_team_threads(sh.lanes) : kNormLongLanes, teams = sh.lanes ? threads / sh.lanes : 1;
-    int64_t blocks = std::min(kMostBlocks, backward_blocks(rows, teams, sms, threads));
+    int64_t blocks = sh.lanes ? std::min(kMostBlocks, backward_blocks(rows, teams, sms, threads)) : 0;
     if (!sh.lanes) blocks = std::max<int64_t>(1, std::min<int64_t>(rows, (2 * sms * 128 + dim - 1) / dim));
     const bool parts = want_cols && (blocks > 1 || !sh.lanes);
     if (!workspace_ok(d_workspace, workspace_bytes, parts ? blocks * 2 * dim * (int64_t)sizeof(float) : 0)) return MLKV_ERR_INVALID;
@@ -278,9 +320,10 @@ extern "C" int mlkv_layer_norm_backward(const void* d_dy, int64_t dy_stride, int
             return;
         }
         a.lanes = sh.lanes;
-        by_width<TX, kBackwardValues>(V, sh.NV, [&](auto v, auto nv) {
-            auto kernel = k_norm_backward<TX, TY, decltype(v)::value, decltype(nv)::value>;
-            const size_t smem = ((d_weight ? 1 : 0) + (sh.lanes < threads ? 2 : 0)) * (size_t)dim * sizeof(float);
+        by_shape<kBackwardValues * (int)sizeof(TX) / 16>(sh.NV, aligned, [&](auto nv, auto al) {
+            auto kernel = k_norm_backward<TX, TY, decltype(nv)::value, decltype(al)::value>;
+            const size_t smem = ((size_t)sh.lanes * sh.NV * V + (sh.lanes < threads ? 2 : 0) * (size_t)dim) * sizeof(float) +
+                                (aligned ? (size_t)kNormAhead * sh.NV * threads * (16 + V * ys) : 0);
             ok = dense_smem(kernel, smem);
             if (ok) launch_kernel(true, kernel, dim3((unsigned)blocks), dim3(threads), smem, st, a);
         });
