@@ -39,6 +39,7 @@ struct Epilogue {
 struct Product {
     int32_t I, J, blocks;            // extents; 64-value blocks along k
     int32_t tiles_i, tiles_j, shares, blocks_per_share;
+    int32_t joined;                  // a tile's shares are a cluster, which adds them up itself
     uint32_t idesc;
     Epilogue e;
 };
@@ -135,6 +136,57 @@ __device__ __forceinline__ void put_columns(const Product& p, const uint32_t (&r
         const float v = __uint_as_float(r[q]);
         if (e.part) e.part[share * e.part_size + (j0 + q) * e.part_stride + i] = v;
         else static_cast<T*>(e.out)[(j0 + q) * e.out_stride + i] = from_float<T>(finish(e, v, j0 + q, i));
+    }
+}
+
+// The shares of a tile, [column j][128 rows i] of sums at `at` in the shared memory
+// of each block of the cluster, added up in order: this block's part of the rows,
+// four of one column a thread (of the 128 epilogue threads) at a time.
+template <class T, int BN>
+__device__ __forceinline__ void join_shares(const Product& p, uint32_t at, int i, int j, uint32_t rank) {
+    const Epilogue& e = p.e;
+    const int rows = kBM / p.shares / 4, columns = min(BN, p.J - j * BN);
+    for (int q = threadIdx.x; q < rows * columns; q += 128) {
+        const int c = q / rows, r = ((int)rank * rows + q % rows) * 4;
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int s = 0; s < p.shares; ++s) {
+            float4 x;
+            asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                         : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w)
+                         : "r"(place_in(at + (c * kBM + r) * 4, s))
+                         : "memory");
+            sum.x += x.x;
+            sum.y += x.y;
+            sum.z += x.z;
+            sum.w += x.w;
+        }
+        const int64_t row = (int64_t)j * BN + c, col = (int64_t)i * kBM + r;  // of the output
+        if (e.wide && col + 4 <= p.I) {
+            float2 v[2] = {make_float2(sum.x, sum.y), make_float2(sum.z, sum.w)};
+            uint2 x = make_uint2(0, 0);
+            if (e.residual) x = *reinterpret_cast<const uint2*>(static_cast<const T*>(e.residual) + row * e.residual_stride + col);
+            if (e.bias) {
+                const T* b = static_cast<const T*>(e.bias) + col;
+                v[0] = add2(v[0], make_float2(to_float(b[0]), to_float(b[1])));
+                v[1] = add2(v[1], make_float2(to_float(b[2]), to_float(b[3])));
+            }
+            if (e.pre)
+                *reinterpret_cast<uint2*>(static_cast<T*>(e.pre) + row * e.pre_stride + col) = make_uint2(word_of_pair<T>(v[0]), word_of_pair<T>(v[1]));
+            by_act(e.act, [&](auto act) {
+                v[0] = activate<decltype(act)::value>(v[0]);
+                v[1] = activate<decltype(act)::value>(v[1]);
+            });
+            if (e.residual) {
+                v[0] = add2(v[0], pair_of_word<T>(x.x));
+                v[1] = add2(v[1], pair_of_word<T>(x.y));
+            }
+            *reinterpret_cast<uint2*>(static_cast<T*>(e.out) + row * e.out_stride + col) = make_uint2(word_of_pair<T>(v[0]), word_of_pair<T>(v[1]));
+            continue;
+        }
+        const float v[4] = {sum.x, sum.y, sum.z, sum.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (col + k < p.I) static_cast<T*>(e.out)[row * e.out_stride + col + k] = from_float<T>(finish(e, v[k], row, col + k));
     }
 }
 
@@ -320,6 +372,7 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR>::kThreads, 1)
     const uint32_t full = smem_of(bars), empty = full + 8 * S, done = empty + 8 * S, drained = done + 16;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = PAIR ? cluster_rank() : 0;
+    const bool joined = SWAP && p.joined;
     if (threadIdx.x == 0) {
         for (int s = 0; s < S; ++s) {
             mbar_init(full + 8 * s, 1);
@@ -342,7 +395,10 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR>::kThreads, 1)
     const uint32_t tmem = tmem_at;
     pdl_enter();
 
-    const int total = p.tiles_i * p.tiles_j * p.shares, first = blockIdx.x / kBlocks, step = gridDim.x / kBlocks;
+    // joined shares: one tile a block, its share by its place in the cluster
+    const int tiles = p.tiles_i * p.tiles_j, mine = joined ? (int)cluster_rank() : 0;
+    const int total = joined ? tiles : tiles * p.shares, first = joined ? blockIdx.x / p.shares : blockIdx.x / kBlocks;
+    const int step = joined ? tiles : gridDim.x / kBlocks;
     if (warp == kTma) {
         if (lane == 0) {
             uint32_t n = 0;  // stages filled
@@ -350,6 +406,7 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR>::kThreads, 1)
             for (int t = first; t < total && ok; t += step) {
                 int i, j, share;
                 tile_at(p, t, i, j, share);
+                if (joined) share = mine;
                 const int k0 = share * p.blocks_per_share, k1 = min(p.blocks, k0 + p.blocks_per_share);
                 const int row = (i * kBlocks + (int)rank) * kBM, col = j * BN + (int)rank * kCols;
                 for (int k = k0; k < k1; ++k, ++n) {
@@ -383,6 +440,7 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR>::kThreads, 1)
             for (int t = first; t < total && ok; t += step, ++u) {
                 int i, j, share;
                 tile_at(p, t, i, j, share);
+                if (joined) share = mine;
                 const int k0 = share * p.blocks_per_share, k1 = min(p.blocks, k0 + p.blocks_per_share);
                 const uint32_t acc = u & 1, d = tmem + acc * BN;
                 if (u >= 2 && !(ok = mbar_wait(drained + 8 * acc, (u / 2 - 1) & 1, &stop))) break;
@@ -421,7 +479,14 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR>::kThreads, 1)
                     __syncwarp();
                     tmem_ld16(at + c, r);
                     tmem_wait_ld();
-                    if (r0 + lane < p.I) put_columns<T>(p, r, r0 + lane, (int64_t)j * BN + c, share);
+                    if (joined) {  // where the ring was: all of it has been read
+                        const bool any = share * p.blocks_per_share < p.blocks;
+#pragma unroll
+                        for (int q = 0; q < 16; ++q)
+                            reinterpret_cast<uint32_t*>(raw + (ring - smem_of(raw)))[(c + q) * kBM + warp * 32 + lane] = any ? r[q] : 0u;
+                    } else if (r0 + lane < p.I) {
+                        put_columns<T>(p, r, r0 + lane, (int64_t)j * BN + c, share);
+                    }
                 }
             } else {
                 const int cols = BN * 4 / R::kEpilogue, c = (warp >> 2) * cols;  // this warp's
@@ -439,7 +504,14 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR>::kThreads, 1)
     }
     tc_fence_before();
     __syncthreads();
-    if (PAIR) cluster_sync();  // nothing of the other block's is on its way here any more
+    if (joined) {
+        int i, j, share;
+        tile_at(p, first, i, j, share);
+        cluster_sync();
+        if (warp < 4) join_shares<T, BN>(p, ring, i, j, mine);
+        __syncwarp();
+    }
+    if (PAIR || joined) cluster_sync();  // nothing of this block's memory is wanted by another any more
     tc_fence_after();
     if (threadIdx.x == 0 && stop) atomicMax(&g_status, (uint32_t)MLKV_ERR_TIMEOUT);
     if (warp == kMma) tmem_free<PAIR>(tmem, R::kColumns);
@@ -456,23 +528,27 @@ __global__ void __launch_bounds__(256) k_product_finish(Epilogue e, int64_t rows
     }
 }
 
-// Rows whose stride or place TMA does not take (multiples of 16 bytes), laid out anew.
-__global__ void __launch_bounds__(256) k_align(const uint16_t* __restrict__ in, int64_t stride, uint16_t* __restrict__ out,
-                                               int64_t out_stride, int64_t rows, int64_t cols) {
+// Rows whose stride or place TMA does not take (multiples of 16 bytes), laid out anew: up to two matrices at a time.
+struct Align {
+    const uint16_t* in;
+    uint16_t* out;
+    int64_t stride, out_stride, rows, cols;
+};
+__global__ void __launch_bounds__(256) k_align(Align a, Align b) {
     pdl_enter();
-    const int64_t per = out_stride / 8;
-    for (int64_t at = blockIdx.x * 256ll + threadIdx.x; at < rows * per; at += gridDim.x * 256ll) {
+    const Align m = blockIdx.y ? b : a;
+    const Span span(m.in, m.rows, m.stride, (int)m.cols);
+    const int64_t per = m.out_stride / 8, step = gridDim.x * 256ll;
+    for (int64_t at = blockIdx.x * 256ll + threadIdx.x; at < m.rows * per; at += step) {
         const int64_t r = at / per, c = (at - r * per) * 8;
-        uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-        for (int q = 0; q < 8; ++q)
-            if (c + q < cols) w[q / 2] |= (uint32_t)in[r * stride + c + q] << (16 * (q & 1));
-        *reinterpret_cast<uint4*>(out + r * out_stride + c) = make_uint4(w[0], w[1], w[2], w[3]);
+        Values<uint16_t, 8, false> v;
+        v.load(m.in + r * m.stride + c, (int)(m.cols - c), span);
+        *reinterpret_cast<uint4*>(m.out + r * m.out_stride + c) = make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]);
     }
 }
 
 // p = dy act'(z), and the sums of its columns over a block's rows.  A thread
-// takes V columns, a block 32 V columns of a share of the rows.
+// takes 8 columns, a block 256 columns of a share of the rows.
 struct Slope {
     const void* dy;
     const void* pre;
@@ -482,70 +558,62 @@ struct Slope {
     int64_t dy_stride, pre_stride, p_stride, rows, cols, share;
     int32_t act;
 };
-template <int V, class T>
+template <class T, bool ALIGNED>
 __global__ void __launch_bounds__(256) k_slope(Slope a) {
     pdl_enter();
-    __shared__ float sums[8][32 * V];
-    constexpr int H = (V + 1) / 2;
+    __shared__ float sums[8][256];
+    using Row = Values<T, 8, ALIGNED>;
+    constexpr int kRows = ALIGNED ? 4 : 2;  // on their way at a time
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t c = (blockIdx.x * 32ll + lane) * V;
+    const int64_t c = (blockIdx.x * 32ll + lane) * 8;
+    const int n = (int)min((int64_t)8, a.cols - c);
     const int64_t r0 = blockIdx.y * a.share, r1 = min(a.rows, r0 + a.share);
-    float2 s[H];
+    const T *dy = static_cast<const T*>(a.dy), *pre = static_cast<const T*>(a.pre);
+    const Span dy_span(dy, a.rows, a.dy_stride, (int)a.cols), pre_span(pre, a.rows, a.pre_stride, (int)a.cols);
+    float2 s[4];
 #pragma unroll
-    for (int q = 0; q < H; ++q) s[q] = splat2(0.f);
-    using Row = Pack<uint16_t, V>;
-    const T* dy = static_cast<const T*>(a.dy) + c;
-    const T* pre = static_cast<const T*>(a.pre) + c;
-    auto pair = [](const Row& x, int q) {
-        if constexpr (V == 1) return make_float2(pair_of_word<T>(x.v[0]).x, 0.f);
-        else return pair_of_word<T>(reinterpret_cast<const uint32_t*>(&x)[q]);
-    };
-    constexpr int kRows = 4;  // on their way at a time
-    if (c < a.cols)
+    for (int q = 0; q < 4; ++q) s[q] = splat2(0.f);
+    if (n > 0)
         for (int64_t r = r0 + warp; r < r1; r += 8 * kRows) {
             Row d[kRows], z[kRows];
 #pragma unroll
             for (int i = 0; i < kRows; ++i) {
                 if (r + 8 * i >= r1) continue;
-                d[i] = *reinterpret_cast<const Row*>(dy + (r + 8 * i) * a.dy_stride);
-                if (a.act != MLKV_ACT_NONE) z[i] = *reinterpret_cast<const Row*>(pre + (r + 8 * i) * a.pre_stride);
+                d[i].load(dy + (r + 8 * i) * a.dy_stride + c, n, dy_span);
+                if (a.act != MLKV_ACT_NONE) z[i].load(pre + (r + 8 * i) * a.pre_stride + c, n, pre_span);
             }
 #pragma unroll
             for (int i = 0; i < kRows; ++i) {
                 if (r + 8 * i >= r1) continue;
                 if (a.act == MLKV_ACT_NONE) {
 #pragma unroll
-                    for (int q = 0; q < H; ++q) s[q] = add2(s[q], pair(d[i], q));
+                    for (int q = 0; q < 4; ++q) s[q] = add2(s[q], d[i].pair(q));
                 }
                 by_act(a.act, [&](auto act) {
 #pragma unroll
-                    for (int q = 0; q < H; ++q) {
-                        const float2 v = mul2(pair(d[i], q), slope<decltype(act)::value>(pair(z[i], q)));
+                    for (int q = 0; q < 4; ++q) {
+                        const float2 v = mul2(d[i].pair(q), slope<decltype(act)::value>(z[i].pair(q)));
                         s[q] = add2(s[q], v);
-                        if constexpr (V == 1) d[i].v[0] = (uint16_t)word_of_pair<T>(v);
-                        else reinterpret_cast<uint32_t*>(&d[i])[q] = word_of_pair<T>(v);
+                        d[i].set(q, v);
                     }
                 });
-                if (a.p) *reinterpret_cast<Row*>(static_cast<T*>(a.p) + (r + 8 * i) * a.p_stride + c) = d[i];
+                if (a.p)  // (rows of whole vectors)
+                    *reinterpret_cast<uint4*>(static_cast<T*>(a.p) + (r + 8 * i) * a.p_stride + c) = make_uint4(d[i].w[0], d[i].w[1], d[i].w[2], d[i].w[3]);
             }
         }
     if (!a.dbias) return;
 #pragma unroll
-    for (int q = 0; q < H; ++q) {
-        sums[warp][lane * V + 2 * q] = s[q].x;
-        if (2 * q + 1 < V) sums[warp][lane * V + 2 * q + 1] = s[q].y;
-    }
+    for (int q = 0; q < 4; ++q) *reinterpret_cast<float2*>(&sums[warp][lane * 8 + 2 * q]) = s[q];
     __syncthreads();
-    for (int q = threadIdx.x; q < 32 * V; q += 256) {
-        const int64_t col = blockIdx.x * 32ll * V + q;
-        if (col >= a.cols) continue;
-        float t = 0.f;
+    const int64_t col = blockIdx.x * 256ll + threadIdx.x;
+    if (col >= a.cols) return;
+    float t = 0.f;
 #pragma unroll
-        for (int w = 0; w < 8; ++w) t += sums[w][q];
-        if (a.part) a.part[blockIdx.y * a.cols + col] = t;
-        else static_cast<T*>(a.dbias)[col] = from_float<T>(t);
-    }
+    for (int w = 0; w < 8; ++w) t += sums[w][threadIdx.x];
+    if (a.part) a.part[blockIdx.y * a.cols + col] = t;
+    else static_cast<T*>(a.dbias)[col] = from_float<T>(t);
 }
+
 // The shares' sums of 32 columns, added up by 32 warps of which each takes every 32nd share, then over the warps.
 __global__ void __launch_bounds__(1024) k_column_sums(const float* __restrict__ part, int shares, int64_t cols, void* out, int32_t type) {
     pdl_enter();
@@ -605,14 +673,20 @@ struct Caller {
     int rc = MLKV_OK;
     unsigned blocks_for(int64_t items) const { return (unsigned)std::max<int64_t>(1, std::min<int64_t>((items + 255) / 256, 16ll * sms)); }
 
-    // The matrix as TMA takes it.
-    Matrix aligned(const Matrix& m) {
-        if (m.aligned()) return m;
-        const int64_t stride = round_up(m.cols, 8);
-        uint16_t* to = static_cast<uint16_t*>(arena.take(m.rows * stride * 2));
-        if (run && m.rows)
-            launch_kernel(true, k_align, dim3(blocks_for(m.rows * stride / 8)), dim3(256), 0, st, m.p, m.stride, to, stride, m.rows, m.cols);
-        return {to, stride, m.rows, m.cols};
+    // Two matrices as TMA takes them.
+    void align(Matrix& a, Matrix& b) {
+        Align to[2] = {};
+        int n = 0;
+        for (Matrix* m : {&a, &b}) {
+            if (m->aligned() || !m->rows || !m->cols) continue;
+            const int64_t stride = round_up(m->cols, 8);
+            uint16_t* p = static_cast<uint16_t*>(arena.take(m->rows * stride * 2));
+            to[n++] = {m->p, p, m->stride, stride, m->rows, m->cols};
+            *m = {p, stride, m->rows, m->cols};
+        }
+        if (!run || !n) return;
+        const int64_t vectors = std::max(to[0].rows * to[0].out_stride, to[1].rows * to[1].out_stride) / 8;
+        launch_kernel(true, k_align, dim3(blocks_for(vectors), n), dim3(256), 0, st, to[0], to[1]);
     }
 
     bool encode(CUtensorMap* map, const Matrix& m, bool mn, int rows) {
@@ -637,22 +711,23 @@ struct Caller {
         const int64_t tiles = (int64_t)p.tiles_i * p.tiles_j * p.shares;
         auto go = [&](auto kernel) {
             if (!dense_smem(kernel, R::kBytes)) rc = MLKV_ERR_CUDA;
-            else if (PAIR) launch_pairs(kernel, std::min<int64_t>(tiles, sms / 2), R::kThreads, R::kBytes, ma, mb, p);
+            else if (PAIR) launch_clusters(kernel, 2, 2 * std::min<int64_t>(tiles, sms / 2), R::kThreads, R::kBytes, ma, mb, p);
+            else if (p.joined) launch_clusters(kernel, p.shares, tiles, R::kThreads, R::kBytes, ma, mb, p);
             else launch_kernel(true, kernel, dim3((unsigned)std::min<int64_t>(tiles, sms)), dim3(R::kThreads), R::kBytes, st, ma, mb, p);
         };
         if (type == MLKV_TYPE_BFLOAT) go(k_product<BN, A_MN, B_MN, SWAP, PAIR, __nv_bfloat16>);
         else go(k_product<BN, A_MN, B_MN, SWAP, PAIR, __half>);
     }
     template <class K>
-    void launch_pairs(K kernel, int64_t pairs, int threads, size_t smem, const CUtensorMap& ma, const CUtensorMap& mb, const Product& p) {
+    void launch_clusters(K kernel, int cluster, int64_t blocks, int threads, size_t smem, const CUtensorMap& ma, const CUtensorMap& mb, const Product& p) {
         cudaLaunchAttribute attr[2];
         attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = 2;
+        attr[0].val.clusterDim.x = cluster;
         attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
         attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
         attr[1].val.programmaticStreamSerializationAllowed = 1;
         cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3((unsigned)(2 * pairs));
+        cfg.gridDim = dim3((unsigned)blocks);
         cfg.blockDim = dim3(threads);
         cfg.dynamicSmemBytes = smem;
         cfg.stream = st;
@@ -677,9 +752,6 @@ struct Caller {
             if (run) launch_kernel(true, k_product_finish, dim3(blocks_for(rows * cols)), dim3(256), 0, st, e, rows, cols, 0);
             return;
         }
-        a = aligned(a);
-        b = aligned(b);
-        e.wide = 1;
         auto wide = [](const void* p, int64_t stride) { return !p || (reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 8 == 0); };
         e.wide = wide(e.out, e.out_stride) && wide(e.pre, e.pre_stride) && wide(e.residual, e.residual_stride);
         const bool swap = !A_MN && rows <= 64;  // few rows: the wide operand fills the tiles' 128 rows
@@ -701,7 +773,15 @@ struct Caller {
         p.blocks_per_share = (int32_t)((p.blocks + shares - 1) / shares);
         p.shares = (p.blocks + p.blocks_per_share - 1) / p.blocks_per_share;
         p.e = e;
-        if (p.shares > 1) {
+        // few rows: the shares of a tile are a cluster (of 2, 4 or 8), one tile a block
+        if (swap && p.shares > 1) {
+            int n = 2;
+            while (n < 8 && 2 * n <= p.shares) n *= 2;
+            p.blocks_per_share = (p.blocks + n - 1) / n;
+            p.shares = n;  // (the last may be of nothing)
+            p.joined = 1;
+        }
+        if (p.shares > 1 && !p.joined) {
             p.e.part_stride = round_up(cols, 4);
             p.e.part_size = rows * p.e.part_stride;
             p.e.part = static_cast<float*>(arena.take(p.shares * p.e.part_size * 4));
@@ -720,7 +800,7 @@ struct Caller {
             else if (pair) launch<256, A_MN, B_MN, false, true>(a, b, p);
             else launch<256, A_MN, B_MN, false>(a, b, p);
         }
-        if (p.shares > 1) {
+        if (p.shares > 1 && !p.joined) {
             Epilogue f = p.e;
             launch_kernel(true, k_product_finish, dim3(blocks_for(rows * cols)), dim3(256), 0, st, f, rows, cols, (int)p.shares);
         }
@@ -730,8 +810,9 @@ struct Caller {
         Epilogue e = {};
         e.bias = g.d_bias; e.residual = g.d_residual; e.residual_stride = g.residual_stride;
         e.pre = g.d_pre; e.pre_stride = g.pre_stride; e.out = g.d_y; e.out_stride = g.y_stride; e.act = g.activation;
-        product<false, false>({(const uint16_t*)g.d_x, g.x_stride, g.m, g.k}, {(const uint16_t*)g.d_weight, g.weight_stride, g.n, g.k},
-                              g.m, g.n, g.k, e);
+        Matrix x = {(const uint16_t*)g.d_x, g.x_stride, g.m, g.k}, w = {(const uint16_t*)g.d_weight, g.weight_stride, g.n, g.k};
+        if (g.m && g.n && g.k) align(x, w);
+        product<false, false>(x, w, g.m, g.n, g.k, e);
     }
 
     void backward(const mlkv_linear_args& g) {
@@ -748,8 +829,8 @@ struct Caller {
                 p = {static_cast<const uint16_t*>(s.p), s.p_stride, g.m, g.n};
             }
             const Matrix dy = {(const uint16_t*)s.dy, s.dy_stride, 0, 0}, pre = {(const uint16_t*)s.pre, s.pre_stride, 0, 0};
-            const int V = g.n % 8 == 0 && dy.aligned() && (!act || pre.aligned()) ? 8 : 1;
-            const int64_t across = (g.n + 32 * V - 1) / (32 * V);
+            const bool whole = g.n % 8 == 0 && dy.aligned() && (!act || pre.aligned());
+            const int64_t across = (g.n + 255) / 256;
             const int64_t shares = std::max<int64_t>(1, std::min<int64_t>((g.m + 31) / 32, 8ll * sms / across));
             s.share = (g.m + shares - 1) / shares;
             const unsigned down = (unsigned)((g.m + s.share - 1) / s.share);
@@ -757,8 +838,8 @@ struct Caller {
             if (run) {
                 const dim3 grid((unsigned)across, down);
                 const bool b = type == MLKV_TYPE_BFLOAT;
-                if (V == 8) launch_kernel(true, b ? k_slope<8, __nv_bfloat16> : k_slope<8, __half>, grid, dim3(256), 0, st, s);
-                else launch_kernel(true, b ? k_slope<1, __nv_bfloat16> : k_slope<1, __half>, grid, dim3(256), 0, st, s);
+                if (whole) launch_kernel(true, b ? k_slope<__nv_bfloat16, true> : k_slope<__half, true>, grid, dim3(256), 0, st, s);
+                else launch_kernel(true, b ? k_slope<__nv_bfloat16, false> : k_slope<__half, false>, grid, dim3(256), 0, st, s);
                 if (s.part) launch_kernel(true, k_column_sums, dim3((unsigned)((g.n + 31) / 32)), dim3(1024), 0, st,
                                           (const float*)s.part, (int)down, g.n, g.d_dbias, type);
             }
@@ -766,13 +847,15 @@ struct Caller {
             if (cudaMemsetAsync(g.d_dbias, 0, g.n * 2, st) != cudaSuccess) rc = MLKV_ERR_CUDA;
         }
         Epilogue e = {};
+        Matrix x = {(const uint16_t*)g.d_x, g.x_stride, g.m, g.k}, w = {(const uint16_t*)g.d_weight, g.weight_stride, g.n, g.k}, none = {};
+        if (g.m && g.n && g.k) align(g.d_dweight ? x : none, g.d_dx ? w : none);
         if (g.d_dx) {
             e.out = g.d_dx; e.out_stride = g.dx_stride;
-            product<false, true>(p, {(const uint16_t*)g.d_weight, g.weight_stride, g.n, g.k}, g.m, g.k, g.n, e);
+            product<false, true>(p, w, g.m, g.k, g.n, e);
         }
         if (g.d_dweight) {
             e.out = g.d_dweight; e.out_stride = g.dweight_stride;
-            product<true, true>(p, {(const uint16_t*)g.d_x, g.x_stride, g.m, g.k}, g.n, g.k, g.m, e);
+            product<true, true>(p, x, g.n, g.k, g.m, e);
         }
     }
 };

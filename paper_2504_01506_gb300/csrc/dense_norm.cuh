@@ -56,128 +56,6 @@ __device__ __forceinline__ void weight_pairs(const float* w, int j, int room, fl
     }
 }
 
-// The memory that a matrix spans, from its first value to its last.
-struct Span {
-    uintptr_t from, to;
-    template <class T>
-    __device__ __forceinline__ Span(const T* p, int64_t rows, int64_t stride, int dim)
-        : from(reinterpret_cast<uintptr_t>(p)), to(reinterpret_cast<uintptr_t>(p + (rows - 1) * stride + dim)) {}
-};
-
-// V values as they lie in memory, read and written in pairs, kept in 32-bit words
-// (16-bit values apart would take a register each).  ALIGNED: on 16 bytes (of x;
-// 8 of a 16-bit y beside an fp32 x), and a row is whole vectors.  Else as wide as
-// the row's place allows (the same for all its vectors): 8 bytes, 4, or, with
-// 16-bit values off a word, the words around them, shifted.
-template <class T, int V, bool ALIGNED> struct Values {
-    static constexpr int W = sizeof(T) * V / 4, kBytes = sizeof(T) * V;
-    uint32_t w[W];
-
-    template <int N>
-    static __device__ __forceinline__ void read(const void* p, uint32_t* to) {
-        const Pack<uint32_t, N> q = *reinterpret_cast<const Pack<uint32_t, N>*>(p);
-#pragma unroll
-        for (int i = 0; i < N; ++i) to[i] = q.v[i];
-    }
-    // The first n values (the rest 0).
-    __device__ __forceinline__ void load(const T* p, int n, const Span& span) {
-        if constexpr (ALIGNED) {
-            read<W>(p, w);
-        } else {
-            const uint32_t* p32 = reinterpret_cast<const uint32_t*>(p);
-            const uint32_t by = (uint32_t)reinterpret_cast<uintptr_t>(p) & (kBytes - 1);
-            if (n < V) {
-                zero();
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    if (e >= n) continue;
-                    if constexpr (sizeof(T) == 4) w[e] = p32[e];
-                    else w[e / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[e] << (16 * (e & 1));
-                }
-            } else if (by == 0) {
-                read<W>(p, w);
-            } else if ((by & 7) == 0) {
-#pragma unroll
-                for (int i = 0; i < W; i += 2) read<2>(p32 + i, w + i);
-            } else if ((by & 3) == 0) {
-#pragma unroll
-                for (int i = 0; i < W; ++i) w[i] = p32[i];
-            } else {
-                // the words around; the values at the matrix's ends by themselves
-                const uint16_t* p16 = reinterpret_cast<const uint16_t*>(p);
-                const uint32_t* around = reinterpret_cast<const uint32_t*>(p16 - 1);
-                uint32_t v[W + 1];
-                v[0] = reinterpret_cast<uintptr_t>(p) > span.from ? around[0] : (uint32_t)p16[0] << 16;
-#pragma unroll
-                for (int i = 1; i < W; ++i) v[i] = around[i];
-                v[W] = reinterpret_cast<uintptr_t>(p + V) < span.to ? around[W] : p16[V - 1];
-#pragma unroll
-                for (int i = 0; i < W; ++i) w[i] = __funnelshift_r(v[i], v[i + 1], 16);
-            }
-        }
-    }
-    __device__ __forceinline__ void zero() {
-#pragma unroll
-        for (int i = 0; i < W; ++i) w[i] = 0;
-    }
-    // What was computed of the values is not to be kept for later: it takes more registers than they do.
-    __device__ __forceinline__ void forget() {
-#pragma unroll
-        for (int i = 0; i < W; ++i) asm volatile("" : "+r"(w[i]));
-    }
-    __device__ __forceinline__ float2 pair(int k) const {
-        if constexpr (sizeof(T) == 4) return make_float2(__uint_as_float(w[2 * k]), __uint_as_float(w[2 * k + 1]));
-        else return pair_of_word<T>(w[k]);
-    }
-    __device__ __forceinline__ void set(int k, float2 x) {
-        if constexpr (sizeof(T) == 4) {
-            w[2 * k] = __float_as_uint(x.x);
-            w[2 * k + 1] = __float_as_uint(x.y);
-        } else {
-            w[k] = word_of_pair<T>(x);
-        }
-    }
-    // The first n values.
-    __device__ __forceinline__ void store(T* p, int n) const {
-        if constexpr (ALIGNED) {
-            Pack<uint32_t, W> q;
-#pragma unroll
-            for (int i = 0; i < W; ++i) q.v[i] = w[i];
-            *reinterpret_cast<Pack<uint32_t, W>*>(p) = q;
-        } else {
-            const uint32_t by = (uint32_t)reinterpret_cast<uintptr_t>(p);
-            uint32_t* p32 = reinterpret_cast<uint32_t*>(p);
-            if (n >= V && !(by & (kBytes - 1))) {
-                Pack<uint32_t, W> q;
-#pragma unroll
-                for (int i = 0; i < W; ++i) q.v[i] = w[i];
-                *reinterpret_cast<Pack<uint32_t, W>*>(p) = q;
-            } else if (n >= V && !(by & 7)) {
-#pragma unroll
-                for (int i = 0; i < W; i += 2) *reinterpret_cast<uint2*>(p32 + i) = make_uint2(w[i], w[i + 1]);
-            } else if (n >= V && !(by & 3)) {
-#pragma unroll
-                for (int i = 0; i < W; ++i) p32[i] = w[i];
-            } else if constexpr (sizeof(T) == 2) {
-                uint16_t* p16 = reinterpret_cast<uint16_t*>(p);
-                if (n >= V) {  // two bytes off a word: a half, the words between, a half
-                    p16[0] = (uint16_t)w[0];
-#pragma unroll
-                    for (int i = 0; i + 1 < W; ++i) *reinterpret_cast<uint32_t*>(p16 + 1 + 2 * i) = __funnelshift_r(w[i], w[i + 1], 16);
-                    p16[V - 1] = (uint16_t)(w[W - 1] >> 16);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < V; ++e)
-                        if (e < n) p16[e] = (uint16_t)(w[e / 2] >> (16 * (e & 1)));
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < W; ++i)
-                    if (i < n) p32[i] = w[i];
-            }
-        }
-    }
-};
 __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 
 // Where a thread stands in its block's teams.

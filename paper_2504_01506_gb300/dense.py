@@ -27,7 +27,7 @@ from . import _lib as L
 from .store import MLKVError, _stream
 
 _TYPES = {torch.float32: L.TYPE_FLOAT, torch.bfloat16: L.TYPE_BFLOAT, torch.float16: L.TYPE_HALF}
-_ACTIVATIONS = {"none": L.ACT_NONE, "relu": L.ACT_RELU, "gelu_tanh": L.ACT_GELU_TANH, "silu": L.ACT_SILU}
+_ACTIVATIONS = {None: L.ACT_NONE, "none": L.ACT_NONE, "relu": L.ACT_RELU, "gelu_tanh": L.ACT_GELU_TANH, "silu": L.ACT_SILU}
 
 
 class TokenLogprobs(typing.NamedTuple):
@@ -46,35 +46,40 @@ def _check(rc: int):
         raise MLKVError(rc, L.load().mlkv_status_string(rc).decode())
 
 
-def _matrix(x, name: str, dtypes=None, shape=None, device=None) -> torch.Tensor:
+def _matrix(x, name: str, dtypes=_TYPES, shape=None, device=None) -> torch.Tensor:
     """The tensor, with contiguous rows that do not overlap."""
-    if not isinstance(x, torch.Tensor) or x.dim() != 2:
-        raise TypeError(f"{name} must be a 2-d tensor")
-    if x.dtype not in (dtypes or _TYPES):
-        raise TypeError(f"{name} must be of {' or '.join(str(d) for d in dtypes or _TYPES)}, not {x.dtype}")
+    try:
+        rows, cols = x.shape
+        dtype = x.dtype
+    except (AttributeError, ValueError):
+        raise TypeError(f"{name} must be a 2-d tensor") from None
+    if dtype not in (dtypes or _TYPES):
+        raise TypeError(f"{name} must be of {' or '.join(str(d) for d in dtypes or _TYPES)}, not {dtype}")
     if device is not None and x.device != device:
         raise TypeError(f"{name} must be on {device}, not {x.device}")
-    if shape is not None and tuple(x.shape) != shape:
+    if shape is not None and (rows, cols) != shape:
         raise ValueError(f"{name} must be {list(shape)}, not {list(x.shape)}")
-    if x.shape[1] > 1 and x.stride(1) != 1 or x.shape[0] > 1 and x.stride(0) < x.shape[1]:
+    along, across = x.stride()
+    if across != 1 and cols > 1 or along < cols and rows > 1:
         return x.contiguous()
     return x
 
 
 def _row_stride(x: torch.Tensor) -> int:
-    return max(x.stride(0), x.shape[1]) if x.shape[0] > 1 else x.shape[1]
+    rows, cols = x.shape
+    return x.stride(0) if rows > 1 else cols
 
 
 def _vector(x, name: str, n: int, device, dtypes) -> torch.Tensor:
-    if not isinstance(x, torch.Tensor) or x.dim() != 1 or x.device != device or x.dtype not in dtypes:
+    if not isinstance(x, torch.Tensor) or x.dim() != 1 or x.dtype not in dtypes or x.device != device:
         raise TypeError(f"{name} must be a 1-d tensor of {' or '.join(str(d) for d in dtypes)} on {device}")
     if x.shape[0] != n:
         raise ValueError(f"{name} must have {n} values, not {x.shape[0]}")
-    return x.contiguous()
+    return x if x.is_contiguous() else x.contiguous()
 
 
 def _on_gpu(x: torch.Tensor, name: str):
-    if x.device.type != "cuda":
+    if not x.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor")
 
 
@@ -156,18 +161,29 @@ _HALVES = (torch.bfloat16, torch.float16)
 
 
 def _linear_args(x, weight, activation):
+    """(x, weight, their device, the call's arguments so far)"""
     x = _matrix(x, "x", _HALVES)
     _on_gpu(x, "x")
     m, k = x.shape
-    weight = _matrix(weight, "weight", (x.dtype,), None, x.device)
-    if weight.shape[1] != k:
+    dtype, device = x.dtype, x.device
+    weight = _matrix(weight, "weight", (dtype,), None, device)
+    n, along = weight.shape
+    if along != k:
         raise ValueError(f"weight must be [n, {k}], not {list(weight.shape)}")
-    act = _ACTIVATIONS.get("none" if activation is None else activation)
+    act = _ACTIVATIONS.get(activation)
     if act is None:
-        raise ValueError(f"activation must be one of {', '.join(_ACTIVATIONS)}, not {activation!r}")
-    a = L.LinearArgs(m=m, n=weight.shape[0], k=k, d_x=x.data_ptr(), x_stride=_row_stride(x), d_weight=weight.data_ptr(),
-                     weight_stride=_row_stride(weight), type=_TYPES[x.dtype], activation=act)
-    return x, weight, a
+        raise ValueError(f"activation must be one of {', '.join(filter(None, _ACTIVATIONS))}, not {activation!r}")
+    return x, weight, device, L.LinearArgs(m=m, n=n, k=k, d_x=x.data_ptr(), x_stride=_row_stride(x), d_weight=weight.data_ptr(),
+                                           weight_stride=_row_stride(weight), type=_TYPES[dtype], activation=act)
+
+
+def _run_linear(call, workspace, args, device):
+    with _current(device):
+        size = workspace(args)
+        if size:
+            ws = _workspace(size, device)
+            args.d_workspace, args.workspace_bytes = ws.data_ptr(), size
+        _check(call(args, _stream(device)))
 
 
 def linear(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None = None, *, activation: str | None = None,
@@ -176,26 +192,22 @@ def linear(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None = No
     [m, n], all of x's type; activation: "none", "relu", "gelu_tanh" or "silu".  With
     save_pre also the value before the activation, [m, n], for linear_backward (None
     without an activation, whose gradient does not need it)."""
-    x, weight, a = _linear_args(x, weight, activation)
-    m, n = a.m, a.n
+    x, weight, device, a = _linear_args(x, weight, activation)
+    m, n, dtype = a.m, a.n, x.dtype
     if bias is not None:
-        bias = _vector(bias, "bias", n, x.device, (x.dtype,))
+        bias = _vector(bias, "bias", n, device, (dtype,))
         a.d_bias = bias.data_ptr()
     if residual is not None:
-        residual = _matrix(residual, "residual", (x.dtype,), (m, n), x.device)
+        residual = _matrix(residual, "residual", (dtype,), (m, n), device)
         a.d_residual, a.residual_stride = residual.data_ptr(), _row_stride(residual)
-    y = torch.empty((m, n), dtype=x.dtype, device=x.device)
+    y = torch.empty((m, n), dtype=dtype, device=device)
     a.d_y, a.y_stride = y.data_ptr(), n
     pre = None
     if save_pre and a.activation != L.ACT_NONE:
-        pre = torch.empty((m, n), dtype=x.dtype, device=x.device)
+        pre = torch.empty((m, n), dtype=dtype, device=device)
         a.d_pre, a.pre_stride = pre.data_ptr(), n
     lib = L.load()
-    with _current(x.device):
-        ws = _workspace(lib.mlkv_linear_workspace(a), x.device)
-        if ws is not None:
-            a.d_workspace, a.workspace_bytes = ws.data_ptr(), ws.numel()
-        _check(lib.mlkv_linear(a, _stream(x.device)))
+    _run_linear(lib.mlkv_linear, lib.mlkv_linear_workspace, a, device)
     return (y, pre) if save_pre else y
 
 
@@ -204,25 +216,27 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, pre
     """Gradients (dx, dweight, dbias) of linear(x, weight, bias, activation=...), all of
     x's type; dbias is None without `bias`, the others where they are not wanted.  pre:
     what save_pre gave (needed with an activation).  The residual's gradient is dy."""
-    x, weight, a = _linear_args(x, weight, activation)
-    m, n, k = a.m, a.n, a.k
-    dy = _matrix(dy, "dy", (x.dtype,), (m, n), x.device)
+    x, weight, device, a = _linear_args(x, weight, activation)
+    m, n, k, dtype = a.m, a.n, a.k, x.dtype
+    dy = _matrix(dy, "dy", (dtype,), (m, n), device)
     a.d_dy, a.dy_stride = dy.data_ptr(), _row_stride(dy)
     if a.activation != L.ACT_NONE:
         if pre is None:
             raise TypeError("pre is needed for the gradient of an activation")
-        pre = _matrix(pre, "pre", (x.dtype,), (m, n), x.device)
+        pre = _matrix(pre, "pre", (dtype,), (m, n), device)
         a.d_pre, a.pre_stride = pre.data_ptr(), _row_stride(pre)
-    dx = torch.empty((m, k), dtype=x.dtype, device=x.device) if want_dx else None
-    dw = torch.empty((n, k), dtype=x.dtype, device=x.device) if want_dweight else None
-    db = torch.empty(n, dtype=x.dtype, device=x.device) if bias else None
-    a.d_dx, a.dx_stride, a.d_dweight, a.dweight_stride, a.d_dbias = _ptr(dx), k, _ptr(dw), k, _ptr(db)
+    dx = dw = db = None
+    if want_dx:
+        dx = torch.empty((m, k), dtype=dtype, device=device)
+        a.d_dx, a.dx_stride = dx.data_ptr(), k
+    if want_dweight:
+        dw = torch.empty((n, k), dtype=dtype, device=device)
+        a.d_dweight, a.dweight_stride = dw.data_ptr(), k
+    if bias:
+        db = torch.empty(n, dtype=dtype, device=device)
+        a.d_dbias = db.data_ptr()
     lib = L.load()
-    with _current(x.device):
-        ws = _workspace(lib.mlkv_linear_backward_workspace(a), x.device)
-        if ws is not None:
-            a.d_workspace, a.workspace_bytes = ws.data_ptr(), ws.numel()
-        _check(lib.mlkv_linear_backward(a, _stream(x.device)))
+    _run_linear(lib.mlkv_linear_backward, lib.mlkv_linear_backward_workspace, a, device)
     return dx, dw, db
 
 
