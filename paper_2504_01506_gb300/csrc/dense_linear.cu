@@ -711,36 +711,18 @@ struct Caller {
         const int64_t tiles = (int64_t)p.tiles_i * p.tiles_j * p.shares;
         auto go = [&](auto kernel) {
             if (!dense_smem(kernel, R::kBytes)) rc = MLKV_ERR_CUDA;
-            else if (PAIR) launch_clusters(kernel, 2, 2 * std::min<int64_t>(tiles, sms / 2), R::kThreads, R::kBytes, ma, mb, p);
-            else if (p.joined) launch_clusters(kernel, p.shares, tiles, R::kThreads, R::kBytes, ma, mb, p);
+            else if (PAIR) launch_clusters(kernel, 2, 2 * std::min<int64_t>(tiles, sms / 2), R::kThreads, R::kBytes, st, ma, mb, p);
+            else if (p.joined) launch_clusters(kernel, p.shares, tiles, R::kThreads, R::kBytes, st, ma, mb, p);
             else launch_kernel(true, kernel, dim3((unsigned)std::min<int64_t>(tiles, sms)), dim3(R::kThreads), R::kBytes, st, ma, mb, p);
         };
         if (type == MLKV_TYPE_BFLOAT) go(k_product<BN, A_MN, B_MN, SWAP, PAIR, __nv_bfloat16>);
         else go(k_product<BN, A_MN, B_MN, SWAP, PAIR, __half>);
     }
-    template <class K>
-    void launch_clusters(K kernel, int cluster, int64_t blocks, int threads, size_t smem, const CUtensorMap& ma, const CUtensorMap& mb, const Product& p) {
-        cudaLaunchAttribute attr[2];
-        attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = cluster;
-        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-        attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr[1].val.programmaticStreamSerializationAllowed = 1;
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3((unsigned)blocks);
-        cfg.blockDim = dim3(threads);
-        cfg.dynamicSmemBytes = smem;
-        cfg.stream = st;
-        cfg.attrs = attr;
-        cfg.numAttrs = MLKV_PDL ? 2 : 1;
-        cudaLaunchKernelEx(&cfg, kernel, ma, mb, p);  // an error stays in cudaGetLastError()
-    }
-
     // Whether pairs of blocks take the tiles of 256 columns: where there are enough for every pair, and k is long
     // enough for the products to count beside the epilogue.  (Single blocks / pairs, us: 16,384 x 4,096 by k = 4,096
     // 331 / 298; 8,192 x 1,024 by 8,192 102 / 86; 4,096 x 4,096 by 1,024 32 / 29; 65,536 x 512 by 416 37 / 42.)
     bool pair_pays(int64_t tiles_i, int64_t tiles_j, int64_t blocks) const {
-        return (tiles_i + 1) / 2 * tiles_j >= sms / 2 && blocks >= 12;
+        return (tiles_i + 1) / 2 * tiles_j * (blocks / 12) >= sms / 2;
     }
 
     // out = epilogue(A B^T): A [rows][k], B [cols][k]; *_mn: held as [k][rows], [k][cols].

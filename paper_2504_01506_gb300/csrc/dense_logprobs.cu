@@ -49,6 +49,7 @@ struct ProbArgs {
     const int64_t* targets;
     float scale;
     int32_t vocab, top, spans, per_span;  // 16-byte pieces of a span
+    int32_t joined;               // a row's spans are a cluster, which joins them itself
     float* logprob;
     float* entropy;
     float* stats;
@@ -292,6 +293,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprobs(ProbArgs a
     __shared__ Key parts[32];        // the parts' largest values, with the batch that has it first
     __shared__ volatile unsigned long long bar;  // (value, last batch), raised by one warp or another
     __shared__ int count, values;
+    __shared__ __align__(16) float4 told;  // to the cluster
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     uint4* ring = reinterpret_cast<uint4*>(shared) + threadIdx.x;  // (a thread reads what it copied itself)
     int* listed = reinterpret_cast<int*>(shared + kStages * kStep * sizeof(uint4));
@@ -501,17 +503,46 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprobs(ProbArgs a
     } else {
         __syncthreads();
     }
-    if (warp != 0) return;
-    const float2 w = lane < kWarps ? sums[lane] : make_float2(0.f, 0.f);
-    sum.s = group_sum(w.x, 32);
-    sum.p = group_sum(w.y, 32);
-    const Key mine = TOP && lane < a.top ? list[lane] : 0ull;
-    if (a.spans == 1) {
-        finish_row<T>(a, r, most, sum.s, sum.p, mine, lane);
-        return;
+    if (warp == 0) {
+        const float2 w = lane < kWarps ? sums[lane] : make_float2(0.f, 0.f);
+        sum.s = group_sum(w.x, 32);
+        sum.p = group_sum(w.y, 32);
+        const Key mine = TOP && lane < a.top ? list[lane] : 0ull;
+        if (a.spans == 1) {
+            finish_row<T>(a, r, most, sum.s, sum.p, mine, lane);
+        } else if (a.joined) {
+            if (lane == 0) told = make_float4(most, sum.s, sum.p, 0.f);
+            if (TOP) parts[lane] = mine;
+        } else {
+            if (lane == 0) a.part[blockIdx.x] = make_float4(most, sum.s, sum.p, 0.f);
+            if (TOP && lane < a.top) a.keys[(int64_t)blockIdx.x * a.top + lane] = mine;
+        }
     }
-    if (lane == 0) a.part[blockIdx.x] = make_float4(most, sum.s, sum.p, 0.f);
-    if (TOP && lane < a.top) a.keys[(int64_t)blockIdx.x * a.top + lane] = mine;
+    if (!a.joined) return;
+    cluster_sync();
+    if (span == 0) {  // the cluster's first block: what the others have told
+        if (TOP) {
+            for (int i = threadIdx.x; i < a.spans * a.top; i += THREADS)
+                asm volatile("ld.shared::cluster.b64 %0, [%1];" : "=l"(list[i]) : "r"(place_in(smem_of(&parts[i % a.top]), i / a.top)) : "memory");
+            select<THREADS>(list, a.spans * a.top, a.top);
+        }
+        if (warp == 0) {
+            float4 its = make_float4(-CUDART_INF_F, 0.f, 0.f, 0.f);
+            if (lane < a.spans)
+                asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                             : "=f"(its.x), "=f"(its.y), "=f"(its.z), "=f"(its.w)
+                             : "r"(place_in(smem_of(&told), lane))
+                             : "memory");
+            float m = its.x;
+            for (int o = 16; o; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
+            Sums one = {0.f, its.y, its.z};
+            if (its.x != -CUDART_INF_F) one.move(0.f, (its.x - m) * c);
+            const float s = group_sum(one.s, 32), p = group_sum(one.p, 32);
+            finish_row<T>(a, r, m, s, p, TOP && lane < a.top ? list[lane] : 0ull, lane);
+        }
+        __syncwarp();
+    }
+    cluster_sync();  // (nothing of a block's memory is wanted by another any more)
 }
 
 // A row's spans joined (a block a row).
@@ -644,6 +675,7 @@ __global__ void __launch_bounds__(kMostThreads, 4) k_logprobs_backward(GradArgs 
 
 struct Split {
     int threads, NV, parts, per_part;
+    bool joined;
 };
 
 // 16-byte pieces of the longest row: one more where rows may begin within one.
@@ -664,24 +696,30 @@ Split spans_of(int64_t n, int64_t pieces, int sms) {
             break;
         }
     const int64_t wave = (int64_t)sms * (1024 / threads);
+    // Few rows: up to 8 spans of at least 256 pieces, a cluster, which saves a launch; where they stay short
+    // beside the time that takes.
+    if (n * 8 <= wave && pieces >= 512 && pieces <= 8 * 8192) {
+        const int64_t s = std::min<int64_t>(8, pieces / 256);
+        return {threads, 0, (int)s, (int)((pieces + s - 1) / s), true};
+    }
     int64_t best = 1, cost = INT64_MAX;
     for (int64_t s = 1; s <= kMostSpans && (s == 1 || pieces / s >= 256); ++s) {
         const int64_t now = (n * s + wave - 1) / wave * (pieces / s + 1700);
         if (now < cost) cost = now, best = s;
         if (n > 4 * wave) break;
     }
-    return {threads, 0, (int)best, (int)((pieces + best - 1) / best)};
+    return {threads, 0, (int)best, (int)((pieces + best - 1) / best), false};
 }
 
 // The backward pass: a block holds what it loads at once, up to 8 pieces a thread.
 Split parts_of(int64_t n, int64_t pieces, int sms) {
     for (int t = 32; t <= kMostThreads; t *= 2)
         for (int nv = 1; nv <= 4; nv *= 2)
-            if (pieces <= (int64_t)t * nv) return {t, nv, 1, (int)pieces};
+            if (pieces <= (int64_t)t * nv) return {t, nv, 1, (int)pieces, false};
     int nv = 8;
     while (nv > 2 && n * ((pieces + kMostThreads * nv - 1) / (kMostThreads * nv)) < 2 * sms) nv /= 2;
     const int64_t parts = (pieces + kMostThreads * nv - 1) / (kMostThreads * nv);
-    return {kMostThreads, nv, (int)parts, (int)((pieces + parts - 1) / parts)};
+    return {kMostThreads, nv, (int)parts, (int)((pieces + parts - 1) / parts), false};
 }
 
 template <class F>
@@ -725,7 +763,7 @@ extern "C" int64_t mlkv_token_logprobs_workspace(int64_t n, int64_t vocab, int32
     int64_t most = 0;  // wherever the rows begin
     for (bool aligned : {false, true}) {
         const Split s = spans_of(n, pieces_of(vocab, dense_type_size(type), aligned), sms);
-        if (s.parts > 1) most = std::max(most, n * s.parts * (16 + 8 * (int64_t)top));
+        if (s.parts > 1 && !s.joined) most = std::max(most, n * s.parts * (16 + 8 * (int64_t)top));
     }
     return most;
 }
@@ -744,10 +782,10 @@ extern "C" int mlkv_token_logprobs(const void* d_logits, int64_t stride, int32_t
     const int size = dense_type_size(type);
     const Split s = spans_of(n, pieces_of(vocab, size, pieces_aligned(d_logits, stride, size)), sms);
     if (!grid_ok(n, s)) return MLKV_ERR_UNSUPPORTED;
-    if (!workspace_ok(d_workspace, workspace_bytes, s.parts > 1 ? n * s.parts * (16 + 8 * (int64_t)top) : 0)) return MLKV_ERR_INVALID;
+    if (!workspace_ok(d_workspace, workspace_bytes, s.parts > 1 && !s.joined ? n * s.parts * (16 + 8 * (int64_t)top) : 0)) return MLKV_ERR_INVALID;
     ProbArgs a = {};
     a.x = d_logits; a.stride = stride; a.n = n; a.targets = d_targets; a.scale = scale; a.vocab = (int32_t)vocab;
-    a.top = top; a.spans = s.parts; a.per_span = s.per_part; a.logprob = d_logprob; a.entropy = d_entropy;
+    a.top = top; a.spans = s.parts; a.per_span = s.per_part; a.joined = s.joined; a.logprob = d_logprob; a.entropy = d_entropy;
     a.stats = d_stats; a.top_logprobs = d_top_logprobs; a.top_ids = d_top_ids;
     a.part = static_cast<float4*>(d_workspace);
     a.keys = reinterpret_cast<Key*>(a.part + n * s.parts);
@@ -759,14 +797,16 @@ extern "C" int mlkv_token_logprobs(const void* d_logits, int64_t stride, int32_t
         auto launch = [&](auto kernel, bool listed) {
             const size_t bytes = (size_t)s.threads * (kStages * kBatch * sizeof(uint4) + (listed ? kListed * sizeof(int) : 0));
             ok = dense_smem(kernel, bytes);
-            if (ok) launch_kernel(true, kernel, grid, block, bytes, st, a);
+            if (!ok) return;
+            if (s.joined) launch_clusters(kernel, s.parts, n * s.parts, s.threads, bytes, st, a);
+            else launch_kernel(true, kernel, grid, block, bytes, st, a);
         };
         by_threads(s.threads, [&](auto n) {
             constexpr int N = decltype(n)::value;
             if (top) launch(k_logprobs<T, true, N>, true);
             else launch(k_logprobs<T, false, N>, false);
         });
-        if (ok && s.parts > 1) launch_kernel(true, k_logprobs_join<T>, dim3((unsigned)n), dim3(kMostThreads), 0, st, a);
+        if (ok && s.parts > 1 && !s.joined) launch_kernel(true, k_logprobs_join<T>, dim3((unsigned)n), dim3(kMostThreads), 0, st, a);
     });
     return ok && cudaGetLastError() == cudaSuccess ? MLKV_OK : MLKV_ERR_CUDA;
 }

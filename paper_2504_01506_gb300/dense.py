@@ -148,10 +148,11 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor 
     db = torch.empty(dim, dtype=wt, device=x.device) if bias else None
     lib = L.load()
     with _current(x.device):
-        ws = _workspace(lib.mlkv_layer_norm_backward_workspace(rows, dim), x.device)
+        size = lib.mlkv_layer_norm_backward_workspace(rows, dim)
+        ws = _workspace(size, x.device)
         _check(lib.mlkv_layer_norm_backward(dy.data_ptr(), _row_stride(dy), _TYPES[dy.dtype], x.data_ptr(), _row_stride(x),
                                             _TYPES[x.dtype], rows, dim, _ptr(w), kind, stats.data_ptr(), dx.data_ptr(), dim,
-                                            _ptr(dw), _ptr(db), _ptr(ws), 0 if ws is None else ws.numel(),
+                                            _ptr(dw), _ptr(db), _ptr(ws), size,
                                             _stream(x.device)))
     return dx, dw, db
 
@@ -276,10 +277,11 @@ def token_logprobs(logits: torch.Tensor, targets: torch.Tensor, *, top: int = 0,
     lib = L.load()
     kind = _TYPES[logits.dtype]
     with _current(dev):
-        ws = _workspace(lib.mlkv_token_logprobs_workspace(n, vocab, kind, top), dev)
+        size = lib.mlkv_token_logprobs_workspace(n, vocab, kind, top)
+        ws = _workspace(size, dev) if size else None
         _check(lib.mlkv_token_logprobs(logits.data_ptr(), _row_stride(logits), kind, n, vocab, targets.data_ptr(), scale,
                                        top, logprob.data_ptr(), entropy.data_ptr(), stats.data_ptr(), _ptr(tops),
-                                       _ptr(ids), _ptr(ws), 0 if ws is None else ws.numel(), _stream(dev)))
+                                       _ptr(ids), _ptr(ws), size, _stream(dev)))
     return TokenLogprobs(logprob, entropy, stats, tops, ids)
 
 
