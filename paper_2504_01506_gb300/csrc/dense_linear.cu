@@ -190,58 +190,54 @@ __device__ __forceinline__ void join_shares(const Product& p, uint32_t at, int i
     }
 }
 
-// A warp's corner of shared memory.  The lane that has a row writes and reads it
-// here; memory is written and read rows side by side.  16-byte pieces are placed
-// so that neither a lane's going along its row nor the lanes' going along one
-// meets a bank twice: 32 rows of 64 bytes (32 values; room for two of these) have
-// piece c at c ^ (row / 2 & 3), 32 rows of 128 bytes (32 sums) at c ^ (row & 7).
-struct Corner {
+// A warp's corner of shared memory: two halves of 32 rows by 32 values (64 bytes a
+// row, 16-byte pieces in the 64-byte swizzle: piece c of a row at c ^ (row / 2 & 3)),
+// or 32 rows by 32 sums (128 bytes a row, piece c at c ^ (row & 7)).  The lane that
+// has a row writes and reads it here without bank conflicts, TMA or, for rows that
+// it does not take, the lanes side by side move it to memory and from it.
+struct Half {
     uint8_t* at;
     __device__ __forceinline__ uint4& piece(int row, int c) const { return *reinterpret_cast<uint4*>(at + row * 64 + ((c ^ (row >> 1 & 3)) << 4)); }
     __device__ __forceinline__ uint16_t& value(int row, int c) const {
         return *reinterpret_cast<uint16_t*>(at + row * 64 + (((c >> 3) ^ (row >> 1 & 3)) << 4) + (c & 7) * 2);
     }
-    __device__ __forceinline__ uint4& sums(int row, int c) const { return *reinterpret_cast<uint4*>(at + row * 128 + ((c ^ (row & 7)) << 4)); }
 };
+constexpr int kHalf = 2048, kCorner = 2 * kHalf, kBias = 128;
 
-// Where a block of 32 rows by 32 columns lies in a matrix of 16-bit values, and how it is moved.
+// A block of 32 rows by 32 columns of a matrix of 16-bit values.
 struct Place {
-    int64_t r0, c0, rows, cols;
-    int lane;
-    bool wide;  // all its columns are there, and 16 bytes of a row can be moved at a time
-    __device__ __forceinline__ int row(int i) const { return i * 8 + (lane >> 2); }  // of the i-th piece that this lane moves
-    template <class T> __device__ __forceinline__ T* at(T* m, int64_t stride, int i) const { return m + (r0 + row(i)) * stride + c0 + (lane & 3) * 8; }
+    int r0, c0, rows, cols, lane;  // (from r0, c0 on; of the matrix)
+    bool whole;                    // all its columns are there, and 16 bytes of a row can be moved at a time
 };
 template <class T>
-__device__ __forceinline__ void put_corner(Corner s, T* m, int64_t stride, const Place& q) {
-    if (q.wide) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (q.r0 + q.row(i) < q.rows) *reinterpret_cast<uint4*>(q.at(m, stride, i)) = s.piece(q.row(i), q.lane & 3);
-    } else if (q.c0 + q.lane < q.cols) {
+__device__ __forceinline__ void put_values(Half s, T* m, int64_t stride, const Place& q) {
+    if (q.c0 + q.lane >= q.cols) return;
+    uint16_t* at = reinterpret_cast<uint16_t*>(m) + q.r0 * stride + q.c0 + q.lane;
+    const int n = min(32, q.rows - q.r0);
 #pragma unroll 8
-        for (int r = 0; r < 32; ++r)
-            if (q.r0 + r < q.rows) reinterpret_cast<uint16_t*>(m)[(q.r0 + r) * stride + q.c0 + q.lane] = s.value(r, q.lane);
-    }
+    for (int r = 0; r < n; ++r, at += stride) *at = s.value(r, q.lane);
 }
-// A block of the residual: loaded ahead of its use, then put into the corner.
+// A block of the residual: loaded ahead of its use, then put into a half.
 template <class T>
 struct Ahead {
     uint4 v[4];
     __device__ __forceinline__ void load(const T* m, int64_t stride, const Place& q) {
-        if (!q.wide) return;
+        if (!q.whole) return;
+        const int row = q.r0 + (q.lane >> 2);
+        const T* at = m + row * stride + q.c0 + (q.lane & 3) * 8;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (q.r0 + q.row(i) < q.rows) v[i] = *reinterpret_cast<const uint4*>(q.at(m, stride, i));
+            if (row + i * 8 < q.rows) v[i] = *reinterpret_cast<const uint4*>(at + i * 8 * stride);
     }
-    __device__ __forceinline__ void settle(Corner s, const T* m, int64_t stride, const Place& q) const {
-        if (q.wide) {
+    __device__ __forceinline__ void settle(Half s, const T* m, int64_t stride, const Place& q) const {
+        if (q.whole) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s.piece(q.row(i), q.lane & 3) = v[i];
+            for (int i = 0; i < 4; ++i) s.piece(i * 8 + (q.lane >> 2), q.lane & 3) = v[i];
         } else if (q.c0 + q.lane < q.cols) {
+            const uint16_t* at = reinterpret_cast<const uint16_t*>(m) + q.r0 * stride + q.c0 + q.lane;
+            const int n = min(32, q.rows - q.r0);
 #pragma unroll 8
-            for (int r = 0; r < 32; ++r)
-                if (q.r0 + r < q.rows) s.value(r, q.lane) = reinterpret_cast<const uint16_t*>(m)[(q.r0 + r) * stride + q.c0 + q.lane];
+            for (int r = 0; r < n; ++r, at += stride) s.value(r, q.lane) = *at;
         }
     }
 };
@@ -251,13 +247,13 @@ struct Ahead {
 // there; the residual's first block is on its way before that, each other while
 // the one before it is worked on.
 template <class T, class W>
-__device__ __forceinline__ bool put_blocks(const Product& p, uint32_t tmem, Corner corner, int64_t r0, int64_t c0, int blocks, int share, int lane, W wait) {
+__device__ __forceinline__ bool put_blocks(const Product& p, const CUtensorMap* out_map, const CUtensorMap* pre_map, uint32_t tmem,
+                                           uint8_t* corner, float* bias_at, int r0, int c0, int blocks, int share, int lane, uint32_t& turn, W wait) {
     const Epilogue& e = p.e;
-    const Corner other = {corner.at + 2048};
     const T* residual = static_cast<const T*>(e.residual);
     auto place = [&](int b) { return Place{r0, c0 + b * 32, p.I, p.J, lane, e.wide && c0 + b * 32 + 32 <= p.J}; };
     auto bias_of = [&](int b) {
-        const int64_t c = c0 + b * 32 + lane;
+        const int c = c0 + b * 32 + lane;
         return c < p.J ? to_float(static_cast<const T*>(e.bias)[c]) : 0.f;
     };
     Ahead<T> ahead;
@@ -265,6 +261,7 @@ __device__ __forceinline__ bool put_blocks(const Product& p, uint32_t tmem, Corn
     if (e.bias) bias = bias_of(0);
     if (residual) ahead.load(residual, e.residual_stride, place(0));
     if (!wait()) return false;
+    const bool two = e.pre || residual;  // both halves have a use of their own; else they take turns, from tile to tile
 #pragma unroll 1
     for (int b = 0; b < blocks && c0 + b * 32 < p.J; ++b) {
         const Place q = place(b);
@@ -273,25 +270,23 @@ __device__ __forceinline__ bool put_blocks(const Product& p, uint32_t tmem, Corn
         tmem_ld32(tmem + b * 32, acc);
         if (e.part) {
             tmem_wait_ld();
-            float* part = e.part + share * e.part_size;  // (rows of whole 16-byte pieces)
+            auto sums = [&](int row, int c) -> uint4& { return *reinterpret_cast<uint4*>(corner + row * 128 + ((c ^ (row & 7)) << 4)); };
 #pragma unroll
-            for (int c = 0; c < 8; ++c) corner.sums(lane, c) = make_uint4(acc[4 * c], acc[4 * c + 1], acc[4 * c + 2], acc[4 * c + 3]);
+            for (int c = 0; c < 8; ++c) sums(lane, c) = make_uint4(acc[4 * c], acc[4 * c + 1], acc[4 * c + 2], acc[4 * c + 3]);
             __syncwarp();
-            const int c = lane & 7;
+            const int row = r0 + (lane >> 3), c = lane & 7;  // (rows of whole 16-byte pieces)
+            float* part = e.part + share * e.part_size + row * e.part_stride + q.c0 + c * 4;
+            if (q.c0 + c * 4 < e.part_stride)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int r = i * 4 + (lane >> 3);
-                if (r0 + r < p.I && q.c0 + c * 4 < e.part_stride)
-                    *reinterpret_cast<uint4*>(part + (r0 + r) * e.part_stride + q.c0 + c * 4) = corner.sums(r, c);
-            }
-            __syncwarp();
+                for (int i = 0; i < 8; ++i)
+                    if (row + i * 4 < p.I) *reinterpret_cast<uint4*>(part + i * 4 * e.part_stride) = sums(i * 4 + (lane >> 3), c);
             continue;
         }
         if (e.bias) {
-            reinterpret_cast<float*>(corner.at)[lane] = bias;
+            bias_at[lane] = bias;
             if (b + 1 < blocks) bias = bias_of(b + 1);
-            __syncwarp();
         }
+        __syncwarp();
         tmem_wait_ld();
         float2 v[16];
 #pragma unroll
@@ -299,55 +294,69 @@ __device__ __forceinline__ bool put_blocks(const Product& p, uint32_t tmem, Corn
         if (e.bias) {
 #pragma unroll
             for (int k = 0; k < 16; k += 2) {
-                const float4 x = reinterpret_cast<const float4*>(corner.at)[k / 2];
+                const float4 x = reinterpret_cast<const float4*>(bias_at)[k / 2];
                 v[k] = add2(v[k], make_float2(x.x, x.y));
                 v[k + 1] = add2(v[k + 1], make_float2(x.z, x.w));
             }
-            __syncwarp();
         }
-        auto stage = [&] {
+        // What a half holds goes to memory; whoever fills it next waits until it has been read.
+        auto put = [&](Half s, const CUtensorMap* map, void* m, int64_t stride) {
 #pragma unroll
             for (int c = 0; c < 4; ++c)
-                corner.piece(lane, c) = make_uint4(word_of_pair<T>(v[4 * c]), word_of_pair<T>(v[4 * c + 1]), word_of_pair<T>(v[4 * c + 2]), word_of_pair<T>(v[4 * c + 3]));
+                s.piece(lane, c) = make_uint4(word_of_pair<T>(v[4 * c]), word_of_pair<T>(v[4 * c + 1]), word_of_pair<T>(v[4 * c + 2]), word_of_pair<T>(v[4 * c + 3]));
+            if (e.wide) fence_async();
+            __syncwarp();
+            if (!e.wide) put_values(s, static_cast<T*>(m), stride, q);
+            else if (lane == 0) tma_store(map, q.c0, q.r0, smem_of(s.at));
+        };
+        auto free_half = [&](bool all) {  // all stores have read theirs, or all but the last
+            if (e.wide && lane == 0) {
+                if (all) tma_store_read<0>();
+                else tma_store_read<1>();
+            }
             __syncwarp();
         };
+        const Half first = {corner}, second = {corner + kHalf};
         if (e.pre) {
-            stage();
-            put_corner(corner, static_cast<T*>(e.pre), e.pre_stride, q);
+            free_half(false);
+            put(first, pre_map, e.pre, e.pre_stride);
         }
         if (residual) {
-            ahead.settle(other, residual, e.residual_stride, q);
+            free_half(!e.pre);
+            ahead.settle(second, residual, e.residual_stride, q);
             if (b + 1 < blocks) ahead.load(residual, e.residual_stride, place(b + 1));
         }
         by_act(e.act, [&](auto act) {
 #pragma unroll
             for (int k = 0; k < 16; ++k) v[k] = activate<decltype(act)::value>(v[k]);
         });
-        __syncwarp();
         if (residual) {
+            __syncwarp();
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-                const uint4 x = other.piece(lane, c);
+                const uint4 x = second.piece(lane, c);
                 v[4 * c] = add2(v[4 * c], pair_of_word<T>(x.x));
                 v[4 * c + 1] = add2(v[4 * c + 1], pair_of_word<T>(x.y));
                 v[4 * c + 2] = add2(v[4 * c + 2], pair_of_word<T>(x.z));
                 v[4 * c + 3] = add2(v[4 * c + 3], pair_of_word<T>(x.w));
             }
+            __syncwarp();
+        } else {
+            free_half(false);
         }
-        stage();
-        put_corner(corner, static_cast<T*>(e.out), e.out_stride, q);
+        put(two || (turn++ & 1) ? second : first, out_map, e.out, e.out_stride);
     }
     return true;
 }
 
-// The shared memory of a block: the ring of operand tiles, and a corner for every
-// epilogue warp.
+// The shared memory of a block: the ring of operand tiles, and a corner and 32
+// bias values for every epilogue warp.
 // A pair of blocks has a tile of 256 rows between them, and half of its columns' operand each.
 template <int BN, bool SWAP, bool PAIR> struct Ring {
     static constexpr int kEpilogue = SWAP || BN < 128 ? 4 : 8;  // warps
     static constexpr int kThreads = (kEpilogue + 2) * 32;       // ... and the TMA warp, and the MMA warp
     static constexpr int kA = kBM * kBK * 2, kB = (PAIR ? BN / 2 : BN) * kBK * 2, kStage = kA + kB;
-    static constexpr int kCorners = SWAP ? 0 : kEpilogue * 4096;
+    static constexpr int kCorners = SWAP ? 0 : kEpilogue * (kCorner + kBias);
     static constexpr int kFit = (kDenseSmem - 1024 - kCorners) / kStage;
     static constexpr int kStages = kFit < 12 ? kFit : 12;
     static constexpr int kBytes = kStages * kStage + kCorners + 1024;  // (aligned to 1,024 within)
@@ -361,7 +370,8 @@ template <int BN, bool SWAP, bool PAIR> struct Ring {
 // products of both, so that B crosses each SM's shared memory half as often.
 template <int BN, bool A_MN, bool B_MN, bool SWAP, bool PAIR, class T>
 __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR>::kThreads, 1)
-    k_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mb, const Product p) {
+    k_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mb,
+              const __grid_constant__ CUtensorMap out_map, const __grid_constant__ CUtensorMap pre_map, const Product p) {
     using R = Ring<BN, SWAP, PAIR>;
     constexpr int S = R::kStages, kTma = R::kEpilogue, kMma = kTma + 1, kBlocks = PAIR ? 2 : 1, kCols = BN / kBlocks;
     extern __shared__ uint8_t raw[];
@@ -459,7 +469,7 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR>::kThreads, 1)
             }
         }
     } else {
-        uint32_t u = 0;
+        uint32_t u = 0, turn = 0;
         const uint32_t told = PAIR ? place_in(drained, 0) : drained;
         for (int t = first; t < total; t += step, ++u) {
             int i, j, share;
@@ -470,7 +480,7 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR>::kThreads, 1)
                 tc_fence_after();
                 return ok;
             };
-            const int64_t r0 = ((int64_t)i * kBlocks + rank) * kBM + (warp & 3) * 32;
+            const int r0 = (i * kBlocks + (int)rank) * kBM + (warp & 3) * 32;
             if constexpr (SWAP) {
                 if (!wait()) break;
 #pragma unroll 1
@@ -490,8 +500,10 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR>::kThreads, 1)
                 }
             } else {
                 const int cols = BN * 4 / R::kEpilogue, c = (warp >> 2) * cols;  // this warp's
-                const Corner corner = {reinterpret_cast<uint8_t*>(raw) + (ring - smem_of(raw)) + S * R::kStage + warp * 4096};
-                if (!put_blocks<T>(p, at + c, corner, r0, (int64_t)j * BN + c, r0 < p.I ? cols / 32 : 0, share, lane, wait)) break;
+                uint8_t* corners = raw + (ring - smem_of(raw)) + S * R::kStage;
+                if (!put_blocks<T>(p, &out_map, &pre_map, at + c, corners + warp * kCorner,
+                                   reinterpret_cast<float*>(corners + R::kEpilogue * kCorner + warp * kBias), r0, j * BN + c,
+                                   r0 < p.I ? cols / 32 : 0, share, lane, turn, wait)) break;
             }
             __syncwarp();
             tc_fence_before();
@@ -502,6 +514,7 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR>::kThreads, 1)
             }
         }
     }
+    if (!SWAP && warp < R::kEpilogue && lane == 0) tma_store_done();
     tc_fence_before();
     __syncthreads();
     if (joined) {
@@ -690,13 +703,16 @@ struct Caller {
     }
 
     bool encode(CUtensorMap* map, const Matrix& m, bool mn, int rows) {
+        return encode(map, m, 64, mn ? kBK : rows, CU_TENSOR_MAP_SWIZZLE_128B);
+    }
+    bool encode(CUtensorMap* map, const Matrix& m, int across, int down, CUtensorMapSwizzle swizzle) {
         const auto fn = tensor_map_encode();
         if (!fn) return false;
         const cuuint64_t dims[2] = {(cuuint64_t)m.cols, (cuuint64_t)m.rows}, strides[1] = {(cuuint64_t)m.stride * 2};
-        const cuuint32_t box[2] = {64, (cuuint32_t)(mn ? kBK : rows)}, step[2] = {1, 1};
+        const cuuint32_t box[2] = {(cuuint32_t)across, (cuuint32_t)down}, step[2] = {1, 1};
         return fn(map, type == MLKV_TYPE_BFLOAT ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
                   const_cast<uint16_t*>(m.p), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+                  swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
     }
 
     template <int BN, bool A_MN, bool B_MN, bool SWAP, bool PAIR = false>
@@ -707,13 +723,21 @@ struct Caller {
             rc = MLKV_ERR_CUDA;
             return;
         }
+        CUtensorMap out = ma, pre = ma;  // (not looked at where the epilogue does not store by TMA)
+        if (!SWAP && p.e.wide && !p.e.part) {
+            if (!encode(&out, {static_cast<const uint16_t*>(p.e.out), p.e.out_stride, p.I, p.J}, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B) ||
+                (p.e.pre && !encode(&pre, {static_cast<const uint16_t*>(p.e.pre), p.e.pre_stride, p.I, p.J}, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B))) {
+                rc = MLKV_ERR_CUDA;
+                return;
+            }
+        }
         p.idesc = mma_desc(type == MLKV_TYPE_BFLOAT, A_MN, B_MN, PAIR ? 2 * kBM : kBM, BN);
         const int64_t tiles = (int64_t)p.tiles_i * p.tiles_j * p.shares;
         auto go = [&](auto kernel) {
             if (!dense_smem(kernel, R::kBytes)) rc = MLKV_ERR_CUDA;
-            else if (PAIR) launch_clusters(kernel, 2, 2 * std::min<int64_t>(tiles, sms / 2), R::kThreads, R::kBytes, st, ma, mb, p);
-            else if (p.joined) launch_clusters(kernel, p.shares, tiles, R::kThreads, R::kBytes, st, ma, mb, p);
-            else launch_kernel(true, kernel, dim3((unsigned)std::min<int64_t>(tiles, sms)), dim3(R::kThreads), R::kBytes, st, ma, mb, p);
+            else if (PAIR) launch_clusters(kernel, 2, 2 * std::min<int64_t>(tiles, sms / 2), R::kThreads, R::kBytes, st, ma, mb, out, pre, p);
+            else if (p.joined) launch_clusters(kernel, p.shares, tiles, R::kThreads, R::kBytes, st, ma, mb, out, pre, p);
+            else launch_kernel(true, kernel, dim3((unsigned)std::min<int64_t>(tiles, sms)), dim3(R::kThreads), R::kBytes, st, ma, mb, out, pre, p);
         };
         if (type == MLKV_TYPE_BFLOAT) go(k_product<BN, A_MN, B_MN, SWAP, PAIR, __nv_bfloat16>);
         else go(k_product<BN, A_MN, B_MN, SWAP, PAIR, __half>);

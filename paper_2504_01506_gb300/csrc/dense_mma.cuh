@@ -75,6 +75,17 @@ __device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap* m
         : "memory");
 }
 
+// From shared memory (what the warp wrote there, each lane having fenced it) to the
+// matrix, clipped at its bounds; a group a store.
+__device__ __forceinline__ void tma_store(const CUtensorMap* m, int x, int y, uint32_t src) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(m), "r"(x), "r"(y), "r"(src) : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+template <int N>  // all but the last N groups of this thread have read their source
+__device__ __forceinline__ void tma_store_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void tma_store_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
 // --- tcgen05 (PAIR: of both blocks of the pair) ----------------------------------
 template <bool PAIR>
 __device__ __forceinline__ void tmem_alloc(uint32_t where, uint32_t columns) {
