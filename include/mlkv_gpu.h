@@ -66,7 +66,8 @@ extern "C" {
 #define MLKV_ERR_PROBE_LIMIT 6 /* an index probe exceeded the probe bound */
 #define MLKV_ERR_NOT_FOUND 7   /* absent key and insert_on_miss == 0 */
 #define MLKV_ERR_TIMEOUT 8     /* a bounded wait inside a kernel ran out: the grid barriers of the
-                                  miss path (new keys) of a call, between blocks of one grid */
+                                  miss path (new keys) of a call, between blocks of one grid; or a
+                                  matrix product's waits for its operands (mlkv_dense.h) */
 
 /* Largest dimension the row kernels take (8 vectors per lane of a warp). */
 #define MLKV_MAX_DIM 1024  /* dim > 256 needs dim % 4 == 0 */
@@ -347,7 +348,10 @@ int64_t mlkv_last_unique(mlkv_table* t);
  * lookups were not in the batch; mlkv_clear_status then makes the table whole
  * again).  While a wait is armed a gradient apply whose plan one thread-block
  * cluster would make (it has no wait that can run out) takes the general
- * kernels.  nth = 0 disarms.  One countdown per kind, shared by the whole
+ * kernels; for MLKV_FAULT_PRODUCT a launch of the matrix products' kernel
+ * (mlkv_dense.h), whose operands then never come: its waits run out (in two
+ * seconds or so), its outputs are not valid and mlkv_dense_sync returns
+ * MLKV_ERR_TIMEOUT once.  nth = 0 disarms.  One countdown per kind, shared by the whole
  * process.  No GPU work is affected: nothing faults on the device.  A failed
  * mlkv_open frees everything it allocated and leaves *out null; a failed
  * *_host call leaves the table usable.  Returns MLKV_ERR_INVALID for an
@@ -355,6 +359,7 @@ int64_t mlkv_last_unique(mlkv_table* t);
 #define MLKV_FAULT_ALLOC 1
 #define MLKV_FAULT_COPY 2
 #define MLKV_FAULT_WAIT 3
+#define MLKV_FAULT_PRODUCT 4
 int mlkv_debug_fail(int32_t kind, int64_t nth);
 
 /* Text of the last error this handle saw (static storage of the handle). */

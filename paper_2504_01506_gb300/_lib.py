@@ -50,6 +50,7 @@ EXPORTED = [
 FAULT_ALLOC = 1
 FAULT_COPY = 2
 FAULT_WAIT = 3
+FAULT_PRODUCT = 4
 STATIC_MAX_KEYS = 65536
 
 # include/mlkv_dense.h

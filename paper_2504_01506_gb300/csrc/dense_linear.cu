@@ -40,6 +40,7 @@ struct Product {
     int32_t I, J, blocks;            // extents; 64-value blocks along k
     int32_t tiles_i, tiles_j, shares, blocks_per_share;
     int32_t joined;                  // a tile's shares are a cluster, which adds them up itself
+    int32_t injected;                // (mlkv_debug_fail) no operands are brought
     uint32_t idesc;
     Epilogue e;
 };
@@ -377,11 +378,11 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR>::kThreads, 1)
     using R = Ring<BN, SWAP, PAIR>;
     constexpr int S = R::kStages, kTma = R::kEpilogue, kMma = kTma + 1, kBlocks = PAIR ? 2 : 1, kCols = BN / kBlocks;
     extern __shared__ uint8_t raw[];
-    __shared__ __align__(8) uint64_t bars[2 * S + 4];
+    __shared__ __align__(8) uint64_t bars[2 * S + 5];
     __shared__ uint32_t tmem_at;
     __shared__ volatile int stop;
     const uint32_t ring = (smem_of(raw) + 1023u) & ~1023u;
-    const uint32_t full = smem_of(bars), empty = full + 8 * S, done = empty + 8 * S, drained = done + 16;
+    const uint32_t full = smem_of(bars), empty = full + 8 * S, done = empty + 8 * S, drained = done + 16, ended = drained + 16;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = PAIR ? cluster_rank() : 0;
     const bool joined = SWAP && p.joined;
@@ -394,6 +395,7 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR>::kThreads, 1)
             mbar_init(done + 8 * s, 1);
             mbar_init(drained + 8 * s, kBlocks * R::kEpilogue);
         }
+        mbar_init(ended, 1);
         stop = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         tma_prefetch(&ma);
@@ -412,7 +414,7 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR>::kThreads, 1)
     const int total = joined ? tiles : tiles * p.shares, first = joined ? blockIdx.x / p.shares : blockIdx.x / kBlocks;
     const int step = joined ? tiles : gridDim.x / kBlocks;
     if (warp == kTma) {
-        if (lane == 0) {
+        if (lane == 0 && !p.injected) {
             uint32_t n = 0;  // stages filled
             bool ok = true;
             for (int t = first; t < total && ok; t += step) {
@@ -468,6 +470,10 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR>::kThreads, 1)
                     tc_commit<PAIR>(empty + 8 * s);
                 }
                 if (ok) tc_commit<PAIR>(done + 8 * acc);
+            }
+            if (!ok) {  // given up: products in flight still write into tensor memory
+                tc_commit<PAIR>(ended);
+                for (uint32_t tries = 0; tries < 1u << 20 && !mbar_try(ended, 0); ++tries) {}
             }
         }
     } else {
@@ -733,6 +739,7 @@ struct Caller {
                 return;
             }
         }
+        p.injected = take_injected_product();
         p.idesc = mma_desc(type == MLKV_TYPE_BFLOAT, A_MN, B_MN, PAIR ? 2 * kBM : kBM, BN);
         const int64_t tiles = (int64_t)p.tiles_i * p.tiles_j * p.shares;
         auto go = [&](auto kernel) {

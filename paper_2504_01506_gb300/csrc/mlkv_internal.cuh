@@ -653,6 +653,7 @@ inline int lookups_per_warp(const mlkv_table* t, int64_t n, int least) {
 // mlkv_table.cu: launch bookkeeping and optional per-kernel timing; the host
 // side of mlkv_debug_fail's wait injection (true once, for the armed launch).
 bool take_injected_wait();
+bool take_injected_product();  // dense_linear.cu's
 bool wait_injection_armed();
 void timer_before(mlkv_table* t, int kernel_id, cudaStream_t st);
 void timer_after(mlkv_table* t, int kernel_id, cudaStream_t st);

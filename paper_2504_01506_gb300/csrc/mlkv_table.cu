@@ -71,6 +71,7 @@ int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 std::atomic<int64_t> g_fail_alloc{0};
 std::atomic<int64_t> g_fail_copy{0};
 std::atomic<int64_t> g_fail_wait{0};
+std::atomic<int64_t> g_fail_product{0};
 
 bool injected(std::atomic<int64_t>& countdown) {
     int64_t v = countdown.load();
@@ -358,6 +359,7 @@ int choose_geom(mlkv_table* t, const void* a, const void* b) {
 namespace mlkv {
 
 bool take_injected_wait() { return injected(g_fail_wait); }
+bool take_injected_product() { return injected(g_fail_product); }
 
 bool wait_injection_armed() { return g_fail_wait.load() > 0; }
 
@@ -1016,6 +1018,7 @@ int mlkv_debug_fail(int32_t kind, int64_t nth) {
         case MLKV_FAULT_ALLOC: g_fail_alloc.store(nth); return MLKV_OK;
         case MLKV_FAULT_COPY: g_fail_copy.store(nth); return MLKV_OK;
         case MLKV_FAULT_WAIT: g_fail_wait.store(nth); return MLKV_OK;
+        case MLKV_FAULT_PRODUCT: g_fail_product.store(nth); return MLKV_OK;
         default: return MLKV_ERR_INVALID;
     }
 }
