@@ -87,7 +87,7 @@ int mlkv_layer_norm_backward(const void* d_dy, int64_t dy_stride, int32_t dy_typ
  * [m][n]; pre: [m][n], z rounded to `type`: an output of the forward pass where
  * not null, an input of the backward pass with an activation (null without).
  * dy: [m][n]; dx: [m][k]; dweight: [n][k]; dbias: [n]; each of the three may be
- * null (not wanted).  m, n, k >= 0, each < 2^31; k == 0 gives z = bias, m == 0
+ * null (not wanted).  m, n, k >= 0, each < 2^30; k == 0 gives z = bias, m == 0
  * gives zero dweight and dbias.  p is rounded to `type` where act is not NONE. */
 typedef struct mlkv_linear_args {
     int64_t m, n, k;

@@ -699,6 +699,7 @@ struct Caller {
         Align to[2] = {};
         int n = 0;
         for (Matrix* m : {&a, &b}) {
+            if (m->rows == 1) m->stride = round_up(m->cols, 8);  // (the one row's end is its end)
             if (m->aligned() || !m->rows || !m->cols) continue;
             const int64_t stride = round_up(m->cols, 8);
             uint16_t* p = static_cast<uint16_t*>(arena.take(m->rows * stride * 2));
@@ -797,9 +798,13 @@ struct Caller {
             p.joined = 1;
         }
         if (p.shares > 1 && !p.joined) {
-            p.e.part_stride = round_up(cols, 4);
-            p.e.part_size = rows * p.e.part_stride;
-            p.e.part = static_cast<float*>(arena.take(p.shares * p.e.part_size * 4));
+            e.part_stride = round_up(cols, 4);
+            e.part_size = rows * e.part_stride;
+            e.part = static_cast<float*>(arena.take(p.shares * e.part_size * 4));
+            p.e = Epilogue{};
+            p.e.part = e.part;
+            p.e.part_stride = e.part_stride;
+            p.e.part_size = e.part_size;
         }
         if (!run) return;
         if constexpr (!A_MN) {
@@ -816,8 +821,7 @@ struct Caller {
             else launch<256, A_MN, B_MN, false>(a, b, p);
         }
         if (p.shares > 1 && !p.joined) {
-            Epilogue f = p.e;
-            launch_kernel(true, k_product_finish, dim3(blocks_for(rows * cols)), dim3(256), 0, st, f, rows, cols, (int)p.shares);
+            launch_kernel(true, k_product_finish, dim3(blocks_for(rows * cols)), dim3(256), 0, st, e, rows, cols, (int)p.shares);
         }
     }
 
@@ -881,7 +885,7 @@ bool rows_ok(const void* p, int64_t stride, int64_t rows, int64_t cols, bool may
 }
 bool linear_ok(const mlkv_linear_args* g) {
     if (!g || g->m < 0 || g->n < 0 || g->k < 0) return false;
-    if (std::max(g->m, std::max(g->n, g->k)) >= (int64_t)1 << 31) return false;
+    if (std::max(g->m, std::max(g->n, g->k)) >= (int64_t)1 << 30) return false;  // (a tile's rows in 32 bits)
     if (g->type != MLKV_TYPE_BFLOAT && g->type != MLKV_TYPE_HALF) return false;
     if (g->activation < MLKV_ACT_NONE || g->activation > MLKV_ACT_SILU) return false;
     return rows_ok(g->d_x, g->x_stride, g->m, g->k, false) && rows_ok(g->d_weight, g->weight_stride, g->n, g->k, false);

@@ -18,7 +18,6 @@ memory comes from torch's allocator for the length of the call.  This module
 only checks arguments (TypeError, ValueError) and passes pointers.  Formulas and
 the treatment of masked and invalid values: include/mlkv_dense.h.
 """
-import contextlib
 import typing
 
 import torch
@@ -41,41 +40,64 @@ class TokenLogprobs(typing.NamedTuple):
     top_ids: torch.Tensor | None
 
 
-def _check(rc: int):
+_current_device = torch.cuda.current_device
+_empty = torch.empty
+
+
+def _call(device, call, *args):
+    """call(*args) with the device current (which it is, as a rule)."""
+    if _current_device() == device.index:
+        rc = call(*args)
+    else:
+        with torch.cuda.device(device):
+            rc = call(*args)
     if rc != L.OK:
         raise MLKVError(rc, L.load().mlkv_status_string(rc).decode())
 
 
-def _matrix(x, name: str, dtypes=_TYPES, shape=None, device=None) -> torch.Tensor:
-    """The tensor, with contiguous rows that do not overlap."""
+def _names(dtypes) -> str:
+    return " or ".join(str(d) for d in dtypes)
+
+
+def _rows(x, name: str, dtypes=_TYPES, shape=None, device=None):
+    """(the tensor, with contiguous rows that do not overlap; rows; columns; row stride)"""
     try:
         rows, cols = x.shape
+        along, across = x.stride()
         dtype = x.dtype
     except (AttributeError, ValueError):
         raise TypeError(f"{name} must be a 2-d tensor") from None
-    if dtype not in (dtypes or _TYPES):
-        raise TypeError(f"{name} must be of {' or '.join(str(d) for d in dtypes or _TYPES)}, not {dtype}")
+    if dtype not in dtypes:
+        raise TypeError(f"{name} must be of {_names(dtypes)}, not {dtype}")
     if device is not None and x.device != device:
         raise TypeError(f"{name} must be on {device}, not {x.device}")
     if shape is not None and (rows, cols) != shape:
-        raise ValueError(f"{name} must be {list(shape)}, not {list(x.shape)}")
-    along, across = x.stride()
+        raise ValueError(f"{name} must be {list(shape)}, not {[rows, cols]}")
     if across != 1 and cols > 1 or along < cols and rows > 1:
-        return x.contiguous()
-    return x
+        return x.contiguous(), rows, cols, cols
+    return x, rows, cols, along if rows > 1 else cols
+
+
+def _matrix(x, name: str, dtypes=None, shape=None, device=None) -> torch.Tensor:
+    return _rows(x, name, dtypes or _TYPES, shape, device)[0]
 
 
 def _row_stride(x: torch.Tensor) -> int:
-    rows, cols = x.shape
-    return x.stride(0) if rows > 1 else cols
+    return _rows(x, "x")[3]
 
 
 def _vector(x, name: str, n: int, device, dtypes) -> torch.Tensor:
-    if not isinstance(x, torch.Tensor) or x.dim() != 1 or x.dtype not in dtypes or x.device != device:
-        raise TypeError(f"{name} must be a 1-d tensor of {' or '.join(str(d) for d in dtypes)} on {device}")
-    if x.shape[0] != n:
-        raise ValueError(f"{name} must have {n} values, not {x.shape[0]}")
-    return x if x.is_contiguous() else x.contiguous()
+    try:
+        (size,) = x.shape
+        (step,) = x.stride()
+        fits = x.dtype in dtypes and x.device == device
+    except (AttributeError, ValueError):
+        fits = False
+    if not fits:
+        raise TypeError(f"{name} must be a 1-d tensor of {_names(dtypes)} on {device}")
+    if size != n:
+        raise ValueError(f"{name} must have {n} values, not {size}")
+    return x if step == 1 else x.contiguous()
 
 
 def _on_gpu(x: torch.Tensor, name: str):
@@ -83,51 +105,42 @@ def _on_gpu(x: torch.Tensor, name: str):
         raise TypeError(f"{name} must be a CUDA tensor")
 
 
-_HERE = contextlib.nullcontext()
-
-
-def _current(device):
-    """Makes the device current for a library call (nothing to do, as a rule)."""
-    return _HERE if torch.cuda.current_device() == device.index else torch.cuda.device(device)
-
-
-def _ptr(x) -> int | None:
-    return None if x is None else x.data_ptr()
-
-
 def _workspace(size: int, device):
-    if size < 0:
-        raise MLKVError(L.ERR_INVALID, "sizes that the operator does not take")
-    return torch.empty(size, dtype=torch.uint8, device=device) if size else None
+    """(a tensor to keep until the call is made, its address) for so many bytes."""
+    if size <= 0:
+        if size < 0:
+            raise MLKVError(L.ERR_INVALID, "sizes that the operator does not take")
+        return None, None
+    ws = _empty(size, dtype=torch.uint8, device=device)
+    return ws, ws.data_ptr()
 
 
 # -- layer norm ------------------------------------------------------------------
-def _norm_weights(weight, bias, dim, device):
-    types = tuple(_TYPES) if weight is None else (weight.dtype,)
-    w = None if weight is None else _vector(weight, "weight", dim, device, tuple(_TYPES))
-    b = None if bias is None else _vector(bias, "bias", dim, device, types)
-    kind = _TYPES[w.dtype] if w is not None else _TYPES[b.dtype] if b is not None else L.TYPE_FLOAT
-    return w, b, kind
-
-
 def layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None, *,
                eps: float = 1e-5, out_dtype: torch.dtype | None = None, save_stats: bool = False):
     """(x - mean) / sqrt(var + eps) * weight + bias, row by row: [rows, dim] of
     out_dtype (x's; any type where x is fp32).  weight and bias: [dim], of one type.
     With save_stats also the rows' (mean, 1 / sqrt(var + eps)), fp32 [rows, 2], for
     layer_norm_backward."""
-    x = _matrix(x, "x")
+    x, rows, dim, stride = _rows(x, "x")
     _on_gpu(x, "x")
-    rows, dim = x.shape
-    out_dtype = x.dtype if out_dtype is None else out_dtype
-    if out_dtype not in _TYPES or x.dtype != torch.float32 and out_dtype != x.dtype:
-        raise TypeError(f"out_dtype {out_dtype} of x's {x.dtype}")
-    w, b, kind = _norm_weights(weight, bias, dim, x.device)
-    y = torch.empty((rows, dim), dtype=out_dtype, device=x.device)
-    stats = torch.empty((rows, 2), dtype=torch.float32, device=x.device) if save_stats else None
-    with _current(x.device):
-        _check(L.load().mlkv_layer_norm(x.data_ptr(), _row_stride(x), _TYPES[x.dtype], rows, dim, _ptr(w), _ptr(b), kind,
-                                        eps, y.data_ptr(), dim, _TYPES[out_dtype], _ptr(stats), _stream(x.device)))
+    dtype, device = x.dtype, x.device
+    if out_dtype is None:
+        out_dtype = dtype
+    elif out_dtype != dtype and (out_dtype not in _TYPES or dtype != torch.float32):
+        raise TypeError(f"out_dtype {out_dtype} of x's {dtype}")
+    w = b = None
+    kind = L.TYPE_FLOAT
+    if weight is not None:
+        weight = _vector(weight, "weight", dim, device, _TYPES)
+        w, kind = weight.data_ptr(), _TYPES[weight.dtype]
+    if bias is not None:
+        bias = _vector(bias, "bias", dim, device, _TYPES if weight is None else (weight.dtype,))
+        b, kind = bias.data_ptr(), _TYPES[bias.dtype]
+    y = _empty((rows, dim), dtype=out_dtype, device=device)
+    stats = _empty((rows, 2), dtype=torch.float32, device=device) if save_stats else None
+    _call(device, L.load().mlkv_layer_norm, x.data_ptr(), stride, _TYPES[dtype], rows, dim, w, b, kind, eps, y.data_ptr(), dim,
+          _TYPES[out_dtype], stats.data_ptr() if save_stats else None, _stream(device))
     return (y, stats) if save_stats else y
 
 
@@ -136,24 +149,27 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor 
     """Gradients (dx of x's type, dweight, dbias of the weight's type or fp32) of a
     layer_norm whose save_stats gave `stats`; dweight is None without a weight, dbias
     with bias=False."""
-    x = _matrix(x, "x")
+    x, rows, dim, stride = _rows(x, "x")
     _on_gpu(x, "x")
-    rows, dim = x.shape
-    dy = _matrix(dy, "dy", tuple(_TYPES) if x.dtype == torch.float32 else (x.dtype,), (rows, dim), x.device)
-    stats = _matrix(stats, "stats", (torch.float32,), (rows, 2), x.device).contiguous()
-    w, _, kind = _norm_weights(weight, None, dim, x.device)
-    dx = torch.empty((rows, dim), dtype=x.dtype, device=x.device)
-    wt = torch.float32 if w is None else w.dtype
-    dw = None if w is None else torch.empty(dim, dtype=wt, device=x.device)
-    db = torch.empty(dim, dtype=wt, device=x.device) if bias else None
+    dtype, device = x.dtype, x.device
+    dy, _, _, dy_stride = _rows(dy, "dy", _TYPES if dtype == torch.float32 else (dtype,), (rows, dim), device)
+    stats = _rows(stats, "stats", (torch.float32,), (rows, 2), device)[0].contiguous()
+    dx = _empty((rows, dim), dtype=dtype, device=device)
+    dw = db = w = wt = None
+    if weight is not None:
+        weight = _vector(weight, "weight", dim, device, _TYPES)
+        w, wt = weight.data_ptr(), weight.dtype
+        dw = _empty(dim, dtype=wt, device=device)
+    else:
+        wt = torch.float32
+    if bias:
+        db = _empty(dim, dtype=wt, device=device)
     lib = L.load()
-    with _current(x.device):
-        size = lib.mlkv_layer_norm_backward_workspace(rows, dim)
-        ws = _workspace(size, x.device)
-        _check(lib.mlkv_layer_norm_backward(dy.data_ptr(), _row_stride(dy), _TYPES[dy.dtype], x.data_ptr(), _row_stride(x),
-                                            _TYPES[x.dtype], rows, dim, _ptr(w), kind, stats.data_ptr(), dx.data_ptr(), dim,
-                                            _ptr(dw), _ptr(db), _ptr(ws), size,
-                                            _stream(x.device)))
+    size = lib.mlkv_layer_norm_backward_workspace(rows, dim)
+    ws, at = _workspace(size, device)
+    _call(device, lib.mlkv_layer_norm_backward, dy.data_ptr(), dy_stride, _TYPES[dy.dtype], x.data_ptr(), stride, _TYPES[dtype],
+          rows, dim, w, _TYPES[wt], stats.data_ptr(), dx.data_ptr(), dim, dw.data_ptr() if w is not None else None,
+          db.data_ptr() if bias else None, at, size, _stream(device))
     return dx, dw, db
 
 
@@ -163,28 +179,27 @@ _HALVES = (torch.bfloat16, torch.float16)
 
 def _linear_args(x, weight, activation):
     """(x, weight, their device, the call's arguments so far)"""
-    x = _matrix(x, "x", _HALVES)
+    x, m, k, x_stride = _rows(x, "x", _HALVES)
     _on_gpu(x, "x")
-    m, k = x.shape
     dtype, device = x.dtype, x.device
-    weight = _matrix(weight, "weight", (dtype,), None, device)
-    n, along = weight.shape
+    weight, n, along, weight_stride = _rows(weight, "weight", (dtype,), None, device)
     if along != k:
-        raise ValueError(f"weight must be [n, {k}], not {list(weight.shape)}")
+        raise ValueError(f"weight must be [n, {k}], not {[n, along]}")
     act = _ACTIVATIONS.get(activation)
     if act is None:
         raise ValueError(f"activation must be one of {', '.join(filter(None, _ACTIVATIONS))}, not {activation!r}")
-    return x, weight, device, L.LinearArgs(m=m, n=n, k=k, d_x=x.data_ptr(), x_stride=_row_stride(x), d_weight=weight.data_ptr(),
-                                           weight_stride=_row_stride(weight), type=_TYPES[dtype], activation=act)
+    a = L.LinearArgs(m, n, k, x.data_ptr(), x_stride, weight.data_ptr(), weight_stride)
+    a.type = _TYPES[dtype]
+    a.activation = act
+    return x, weight, dtype, device, m, n, k, act, a
 
 
 def _run_linear(call, workspace, args, device):
-    with _current(device):
-        size = workspace(args)
-        if size:
-            ws = _workspace(size, device)
-            args.d_workspace, args.workspace_bytes = ws.data_ptr(), size
-        _check(call(args, _stream(device)))
+    size = workspace(args)
+    if size:
+        ws, args.d_workspace = _workspace(size, device)
+        args.workspace_bytes = size
+    _call(device, call, args, _stream(device))
 
 
 def linear(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None = None, *, activation: str | None = None,
@@ -193,19 +208,18 @@ def linear(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None = No
     [m, n], all of x's type; activation: "none", "relu", "gelu_tanh" or "silu".  With
     save_pre also the value before the activation, [m, n], for linear_backward (None
     without an activation, whose gradient does not need it)."""
-    x, weight, device, a = _linear_args(x, weight, activation)
-    m, n, dtype = a.m, a.n, x.dtype
+    x, weight, dtype, device, m, n, k, act, a = _linear_args(x, weight, activation)
     if bias is not None:
         bias = _vector(bias, "bias", n, device, (dtype,))
         a.d_bias = bias.data_ptr()
     if residual is not None:
-        residual = _matrix(residual, "residual", (dtype,), (m, n), device)
-        a.d_residual, a.residual_stride = residual.data_ptr(), _row_stride(residual)
-    y = torch.empty((m, n), dtype=dtype, device=device)
+        residual, _, _, a.residual_stride = _rows(residual, "residual", (dtype,), (m, n), device)
+        a.d_residual = residual.data_ptr()
+    y = _empty((m, n), dtype=dtype, device=device)
     a.d_y, a.y_stride = y.data_ptr(), n
     pre = None
-    if save_pre and a.activation != L.ACT_NONE:
-        pre = torch.empty((m, n), dtype=dtype, device=device)
+    if save_pre and act != L.ACT_NONE:
+        pre = _empty((m, n), dtype=dtype, device=device)
         a.d_pre, a.pre_stride = pre.data_ptr(), n
     lib = L.load()
     _run_linear(lib.mlkv_linear, lib.mlkv_linear_workspace, a, device)
@@ -217,24 +231,23 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, pre
     """Gradients (dx, dweight, dbias) of linear(x, weight, bias, activation=...), all of
     x's type; dbias is None without `bias`, the others where they are not wanted.  pre:
     what save_pre gave (needed with an activation).  The residual's gradient is dy."""
-    x, weight, device, a = _linear_args(x, weight, activation)
-    m, n, k, dtype = a.m, a.n, a.k, x.dtype
-    dy = _matrix(dy, "dy", (dtype,), (m, n), device)
-    a.d_dy, a.dy_stride = dy.data_ptr(), _row_stride(dy)
-    if a.activation != L.ACT_NONE:
+    x, weight, dtype, device, m, n, k, act, a = _linear_args(x, weight, activation)
+    dy, _, _, a.dy_stride = _rows(dy, "dy", (dtype,), (m, n), device)
+    a.d_dy = dy.data_ptr()
+    if act != L.ACT_NONE:
         if pre is None:
             raise TypeError("pre is needed for the gradient of an activation")
-        pre = _matrix(pre, "pre", (dtype,), (m, n), device)
-        a.d_pre, a.pre_stride = pre.data_ptr(), _row_stride(pre)
+        pre, _, _, a.pre_stride = _rows(pre, "pre", (dtype,), (m, n), device)
+        a.d_pre = pre.data_ptr()
     dx = dw = db = None
     if want_dx:
-        dx = torch.empty((m, k), dtype=dtype, device=device)
+        dx = _empty((m, k), dtype=dtype, device=device)
         a.d_dx, a.dx_stride = dx.data_ptr(), k
     if want_dweight:
-        dw = torch.empty((n, k), dtype=dtype, device=device)
+        dw = _empty((n, k), dtype=dtype, device=device)
         a.d_dweight, a.dweight_stride = dw.data_ptr(), k
     if bias:
-        db = torch.empty(n, dtype=dtype, device=device)
+        db = _empty(n, dtype=dtype, device=device)
         a.d_dbias = db.data_ptr()
     lib = L.load()
     _run_linear(lib.mlkv_linear_backward, lib.mlkv_linear_backward_workspace, a, device)
@@ -245,43 +258,43 @@ def sync(device=None):
     """Waits for the current stream; raises if a bounded wait inside a product's kernel
     ran out since the last call (its outputs are then not valid)."""
     device = torch.device("cuda", torch.cuda.current_device() if device is None else torch.device(device).index or 0)
-    with torch.cuda.device(device):
-        _check(L.load().mlkv_dense_sync(_stream(device)))
+    _call(device, L.load().mlkv_dense_sync, _stream(device))
 
 
 # -- log probabilities ------------------------------------------------------------------
 def _logits(logits, targets, scale):
-    logits = _matrix(logits, "logits")
+    logits, n, vocab, stride = _rows(logits, "logits")
     _on_gpu(logits, "logits")
-    if logits.shape[1] < 1:
+    if vocab < 1:
         raise ValueError("logits must have at least one column")
     if not 0 < scale < float("inf"):
         raise ValueError(f"scale must be positive and finite, not {scale}")
-    return logits, _vector(targets, "targets", logits.shape[0], logits.device, (torch.int64,))
+    device = logits.device
+    return logits, n, vocab, stride, device, _vector(targets, "targets", n, device, (torch.int64,))
 
 
 def token_logprobs(logits: torch.Tensor, targets: torch.Tensor, *, top: int = 0, scale: float = 1.0) -> TokenLogprobs:
     """Of every row of softmax(scale * logits) ([n, vocab]): the log probability of
     targets[i] (int64 [n]; negative: none, log probability 0), the entropy, and the
     `top` (at most 32) likeliest tokens, ties by the lowest index.  -inf masks a token."""
-    logits, targets = _logits(logits, targets, scale)
+    logits, n, vocab, stride, device, targets = _logits(logits, targets, scale)
     if not 0 <= top <= L.MAX_TOP:
         raise ValueError(f"top must be 0 to {L.MAX_TOP}, not {top}")
-    n, vocab = logits.shape
-    dev = logits.device
-    logprob = torch.empty(n, dtype=torch.float32, device=dev)
-    entropy = torch.empty(n, dtype=torch.float32, device=dev)
-    stats = torch.empty((n, 2), dtype=torch.float32, device=dev)
-    tops = torch.empty((n, top), dtype=torch.float32, device=dev) if top else None
-    ids = torch.empty((n, top), dtype=torch.int64, device=dev) if top else None
+    f32 = torch.float32
+    logprob = _empty(n, dtype=f32, device=device)
+    entropy = _empty(n, dtype=f32, device=device)
+    stats = _empty((n, 2), dtype=f32, device=device)
+    tops = ids = tops_at = ids_at = None
+    if top:
+        tops = _empty((n, top), dtype=f32, device=device)
+        ids = _empty((n, top), dtype=torch.int64, device=device)
+        tops_at, ids_at = tops.data_ptr(), ids.data_ptr()
     lib = L.load()
     kind = _TYPES[logits.dtype]
-    with _current(dev):
-        size = lib.mlkv_token_logprobs_workspace(n, vocab, kind, top)
-        ws = _workspace(size, dev) if size else None
-        _check(lib.mlkv_token_logprobs(logits.data_ptr(), _row_stride(logits), kind, n, vocab, targets.data_ptr(), scale,
-                                       top, logprob.data_ptr(), entropy.data_ptr(), stats.data_ptr(), _ptr(tops),
-                                       _ptr(ids), _ptr(ws), size, _stream(dev)))
+    size = lib.mlkv_token_logprobs_workspace(n, vocab, kind, top)
+    ws, at = _workspace(size, device)
+    _call(device, lib.mlkv_token_logprobs, logits.data_ptr(), stride, kind, n, vocab, targets.data_ptr(), scale, top,
+          logprob.data_ptr(), entropy.data_ptr(), stats.data_ptr(), tops_at, ids_at, at, size, _stream(device))
     return TokenLogprobs(logprob, entropy, stats, tops, ids)
 
 
@@ -292,18 +305,19 @@ def token_logprobs_backward(logits: torch.Tensor, targets: torch.Tensor, result:
     and entropies (fp32 [n]; None: 0) that token_logprobs of the same arguments gave in
     `result`.  in_place: written over the logits."""
     given = logits
-    logits, targets = _logits(logits, targets, scale)
-    n, vocab = logits.shape
-    dev = logits.device
-    stats = _matrix(result.stats, "result.stats", (torch.float32,), (n, 2), dev).contiguous()
-    entropy = _vector(result.entropy, "result.entropy", n, dev, (torch.float32,))
-    g = None if dlogprob is None else _vector(dlogprob, "dlogprob", n, dev, (torch.float32,))
-    h = None if dentropy is None else _vector(dentropy, "dentropy", n, dev, (torch.float32,))
-    if in_place and logits is not given:
-        raise TypeError("logits written in place must have contiguous rows")
-    out = logits if in_place else torch.empty((n, vocab), dtype=logits.dtype, device=dev)
-    with _current(dev):
-        _check(L.load().mlkv_token_logprobs_backward(logits.data_ptr(), _row_stride(logits), _TYPES[logits.dtype], n, vocab,
-                                                     targets.data_ptr(), scale, entropy.data_ptr(), stats.data_ptr(),
-                                                     _ptr(g), _ptr(h), out.data_ptr(), _row_stride(out), _stream(dev)))
+    logits, n, vocab, stride, device, targets = _logits(logits, targets, scale)
+    f32 = (torch.float32,)
+    stats = _rows(result.stats, "result.stats", f32, (n, 2), device)[0].contiguous()
+    entropy = _vector(result.entropy, "result.entropy", n, device, f32)
+    g = None if dlogprob is None else _vector(dlogprob, "dlogprob", n, device, f32)
+    h = None if dentropy is None else _vector(dentropy, "dentropy", n, device, f32)
+    if in_place:
+        if logits is not given:
+            raise TypeError("logits written in place must have contiguous rows")
+        out, out_stride = logits, stride
+    else:
+        out, out_stride = _empty((n, vocab), dtype=logits.dtype, device=device), vocab
+    _call(device, L.load().mlkv_token_logprobs_backward, logits.data_ptr(), stride, _TYPES[logits.dtype], n, vocab,
+          targets.data_ptr(), scale, entropy.data_ptr(), stats.data_ptr(), None if g is None else g.data_ptr(),
+          None if h is None else h.data_ptr(), out.data_ptr(), out_stride, _stream(device))
     return out
