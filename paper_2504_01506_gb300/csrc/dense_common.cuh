@@ -71,17 +71,18 @@ inline bool dense_smem(K* kernel, size_t bytes) {
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kDenseSmem) == cudaSuccess;
 }
 
-// A launch in clusters of `cluster` blocks; an error stays in cudaGetLastError().
+// A launch in clusters of blocks; an error stays in cudaGetLastError().
 template <typename... Params, typename... Args>
-inline void launch_clusters(void (*kernel)(Params...), int cluster, int64_t blocks, int threads, size_t smem, cudaStream_t st, Args&&... args) {
+inline void launch_clusters(void (*kernel)(Params...), dim3 cluster, dim3 grid, int threads, size_t smem, cudaStream_t st, Args&&... args) {
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = cluster;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[0].val.clusterDim.x = cluster.x;
+    attr[0].val.clusterDim.y = cluster.y;
+    attr[0].val.clusterDim.z = cluster.z;
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)blocks);
+    cfg.gridDim = grid;
     cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;

@@ -140,12 +140,42 @@ __device__ __forceinline__ void put_columns(const Product& p, const uint32_t (&r
     }
 }
 
-// The shares of a tile, [column j][128 rows i] of sums at `at` in the shared memory
-// of each block of the cluster, added up in order: this block's part of the rows,
-// four of one column a thread (of the 128 epilogue threads) at a time.
+// Four sums of one row of the output, from col on, through the epilogue.
+template <class T>
+__device__ __forceinline__ void put_four(const Epilogue& e, const float4& sum, int64_t row, int64_t col, int64_t cols) {
+    if (e.wide && col + 4 <= cols) {
+        float2 v[2] = {make_float2(sum.x, sum.y), make_float2(sum.z, sum.w)};
+        uint2 x = make_uint2(0, 0);
+        if (e.residual) x = *reinterpret_cast<const uint2*>(static_cast<const T*>(e.residual) + row * e.residual_stride + col);
+        if (e.bias) {
+            const T* b = static_cast<const T*>(e.bias) + col;
+            v[0] = add2(v[0], make_float2(to_float(b[0]), to_float(b[1])));
+            v[1] = add2(v[1], make_float2(to_float(b[2]), to_float(b[3])));
+        }
+        if (e.pre)
+            *reinterpret_cast<uint2*>(static_cast<T*>(e.pre) + row * e.pre_stride + col) = make_uint2(word_of_pair<T>(v[0]), word_of_pair<T>(v[1]));
+        by_act(e.act, [&](auto act) {
+            v[0] = activate<decltype(act)::value>(v[0]);
+            v[1] = activate<decltype(act)::value>(v[1]);
+        });
+        if (e.residual) {
+            v[0] = add2(v[0], pair_of_word<T>(x.x));
+            v[1] = add2(v[1], pair_of_word<T>(x.y));
+        }
+        *reinterpret_cast<uint2*>(static_cast<T*>(e.out) + row * e.out_stride + col) = make_uint2(word_of_pair<T>(v[0]), word_of_pair<T>(v[1]));
+        return;
+    }
+    const float v[4] = {sum.x, sum.y, sum.z, sum.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (col + k < cols) static_cast<T*>(e.out)[row * e.out_stride + col + k] = from_float<T>(finish(e, v[k], row, col + k));
+}
+
+// The shares of a tile whose rows run along the output's columns, [column j][128
+// rows i] of sums at `at` in the shared memory of each block of the cluster, added
+// up in order: this block's part of the rows, four of one column a thread (of 128) at a time.
 template <class T, int BN>
-__device__ __forceinline__ void join_shares(const Product& p, uint32_t at, int i, int j, uint32_t rank) {
-    const Epilogue& e = p.e;
+__device__ __forceinline__ void join_columns(const Product& p, uint32_t at, int i, int j, uint32_t rank) {
     const int rows = kBM / p.shares / 4, columns = min(BN, p.J - j * BN);
     for (int q = threadIdx.x; q < rows * columns; q += 128) {
         const int c = q / rows, r = ((int)rank * rows + q % rows) * 4;
@@ -156,38 +186,9 @@ __device__ __forceinline__ void join_shares(const Product& p, uint32_t at, int i
                          : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w)
                          : "r"(place_in(at + (c * kBM + r) * 4, s))
                          : "memory");
-            sum.x += x.x;
-            sum.y += x.y;
-            sum.z += x.z;
-            sum.w += x.w;
+            sum = make_float4(sum.x + x.x, sum.y + x.y, sum.z + x.z, sum.w + x.w);
         }
-        const int64_t row = (int64_t)j * BN + c, col = (int64_t)i * kBM + r;  // of the output
-        if (e.wide && col + 4 <= p.I) {
-            float2 v[2] = {make_float2(sum.x, sum.y), make_float2(sum.z, sum.w)};
-            uint2 x = make_uint2(0, 0);
-            if (e.residual) x = *reinterpret_cast<const uint2*>(static_cast<const T*>(e.residual) + row * e.residual_stride + col);
-            if (e.bias) {
-                const T* b = static_cast<const T*>(e.bias) + col;
-                v[0] = add2(v[0], make_float2(to_float(b[0]), to_float(b[1])));
-                v[1] = add2(v[1], make_float2(to_float(b[2]), to_float(b[3])));
-            }
-            if (e.pre)
-                *reinterpret_cast<uint2*>(static_cast<T*>(e.pre) + row * e.pre_stride + col) = make_uint2(word_of_pair<T>(v[0]), word_of_pair<T>(v[1]));
-            by_act(e.act, [&](auto act) {
-                v[0] = activate<decltype(act)::value>(v[0]);
-                v[1] = activate<decltype(act)::value>(v[1]);
-            });
-            if (e.residual) {
-                v[0] = add2(v[0], pair_of_word<T>(x.x));
-                v[1] = add2(v[1], pair_of_word<T>(x.y));
-            }
-            *reinterpret_cast<uint2*>(static_cast<T*>(e.out) + row * e.out_stride + col) = make_uint2(word_of_pair<T>(v[0]), word_of_pair<T>(v[1]));
-            continue;
-        }
-        const float v[4] = {sum.x, sum.y, sum.z, sum.w};
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (col + k < p.I) static_cast<T*>(e.out)[row * e.out_stride + col + k] = from_float<T>(finish(e, v[k], row, col + k));
+        put_four<T>(p.e, sum, (int64_t)j * BN + c, (int64_t)i * kBM + r, p.I);
     }
 }
 
@@ -529,7 +530,7 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR>::kThreads, 1)
         int i, j, share;
         tile_at(p, first, i, j, share);
         cluster_sync();
-        if (warp < 4) join_shares<T, BN>(p, ring, i, j, mine);
+        if (warp < 4) join_columns<T, BN>(p, ring, i, j, mine);
         __syncwarp();
     }
     if (PAIR || joined) cluster_sync();  // nothing of this block's memory is wanted by another any more
@@ -538,14 +539,21 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR>::kThreads, 1)
     if (warp == kMma) tmem_free<PAIR>(tmem, R::kColumns);
 }
 
-// The shares of k added up in order, and the epilogue (shares == 0: of zeros).
+// The shares of k added up in order, and the epilogue (shares == 0: of zeros): four columns a thread.
+template <class T>
 __global__ void __launch_bounds__(256) k_product_finish(Epilogue e, int64_t rows, int64_t cols, int shares) {
     pdl_enter();
-    for (int64_t at = blockIdx.x * 256ll + threadIdx.x; at < rows * cols; at += gridDim.x * 256ll) {
-        const int64_t r = at / cols, c = at - r * cols;
-        float v = 0.f;
-        for (int s = 0; s < shares; ++s) v += e.part[s * e.part_size + r * e.part_stride + c];
-        static_cast<uint16_t*>(e.out)[r * e.out_stride + c] = narrow(e.type, finish(e, v, r, c));
+    const int64_t per = (cols + 3) / 4;
+    for (int64_t at = blockIdx.x * 256ll + threadIdx.x; at < rows * per; at += gridDim.x * 256ll) {
+        const int64_t r = at / per, c = (at - r * per) * 4;
+        const float4* part = reinterpret_cast<const float4*>(e.part + r * e.part_stride + c);
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+        for (int s = 0; s < shares; ++s) {
+            const float4 x = part[s * (e.part_size / 4)];
+            sum = make_float4(sum.x + x.x, sum.y + x.y, sum.z + x.z, sum.w + x.w);
+        }
+        put_four<T>(e, sum, r, c, cols);
     }
 }
 
@@ -574,15 +582,15 @@ struct Slope {
     const void* dy;
     const void* pre;
     void* p;           // null: not wanted (p is dy)
-    float* part;       // [shares][cols], null with one share or no sums
+    float* part;       // [shares][cols], null with one share, joined ones or no sums
     void* dbias;
     int64_t dy_stride, pre_stride, p_stride, rows, cols, share;
-    int32_t act;
+    int32_t act, joined;  // (the blocks of a column are a cluster)
 };
 template <class T, bool ALIGNED>
 __global__ void __launch_bounds__(256) k_slope(Slope a) {
     pdl_enter();
-    __shared__ float sums[8][256];
+    __shared__ float sums[8][256], mine[256];
     using Row = Values<T, 8, ALIGNED>;
     constexpr int kRows = ALIGNED ? 4 : 2;  // on their way at a time
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -627,10 +635,24 @@ __global__ void __launch_bounds__(256) k_slope(Slope a) {
     for (int q = 0; q < 4; ++q) *reinterpret_cast<float2*>(&sums[warp][lane * 8 + 2 * q]) = s[q];
     __syncthreads();
     const int64_t col = blockIdx.x * 256ll + threadIdx.x;
-    if (col >= a.cols) return;
     float t = 0.f;
 #pragma unroll
     for (int w = 0; w < 8; ++w) t += sums[w][threadIdx.x];
+    if (a.joined) {  // the first block adds the others' sums up, in order
+        mine[threadIdx.x] = t;
+        cluster_sync();
+        if (blockIdx.y == 0) {
+            t = 0.f;
+            for (int b = 0; b < (int)gridDim.y; ++b) {
+                float x;
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(place_in(smem_of(&mine[threadIdx.x]), b)) : "memory");
+                t += x;
+            }
+        }
+        cluster_sync();
+        if (blockIdx.y) return;
+    }
+    if (col >= a.cols) return;
     if (a.part) a.part[blockIdx.y * a.cols + col] = t;
     else static_cast<T*>(a.dbias)[col] = from_float<T>(t);
 }
@@ -752,11 +774,44 @@ struct Caller {
         if (type == MLKV_TYPE_BFLOAT) go(k_product<BN, A_MN, B_MN, SWAP, PAIR, __nv_bfloat16>);
         else go(k_product<BN, A_MN, B_MN, SWAP, PAIR, __half>);
     }
+    void finish_shares(const Epilogue& e, int64_t rows, int64_t cols, int shares) {
+        if (!run) return;
+        const dim3 grid(blocks_for(rows * ((cols + 3) / 4)));
+        launch_kernel(true, type == MLKV_TYPE_BFLOAT ? k_product_finish<__nv_bfloat16> : k_product_finish<__half>, grid, dim3(256), 0, st, e, rows, cols, shares);
+    }
     // Whether pairs of blocks take the tiles of 256 columns: where there are enough for every pair, and k is long
     // enough for the products to count beside the epilogue.  (Single blocks / pairs, us: 16,384 x 4,096 by k = 4,096
     // 331 / 298; 8,192 x 1,024 by 8,192 102 / 86; 4,096 x 4,096 by 1,024 32 / 29; 65,536 x 512 by 416 37 / 42.)
     bool pair_pays(int64_t tiles_i, int64_t tiles_j, int64_t blocks) const {
         return blocks >= 12 && (tiles_i + 1) / 2 * tiles_j * (blocks / 12) >= sms / 2;
+    }
+
+    // How few tiles share the GPU: columns a tile, and shares of k (of at least 4 blocks), which another launch adds up.
+    struct Shape { int bn; int64_t shares; };
+    // By the time of a block's work, in us: what each width takes besides k; a block of 64 along k (its operands' latency,
+    // or their bytes through L2 on all SMs); and the launch that adds the shares up, with its bytes.  (Widths of 256 /
+    // 128 / 64 at their best, us: 300 x 1,000 by k = 520 9.7 / 7.8 / 7.2; 1,000 x 1,000 by 1,000 12.8 / 9.9 / 8.3; 200 x
+    // 512 by 8,192 12.3 / 10.5 / 10.3; 512 x 512 by 8,000 13.1 / 12.4 / 14.6; 4,096 x 1,000 by 776 14.6 / 16.0 / 21.0.)
+    Shape few_tiles(int64_t rows, int64_t cols, int64_t blocks) const {
+        constexpr float kFixed[3] = {5.f, 6.5f, 8.5f}, kBlock = 0.25f, kL2 = 15e6f, kLaunch = 4.f, kFinish = 6e6f;
+        Shape best = {cols <= 64 ? 64 : cols <= 128 ? 128 : 256, 1};
+        float least = 3e38f;
+        for (int w = 0; w < 3; ++w) {
+            const int bn = 64 << w;
+            const int64_t tiles = (rows + kBM - 1) / kBM * ((cols + bn - 1) / bn);
+            if (tiles <= sms)
+                for (int64_t s = std::max<int64_t>(1, std::min<int64_t>(sms / tiles, blocks / 4));; s /= 2) {
+                    const float block = std::max(kBlock, (float)(tiles * s) * (kBM + bn) * kBK * 2 / kL2);
+                    const float time = kFixed[w] + (float)((blocks + s - 1) / s) * block + (s > 1 ? kLaunch + (float)(s + 1) * rows * cols * 4 / kFinish : 0.f);
+                    if (time < least) {
+                        least = time;
+                        best = {bn, s};
+                    }
+                    if (s == 1) break;
+                }
+            if (bn >= cols) break;
+        }
+        return best;
     }
 
     // out = epilogue(A B^T): A [rows][k], B [cols][k]; *_mn: held as [k][rows], [k][cols].
@@ -765,27 +820,30 @@ struct Caller {
         if (!rows || !cols) return;
         e.type = type;
         if (k == 0) {
-            if (run) launch_kernel(true, k_product_finish, dim3(blocks_for(rows * cols)), dim3(256), 0, st, e, rows, cols, 0);
+            finish_shares(e, rows, cols, 0);
             return;
         }
         auto wide = [](const void* p, int64_t stride) { return !p || (reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 8 == 0); };
         e.wide = wide(e.out, e.out_stride) && wide(e.pre, e.pre_stride) && wide(e.residual, e.residual_stride);
         const bool swap = !A_MN && rows <= 64;  // few rows: the wide operand fills the tiles' 128 rows
-        const int bn = swap ? (rows <= 16 ? 16 : rows <= 32 ? 32 : 64) : cols <= 64 ? 64 : cols <= 128 ? 128 : 256;
         Product p = {};
         p.I = (int32_t)(swap ? cols : rows);
         p.J = (int32_t)(swap ? rows : cols);
         p.blocks = (int32_t)((k + kBK - 1) / kBK);
+        p.tiles_i = (p.I + kBM - 1) / kBM;
+        auto shares_of = [&](int64_t places) { return std::max<int64_t>(1, std::min<int64_t>(places / ((int64_t)p.tiles_i * p.tiles_j), p.blocks / 4)); };
+        const bool pair = !swap && cols > 128 && pair_pays(p.tiles_i, (p.J + 255) / 256, p.blocks);
+        Shape shape = {256, 1};
+        if (swap) shape.bn = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+        else if (!pair) shape = few_tiles(rows, cols, p.blocks);
+        const int bn = shape.bn;
         p.tiles_j = (p.J + bn - 1) / bn;
-        const bool pair = !swap && bn == 256 && pair_pays((p.I + kBM - 1) / kBM, p.tiles_j, p.blocks);
-        p.tiles_i = (p.I + (pair ? 2 * kBM : kBM) - 1) / (pair ? 2 * kBM : kBM);
+        if (pair) p.tiles_i = (p.I + 2 * kBM - 1) / (2 * kBM);
         if ((int64_t)p.tiles_i * p.tiles_j >= (int64_t)1 << 30) {
             rc = MLKV_ERR_UNSUPPORTED;
             return;
         }
-        // too few tiles for the GPU: k in shares of at least 4 blocks
-        const int64_t tiles = (int64_t)p.tiles_i * p.tiles_j;
-        int64_t shares = std::max<int64_t>(1, std::min<int64_t>((pair ? sms / 2 : sms) / tiles, p.blocks / 4));
+        const int64_t shares = swap ? shares_of(sms) : pair ? shares_of(sms / 2) : shape.shares;
         p.blocks_per_share = (int32_t)((p.blocks + shares - 1) / shares);
         p.shares = (p.blocks + p.blocks_per_share - 1) / p.blocks_per_share;
         p.e = e;
@@ -820,9 +878,7 @@ struct Caller {
             else if (pair) launch<256, A_MN, B_MN, false, true>(a, b, p);
             else launch<256, A_MN, B_MN, false>(a, b, p);
         }
-        if (p.shares > 1 && !p.joined) {
-            launch_kernel(true, k_product_finish, dim3(blocks_for(rows * cols)), dim3(256), 0, st, e, rows, cols, (int)p.shares);
-        }
+        if (p.shares > 1 && !p.joined) finish_shares(e, rows, cols, p.shares);
     }
 
     void forward(const mlkv_linear_args& g) {
@@ -850,15 +906,22 @@ struct Caller {
             const Matrix dy = {(const uint16_t*)s.dy, s.dy_stride, 0, 0}, pre = {(const uint16_t*)s.pre, s.pre_stride, 0, 0};
             const bool whole = g.n % 8 == 0 && dy.aligned() && (!act || pre.aligned());
             const int64_t across = (g.n + 255) / 256;
-            const int64_t shares = std::max<int64_t>(1, std::min<int64_t>((g.m + 31) / 32, 8ll * sms / across));
+            // a block's warps take 4 rows each at a time; up to 1,024 rows no column has more blocks than a cluster
+            const int64_t most = g.d_dbias && g.m <= 1024 ? 8 : 8ll * sms / across;
+            const int64_t shares = std::max<int64_t>(1, std::min<int64_t>((g.m + 31) / 32, most));
             s.share = (g.m + shares - 1) / shares;
             const unsigned down = (unsigned)((g.m + s.share - 1) / s.share);
-            if (g.d_dbias && down > 1) s.part = static_cast<float*>(arena.take((int64_t)down * g.n * 4));
+            s.joined = g.d_dbias && down > 1 && down <= 8;
+            if (g.d_dbias && down > 8) s.part = static_cast<float*>(arena.take((int64_t)down * g.n * 4));
             if (run) {
                 const dim3 grid((unsigned)across, down);
+                auto go = [&](auto kernel) {
+                    if (s.joined) launch_clusters(kernel, dim3(1, down), grid, 256, 0, st, s);
+                    else launch_kernel(true, kernel, grid, dim3(256), 0, st, s);
+                };
                 const bool b = type == MLKV_TYPE_BFLOAT;
-                if (whole) launch_kernel(true, b ? k_slope<__nv_bfloat16, true> : k_slope<__half, true>, grid, dim3(256), 0, st, s);
-                else launch_kernel(true, b ? k_slope<__nv_bfloat16, false> : k_slope<__half, false>, grid, dim3(256), 0, st, s);
+                if (whole) go(b ? k_slope<__nv_bfloat16, true> : k_slope<__half, true>);
+                else go(b ? k_slope<__nv_bfloat16, false> : k_slope<__half, false>);
                 if (s.part) launch_kernel(true, k_column_sums, dim3((unsigned)((g.n + 31) / 32)), dim3(1024), 0, st,
                                           (const float*)s.part, (int)down, g.n, g.d_dbias, type);
             }
