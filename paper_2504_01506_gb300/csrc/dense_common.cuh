@@ -168,57 +168,101 @@ struct Span {
         : from(reinterpret_cast<uintptr_t>(p)), to(reinterpret_cast<uintptr_t>(p + (rows - 1) * stride + dim)) {}
 };
 
+// N bytes (4, 8 or 16, aligned) on their way into shared memory.
+template <int N>
+__device__ __forceinline__ void copy_async(void* to, const void* from) {
+    const uint32_t at = (uint32_t)__cvta_generic_to_shared(to);
+    if constexpr (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at), "l"(from) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(at), "l"(from), "n"(N) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
 // V values as they lie in memory, read and written in pairs, kept in 32-bit words
 // (16-bit values apart would take a register each).  ALIGNED: on 16 bytes (of x;
-// 8 of a 16-bit y beside an fp32 x), and a row is whole vectors.  Else as wide as
-// the row's place allows (the same for all its vectors): 8 bytes, 4, or, with
-// 16-bit values off a word, the words around them, shifted.
+// 8 of a 16-bit y beside an fp32 x), and a row is whole vectors.  Else read as the
+// two aligned pieces of that size around them, which are then shifted: nothing
+// waits for the loads before that.  Written as wide as the row's place allows (the
+// same for all its vectors): 8 bytes, 4, or, two bytes off, a half, words, a half.
 template <class T, int V, bool ALIGNED> struct Values {
-    static constexpr int W = sizeof(T) * V / 4, kBytes = sizeof(T) * V;
+    static constexpr int W = sizeof(T) * V / 4, kBytes = sizeof(T) * V, kPieces = ALIGNED ? 1 : 2;
     uint32_t w[W];
+    struct Around { uint32_t v[kPieces * W]; };
 
-    template <int N>
-    static __device__ __forceinline__ void read(const void* p, uint32_t* to) {
-        const Pack<uint32_t, N> q = *reinterpret_cast<const Pack<uint32_t, N>*>(p);
-#pragma unroll
-        for (int i = 0; i < N; ++i) to[i] = q.v[i];
+    static __device__ __forceinline__ const uint8_t* piece(const T* p) {
+        return reinterpret_cast<const uint8_t*>(reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)(kBytes - 1));
     }
-    // The first n values (the rest 0).
-    __device__ __forceinline__ void load(const T* p, int n, const Span& span) {
+    static __device__ __forceinline__ bool inside(const uint8_t* at, int bytes, const Span& span) {
+        return reinterpret_cast<uintptr_t>(at) >= span.from && reinterpret_cast<uintptr_t>(at) + bytes <= span.to;
+    }
+    // Of pieces that are not all the matrix's: the values that are, as words.
+    static __device__ __forceinline__ uint32_t edge(const uint8_t* at, int i, const Span& span) {
+        uint32_t r = 0;
+#pragma unroll
+        for (int h = 0; h < 4; h += sizeof(T)) {
+            const uint8_t* q = at + i * 4 + h;
+            if (reinterpret_cast<uintptr_t>(q) < span.from || reinterpret_cast<uintptr_t>(q) >= span.to) continue;
+            if constexpr (sizeof(T) == 4) r = *reinterpret_cast<const uint32_t*>(q);
+            else r |= (uint32_t)*reinterpret_cast<const uint16_t*>(q) << (8 * h);
+        }
+        return r;
+    }
+    static __device__ __forceinline__ void read(const void* p, uint32_t* to) {
+        const Pack<uint32_t, W> q = *reinterpret_cast<const Pack<uint32_t, W>*>(p);
+#pragma unroll
+        for (int i = 0; i < W; ++i) to[i] = q.v[i];
+    }
+    // In two steps: what holds the values, ...
+    static __device__ __forceinline__ Around around(const T* p, const Span& span) {
+        Around r;
         if constexpr (ALIGNED) {
-            read<W>(p, w);
+            read(p, r.v);
         } else {
-            const uint32_t* p32 = reinterpret_cast<const uint32_t*>(p);
-            const uint32_t by = (uint32_t)reinterpret_cast<uintptr_t>(p) & (kBytes - 1);
-            if (n < V) {
-                zero();
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    if (e >= n) continue;
-                    if constexpr (sizeof(T) == 4) w[e] = p32[e];
-                    else w[e / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[e] << (16 * (e & 1));
-                }
-            } else if (by == 0) {
-                read<W>(p, w);
-            } else if ((by & 7) == 0) {
-#pragma unroll
-                for (int i = 0; i < W; i += 2) read<2>(p32 + i, w + i);
-            } else if ((by & 3) == 0) {
-#pragma unroll
-                for (int i = 0; i < W; ++i) w[i] = p32[i];
+            const uint8_t* at = piece(p);
+            if (inside(at, 2 * kBytes, span)) {
+                read(at, r.v);
+                read(at + kBytes, r.v + W);
             } else {
-                // the words around; the values at the matrix's ends by themselves
-                const uint16_t* p16 = reinterpret_cast<const uint16_t*>(p);
-                const uint32_t* around = reinterpret_cast<const uint32_t*>(p16 - 1);
-                uint32_t v[W + 1];
-                v[0] = reinterpret_cast<uintptr_t>(p) > span.from ? around[0] : (uint32_t)p16[0] << 16;
 #pragma unroll
-                for (int i = 1; i < W; ++i) v[i] = around[i];
-                v[W] = reinterpret_cast<uintptr_t>(p + V) < span.to ? around[W] : p16[V - 1];
-#pragma unroll
-                for (int i = 0; i < W; ++i) w[i] = __funnelshift_r(v[i], v[i + 1], 16);
+                for (int i = 0; i < 2 * W; ++i) r.v[i] = edge(at, i, span);
             }
         }
+        return r;
+    }
+    // ... and the first n of them (the rest 0), `by` bytes after a boundary.
+    __device__ __forceinline__ void settle(Around r, uint32_t by, int n) {
+        if constexpr (!ALIGNED) {
+#pragma unroll
+            for (int step = W / 2; step; step /= 2)
+#pragma unroll
+                for (int i = 0; i + step < 2 * W; ++i) r.v[i] = by & (4 * step) ? r.v[i + step] : r.v[i];
+            if (sizeof(T) == 2)
+#pragma unroll
+                for (int i = 0; i < W; ++i) r.v[i] = __funnelshift_r(r.v[i], r.v[i + 1], (by & 2) * 8);
+        }
+#pragma unroll
+        for (int i = 0; i < W; ++i) w[i] = r.v[i];
+        if (!ALIGNED && n < V)
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                if constexpr (sizeof(T) == 4) w[i] = i < n ? w[i] : 0u;
+                else w[i] = 2 * i + 1 < n ? w[i] : 2 * i < n ? w[i] & 0xFFFFu : 0u;
+            }
+    }
+    static __device__ __forceinline__ uint32_t place(const T* p) { return (uint32_t)reinterpret_cast<uintptr_t>(p) & (kBytes - 1); }
+    __device__ __forceinline__ void load(const T* p, int n, const Span& span) { settle(around(p, span), place(p), n); }
+
+    // From shared memory, where a matrix's pieces lie as they do in memory: the first n values from `at` on.
+    __device__ __forceinline__ void take(const uint8_t* from, uint32_t at, int n) {
+        Around r;
+        if constexpr (ALIGNED) {
+            read(from + at, r.v);
+        } else {
+            read(from + (at & ~(uint32_t)(kBytes - 1)), r.v);
+            read(from + (at & ~(uint32_t)(kBytes - 1)) + kBytes, r.v + W);
+        }
+        settle(r, at & (kBytes - 1), n);
     }
     __device__ __forceinline__ void zero() {
 #pragma unroll
@@ -241,57 +285,40 @@ template <class T, int V, bool ALIGNED> struct Values {
             w[k] = word_of_pair<T>(x);
         }
     }
-    // The first n values.
+    // The first n values: as wide as the row's place allows (the same for all its vectors).
     __device__ __forceinline__ void store(T* p, int n) const {
-        if constexpr (ALIGNED) {
+        const uint32_t by = (uint32_t)reinterpret_cast<uintptr_t>(p);
+        uint32_t* p32 = reinterpret_cast<uint32_t*>(p);
+        uint16_t* p16 = reinterpret_cast<uint16_t*>(p);
+        if (ALIGNED || (n >= V && !(by & (kBytes - 1)))) {
             Pack<uint32_t, W> q;
 #pragma unroll
             for (int i = 0; i < W; ++i) q.v[i] = w[i];
             *reinterpret_cast<Pack<uint32_t, W>*>(p) = q;
-        } else {
-            const uint32_t by = (uint32_t)reinterpret_cast<uintptr_t>(p);
-            uint32_t* p32 = reinterpret_cast<uint32_t*>(p);
-            if (n >= V && !(by & (kBytes - 1))) {
-                Pack<uint32_t, W> q;
+        } else if (n >= V && !(by & 7)) {
 #pragma unroll
-                for (int i = 0; i < W; ++i) q.v[i] = w[i];
-                *reinterpret_cast<Pack<uint32_t, W>*>(p) = q;
-            } else if (n >= V && !(by & 7)) {
+            for (int i = 0; i < W; i += 2) *reinterpret_cast<uint2*>(p32 + i) = make_uint2(w[i], w[i + 1]);
+        } else if (n >= V && !(by & 3)) {
 #pragma unroll
-                for (int i = 0; i < W; i += 2) *reinterpret_cast<uint2*>(p32 + i) = make_uint2(w[i], w[i + 1]);
-            } else if (n >= V && !(by & 3)) {
+            for (int i = 0; i < W; ++i) p32[i] = w[i];
+        } else if constexpr (sizeof(T) == 2) {
+            if (n >= V) {  // two bytes off a word: a half, the words between, a half
+                p16[0] = (uint16_t)w[0];
 #pragma unroll
-                for (int i = 0; i < W; ++i) p32[i] = w[i];
-            } else if constexpr (sizeof(T) == 2) {
-                uint16_t* p16 = reinterpret_cast<uint16_t*>(p);
-                if (n >= V) {  // two bytes off a word: a half, the words between, a half
-                    p16[0] = (uint16_t)w[0];
-#pragma unroll
-                    for (int i = 0; i + 1 < W; ++i) *reinterpret_cast<uint32_t*>(p16 + 1 + 2 * i) = __funnelshift_r(w[i], w[i + 1], 16);
-                    p16[V - 1] = (uint16_t)(w[W - 1] >> 16);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < V; ++e)
-                        if (e < n) p16[e] = (uint16_t)(w[e / 2] >> (16 * (e & 1)));
-                }
+                for (int i = 0; i + 1 < W; ++i) *reinterpret_cast<uint32_t*>(p16 + 1 + 2 * i) = __funnelshift_r(w[i], w[i + 1], 16);
+                p16[V - 1] = (uint16_t)(w[W - 1] >> 16);
             } else {
 #pragma unroll
-                for (int i = 0; i < W; ++i)
-                    if (i < n) p32[i] = w[i];
+                for (int e = 0; e < V; ++e)
+                    if (e < n) p16[e] = (uint16_t)(w[e / 2] >> (16 * (e & 1)));
             }
+        } else {
+#pragma unroll
+            for (int i = 0; i < W; ++i)
+                if (i < n) p32[i] = w[i];
         }
     }
 };
-// N bytes (4, 8 or 16, aligned) on their way into shared memory.
-template <int N>
-__device__ __forceinline__ void copy_async(void* to, const void* from) {
-    const uint32_t at = (uint32_t)__cvta_generic_to_shared(to);
-    if constexpr (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at), "l"(from) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(at), "l"(from), "n"(N) : "memory");
-}
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 // --- clusters of blocks ---------------------------------------------------------
 __device__ __forceinline__ uint32_t cluster_rank() {

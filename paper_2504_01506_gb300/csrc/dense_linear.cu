@@ -605,15 +605,18 @@ __global__ void __launch_bounds__(256) k_slope(Slope a) {
     if (n > 0)
         for (int64_t r = r0 + warp; r < r1; r += 8 * kRows) {
             Row d[kRows], z[kRows];
+            typename Row::Around d_at[kRows], z_at[kRows];
 #pragma unroll
             for (int i = 0; i < kRows; ++i) {
                 if (r + 8 * i >= r1) continue;
-                d[i].load(dy + (r + 8 * i) * a.dy_stride + c, n, dy_span);
-                if (a.act != MLKV_ACT_NONE) z[i].load(pre + (r + 8 * i) * a.pre_stride + c, n, pre_span);
+                d_at[i] = Row::around(dy + (r + 8 * i) * a.dy_stride + c, dy_span);
+                if (a.act != MLKV_ACT_NONE) z_at[i] = Row::around(pre + (r + 8 * i) * a.pre_stride + c, pre_span);
             }
 #pragma unroll
             for (int i = 0; i < kRows; ++i) {
                 if (r + 8 * i >= r1) continue;
+                d[i].settle(d_at[i], Row::place(dy + (r + 8 * i) * a.dy_stride), n);
+                if (a.act != MLKV_ACT_NONE) z[i].settle(z_at[i], Row::place(pre + (r + 8 * i) * a.pre_stride), n);
                 if (a.act == MLKV_ACT_NONE) {
 #pragma unroll
                     for (int q = 0; q < 4; ++q) s[q] = add2(s[q], d[i].pair(q));

@@ -15,7 +15,7 @@ constexpr int kForwardLanes = 256;   // a block's threads
 constexpr int kForwardBlocks = 3;    // blocks an SM: 80 registers a thread
 
 // A block's teams take rows in turn; the weights are staged once a block.  Rows
-// that are aligned come through shared memory, two of each team on their way (a
+// come through shared memory, the next one or two of each team on their way (a
 // thread reads what it copied itself).  What a lane holds beyond the row's end is
 // a copy of its last vector, or 0, left out of the sums.
 template <class TX, class TY, int NV, bool ALIGNED>
@@ -31,27 +31,21 @@ __global__ void __launch_bounds__(kForwardLanes, kForwardBlocks) k_norm(NormArgs
     int at[NV];  // of this lane's vectors, the last one again where there are no more
 #pragma unroll
     for (int i = 0; i < NV; ++i) at[i] = min(tm.lane + i * tm.L, nvec - 1) * V;
-    Values<TX, V, ALIGNED> q[NV];
-    uint4* ring = reinterpret_cast<uint4*>(weights + 2 * room) + threadIdx.x;
+    using Row = Values<TX, V, ALIGNED>;
+    const RowRing<TX, V, NV, ALIGNED> ring(reinterpret_cast<uint8_t*>(weights + 2 * room), tm, room);
     int r = (int)blockIdx.x * tm.count + tm.index, ahead = r;
     const TX* x = static_cast<const TX*>(a.x) + r * a.x_stride;
     TY* y = static_cast<TY*>(a.out) + r * a.out_stride;
     const int64_t x_step = step * a.x_stride, y_step = step * a.out_stride;
-    // the next row not yet on its way: into slot `slot`, or (unaligned) registers
+    uint32_t by = (uint32_t)reinterpret_cast<uintptr_t>(x) & 15;  // of the row worked on
+    // the next row not yet on its way, into slot `slot`
     auto fetch = [&](int slot) {
-        if (ahead < rows) {
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                if constexpr (ALIGNED) copy_async<16>(ring + (slot * NV + i) * (int)blockDim.x, x + at[i]);
-                else q[i].load(x + at[i], a.dim - at[i], span);
-            }
-        }
-        if (ALIGNED) copy_commit();
+        if (ahead < rows) ring.fetch(tm, slot, x, at, a.dim, span);
+        copy_commit();
         x += x_step;
         ahead += step;
     };
-    fetch(0);
-    if (ALIGNED) fetch(1);
+    for (int i = 0; i < kNormAhead; ++i) fetch(i);
     stage_weights<V>(weights, a.w, a.w_type, a.dim, room, 1.f);
     stage_weights<V>(weights + room, a.b, a.w_type, a.dim, room, 0.f);
     __syncthreads();
@@ -60,18 +54,22 @@ __global__ void __launch_bounds__(kForwardLanes, kForwardBlocks) k_norm(NormArgs
     // the lanes of a warp take as many turns as its first team does
     for (int first = tm.L < 32 ? r - (int)(threadIdx.x & 31) / tm.L : r; first < rows; first += step, r += step, y += y_step, slot ^= 1) {
         float2 f[NV][H], s = both(0.f), v = both(0.f);
-        if constexpr (ALIGNED) copy_wait<kNormAhead - 1>();
+        copy_wait<kNormAhead - 1>();
+        if (!ALIGNED) tm.sync();
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            if constexpr (ALIGNED) q[i].load(reinterpret_cast<const TX*>(ring + (slot * NV + i) * (int)blockDim.x), V, span);
+            Row q;
+            ring.take(q, slot, i, at[i], by, a.dim);
 #pragma unroll
-            for (int k = 0; k < H; ++k) f[i][k] = q[i].pair(k);
+            for (int k = 0; k < H; ++k) f[i][k] = q.pair(k);
             if (tm.lane + i * tm.L < nvec)
 #pragma unroll
                 for (int k = 0; k < H; ++k) s = add2(s, f[i][k]);
         }
         const float mu = tm.sum(s.x + s.y, 0) * inverse;
-        if (ALIGNED || sizeof(TX) == 2) fetch(slot);  // (an unaligned fp32 row is too wide to have the next one beside it)
+        if (!ALIGNED) __syncwarp();  // (a team of a warp or less: all have read the row)
+        fetch(slot);
+        by = (by + (uint32_t)(x_step * sizeof(TX))) & 15;
         const float2 minus = both(-mu);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -103,7 +101,6 @@ __global__ void __launch_bounds__(kForwardLanes, kForwardBlocks) k_norm(NormArgs
                 if (j < nvec) o.store(y + j * V, a.dim - j * V);
             }
         }
-        if (!(ALIGNED || sizeof(TX) == 2)) fetch(0);
     }
 }
 
@@ -167,7 +164,9 @@ extern "C" int mlkv_layer_norm(const void* d_x, int64_t x_stride, int32_t x_type
         }
         a.lanes = sh.lanes;
         const int threads = norm_team_threads(sh.lanes), teams = threads / sh.lanes;
-        const size_t smem = 2 * (size_t)sh.lanes * sh.NV * V * sizeof(float) + (aligned ? (size_t)kNormAhead * sh.NV * threads * 16 : 0);
+        const int room = sh.lanes * sh.NV * V;
+        const size_t smem = 2 * (size_t)room * sizeof(float) +
+                            kNormAhead * (aligned ? (size_t)sh.NV * threads * 16 : (size_t)teams * norm_row(room, xs));
         const int64_t resident = std::max<int64_t>(1, std::min<int64_t>(kForwardBlocks, kDenseSmem / (int64_t)(smem + 2048)));
         const unsigned blocks = (unsigned)std::min<int64_t>(sms * resident, (rows + teams - 1) / teams);
         by_shape<kForwardValues * (int)sizeof(TX) / 16>(sh.NV, aligned, [&](auto nv, auto al) {

@@ -100,6 +100,10 @@ struct Team {
         a = s.x;
         b = s.y;
     }
+    __device__ __forceinline__ void sync() const {
+        if (L <= 32) __syncwarp();
+        else asm volatile("bar.sync %0, %1;" ::"r"(index + 1), "r"(L) : "memory");
+    }
     static __device__ __forceinline__ float2 pair_sum(float2 s, const float2* two) {
         const float4 q = *reinterpret_cast<const float4*>(two);
         return add2(add2(s, make_float2(q.x, q.y)), make_float2(q.z, q.w));
@@ -116,7 +120,50 @@ inline bool norm_aligned(const void* p, int64_t stride, int size, int64_t dim, i
     return !p || (reinterpret_cast<uintptr_t>(p) % (V * size) == 0 && stride % V == 0 && dim % V == 0);
 }
 
-constexpr int kNormAhead = 2;  // rows on their way into shared memory, where rows are aligned
+constexpr int kNormAhead = 2;  // rows of each team on their way into shared memory
+
+// Bytes of a team's row in shared memory, with what lies around it.
+__host__ __device__ constexpr int norm_row(int room, int size) { return (room * size + 47) / 16 * 16; }
+
+// Rows on their way into shared memory.  ALIGNED: each thread has its own vectors, and reads only what it copied
+// itself.  Else a team has the row, in the aligned pieces that it lies in, of which a lane's vector is parts of two.
+// (20,000 rows of 4,001 bf16 values, forward / backward: each lane's words loaded into registers a row ahead 140 / 272
+// us; this way 108 / 193, and, with the row on its way out in shared memory too, to be stored in 16-byte pieces, 124 /
+// 185: its barriers and shifts cost what the wider stores save.)
+template <class T, int V, int NV, bool ALIGNED> struct RowRing {
+    using Row = Values<T, V, ALIGNED>;
+    uint8_t* at;
+    int apart, slot_bytes;  // bytes from a thread's vector to its next; of a slot
+    static __device__ __forceinline__ int bytes(const Team& tm, int room) {
+        return kNormAhead * (ALIGNED ? NV * (int)blockDim.x * Row::kBytes : tm.count * norm_row(room, sizeof(T)));
+    }
+    __device__ __forceinline__ RowRing(uint8_t* from, const Team& tm, int room)
+        : at(from + (ALIGNED ? threadIdx.x * Row::kBytes : tm.index * norm_row(room, sizeof(T)))), apart((int)blockDim.x * Row::kBytes),
+          slot_bytes(bytes(tm, room) / kNormAhead) {}
+    // Of this lane, whose vectors start at columns c.
+    __device__ __forceinline__ void fetch(const Team& tm, int slot, const T* row, const int (&c)[NV], int dim, const Span& span) const {
+        uint8_t* to = at + slot * slot_bytes;
+        if constexpr (ALIGNED) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) copy_async<Row::kBytes>(to + i * apart, row + c[i]);
+        } else {
+            using Piece = Values<T, 16 / sizeof(T), false>;
+            const uint8_t* from = Piece::piece(row);
+            const int end = (int)Piece::place(row) + dim * (int)sizeof(T);
+            for (int p = tm.lane * 16; p < end; p += tm.L * 16) {
+                if (Piece::inside(from + p, 16, span)) copy_async<16>(to + p, from + p);
+                else
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) reinterpret_cast<uint32_t*>(to + p)[i] = Piece::edge(from + p, i, span);
+            }
+        }
+    }
+    // Vector i, from column c on, of a row `by` bytes after a boundary.
+    __device__ __forceinline__ void take(Row& v, int slot, int i, int c, uint32_t by, int dim) const {
+        if (ALIGNED) v.take(at + slot * slot_bytes, i * apart, V);
+        else v.take(at + slot * slot_bytes, by + c * (int)sizeof(T), dim - c);
+    }
+};
 
 struct NormShape {
     int NV, lanes;  // lanes == 0: the row does not fit

@@ -16,7 +16,7 @@ constexpr int kBackwardValues = 16;  // most values of x and dy each that a lane
 constexpr int kBackwardLanes = 512;  // threads an SM: 128 registers each
 
 // The rows' gradients, and the sums over this block's rows of dy xh and dy.  Rows
-// that are aligned come through shared memory, two of each team on their way (a
+// come through shared memory, the next one or two of each team on their way (a
 // thread reads what it copied itself).  What a lane holds beyond the row's end is a copy of its last vector, or 0, with weight 0.
 template <class TX, class TY, int NV, bool ALIGNED>
 __global__ void __launch_bounds__(kBackwardLanes, 1) k_norm_backward(NormArgs a) {
@@ -44,39 +44,27 @@ __global__ void __launch_bounds__(kBackwardLanes, 1) k_norm_backward(NormArgs a)
     const TY* dy_at = static_cast<const TY*>(a.dy) + r * a.dy_stride;
     TX* o = static_cast<TX*>(a.out) + r * a.out_stride;
     const int64_t x_step = step * a.x_stride, dy_step = step * a.dy_stride, o_step = step * a.out_stride;
-    constexpr int kBytes = sizeof(TY) * V;  // of a vector of dy
-    uint8_t* x_ring = reinterpret_cast<uint8_t*>(shared + room) + threadIdx.x * 16;
-    uint8_t* dy_ring = reinterpret_cast<uint8_t*>(shared + room) + (ALIGNED ? kNormAhead * NV * blockDim.x * 16 : 0) + threadIdx.x * kBytes;
+    uint8_t* rows_at = reinterpret_cast<uint8_t*>(shared + room);
+    const RowRing<TX, V, NV, ALIGNED> x_ring(rows_at, tm, room);
+    rows_at += x_ring.bytes(tm, room);
+    const RowRing<TY, V, NV, ALIGNED> dy_ring(rows_at, tm, room);
+    rows_at += dy_ring.bytes(tm, room);
+    uint32_t x_by = (uint32_t)reinterpret_cast<uintptr_t>(x_at) & 15, dy_by = (uint32_t)reinterpret_cast<uintptr_t>(dy_at) & 15;  // of the row worked on
     float2 stats_ahead[2] = {both(0.f), both(0.f)};
     int ahead = r;
-    // the next row not yet on its way: into slot `slot`, or (unaligned) registers
+    // the next row not yet on its way, into slot `slot`
     auto fetch = [&](int slot, float2& its) {
         if (ahead < rows) {
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                if constexpr (ALIGNED) {
-                    copy_async<16>(x_ring + (slot * NV + i) * (int)blockDim.x * 16, x_at + at[i]);
-                    copy_async<kBytes>(dy_ring + (slot * NV + i) * (int)blockDim.x * kBytes, dy_at + at[i]);
-                } else {
-                    x[i].load(x_at + at[i], a.dim - at[i], x_span);
-                    dy[i].load(dy_at + at[i], a.dim - at[i], dy_span);
-                }
-            }
+            x_ring.fetch(tm, slot, x_at, at, a.dim, x_span);
+            dy_ring.fetch(tm, slot, dy_at, at, a.dim, dy_span);
             its = reinterpret_cast<const float2*>(a.stats)[ahead];
-        } else if (!ALIGNED) {  // a team past the last row, beside one that is not
-#pragma unroll
-            for (int i = 0; i < NV; ++i) dy[i].zero();
         }
-        if (ALIGNED) copy_commit();
+        copy_commit();
         x_at += x_step;
         dy_at += dy_step;
         ahead += step;
     };
-    if (!ALIGNED)
-#pragma unroll
-        for (int i = 0; i < NV; ++i) x[i].zero();
-    fetch(0, stats_ahead[0]);
-    if (ALIGNED) fetch(1, stats_ahead[1]);
+    for (int i = 0; i < kNormAhead; ++i) fetch(i, stats_ahead[i]);
     const float inverse = -1.f / (float)a.dim;
     stage_weights<V>(shared, a.w, a.w_type, a.dim, room, 1.f);
     __syncthreads();
@@ -84,16 +72,15 @@ __global__ void __launch_bounds__(kBackwardLanes, 1) k_norm_backward(NormArgs a)
     // the lanes of a warp take as many turns as its first team does
     for (int first = tm.L < 32 ? r - (int)(threadIdx.x & 31) / tm.L : r; first < rows; first += step, r += step, o += o_step, turn ^= 1) {
         const float2 stats = stats_ahead[0];
-        if constexpr (ALIGNED) {
-            copy_wait<kNormAhead - 1>();
+        copy_wait<kNormAhead - 1>();
+        if (!ALIGNED) tm.sync();
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                x[i].load(reinterpret_cast<const TX*>(x_ring + (turn * NV + i) * (int)blockDim.x * 16), V, x_span);
-                dy[i].load(reinterpret_cast<const TY*>(dy_ring + (turn * NV + i) * (int)blockDim.x * kBytes), V, dy_span);
-                if (r >= rows) {  // a team past the last row, beside one that is not
-                    x[i].zero();
-                    dy[i].zero();
-                }
+        for (int i = 0; i < NV; ++i) {
+            x_ring.take(x[i], turn, i, at[i], x_by, a.dim);
+            dy_ring.take(dy[i], turn, i, at[i], dy_by, a.dim);
+            if (r >= rows) {  // a team past the last row, beside one that is not
+                x[i].zero();
+                dy[i].zero();
             }
         }
         const float2 minus = both(-stats.x), rs = both(stats.y);
@@ -111,10 +98,11 @@ __global__ void __launch_bounds__(kBackwardLanes, 1) k_norm_backward(NormArgs a)
                 db[i][k] = add2(db[i][k], d);
             }
         }
-        if (ALIGNED) {
-            stats_ahead[0] = stats_ahead[1];
-            fetch(turn, stats_ahead[1]);
-        }
+        stats_ahead[0] = stats_ahead[1];
+        if (!ALIGNED) tm.sync();  // all have read the row
+        fetch(turn, stats_ahead[1]);
+        x_by = (x_by + (uint32_t)(x_step * sizeof(TX))) & 15;
+        dy_by = (dy_by + (uint32_t)(dy_step * sizeof(TY))) & 15;
         if (a.out) {
             float s1 = c1.x + c1.y, s2 = c2.x + c2.y;
             tm.sum(s1, s2, turn);
@@ -140,7 +128,6 @@ __global__ void __launch_bounds__(kBackwardLanes, 1) k_norm_backward(NormArgs a)
                 }
             }
         }
-        if (!ALIGNED) fetch(0, stats_ahead[0]);
     }
     if (!a.part && !a.dweight && !a.dbias) return;
     // the lanes of a warp that hold the same columns
@@ -155,7 +142,7 @@ __global__ void __launch_bounds__(kBackwardLanes, 1) k_norm_backward(NormArgs a)
                 db[i][k].y += __shfl_xor_sync(0xffffffffu, db[i][k].y, o);
             }
     // ... then the block's teams (a warp's, where it holds several), one after another
-    float* cols = shared + room + (ALIGNED ? kNormAhead * NV * (int)blockDim.x * (16 + kBytes) / 4 : 0);
+    float* cols = reinterpret_cast<float*>(rows_at);
     const int teams = tm.L < 32 ? blockDim.x / 32 : tm.count, mine = tm.L < 32 ? threadIdx.x / 32 : tm.index;
     const bool holds = tm.L >= 32 || (threadIdx.x & 31) < tm.L;
     auto each = [&](auto f) {  // f(column, dw, db)
@@ -322,8 +309,9 @@ extern "C" int mlkv_layer_norm_backward(const void* d_dy, int64_t dy_stride, int
         a.lanes = sh.lanes;
         by_shape<kBackwardValues * (int)sizeof(TX) / 16>(sh.NV, aligned, [&](auto nv, auto al) {
             auto kernel = k_norm_backward<TX, TY, decltype(nv)::value, decltype(al)::value>;
-            const size_t smem = ((size_t)sh.lanes * sh.NV * V + (sh.lanes < threads ? 2 : 0) * (size_t)dim) * sizeof(float) +
-                                (aligned ? (size_t)kNormAhead * sh.NV * threads * (16 + V * ys) : 0);
+            const int room = sh.lanes * sh.NV * V;
+            const size_t smem = ((size_t)room + (sh.lanes < threads ? 2 : 0) * (size_t)dim) * sizeof(float) +
+                                kNormAhead * (aligned ? (size_t)sh.NV * threads * (16 + V * ys) : (size_t)teams * (norm_row(room, xs) + norm_row(room, ys)));
             ok = dense_smem(kernel, smem);
             if (ok) launch_kernel(true, kernel, dim3((unsigned)blocks), dim3(threads), smem, st, a);
         });
