@@ -29,16 +29,18 @@ struct Epilogue {
     const void* bias;
     const void* residual;
     void* pre;
-    void* out;          // rows of 16-bit values ...
-    float* part;        // ... or, where not null, fp32 sums of a share of k: [share][rows][part_stride]
-    int64_t residual_stride, pre_stride, out_stride, part_stride, part_size;
+    void* out;
+    int64_t residual_stride, pre_stride, out_stride;
     int32_t type, act;
     int32_t wide;       // rows of out, pre and residual can be moved 16 bytes at a time
 };
 
 struct Product {
     int32_t I, J, blocks;            // extents; 64-value blocks along k
-    int32_t tiles_i, tiles_j, shares, blocks_per_share;
+    int32_t tiles_i, tiles_j;
+    int32_t whole;                   // tiles that are computed whole; of the others, in shares of k, ...
+    int32_t shares, blocks_per_share;
+    float* part;                     // ... the sums: [share][tile][rows of a tile][columns of a tile]
     int32_t joined;                  // a tile's shares are a cluster, which adds them up itself
     int32_t injected;                // (mlkv_debug_fail) no operands are brought
     uint32_t idesc;
@@ -114,29 +116,41 @@ __device__ __forceinline__ float finish(const Epilogue& e, float v, int64_t row,
     return v;
 }
 
-// The tile (of i, j and k shares) that comes t-th: groups of 8 tiles along i by
-// all along j, so that tiles that run at the same time share operands in L2.
-__device__ __forceinline__ void tile_at(const Product& p, int t, int& i, int& j, int& share) {
-    const int plane = p.tiles_i * p.tiles_j;
-    share = t / plane;
-    t -= share * plane;
+// A tile: groups of 8 tiles along i by all along j, so that tiles that run at the same time share operands in L2.
+__device__ __forceinline__ void tile_at(const Product& p, int t, int& i, int& j) {
     const int group = t / (8 * p.tiles_j), first = group * 8, size = min(8, p.tiles_i - first);
     t -= group * 8 * p.tiles_j;
     i = first + t % size;
     j = t / size;
 }
+// What a block does t-th: a tile, or a share of one.
+struct Work {
+    int i, j, share, k0, k1;
+    int64_t part;  // which of the tiles' shares
+    __device__ __forceinline__ Work(const Product& p, int t, bool joined, int mine) {
+        share = joined ? mine : 0;
+        part = -1;
+        if (!joined && t >= p.whole) {
+            const int rest = p.tiles_i * p.tiles_j - p.whole;
+            part = t - p.whole;
+            share = (t - p.whole) / rest;
+            t = p.whole + (t - p.whole) % rest;
+        }
+        tile_at(p, t, i, j);
+        k0 = joined || part >= 0 ? share * p.blocks_per_share : 0;
+        k1 = joined || part >= 0 ? min(p.blocks, k0 + p.blocks_per_share) : p.blocks;
+    }
+};
 
 // 16 sums of a tile whose rows run along the output's columns: this lane's
 // column i of the output, from row j0 on.  A warp writes 32 columns of a row at a time.
 template <class T>
-__device__ __forceinline__ void put_columns(const Product& p, const uint32_t (&r)[16], int64_t i, int64_t j0, int share) {
+__device__ __forceinline__ void put_columns(const Product& p, const uint32_t (&r)[16], int64_t i, int64_t j0) {
     const Epilogue& e = p.e;
 #pragma unroll
     for (int q = 0; q < 16; ++q) {
         if (j0 + q >= p.J) break;
-        const float v = __uint_as_float(r[q]);
-        if (e.part) e.part[share * e.part_size + (j0 + q) * e.part_stride + i] = v;
-        else static_cast<T*>(e.out)[(j0 + q) * e.out_stride + i] = from_float<T>(finish(e, v, j0 + q, i));
+        static_cast<T*>(e.out)[(j0 + q) * e.out_stride + i] = from_float<T>(finish(e, __uint_as_float(r[q]), j0 + q, i));
     }
 }
 
@@ -247,12 +261,15 @@ struct Ahead {
 // A warp's 32 rows of a tile's sums, from column c0 on, 32 columns at a time: out
 // of tensor memory and through the epilogue.  `wait` returns when the sums are
 // there; the residual's first block is on its way before that, each other while
-// the one before it is worked on.
+// the one before it is worked on.  `part`: where the sums of a share go as they
+// are, this warp's part of it (rows of `stride`).
 template <class T, class W>
 __device__ __forceinline__ bool put_blocks(const Product& p, const CUtensorMap* out_map, const CUtensorMap* pre_map, uint32_t tmem,
-                                           uint8_t* corner, float* bias_at, int r0, int c0, int blocks, int share, int lane, uint32_t& turn, W wait) {
+                                           uint8_t* corner, float* bias_at, int r0, int c0, int blocks, float* part, int stride, int lane,
+                                           uint32_t& turn, W wait) {
     const Epilogue& e = p.e;
-    const T* residual = static_cast<const T*>(e.residual);
+    const T* residual = part ? nullptr : static_cast<const T*>(e.residual);
+    const bool biased = e.bias && !part;
     auto place = [&](int b) { return Place{r0, c0 + b * 32, p.I, p.J, lane, e.wide && c0 + b * 32 + 32 <= p.J}; };
     auto bias_of = [&](int b) {
         const int c = c0 + b * 32 + lane;
@@ -260,7 +277,7 @@ __device__ __forceinline__ bool put_blocks(const Product& p, const CUtensorMap* 
     };
     Ahead<T> ahead;
     float bias = 0.f;
-    if (e.bias) bias = bias_of(0);
+    if (biased) bias = bias_of(0);
     if (residual) ahead.load(residual, e.residual_stride, place(0));
     if (!wait()) return false;
     const bool two = e.pre || residual;  // both halves have a use of their own; else they take turns, from tile to tile
@@ -270,21 +287,22 @@ __device__ __forceinline__ bool put_blocks(const Product& p, const CUtensorMap* 
         uint32_t acc[32];
         __syncwarp();
         tmem_ld32(tmem + b * 32, acc);
-        if (e.part) {
+        if (part) {  // (a corner's 4 KB as 32 rows of 128 bytes)
+            if (b == 0) {  // what an earlier tile has left there is still on its way
+                if (e.wide && lane == 0) tma_store_read<0>();
+                __syncwarp();
+            }
             tmem_wait_ld();
             auto sums = [&](int row, int c) -> uint4& { return *reinterpret_cast<uint4*>(corner + row * 128 + ((c ^ (row & 7)) << 4)); };
 #pragma unroll
             for (int c = 0; c < 8; ++c) sums(lane, c) = make_uint4(acc[4 * c], acc[4 * c + 1], acc[4 * c + 2], acc[4 * c + 3]);
             __syncwarp();
-            const int row = r0 + (lane >> 3), c = lane & 7;  // (rows of whole 16-byte pieces)
-            float* part = e.part + share * e.part_size + row * e.part_stride + q.c0 + c * 4;
-            if (q.c0 + c * 4 < e.part_stride)
+            float* to = part + (lane >> 3) * stride + b * 32 + (lane & 7) * 4;
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (row + i * 4 < p.I) *reinterpret_cast<uint4*>(part + i * 4 * e.part_stride) = sums(i * 4 + (lane >> 3), c);
+            for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4*>(to + i * 4 * stride) = sums(i * 4 + (lane >> 3), lane & 7);
             continue;
         }
-        if (e.bias) {
+        if (biased) {
             bias_at[lane] = bias;
             if (b + 1 < blocks) bias = bias_of(b + 1);
         }
@@ -293,7 +311,7 @@ __device__ __forceinline__ bool put_blocks(const Product& p, const CUtensorMap* 
         float2 v[16];
 #pragma unroll
         for (int k = 0; k < 16; ++k) v[k] = make_float2(__uint_as_float(acc[2 * k]), __uint_as_float(acc[2 * k + 1]));
-        if (e.bias) {
+        if (biased) {
 #pragma unroll
             for (int k = 0; k < 16; k += 2) {
                 const float4 x = reinterpret_cast<const float4*>(bias_at)[k / 2];
@@ -412,19 +430,16 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR>::kThreads, 1)
 
     // joined shares: one tile a block, its share by its place in the cluster
     const int tiles = p.tiles_i * p.tiles_j, mine = joined ? (int)cluster_rank() : 0;
-    const int total = joined ? tiles : tiles * p.shares, first = joined ? blockIdx.x / p.shares : blockIdx.x / kBlocks;
+    const int total = joined ? tiles : p.whole + (tiles - p.whole) * p.shares, first = joined ? blockIdx.x / p.shares : blockIdx.x / kBlocks;
     const int step = joined ? tiles : gridDim.x / kBlocks;
     if (warp == kTma) {
         if (lane == 0 && !p.injected) {
             uint32_t n = 0;  // stages filled
             bool ok = true;
             for (int t = first; t < total && ok; t += step) {
-                int i, j, share;
-                tile_at(p, t, i, j, share);
-                if (joined) share = mine;
-                const int k0 = share * p.blocks_per_share, k1 = min(p.blocks, k0 + p.blocks_per_share);
-                const int row = (i * kBlocks + (int)rank) * kBM, col = j * BN + (int)rank * kCols;
-                for (int k = k0; k < k1; ++k, ++n) {
+                const Work w(p, t, joined, mine);
+                const int row = (w.i * kBlocks + (int)rank) * kBM, col = w.j * BN + (int)rank * kCols;
+                for (int k = w.k0; k < w.k1; ++k, ++n) {
                     const uint32_t s = n % S, at = ring + s * R::kStage;
                     if (n >= S && !(ok = mbar_wait(empty + 8 * s, (n / S - 1) & 1, &stop))) break;
                     if (rank == 0) mbar_expect(full + 8 * s, kBlocks * R::kStage);
@@ -453,21 +468,18 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR>::kThreads, 1)
             uint32_t n = 0, u = 0;  // stages read, accumulators used
             bool ok = true;
             for (int t = first; t < total && ok; t += step, ++u) {
-                int i, j, share;
-                tile_at(p, t, i, j, share);
-                if (joined) share = mine;
-                const int k0 = share * p.blocks_per_share, k1 = min(p.blocks, k0 + p.blocks_per_share);
+                const Work w(p, t, joined, mine);
                 const uint32_t acc = u & 1, d = tmem + acc * BN;
                 if (u >= 2 && !(ok = mbar_wait(drained + 8 * acc, (u / 2 - 1) & 1, &stop))) break;
                 tc_fence_after();
-                for (int k = k0; k < k1; ++k, ++n) {
+                for (int k = w.k0; k < w.k1; ++k, ++n) {
                     const uint32_t s = n % S, at = ring + s * R::kStage;
                     if (!(ok = mbar_wait(full + 8 * s, (n / S) & 1, &stop))) break;
                     tc_fence_after();
                     const uint64_t da = smem_desc(at, A_MN ? 8192 : 16), db = smem_desc(at + R::kA, B_MN ? 8192 : 16);
 #pragma unroll
                     for (int q = 0; q < kBK / 16; ++q)  // 16 values along k: 32 bytes of a row, or 16 rows
-                        tc_mma<PAIR>(d, da + q * (A_MN ? 128 : 2), db + q * (B_MN ? 128 : 2), p.idesc, k > k0 || q > 0);
+                        tc_mma<PAIR>(d, da + q * (A_MN ? 128 : 2), db + q * (B_MN ? 128 : 2), p.idesc, k > w.k0 || q > 0);
                     tc_commit<PAIR>(empty + 8 * s);
                 }
                 if (ok) tc_commit<PAIR>(done + 8 * acc);
@@ -481,15 +493,14 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR>::kThreads, 1)
         uint32_t u = 0, turn = 0;
         const uint32_t told = PAIR ? place_in(drained, 0) : drained;
         for (int t = first; t < total; t += step, ++u) {
-            int i, j, share;
-            tile_at(p, t, i, j, share);
+            const Work w(p, t, joined, mine);
             const uint32_t acc = u & 1, at = tmem + acc * BN + ((uint32_t)(warp & 3) << 21);
             auto wait = [&] {
                 const bool ok = __all_sync(0xffffffffu, mbar_wait(done + 8 * acc, (u / 2) & 1, &stop));
                 tc_fence_after();
                 return ok;
             };
-            const int r0 = (i * kBlocks + (int)rank) * kBM + (warp & 3) * 32;
+            const int in_tile = (int)rank * kBM + (warp & 3) * 32, r0 = w.i * kBlocks * kBM + in_tile;
             if constexpr (SWAP) {
                 if (!wait()) break;
 #pragma unroll 1
@@ -499,20 +510,21 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR>::kThreads, 1)
                     tmem_ld16(at + c, r);
                     tmem_wait_ld();
                     if (joined) {  // where the ring was: all of it has been read
-                        const bool any = share * p.blocks_per_share < p.blocks;
+                        const bool any = w.k0 < w.k1;
 #pragma unroll
                         for (int q = 0; q < 16; ++q)
                             reinterpret_cast<uint32_t*>(raw + (ring - smem_of(raw)))[(c + q) * kBM + warp * 32 + lane] = any ? r[q] : 0u;
                     } else if (r0 + lane < p.I) {
-                        put_columns<T>(p, r, r0 + lane, (int64_t)j * BN + c, share);
+                        put_columns<T>(p, r, r0 + lane, (int64_t)w.j * BN + c);
                     }
                 }
             } else {
                 const int cols = BN * 4 / R::kEpilogue, c = (warp >> 2) * cols;  // this warp's
                 uint8_t* corners = raw + (ring - smem_of(raw)) + S * R::kStage;
+                float* part = w.part < 0 ? nullptr : p.part + (w.part * kBlocks * kBM + in_tile) * BN + c;
                 if (!put_blocks<T>(p, &out_map, &pre_map, at + c, corners + warp * kCorner,
-                                   reinterpret_cast<float*>(corners + R::kEpilogue * kCorner + warp * kBias), r0, j * BN + c,
-                                   r0 < p.I ? cols / 32 : 0, share, lane, turn, wait)) break;
+                                   reinterpret_cast<float*>(corners + R::kEpilogue * kCorner + warp * kBias), r0, w.j * BN + c,
+                                   r0 < p.I ? cols / 32 : 0, part, BN, lane, turn, wait)) break;
             }
             __syncwarp();
             tc_fence_before();
@@ -527,10 +539,9 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR>::kThreads, 1)
     tc_fence_before();
     __syncthreads();
     if (joined) {
-        int i, j, share;
-        tile_at(p, first, i, j, share);
+        const Work w(p, first, true, mine);
         cluster_sync();
-        if (warp < 4) join_columns<T, BN>(p, ring, i, j, mine);
+        if (warp < 4) join_columns<T, BN>(p, ring, w.i, w.j, mine);
         __syncwarp();
     }
     if (PAIR || joined) cluster_sync();  // nothing of this block's memory is wanted by another any more
@@ -539,22 +550,34 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR>::kThreads, 1)
     if (warp == kMma) tmem_free<PAIR>(tmem, R::kColumns);
 }
 
-// The shares of k added up in order, and the epilogue (shares == 0: of zeros): four columns a thread.
-template <class T>
-__global__ void __launch_bounds__(256) k_product_finish(Epilogue e, int64_t rows, int64_t cols, int shares) {
+// The shares of the tiles that are not whole, added up in a fixed order, and the epilogue: four columns a thread, or,
+// where there are many shares, four threads (GROUPS), each with every fourth share; 2^blocks_per_tile blocks a tile of
+// 2^(wide + 2) columns.  (No shares: of zeros.  With one thread / four, us: 64 shares of a 64 x 64 gradient 12.2 / 5.2, 9 of
+// 512 x 512 5.7 / 5.2, 4 of 1,000 x 776 6.2 / 8.1.)
+template <class T, int GROUPS>
+__global__ void __launch_bounds__(256) k_product_finish(const Product p, int blocks_per_tile, int wide) {
     pdl_enter();
-    const int64_t per = (cols + 3) / 4;
-    for (int64_t at = blockIdx.x * 256ll + threadIdx.x; at < rows * per; at += gridDim.x * 256ll) {
-        const int64_t r = at / per, c = (at - r * per) * 4;
-        const float4* part = reinterpret_cast<const float4*>(e.part + r * e.part_stride + c);
-        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    constexpr int kOf = 256 / GROUPS;
+    __shared__ float4 sums[GROUPS][kOf];
+    const int mine = threadIdx.x % kOf, group = threadIdx.x / kOf;
+    const int64_t all = gridDim.x * (int64_t)kOf;
+    const float4* part = reinterpret_cast<const float4*>(p.part) + blockIdx.x * (int64_t)kOf + mine;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](const float4& x) { sum = make_float4(sum.x + x.x, sum.y + x.y, sum.z + x.z, sum.w + x.w); };
 #pragma unroll 8
-        for (int s = 0; s < shares; ++s) {
-            const float4 x = part[s * (e.part_size / 4)];
-            sum = make_float4(sum.x + x.x, sum.y + x.y, sum.z + x.z, sum.w + x.w);
-        }
-        put_four<T>(e, sum, r, c, cols);
+    for (int s = group; s < p.shares; s += GROUPS) add(part[s * all]);
+    if (GROUPS > 1) {
+        sums[group][mine] = sum;
+        __syncthreads();
+        if (group) return;
+        for (int g = 1; g < GROUPS; ++g) add(sums[g][mine]);
     }
+    const int q = (int)(blockIdx.x & ((1u << blocks_per_tile) - 1)) * kOf + mine;
+    int i, j;
+    tile_at(p, p.whole + (int)(blockIdx.x >> blocks_per_tile), i, j);
+    const int64_t row = (int64_t)i * ((kOf << blocks_per_tile) >> wide) + (q >> wide);
+    const int64_t col = ((int64_t)j << (wide + 2)) + (q & ((1 << wide) - 1)) * 4;
+    if (row < p.I && col < p.J) put_four<T>(p.e, sum, row, col, p.J);
 }
 
 // Rows whose stride or place TMA does not take (multiples of 16 bytes), laid out anew: up to two matrices at a time.
@@ -758,7 +781,7 @@ struct Caller {
             return;
         }
         CUtensorMap out = ma, pre = ma;  // (not looked at where the epilogue does not store by TMA)
-        if (!SWAP && p.e.wide && !p.e.part) {
+        if (!SWAP && p.e.wide) {
             if (!encode(&out, {static_cast<const uint16_t*>(p.e.out), p.e.out_stride, p.I, p.J}, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B) ||
                 (p.e.pre && !encode(&pre, {static_cast<const uint16_t*>(p.e.pre), p.e.pre_stride, p.I, p.J}, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B))) {
                 rc = MLKV_ERR_CUDA;
@@ -767,7 +790,7 @@ struct Caller {
         }
         p.injected = take_injected_product();
         p.idesc = mma_desc(type == MLKV_TYPE_BFLOAT, A_MN, B_MN, PAIR ? 2 * kBM : kBM, BN);
-        const int64_t tiles = (int64_t)p.tiles_i * p.tiles_j * p.shares;
+        const int64_t all = (int64_t)p.tiles_i * p.tiles_j, tiles = p.joined ? all * p.shares : p.whole + (all - p.whole) * p.shares;
         auto go = [&](auto kernel) {
             if (!dense_smem(kernel, R::kBytes)) rc = MLKV_ERR_CUDA;
             else if (PAIR) launch_clusters(kernel, 2, 2 * std::min<int64_t>(tiles, sms / 2), R::kThreads, R::kBytes, st, ma, mb, out, pre, p);
@@ -777,10 +800,16 @@ struct Caller {
         if (type == MLKV_TYPE_BFLOAT) go(k_product<BN, A_MN, B_MN, SWAP, PAIR, __nv_bfloat16>);
         else go(k_product<BN, A_MN, B_MN, SWAP, PAIR, __half>);
     }
-    void finish_shares(const Epilogue& e, int64_t rows, int64_t cols, int shares) {
+    void finish_shares(const Product& p, int high, int bn) {
         if (!run) return;
-        const dim3 grid(blocks_for(rows * ((cols + 3) / 4)));
-        launch_kernel(true, type == MLKV_TYPE_BFLOAT ? k_product_finish<__nv_bfloat16> : k_product_finish<__half>, grid, dim3(256), 0, st, e, rows, cols, shares);
+        const int groups = p.shares >= 8 ? 4 : 1, blocks = high * bn / 1024 * groups, wide = bn == 64 ? 4 : bn == 128 ? 5 : 6;
+        int per = 0;
+        while (1 << per < blocks) ++per;
+        const dim3 grid((unsigned)((int64_t)(p.tiles_i * p.tiles_j - p.whole) * blocks));
+        const bool b = type == MLKV_TYPE_BFLOAT;
+        const auto kernel = groups == 4 ? (b ? k_product_finish<__nv_bfloat16, 4> : k_product_finish<__half, 4>)
+                                        : (b ? k_product_finish<__nv_bfloat16, 1> : k_product_finish<__half, 1>);
+        launch_kernel(true, kernel, grid, dim3(256), 0, st, p, per, wide);
     }
     // Whether pairs of blocks take the tiles of 256 columns: where there are enough for every pair, and k is long
     // enough for the products to count beside the epilogue.  (Single blocks / pairs, us: 16,384 x 4,096 by k = 4,096
@@ -789,29 +818,55 @@ struct Caller {
         return blocks >= 12 && (tiles_i + 1) / 2 * tiles_j * (blocks / 12) >= sms / 2;
     }
 
-    // How few tiles share the GPU: columns a tile, and shares of k (of at least 4 blocks), which another launch adds up.
-    struct Shape { int bn; int64_t shares; };
-    // By the time of a block's work, in us: what each width takes besides k; a block of 64 along k (its operands' latency,
-    // or their bytes through L2 on all SMs); and the launch that adds the shares up, with its bytes.  (Widths of 256 /
-    // 128 / 64 at their best, us: 300 x 1,000 by k = 520 9.7 / 7.8 / 7.2; 1,000 x 1,000 by 1,000 12.8 / 9.9 / 8.3; 200 x
-    // 512 by 8,192 12.3 / 10.5 / 10.3; 512 x 512 by 8,000 13.1 / 12.4 / 14.6; 4,096 x 1,000 by 776 14.6 / 16.0 / 21.0.)
-    Shape few_tiles(int64_t rows, int64_t cols, int64_t blocks) const {
-        constexpr float kFixed[3] = {5.f, 6.5f, 8.5f}, kBlock = 0.25f, kL2 = 15e6f, kLaunch = 4.f, kFinish = 6e6f;
-        Shape best = {cols <= 64 ? 64 : cols <= 128 ? 128 : 256, 1};
+    // The time, in us, of `rounds` of work after one another, each of a tile of bn columns (and 128 rows a block) and
+    // `blocks` blocks of k, on `busy` SMs: what a width takes besides k, once; a block of k, by its operands' latency,
+    // their bytes through L2 on all those SMs, or the matrix unit's rate.
+    static float time_of(int64_t rounds, int bn, int64_t blocks, int64_t busy, bool pair) {
+        constexpr float kLatency = 0.25f, kL2 = 15e6f;
+        const float fixed = bn == 64 ? 5.f : bn == 128 ? 6.5f : 8.5f, bytes = (float)(kBM + (pair ? bn / 2 : bn)) * kBK * 2;
+        const float block = std::max(rounds > 1 ? 0.f : kLatency, std::max((float)busy * bytes / kL2, 0.34f * bn / 256));
+        return fixed + (float)(rounds * blocks) * block;
+    }
+    // The launch that adds shares of tiles up.
+    static float time_to_finish(int64_t tiles, int64_t shares, int high, int bn) {
+        constexpr float kLaunch = 4.f, kBytes = 6e6f;
+        return kLaunch + (float)((shares + 1) * tiles * high * bn) * 4 / kBytes;
+    }
+    // Tiles (the last ones) whose k is shared out, and their shares, of at least 4 blocks: where the tiles do not fill
+    // the GPU, or its last round.  (Gradients of a 4,096 x 4,096 weight over 16,384 rows: 256 tiles on 76 pairs of SMs.)
+    struct Split { int64_t tiles, shares; float time; };
+    Split split(int64_t tiles, int high, int bn, int64_t blocks) const {
+        const bool pair = high > kBM;
+        const int64_t places = pair ? sms / 2 : sms, full = tiles / places, rest = tiles % places;
+        const int64_t busy = full ? sms : rest * (pair ? 2 : 1);
+        Split best = {0, 1, time_of(full + (rest > 0), bn, blocks, busy, pair)};
+        const float before = full ? time_of(full, bn, blocks, busy, pair) : 0.f;
+        if (!rest) return best;
+        auto look = [&](int64_t s) {
+            const int64_t rounds = (rest * s + places - 1) / places;
+            if (s < 2 || s * 4 > blocks || rounds >= s) return;
+            const float t = before + time_of(rounds, bn, (blocks + s - 1) / s, std::min(rest * s, places) * (pair ? 2 : 1), pair) + time_to_finish(rest, s, high, bn);
+            if (t < best.time) best = {rest, s, t};
+        };
+        for (int64_t s = std::min(places / rest, blocks / 4); s > 1; s /= 2) look(s);  // within a round
+        for (int64_t r = 2; r <= 4 && full; ++r) look(r * places / rest);               // the most in r short ones
+        return best;
+    }
+    // The width of single blocks' tiles, where the narrower ones fit on the GPU at once.  (Widths of 256 / 128 / 64 at
+    // their best, us: 300 x 1,000 by k = 520 9.7 / 7.8 / 7.2; 1,000 x 1,000 by 1,000 12.8 / 9.9 / 8.3; 200 x 512 by 8,192
+    // 12.3 / 10.5 / 10.3; 512 x 512 by 8,000 13.1 / 12.4 / 14.6; 4,096 x 1,000 by 776 14.6 / 16.0 / 21.0.)
+    int width(int64_t rows, int64_t cols, int64_t blocks) const {
+        int best = cols <= 64 ? 64 : cols <= 128 ? 128 : 256;
         float least = 3e38f;
-        for (int w = 0; w < 3; ++w) {
-            const int bn = 64 << w;
+        for (int bn = 64; bn <= 256; bn *= 2) {
             const int64_t tiles = (rows + kBM - 1) / kBM * ((cols + bn - 1) / bn);
-            if (tiles <= sms)
-                for (int64_t s = std::max<int64_t>(1, std::min<int64_t>(sms / tiles, blocks / 4));; s /= 2) {
-                    const float block = std::max(kBlock, (float)(tiles * s) * (kBM + bn) * kBK * 2 / kL2);
-                    const float time = kFixed[w] + (float)((blocks + s - 1) / s) * block + (s > 1 ? kLaunch + (float)(s + 1) * rows * cols * 4 / kFinish : 0.f);
-                    if (time < least) {
-                        least = time;
-                        best = {bn, s};
-                    }
-                    if (s == 1) break;
+            if (tiles <= sms) {
+                const float t = split(tiles, kBM, bn, blocks).time;
+                if (t < least) {
+                    least = t;
+                    best = bn;
                 }
+            }
             if (bn >= cols) break;
         }
         return best;
@@ -822,50 +877,46 @@ struct Caller {
     void product(Matrix a, Matrix b, int64_t rows, int64_t cols, int64_t k, Epilogue e) {
         if (!rows || !cols) return;
         e.type = type;
-        if (k == 0) {
-            finish_shares(e, rows, cols, 0);
-            return;
-        }
         auto wide = [](const void* p, int64_t stride) { return !p || (reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 8 == 0); };
         e.wide = wide(e.out, e.out_stride) && wide(e.pre, e.pre_stride) && wide(e.residual, e.residual_stride);
-        const bool swap = !A_MN && rows <= 64;  // few rows: the wide operand fills the tiles' 128 rows
+        const bool swap = !A_MN && rows <= 64 && k > 0;  // few rows: the wide operand fills the tiles' 128 rows
         Product p = {};
         p.I = (int32_t)(swap ? cols : rows);
         p.J = (int32_t)(swap ? rows : cols);
         p.blocks = (int32_t)((k + kBK - 1) / kBK);
-        p.tiles_i = (p.I + kBM - 1) / kBM;
-        auto shares_of = [&](int64_t places) { return std::max<int64_t>(1, std::min<int64_t>(places / ((int64_t)p.tiles_i * p.tiles_j), p.blocks / 4)); };
-        const bool pair = !swap && cols > 128 && pair_pays(p.tiles_i, (p.J + 255) / 256, p.blocks);
-        Shape shape = {256, 1};
-        if (swap) shape.bn = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
-        else if (!pair) shape = few_tiles(rows, cols, p.blocks);
-        const int bn = shape.bn;
-        p.tiles_j = (p.J + bn - 1) / bn;
-        if (pair) p.tiles_i = (p.I + 2 * kBM - 1) / (2 * kBM);
-        if ((int64_t)p.tiles_i * p.tiles_j >= (int64_t)1 << 30) {
+        p.e = e;
+        const int64_t down = ((int64_t)p.I + kBM - 1) / kBM;
+        const bool pair = !swap && cols > 128 && pair_pays(down, (p.J + 255) / 256, p.blocks);
+        const int bn = swap ? (rows <= 16 ? 16 : rows <= 32 ? 32 : 64) : pair ? 256 : width(rows, cols, p.blocks);
+        const int64_t across = (p.J + bn - 1) / bn, high = pair ? 2 * kBM : kBM, tiles = ((int64_t)p.I + high - 1) / high * across;
+        if (tiles >= (int64_t)1 << 30) {
             rc = MLKV_ERR_UNSUPPORTED;
             return;
         }
-        const int64_t shares = swap ? shares_of(sms) : pair ? shares_of(sms / 2) : shape.shares;
-        p.blocks_per_share = (int32_t)((p.blocks + shares - 1) / shares);
-        p.shares = (p.blocks + p.blocks_per_share - 1) / p.blocks_per_share;
-        p.e = e;
-        // few rows: the shares of a tile are a cluster (of 2, 4 or 8), one tile a block
-        if (swap && p.shares > 1) {
-            int n = 2;
-            while (n < 8 && 2 * n <= p.shares) n *= 2;
-            p.blocks_per_share = (p.blocks + n - 1) / n;
-            p.shares = n;  // (the last may be of nothing)
-            p.joined = 1;
+        p.tiles_i = (int32_t)(tiles / across);
+        p.tiles_j = (int32_t)across;
+        p.whole = (int32_t)tiles;
+        p.shares = 1;
+        if (k == 0) {
+            p.whole = p.shares = 0;
+            finish_shares(p, (int)high, bn);
+            return;
         }
-        if (p.shares > 1 && !p.joined) {
-            e.part_stride = round_up(cols, 4);
-            e.part_size = rows * e.part_stride;
-            e.part = static_cast<float*>(arena.take(p.shares * e.part_size * 4));
-            p.e = Epilogue{};
-            p.e.part = e.part;
-            p.e.part_stride = e.part_stride;
-            p.e.part_size = e.part_size;
+        if (swap) {
+            // few rows: k in shares of at least 4 blocks, those of a tile a cluster (of 2, 4 or 8), one tile a block
+            int n = 1;
+            while (n < 8 && 2 * n <= std::min<int64_t>(sms / tiles, p.blocks / 4)) n *= 2;
+            p.shares = n;
+            p.joined = n > 1;
+            p.blocks_per_share = (p.blocks + n - 1) / n;  // (the last may be of nothing)
+        } else {
+            const Split s = split(tiles, (int)high, bn, p.blocks);
+            if (s.shares > 1) {
+                p.whole = (int32_t)(tiles - s.tiles);
+                p.blocks_per_share = (int32_t)((p.blocks + s.shares - 1) / s.shares);
+                p.shares = (p.blocks + p.blocks_per_share - 1) / p.blocks_per_share;
+                p.part = static_cast<float*>(arena.take(s.tiles * p.shares * high * bn * 4));
+            }
         }
         if (!run) return;
         if constexpr (!A_MN) {
@@ -881,7 +932,7 @@ struct Caller {
             else if (pair) launch<256, A_MN, B_MN, false, true>(a, b, p);
             else launch<256, A_MN, B_MN, false>(a, b, p);
         }
-        if (p.shares > 1 && !p.joined) finish_shares(e, rows, cols, p.shares);
+        if (p.part) finish_shares(p, (int)high, bn);
     }
 
     void forward(const mlkv_linear_args& g) {
