@@ -44,6 +44,12 @@ struct Product {
     int32_t joined;                  // a tile's shares are a cluster, which adds them up itself
     int32_t injected;                // (mlkv_debug_fail) no operands are brought
     uint32_t idesc;
+    // The operands (rows of k values), where sums near 0 are computed again (relu's): below `doubt` of the
+    // largest beside them.
+    const void *a, *b;
+    int64_t a_stride, b_stride;
+    int32_t k;
+    float doubt;
     Epilogue e;
 };
 
@@ -258,12 +264,52 @@ struct Ahead {
     }
 };
 
+// relu's slope jumps at 0, where the matrix unit's rounding (about 2^-24 of the
+// sums on the way, every 16 values of k) decides it at random: one such value moves
+// a whole row of dx.  So of a lane's 32 values the smallest, where it is that near
+// 0, is computed again by the warp, in 64 bits.  (65,536 x 416 by 512: about 45 of
+// 33.5 million.  Of sums that go out as shares, or of 64 rows or fewer, it is not:
+// they are a few million at the most.)
+template <class T>
+__device__ __forceinline__ void doubtful(const Product& p, float2 (&v)[16], int r0, int c0, int lane) {
+    float least = INFINITY, most = 0.f;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+        least = fminf(least, fminf(fabsf(v[k].x), fabsf(v[k].y)));
+        most = fmaxf(most, fmaxf(fabsf(v[k].x), fabsf(v[k].y)));
+    }
+    uint32_t again = __ballot_sync(0xffffffffu, r0 + lane < p.I && least < most * p.doubt && most < 1e30f);
+    if (!again) return;
+    int at = 32;  // this lane's smallest
+#pragma unroll
+    for (int k = 15; k >= 0; --k) {
+        if (fabsf(v[k].y) == least) at = 2 * k + 1;
+        if (fabsf(v[k].x) == least) at = 2 * k;
+    }
+    for (; again; again &= again - 1) {
+        const int from = __ffs(again) - 1, c = __shfl_sync(0xffffffffu, at, from), col = c0 + c;
+        if (c == 32 || col >= p.J) continue;
+        const T *a = static_cast<const T*>(p.a) + (r0 + from) * p.a_stride, *b = static_cast<const T*>(p.b) + col * p.b_stride;
+        double sum = 0;
+#pragma unroll 8
+        for (int k = lane; k < p.k; k += 32) sum += (double)to_float(a[k]) * (double)to_float(b[k]);
+#pragma unroll
+        for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (p.e.bias) sum += (double)to_float(static_cast<const T*>(p.e.bias)[col]);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            if (lane == from && c == 2 * k) v[k].x = (float)sum;
+            if (lane == from && c == 2 * k + 1) v[k].y = (float)sum;
+        }
+    }
+}
+
 // A warp's 32 rows of a tile's sums, from column c0 on, 32 columns at a time: out
 // of tensor memory and through the epilogue.  `wait` returns when the sums are
 // there; the residual's first block is on its way before that, each other while
 // the one before it is worked on.  `part`: where the sums of a share go as they
 // are, this warp's part of it (rows of `stride`).
-template <class T, class W>
+template <class T, bool DOUBT, class W>
 __device__ __forceinline__ bool put_blocks(const Product& p, const CUtensorMap* out_map, const CUtensorMap* pre_map, uint32_t tmem,
                                            uint8_t* corner, float* bias_at, int r0, int c0, int blocks, float* part, int stride, int lane,
                                            uint32_t& turn, W wait) {
@@ -319,6 +365,7 @@ __device__ __forceinline__ bool put_blocks(const Product& p, const CUtensorMap* 
                 v[k + 1] = add2(v[k + 1], make_float2(x.z, x.w));
             }
         }
+        if (DOUBT && p.a) doubtful<T>(p, v, r0, q.c0, lane);
         // What a half holds goes to memory; whoever fills it next waits until it has been read.
         auto put = [&](Half s, const CUtensorMap* map, void* m, int64_t stride) {
 #pragma unroll
@@ -522,7 +569,7 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR>::kThreads, 1)
                 const int cols = BN * 4 / R::kEpilogue, c = (warp >> 2) * cols;  // this warp's
                 uint8_t* corners = raw + (ring - smem_of(raw)) + S * R::kStage;
                 float* part = w.part < 0 ? nullptr : p.part + (w.part * kBlocks * kBM + in_tile) * BN + c;
-                if (!put_blocks<T>(p, &out_map, &pre_map, at + c, corners + warp * kCorner,
+                if (!put_blocks<T, !A_MN && !B_MN>(p, &out_map, &pre_map, at + c, corners + warp * kCorner,
                                    reinterpret_cast<float*>(corners + R::kEpilogue * kCorner + warp * kBias), r0, w.j * BN + c,
                                    r0 < p.I ? cols / 32 : 0, part, BN, lane, turn, wait)) break;
             }
@@ -600,7 +647,11 @@ __global__ void __launch_bounds__(256) k_align(Align a, Align b) {
 }
 
 // p = dy act'(z), and the sums of its columns over a block's rows.  A thread
-// takes 8 columns, a block 256 columns of a share of the rows.
+// takes 8 columns, a block 256 columns of a share of the rows: one round of
+// blocks, four an SM, of two rows a warp at a time.  Bound by HBM (65,536 x 512
+// bf16, relu: 41 us, with two blocks an SM, four rows and two rounds 46; 16,384 x
+// 4,096, gelu: 70, before 79: 5.8 TB/s).
+constexpr int kSlopeBlocks = 4;
 struct Slope {
     const void* dy;
     const void* pre;
@@ -611,11 +662,11 @@ struct Slope {
     int32_t act, joined;  // (the blocks of a column are a cluster)
 };
 template <class T, bool ALIGNED>
-__global__ void __launch_bounds__(256) k_slope(Slope a) {
+__global__ void __launch_bounds__(256, ALIGNED ? kSlopeBlocks : 2) k_slope(Slope a) {
     pdl_enter();
     __shared__ float sums[8][256], mine[256];
     using Row = Values<T, 8, ALIGNED>;
-    constexpr int kRows = ALIGNED ? 4 : 2;  // on their way at a time
+    constexpr int kRows = 2;  // on their way at a time
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t c = (blockIdx.x * 32ll + lane) * 8;
     const int n = (int)min((int64_t)8, a.cols - c);
@@ -885,6 +936,11 @@ struct Caller {
         p.J = (int32_t)(swap ? rows : cols);
         p.blocks = (int32_t)((k + kBK - 1) / kBK);
         p.e = e;
+        if (!A_MN && !B_MN && !swap && e.act == MLKV_ACT_RELU) {
+            p.a = a.p; p.a_stride = a.stride; p.b = b.p; p.b_stride = b.stride;
+            p.k = (int32_t)k;
+            p.doubt = (float)p.blocks / (1 << 23);
+        }
         const int64_t down = ((int64_t)p.I + kBM - 1) / kBM;
         const bool pair = !swap && cols > 128 && pair_pays(down, (p.J + 255) / 256, p.blocks);
         const int bn = swap ? (rows <= 16 ? 16 : rows <= 32 ? 32 : 64) : pair ? 256 : width(rows, cols, p.blocks);
@@ -960,8 +1016,8 @@ struct Caller {
             const Matrix dy = {(const uint16_t*)s.dy, s.dy_stride, 0, 0}, pre = {(const uint16_t*)s.pre, s.pre_stride, 0, 0};
             const bool whole = g.n % 8 == 0 && dy.aligned() && (!act || pre.aligned());
             const int64_t across = (g.n + 255) / 256;
-            // a block's warps take 4 rows each at a time; up to 1,024 rows no column has more blocks than a cluster
-            const int64_t most = g.d_dbias && g.m <= 1024 ? 8 : 8ll * sms / across;
+            // a block's warps take 4 rows each at least; up to 1,024 rows no column has more blocks than a cluster
+            const int64_t most = g.d_dbias && g.m <= 1024 ? 8 : (int64_t)kSlopeBlocks * sms / across;
             const int64_t shares = std::max<int64_t>(1, std::min<int64_t>((g.m + 31) / 32, most));
             s.share = (g.m + shares - 1) / shares;
             const unsigned down = (unsigned)((g.m + s.share - 1) / s.share);

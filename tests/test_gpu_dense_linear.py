@@ -178,3 +178,29 @@ def test_more_tiles_than_blocks():
     torch = torch_cuda()
     _run(torch, 5000, 2304, 136, torch.bfloat16, "relu", True, True)
     _run(torch, 9000, 264, 72, torch.float16, "none", True, False)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_relu_near_zero(dtype):
+    """Sums that cancel to next to nothing beside large ones: their signs, which decide relu's slope, are the exact ones."""
+    torch = torch_cuda()
+    dtype = _t(dtype)
+    from paper_2504_01506_gb300 import dense
+
+    gen = torch.Generator("cuda")
+    gen.manual_seed(3)
+    m, n, half = 400, 96, 256
+    u = _matrix(torch, m, half, dtype, gen)
+    w = _matrix(torch, n, half, dtype, gen, 0.06)
+    sign = torch.where(torch.rand((m, 1), generator=gen, device="cuda") < 0.5, -1.0, 1.0)
+    tiny = (sign * 2.0 ** -20).to(dtype)  # (exact in both types: subnormal in fp16)
+    x = torch.cat([u, u, tiny], 1)
+    weight = torch.cat([w, w, torch.zeros((n, 1), dtype=w.dtype, device="cuda")], 1)
+    for column in (5, 37, 95):  # u v - u v + tiny: z is tiny
+        weight[column, half:2 * half] = -w[column]
+        weight[column, 2 * half] = 1
+    y, pre = dense.linear(x, weight, activation="relu", save_pre=True)
+    exact = x.double() @ weight.double().T
+    for column in (5, 37, 95):
+        assert torch.equal(pre[:, column].double(), exact[:, column])
+        assert torch.equal(y[:, column].double(), exact[:, column].clamp(min=0))
