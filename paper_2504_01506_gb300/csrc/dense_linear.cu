@@ -8,8 +8,11 @@
 // in memory run along k, or along i or j (dx: W's; dW: both), which the matrix
 // unit takes as they lie.  One kernel computes them (k_product): TMA brings
 // tiles into a ring in shared memory, one thread issues tcgen05.mma into one of
-// two accumulators in tensor memory, and four warps take the other one out
-// through the epilogue.
+// two accumulators in tensor memory, and 4 to 16 warps take the other one out
+// through the epilogue, whose blocks leave by TMA too.
+//
+// Sums are fp32 all the way; what is rounded to 16 bits is z (`pre`, which the
+// slopes are taken at, while y goes by z itself), y, p and the gradients, once each.
 #include <cudaTypedefs.h>
 
 #include <algorithm>
@@ -43,6 +46,7 @@ struct Product {
     float* part;                     // ... the sums: [share][tile][rows of a tile][columns of a tile]
     int32_t joined;                  // a tile's shares are a cluster, which adds them up itself
     int32_t injected;                // (mlkv_debug_fail) no operands are brought
+    int32_t beside;                  // needs nothing of the launch before it, which needs nothing of its outputs
     uint32_t idesc;
     // The operands (rows of k values), where sums near 0 are computed again (relu's): below `doubt` of the
     // largest beside them.
@@ -432,6 +436,11 @@ template <int BN, bool SWAP, bool PAIR> struct Ring {
     static constexpr uint32_t kColumns = 2 * BN < 32 ? 32 : 2 * BN;
 };
 
+// Bound by the matrix unit where k is long: 16,384 x 4,096 by k = 4,096 (pairs) 284 us, 1.94 PFLOP/s, its pipe active
+// 81 to 87% of the time.  By what L2 hands to the SMs (48 KB a block of k and tile) and the epilogue's bytes where k is
+// short: 65,536 x 512 by 416, relu and pre 41 us, 189 MB of them to HBM at 4.6 TB/s.  By the weight's bytes where rows are few: one
+// row by a weight of 4,096 x 4,096 8.3 us, 4.0 TB/s.
+//
 // A_MN, B_MN: the operand's rows run along i (j), not k.  SWAP: i runs along
 // the output's columns (few rows: the weight is the operand of 128 rows a tile).
 // PAIR: two blocks on neighbouring SMs share a tile of 256 rows.  Each holds its
@@ -473,7 +482,10 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR>::kThreads, 1)
     if (PAIR) cluster_sync();
     tc_fence_after();
     const uint32_t tmem = tmem_at;
-    pdl_enter();
+    // Beside the product before it: by the time this is placed, that one's blocks have all seen what is before it
+    // complete, and this reads by TMA alone (L1 holds nothing of it).
+    if (p.beside) pdl_next();
+    else pdl_enter();
 
     // joined shares: one tile a block, its share by its place in the cluster
     const int tiles = p.tiles_i * p.tiles_j, mine = joined ? (int)cluster_rank() : 0;
@@ -595,6 +607,7 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR>::kThreads, 1)
     tc_fence_after();
     if (threadIdx.x == 0 && stop) atomicMax(&g_status, (uint32_t)MLKV_ERR_TIMEOUT);
     if (warp == kMma) tmem_free<PAIR>(tmem, R::kColumns);
+    if (p.beside) pdl_enter_last();  // whoever waits for this grid waits for those before it
 }
 
 // The shares of the tiles that are not whole, added up in a fixed order, and the epilogue: four columns a thread, or,
@@ -628,6 +641,7 @@ __global__ void __launch_bounds__(256) k_product_finish(const Product p, int blo
 }
 
 // Rows whose stride or place TMA does not take (multiples of 16 bytes), laid out anew: up to two matrices at a time.
+// Bound by latency at the sizes met (4,099 x 777 and 1,001 x 777: 6 us, 16 MB), by HBM above.
 struct Align {
     const uint16_t* in;
     uint16_t* out;
@@ -734,7 +748,8 @@ __global__ void __launch_bounds__(256, ALIGNED ? kSlopeBlocks : 2) k_slope(Slope
     else static_cast<T*>(a.dbias)[col] = from_float<T>(t);
 }
 
-// The shares' sums of 32 columns, added up by 32 warps of which each takes every 32nd share, then over the warps.
+// The shares' sums of 32 columns, added up by 32 warps of which each takes every 32nd share, then over the warps (608
+// shares of 512 columns: 6 us with the launch, from L2).
 __global__ void __launch_bounds__(1024) k_column_sums(const float* __restrict__ part, int shares, int64_t cols, void* out, int32_t type) {
     pdl_enter();
     __shared__ float s[32][33];
@@ -923,10 +938,19 @@ struct Caller {
         return best;
     }
 
+    // What a product leaves to another launch: shares to be added up.
+    struct Rest {
+        Product p;
+        int high, bn;
+    };
+    void finish(const Rest& r) {
+        if (r.p.part) finish_shares(r.p, r.high, r.bn);
+    }
+
     // out = epilogue(A B^T): A [rows][k], B [cols][k]; *_mn: held as [k][rows], [k][cols].
     template <bool A_MN, bool B_MN>
-    void product(Matrix a, Matrix b, int64_t rows, int64_t cols, int64_t k, Epilogue e) {
-        if (!rows || !cols) return;
+    Rest product(Matrix a, Matrix b, int64_t rows, int64_t cols, int64_t k, Epilogue e, bool beside = false) {
+        if (!rows || !cols) return {};
         e.type = type;
         auto wide = [](const void* p, int64_t stride) { return !p || (reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 8 == 0); };
         e.wide = wide(e.out, e.out_stride) && wide(e.pre, e.pre_stride) && wide(e.residual, e.residual_stride);
@@ -947,7 +971,7 @@ struct Caller {
         const int64_t across = (p.J + bn - 1) / bn, high = pair ? 2 * kBM : kBM, tiles = ((int64_t)p.I + high - 1) / high * across;
         if (tiles >= (int64_t)1 << 30) {
             rc = MLKV_ERR_UNSUPPORTED;
-            return;
+            return {};
         }
         p.tiles_i = (int32_t)(tiles / across);
         p.tiles_j = (int32_t)across;
@@ -956,7 +980,7 @@ struct Caller {
         if (k == 0) {
             p.whole = p.shares = 0;
             finish_shares(p, (int)high, bn);
-            return;
+            return {};
         }
         if (swap) {
             // few rows: k in shares of at least 4 blocks, those of a tile a cluster (of 2, 4 or 8), one tile a block
@@ -974,7 +998,9 @@ struct Caller {
                 p.part = static_cast<float*>(arena.take(s.tiles * p.shares * high * bn * 4));
             }
         }
-        if (!run) return;
+        p.beside = beside;
+        const Rest rest = {p, (int)high, bn};
+        if (!run) return rest;
         if constexpr (!A_MN) {
             if (swap) {
                 if (bn == 16) launch<16, B_MN, false, true>(b, a, p);
@@ -988,7 +1014,7 @@ struct Caller {
             else if (pair) launch<256, A_MN, B_MN, false, true>(a, b, p);
             else launch<256, A_MN, B_MN, false>(a, b, p);
         }
-        if (p.part) finish_shares(p, (int)high, bn);
+        return rest;
     }
 
     void forward(const mlkv_linear_args& g) {
@@ -997,7 +1023,7 @@ struct Caller {
         e.pre = g.d_pre; e.pre_stride = g.pre_stride; e.out = g.d_y; e.out_stride = g.y_stride; e.act = g.activation;
         Matrix x = {(const uint16_t*)g.d_x, g.x_stride, g.m, g.k}, w = {(const uint16_t*)g.d_weight, g.weight_stride, g.n, g.k};
         if (g.m && g.n && g.k) align(x, w);
-        product<false, false>(x, w, g.m, g.n, g.k, e);
+        finish(product<false, false>(x, w, g.m, g.n, g.k, e));
     }
 
     void backward(const mlkv_linear_args& g) {
@@ -1041,14 +1067,19 @@ struct Caller {
         Epilogue e = {};
         Matrix x = {(const uint16_t*)g.d_x, g.x_stride, g.m, g.k}, w = {(const uint16_t*)g.d_weight, g.weight_stride, g.n, g.k}, none = {};
         if (g.m && g.n && g.k) align(g.d_dweight ? x : none, g.d_dx ? w : none);
+        // dW's blocks take the SMs that dx has no work for, at its start or as its last tiles run out.  (A step of 300 x 520
+        // to 1,000: 21.3 us on the GPU, one after the other 25.2; of 16,384 x 4,096 to 4,096 1,106, 1,135.)
+        Rest dx = {}, dw = {};
         if (g.d_dx) {
             e.out = g.d_dx; e.out_stride = g.dx_stride;
-            product<false, true>(p, w, g.m, g.k, g.n, e);
+            dx = product<false, true>(p, w, g.m, g.k, g.n, e);
         }
         if (g.d_dweight) {
             e.out = g.d_dweight; e.out_stride = g.dweight_stride;
-            product<true, true>(p, x, g.n, g.k, g.m, e);
+            dw = product<true, true>(p, x, g.n, g.k, g.m, e, rc == MLKV_OK && g.d_dx && g.m && g.n && g.k);
         }
+        finish(dx);
+        finish(dw);
     }
 };
 

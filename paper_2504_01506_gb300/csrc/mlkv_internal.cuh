@@ -463,6 +463,9 @@ __device__ __forceinline__ void pdl_enter() {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     if (!MLKV_PDL_TRIGGER_FIRST) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
+// pdl_next is the second alone, for a kernel that runs beside the one before it;
+// it ends with pdl_enter_last(), so that its completion too implies theirs.
+__device__ __forceinline__ void pdl_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void pdl_enter_last() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 // Whether the miss kernel is placed late behind a Get, or behind a probe, of n
