@@ -6,17 +6,23 @@ No fast-math: every floating-point operation of the store's kernels is an
 explicitly rounded intrinsic, and --fmad=false keeps the compiler from
 contracting any other.  The dense operators are held to a tolerance, not to an
 order of operations, and may contract.
+
+Beside it _dense_calls.so, by g++: the dense operators' calls from Python
+(csrc/dense_calls.cpp), against the installed torch.
 """
 import concurrent.futures as cf
+import importlib.util
 import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libmlkv_gb300.so")
+CALLS = os.path.join(HERE, "_dense_calls.so")
 BUILD = os.path.join(ROOT, "_build")
 SOURCES = ["mlkv_index.cu", "mlkv_sort.cu", "mlkv_apply.cu", "mlkv_plan.cu", "mlkv_table.cu", "mlkv_tier.cu", "mlkv_static.cu"]
 DENSE = ["dense_norm.cu", "dense_norm_backward.cu", "dense_linear.cu", "dense_logprobs.cu"]
@@ -40,10 +46,27 @@ def _deps():
 
 
 def up_to_date() -> bool:
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not os.path.exists(CALLS):
         return False
-    t = os.path.getmtime(LIB)
+    t = min(os.path.getmtime(LIB), os.path.getmtime(CALLS))
     return all(os.path.getmtime(f) <= t for f in _deps())
+
+
+def build_calls() -> str:
+    """The extension module of the dense operators' calls."""
+    torch = importlib.util.find_spec("torch").submodule_search_locations[0]
+    cuda = os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(nvcc()))), "include")
+    include = [os.path.join(ROOT, "include"), sysconfig.get_paths()["include"], os.path.join(torch, "include"),
+               os.path.join(torch, "include", "torch", "csrc", "api", "include"), cuda]
+    tmp = CALLS + f".tmp{os.getpid()}"
+    cmd = [shutil.which("g++") or "g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden", *(f"-I{d}" for d in include),
+           os.path.join(CSRC, "dense_calls.cpp"), "-o", tmp, f"-L{os.path.join(torch, 'lib')}",
+           *(f"-l{n}" for n in ("torch_python", "torch", "torch_cpu", "torch_cuda", "c10", "c10_cuda"))]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"g++ failed on dense_calls.cpp:\n{r.stderr}")
+    os.replace(tmp, CALLS)
+    return CALLS
 
 
 def build(force: bool = False, verbose: bool = False, extra=()) -> str:
@@ -67,8 +90,10 @@ def build(force: bool = False, verbose: bool = False, extra=()) -> str:
             sys.stderr.write(r.stderr)
         return obj
 
-    with cf.ThreadPoolExecutor(max_workers=len(SOURCES) + len(DENSE)) as ex:
+    with cf.ThreadPoolExecutor(max_workers=len(SOURCES) + len(DENSE) + 1) as ex:
+        calls = ex.submit(build_calls)
         objs = list(ex.map(compile_one, [*DENSE, *SOURCES]))
+        calls.result()
     tmp = LIB + f".tmp{os.getpid()}"
     r = subprocess.run([cc, *ARCH, "-shared", "-o", tmp, *objs], capture_output=True, text=True)
     if r.returncode != 0:

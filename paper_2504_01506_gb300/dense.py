@@ -15,7 +15,9 @@ Matrices are 2-d CUDA tensors of torch.float32, torch.bfloat16 or torch.float16
 contiguous, or overlap, is copied first.  Every call is enqueued on the current
 torch stream of its first tensor's device and runs in the CUDA library; working
 memory comes from torch's allocator for the length of the call.  This module
-only checks arguments (TypeError, ValueError) and passes pointers.  Formulas and
+only checks arguments (TypeError, ValueError) and passes pointers; where nothing
+is wrong with them and nothing has to be copied, _dense_calls does (csrc/dense_calls.cpp:
+the host's part of a call is what a small one takes).  Formulas and
 the treatment of masked and invalid values: include/mlkv_dense.h.
 """
 import typing
@@ -38,6 +40,32 @@ class TokenLogprobs(typing.NamedTuple):
     stats: torch.Tensor
     top_logprobs: torch.Tensor | None
     top_ids: torch.Tensor | None
+
+
+_calls = None
+
+
+def _native(x):
+    """The calls for arguments as the library takes them, where x is a CUDA tensor."""
+    global _calls
+    if not getattr(x, "is_cuda", False):
+        return None
+    if _calls is None:
+        lib = L.load()
+        try:
+            from . import _dense_calls
+        except ImportError as e:
+            raise ImportError(f"the dense operators' calls are missing: build them with __graft_entry__.build() ({e})") from None
+        _dense_calls.bind(lib._name)
+        _calls = _dense_calls
+    return _calls
+
+
+def _done(result):
+    """What a call of _native's gave, or the error that it tells."""
+    if type(result) is int:
+        raise MLKVError(result, L.load().mlkv_status_string(result).decode())
+    return result
 
 
 _current_device = torch.cuda.current_device
@@ -122,6 +150,10 @@ def layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.
     out_dtype (x's; any type where x is fp32).  weight and bias: [dim], of one type.
     With save_stats also the rows' (mean, 1 / sqrt(var + eps)), fp32 [rows, 2], for
     layer_norm_backward."""
+    if (native := _native(x)) is not None:
+        r = native.layer_norm(x, weight, bias, eps, -1 if out_dtype is None else _TYPES.get(out_dtype, -2), save_stats)
+        if r is not NotImplemented:
+            return _done(r)
     x, rows, dim, stride = _rows(x, "x")
     _on_gpu(x, "x")
     dtype, device = x.dtype, x.device
@@ -149,6 +181,10 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor 
     """Gradients (dx of x's type, dweight, dbias of the weight's type or fp32) of a
     layer_norm whose save_stats gave `stats`; dweight is None without a weight, dbias
     with bias=False."""
+    if (native := _native(x)) is not None:
+        r = native.layer_norm_backward(dy, x, weight, stats, bias)
+        if r is not NotImplemented:
+            return _done(r)
     x, rows, dim, stride = _rows(x, "x")
     _on_gpu(x, "x")
     dtype, device = x.dtype, x.device
@@ -208,6 +244,10 @@ def linear(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None = No
     [m, n], all of x's type; activation: "none", "relu", "gelu_tanh" or "silu".  With
     save_pre also the value before the activation, [m, n], for linear_backward (None
     without an activation, whose gradient does not need it)."""
+    if (native := _native(x)) is not None:
+        r = native.linear(x, weight, bias, _ACTIVATIONS.get(activation, -1), residual, save_pre)
+        if r is not NotImplemented:
+            return _done(r)
     x, weight, dtype, device, m, n, k, act, a = _linear_args(x, weight, activation)
     if bias is not None:
         bias = _vector(bias, "bias", n, device, (dtype,))
@@ -231,6 +271,10 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, pre
     """Gradients (dx, dweight, dbias) of linear(x, weight, bias, activation=...), all of
     x's type; dbias is None without `bias`, the others where they are not wanted.  pre:
     what save_pre gave (needed with an activation).  The residual's gradient is dy."""
+    if (native := _native(x)) is not None:
+        r = native.linear_backward(dy, x, weight, pre, _ACTIVATIONS.get(activation, -1), bias, want_dx, want_dweight)
+        if r is not NotImplemented:
+            return _done(r)
     x, weight, dtype, device, m, n, k, act, a = _linear_args(x, weight, activation)
     dy, _, _, a.dy_stride = _rows(dy, "dy", (dtype,), (m, n), device)
     a.d_dy = dy.data_ptr()
@@ -277,6 +321,10 @@ def token_logprobs(logits: torch.Tensor, targets: torch.Tensor, *, top: int = 0,
     """Of every row of softmax(scale * logits) ([n, vocab]): the log probability of
     targets[i] (int64 [n]; negative: none, log probability 0), the entropy, and the
     `top` (at most 32) likeliest tokens, ties by the lowest index.  -inf masks a token."""
+    if (native := _native(logits)) is not None:
+        r = native.token_logprobs(logits, targets, top, scale)
+        if r is not NotImplemented:
+            return TokenLogprobs(*_done(r))
     logits, n, vocab, stride, device, targets = _logits(logits, targets, scale)
     if not 0 <= top <= L.MAX_TOP:
         raise ValueError(f"top must be 0 to {L.MAX_TOP}, not {top}")
@@ -304,6 +352,10 @@ def token_logprobs_backward(logits: torch.Tensor, targets: torch.Tensor, result:
     """The gradient of the logits, of their type, from those of the log probabilities
     and entropies (fp32 [n]; None: 0) that token_logprobs of the same arguments gave in
     `result`.  in_place: written over the logits."""
+    if (native := _native(logits)) is not None:
+        r = native.token_logprobs_backward(logits, targets, result.entropy, result.stats, dlogprob, dentropy, scale, in_place)
+        if r is not NotImplemented:
+            return _done(r)
     given = logits
     logits, n, vocab, stride, device, targets = _logits(logits, targets, scale)
     f32 = (torch.float32,)
