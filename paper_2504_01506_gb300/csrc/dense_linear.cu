@@ -295,8 +295,19 @@ __device__ __forceinline__ void doubtful(const Product& p, float2 (&v)[16], int 
         if (c == 32 || col >= p.J) continue;
         const T *a = static_cast<const T*>(p.a) + (r0 + from) * p.a_stride, *b = static_cast<const T*>(p.b) + col * p.b_stride;
         double sum = 0;
-#pragma unroll 8
-        for (int k = lane; k < p.k; k += 32) sum += (double)to_float(a[k]) * (double)to_float(b[k]);
+#pragma unroll 4
+        for (int k = lane * 8; k + 8 <= p.k; k += 256) {  // (rows that TMA takes: on 16 bytes)
+            const uint4 x = *reinterpret_cast<const uint4*>(a + k), y = *reinterpret_cast<const uint4*>(b + k);
+            auto add = [&](uint32_t u, uint32_t w) {
+                const float2 m = mul2(pair_of_word<T>(u), pair_of_word<T>(w));  // (exact)
+                sum += (double)m.x + (double)m.y;
+            };
+            add(x.x, y.x);
+            add(x.y, y.y);
+            add(x.z, y.z);
+            add(x.w, y.w);
+        }
+        if (lane < (p.k & 7)) sum += (double)to_float(a[(p.k & ~7) + lane]) * (double)to_float(b[(p.k & ~7) + lane]);
 #pragma unroll
         for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
         if (p.e.bias) sum += (double)to_float(static_cast<const T*>(p.e.bias)[col]);
@@ -750,19 +761,22 @@ __global__ void __launch_bounds__(256, ALIGNED ? kSlopeBlocks : 2) k_slope(Slope
 
 // The shares' sums of 32 columns, added up by 32 warps of which each takes every 32nd share, then over the warps (608
 // shares of 512 columns: 6 us with the launch, from L2).
-__global__ void __launch_bounds__(1024) k_column_sums(const float* __restrict__ part, int shares, int64_t cols, void* out, int32_t type) {
-    pdl_enter();
+// beside: as in k_product (the shares are complete, and read from L2).
+__global__ void __launch_bounds__(1024) k_column_sums(const float* part, int shares, int64_t cols, void* out, int32_t type, int beside) {
+    if (beside) pdl_next();
+    else pdl_enter();
     __shared__ float s[32][33];
     const int64_t c = blockIdx.x * 32ll + (threadIdx.x & 31);
     const int w = threadIdx.x >> 5;
     float t = 0.f;
     if (c < cols)
-        for (int b = w; b < shares; b += 32) t += part[b * cols + c];
+        for (int b = w; b < shares; b += 32) t += __ldcg(part + b * cols + c);
     s[w][threadIdx.x & 31] = t;
     __syncthreads();
     t = group_sum(s[threadIdx.x & 31][w], 32);  // warp w: column w of the block's
     const int64_t o = blockIdx.x * 32ll + w;
     if ((threadIdx.x & 31) == 0 && o < cols) static_cast<uint16_t*>(out)[o] = narrow(type, t);
+    if (beside) pdl_enter_last();
 }
 
 // --- host ----------------------------------------------------------------------
@@ -1030,6 +1044,8 @@ struct Caller {
         Matrix p = {(const uint16_t*)g.d_dy, g.dy_stride, g.m, g.n};
         const bool act = g.activation != MLKV_ACT_NONE, products = (g.d_dx || g.d_dweight) && g.m && g.n;
         const bool copy = products && (act || !p.aligned());
+        const float* part = nullptr;  // of dbias, from `shares` blocks
+        int shares = 0;
         if (g.m && g.n && (copy || g.d_dbias)) {
             Slope s = {};
             s.dy = p.p; s.dy_stride = g.dy_stride; s.pre = g.d_pre; s.pre_stride = g.pre_stride;
@@ -1044,8 +1060,8 @@ struct Caller {
             const int64_t across = (g.n + 255) / 256;
             // a block's warps take 4 rows each at least; up to 1,024 rows no column has more blocks than a cluster
             const int64_t most = g.d_dbias && g.m <= 1024 ? 8 : (int64_t)kSlopeBlocks * sms / across;
-            const int64_t shares = std::max<int64_t>(1, std::min<int64_t>((g.m + 31) / 32, most));
-            s.share = (g.m + shares - 1) / shares;
+            const int64_t wanted = std::max<int64_t>(1, std::min<int64_t>((g.m + 31) / 32, most));
+            s.share = (g.m + wanted - 1) / wanted;
             const unsigned down = (unsigned)((g.m + s.share - 1) / s.share);
             s.joined = g.d_dbias && down > 1 && down <= 8;
             if (g.d_dbias && down > 8) s.part = static_cast<float*>(arena.take((int64_t)down * g.n * 4));
@@ -1058,8 +1074,8 @@ struct Caller {
                 const bool b = type == MLKV_TYPE_BFLOAT;
                 if (whole) go(b ? k_slope<__nv_bfloat16, true> : k_slope<__half, true>);
                 else go(b ? k_slope<__nv_bfloat16, false> : k_slope<__half, false>);
-                if (s.part) launch_kernel(true, k_column_sums, dim3((unsigned)((g.n + 31) / 32)), dim3(1024), 0, st,
-                                          (const float*)s.part, (int)down, g.n, g.d_dbias, type);
+                part = s.part;
+                shares = (int)down;
             }
         } else if (run && g.d_dbias && g.n) {
             if (cudaMemsetAsync(g.d_dbias, 0, g.n * 2, st) != cudaSuccess) rc = MLKV_ERR_CUDA;
@@ -1067,16 +1083,18 @@ struct Caller {
         Epilogue e = {};
         Matrix x = {(const uint16_t*)g.d_x, g.x_stride, g.m, g.k}, w = {(const uint16_t*)g.d_weight, g.weight_stride, g.n, g.k}, none = {};
         if (g.m && g.n && g.k) align(g.d_dweight ? x : none, g.d_dx ? w : none);
-        // dW's blocks take the SMs that dx has no work for, at its start or as its last tiles run out.  (A step of 300 x 520
+        // The bias's sums and dW's blocks take the SMs that dx has no work for, at its start or as its last tiles run out.  (A step of 300 x 520
         // to 1,000: 21.3 us on the GPU, one after the other 25.2; of 16,384 x 4,096 to 4,096 1,106, 1,135.)
         Rest dx = {}, dw = {};
         if (g.d_dx) {
             e.out = g.d_dx; e.out_stride = g.dx_stride;
             dx = product<false, true>(p, w, g.m, g.k, g.n, e);
         }
+        const bool beside = rc == MLKV_OK && g.d_dx && g.m && g.n && g.k;
+        if (part) launch_kernel(true, k_column_sums, dim3((unsigned)((g.n + 31) / 32)), dim3(1024), 0, st, part, shares, g.n, g.d_dbias, type, (int)beside);
         if (g.d_dweight) {
             e.out = g.d_dweight; e.out_stride = g.dweight_stride;
-            dw = product<true, true>(p, x, g.n, g.k, g.m, e, rc == MLKV_OK && g.d_dx && g.m && g.n && g.k);
+            dw = product<true, true>(p, x, g.n, g.k, g.m, e, beside);
         }
         finish(dx);
         finish(dw);
