@@ -25,7 +25,7 @@
 // reaches the last bar.  The bar is raised after 1, 3, 5, 9, 17 ... batches, by one
 // warp and without a barrier but for the first time.
 //
-// 8,192 x 131,072 bf16 values with 20 alternatives: 405 us (5.3 TB/s; 17
+// 8,192 x 131,072 bf16 values with 20 alternatives: 398 us (5.4 TB/s; 17
 // instructions a value), 2,048 rows without 86 (6.3; 9.5); one such row, 8 spans of a
 // cluster, 11 us (latency: a stream of 8 batches, a sort of what was listed).  515
 // x 50,001 fp32, 5 alternatives: 29 us.
@@ -695,10 +695,18 @@ bool pieces_aligned(const void* p, int64_t stride, int size) {
 // time as hold 1,024 threads an SM; the spans are what makes the last of these
 // waves end soonest, a block costing about 1,700 pieces beside its own (2.4 us
 // of latencies at 1.4 ns a piece).
+// Threads a block: as few as give a thread no more than 16 pieces, or, where rows
+// are many, as few as still make 4 waves: what a block does besides streaming
+// (its first loads, the sums over it, the alternatives' sort) is then done by fewer
+// warps, beside more blocks that stream.  (At most 8 to 16 pieces a thread / this,
+// us: 16,384 x 15,000 fp16 91 / 81; 15,000 x 8,000 bf16, 5 alternatives, 104 / 82;
+// 16,384 x 50,000 bf16 263 / 233; 8,192 x 50,000, 20 alternatives, 233 / 193; 3 waves
+// instead: 8,192 x 131,072, 20 alternatives, 497, 398 with 4.)
+constexpr int64_t kWaves = 4;
 Split spans_of(int64_t n, int64_t pieces, int sms) {
     int threads = kMostThreads;
     for (int t = 32; t < kMostThreads; t *= 2)
-        if (pieces <= (int64_t)t * (t < 128 ? 8 : 16)) {
+        if (pieces <= (int64_t)t * 16 || (n >= kWaves * sms * (1024 / t) && pieces <= (int64_t)t * 256)) {
             threads = t;
             break;
         }
