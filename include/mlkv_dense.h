@@ -88,7 +88,9 @@ int mlkv_layer_norm_backward(const void* d_dy, int64_t dy_stride, int32_t dy_typ
  * not null, an input of the backward pass with an activation (null without).
  * dy: [m][n]; dx: [m][k]; dweight: [n][k]; dbias: [n]; each of the three may be
  * null (not wanted).  m, n, k >= 0, each < 2^30; k == 0 gives z = bias, m == 0
- * gives zero dweight and dbias.  p is rounded to `type` where act is not NONE. */
+ * gives zero dweight and dbias.  p is rounded to `type` where act is not NONE.
+ * With MLKV_ACT_RELU, whose slope jumps there, sums next to 0 are computed again
+ * in 64 bits (of more than 64 rows, where a tile's k is not shared out). */
 typedef struct mlkv_linear_args {
     int64_t m, n, k;
     const void* d_x;

@@ -281,22 +281,24 @@ PyObject* bind(PyObject*, PyObject* path) {
     const char* p = PyUnicode_AsUTF8(path);
     if (!p) return nullptr;
     void* h = dlopen(p, RTLD_NOW | RTLD_LOCAL);
+    Library found = {};
     bool ok = h != nullptr;
     auto get = [&](auto& f, const char* name) {
         f = h ? reinterpret_cast<std::remove_reference_t<decltype(f)>>(dlsym(h, name)) : nullptr;
         ok = ok && f;
     };
-    get(lib.layer_norm, "mlkv_layer_norm");
-    get(lib.layer_norm_backward, "mlkv_layer_norm_backward");
-    get(lib.layer_norm_backward_workspace, "mlkv_layer_norm_backward_workspace");
-    get(lib.linear, "mlkv_linear");
-    get(lib.linear_workspace, "mlkv_linear_workspace");
-    get(lib.linear_backward, "mlkv_linear_backward");
-    get(lib.linear_backward_workspace, "mlkv_linear_backward_workspace");
-    get(lib.token_logprobs, "mlkv_token_logprobs");
-    get(lib.token_logprobs_workspace, "mlkv_token_logprobs_workspace");
-    get(lib.token_logprobs_backward, "mlkv_token_logprobs_backward");
+    get(found.layer_norm, "mlkv_layer_norm");
+    get(found.layer_norm_backward, "mlkv_layer_norm_backward");
+    get(found.layer_norm_backward_workspace, "mlkv_layer_norm_backward_workspace");
+    get(found.linear, "mlkv_linear");
+    get(found.linear_workspace, "mlkv_linear_workspace");
+    get(found.linear_backward, "mlkv_linear_backward");
+    get(found.linear_backward_workspace, "mlkv_linear_backward_workspace");
+    get(found.token_logprobs, "mlkv_token_logprobs");
+    get(found.token_logprobs_workspace, "mlkv_token_logprobs_workspace");
+    get(found.token_logprobs_backward, "mlkv_token_logprobs_backward");
     if (!ok) return PyErr_Format(PyExc_ImportError, "%s: not the library of these calls", p);
+    lib = found;
     Py_RETURN_NONE;
 }
 

@@ -1090,7 +1090,7 @@ struct Caller {
             e.out = g.d_dx; e.out_stride = g.dx_stride;
             dx = product<false, true>(p, w, g.m, g.k, g.n, e);
         }
-        const bool beside = rc == MLKV_OK && g.d_dx && g.m && g.n && g.k;
+        const bool beside = !MLKV_PDL_TRIGGER_FIRST && rc == MLKV_OK && g.d_dx && g.m && g.n && g.k;  // (dx's blocks have waited first)
         if (part) launch_kernel(true, k_column_sums, dim3((unsigned)((g.n + 31) / 32)), dim3(1024), 0, st, part, shares, g.n, g.d_dbias, type, (int)beside);
         if (g.d_dweight) {
             e.out = g.d_dweight; e.out_stride = g.dweight_stride;
