@@ -271,20 +271,22 @@ struct Ahead {
 // relu's slope jumps at 0, where the matrix unit's rounding (about 2^-24 of the
 // sums on the way, every 16 values of k) decides it at random: one such value moves
 // a whole row of dx.  So of a lane's 32 values the smallest, where it is that near
-// 0, is computed again by the warp, in 64 bits.  (65,536 x 416 by 512: about 45 of
+// 0, is computed again by the warp, in 64 bits.  (65,536 x 416 by 512: about 90 of
 // 33.5 million.  Of sums that go out as shares, or of 64 rows or fewer, it is not:
-// they are a few million at the most.)
+// they are a few million at the most.  A column alone in its block of 32 has none
+// to be small beside, and stays as it is.)
 template <class T>
 __device__ __forceinline__ void doubtful(const Product& p, float2 (&v)[16], int r0, int c0, int lane) {
+    const int columns = p.J - c0;  // (the sums past the last are 0)
     float least = INFINITY, most = 0.f;
 #pragma unroll
     for (int k = 0; k < 16; ++k) {
-        least = fminf(least, fminf(fabsf(v[k].x), fabsf(v[k].y)));
+        least = fminf(least, fminf(2 * k < columns ? fabsf(v[k].x) : INFINITY, 2 * k + 1 < columns ? fabsf(v[k].y) : INFINITY));
         most = fmaxf(most, fmaxf(fabsf(v[k].x), fabsf(v[k].y)));
     }
     uint32_t again = __ballot_sync(0xffffffffu, r0 + lane < p.I && least < most * p.doubt && most < 1e30f);
     if (!again) return;
-    int at = 32;  // this lane's smallest
+    int at = 32;  // this lane's smallest (the first one)
 #pragma unroll
     for (int k = 15; k >= 0; --k) {
         if (fabsf(v[k].y) == least) at = 2 * k + 1;
@@ -292,7 +294,7 @@ __device__ __forceinline__ void doubtful(const Product& p, float2 (&v)[16], int 
     }
     for (; again; again &= again - 1) {
         const int from = __ffs(again) - 1, c = __shfl_sync(0xffffffffu, at, from), col = c0 + c;
-        if (c == 32 || col >= p.J) continue;
+        if (c == 32) continue;
         const T *a = static_cast<const T*>(p.a) + (r0 + from) * p.a_stride, *b = static_cast<const T*>(p.b) + col * p.b_stride;
         double sum = 0;
 #pragma unroll 4
@@ -977,7 +979,7 @@ struct Caller {
         if (!A_MN && !B_MN && !swap && e.act == MLKV_ACT_RELU) {
             p.a = a.p; p.a_stride = a.stride; p.b = b.p; p.b_stride = b.stride;
             p.k = (int32_t)k;
-            p.doubt = (float)p.blocks / (1 << 23);
+            p.doubt = (float)p.blocks / (1 << 22);
         }
         const int64_t down = ((int64_t)p.I + kBM - 1) / kBM;
         const bool pair = !swap && cols > 128 && pair_pays(down, (p.J + 255) / 256, p.blocks);

@@ -13,7 +13,6 @@
 namespace mlkv {
 
 constexpr int64_t kNormMaxDim = (int64_t)1 << 20;
-constexpr int kNormLanes = 512;       // most lanes of a team
 constexpr int kNormLongLanes = 1024;  // lanes of the kernels of rows too long for registers
 
 struct NormArgs {

@@ -204,3 +204,26 @@ def test_relu_near_zero(dtype):
     for column in (5, 37, 95):
         assert torch.equal(pre[:, column].double(), exact[:, column])
         assert torch.equal(y[:, column].double(), exact[:, column].clamp(min=0))
+
+
+@pytest.mark.parametrize("n", [77, 256, 300])
+def test_relu_near_zero_at_the_last_columns(n):
+    """The same where the last block of columns is not whole, and with a bias."""
+    torch = torch_cuda()
+    from paper_2504_01506_gb300 import dense
+
+    gen = torch.Generator("cuda")
+    gen.manual_seed(n)
+    m, half, dtype = 200, 128, torch.bfloat16
+    u, w = _matrix(torch, m, half, dtype, gen), _matrix(torch, n, half, dtype, gen, 0.08)
+    bias = _matrix(torch, 1, n, dtype, gen, 0.5)[0]
+    sign = torch.where(torch.rand((m, 1), generator=gen, device="cuda") < 0.5, -1.0, 1.0)
+    x = torch.cat([u, u, (sign * 2.0 ** -21).to(dtype), torch.ones((m, 1), dtype=dtype, device="cuda")], 1)
+    weight = torch.cat([w, w, torch.zeros((n, 2), dtype=dtype, device="cuda")], 1)
+    weight[n - 1, half:2 * half] = -w[n - 1]
+    weight[n - 1, 2 * half] = 1
+    weight[n - 1, 2 * half + 1] = -bias[n - 1]
+    y, pre = dense.linear(x, weight, bias, activation="relu", save_pre=True)
+    exact = sign[:, 0].double() * 2.0 ** -21
+    assert torch.equal(pre[:, n - 1].double(), exact)
+    assert torch.equal(y[:, n - 1].double(), exact.clamp(min=0))
