@@ -219,20 +219,22 @@ __device__ __forceinline__ Key best_of(const Key* keys, int count, int lane) {
     return best;
 }
 // Leaves the `top` best of list[0 .. count) in list[0 .. top), in order, 0 where
-// there are fewer (the block; keys are distinct).  Each warp cuts its share of a
-// long list to 32; what is left is placed by counting the better ones.
+// there are fewer (the block, whose threads may just have written the list; keys
+// are distinct).  Each warp cuts its share of a long list to 32; what is left is
+// placed by counting the better ones.
 template <int THREADS>
 __device__ __noinline__ void select(Key* list, int count, int top) {
     constexpr int kWarps = THREADS / 32;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    __syncthreads();
     if (count > THREADS) {
         const int share = (count + kWarps - 1) / kWarps, from = warp * share;
         const Key k = best_of(list + from, max(0, min(share, count - from)), lane);
         __syncthreads();
         list[threadIdx.x] = k;
         count = THREADS;
+        __syncthreads();
     }
-    __syncthreads();
     const Key mine = (int)threadIdx.x < count ? list[threadIdx.x] : 0;
     int rank = 0;
 #pragma unroll 4

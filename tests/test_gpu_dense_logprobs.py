@@ -66,6 +66,26 @@ def test_alternatives(n, v, top):
     _check(torch, x, t, top, scale=1.25)
 
 
+@pytest.mark.parametrize("n", [1, 9, 148])
+@pytest.mark.parametrize("v,dtype", [(6144, "bf16"), (8192, "fp16"), (12000, "bf16"), (16384, "bf16"), (4100, "fp32"), (8192, "fp32")])
+def test_alternatives_of_spans_joined_by_few_threads(v, dtype, n):
+    """A row's spans have more alternatives between them than the block that joins them has threads: all of them are
+    there before any is looked at, call after call (two inputs in turn, so that what is left of one would show in the other)."""
+    torch = torch_cuda()
+    from paper_2504_01506_gb300 import dense
+
+    inputs = [_logits(torch, n, v, _t(dtype), seed=s) for s in (21, 22)]
+    for top in (20, 32):
+        wants = [R.alternatives(x, top) for x, _ in inputs]
+        wrong = torch.zeros((), dtype=torch.int64, device="cuda")
+        for _ in range(100):
+            for (x, t), want in zip(inputs, wants):
+                wrong += (dense.token_logprobs(x, t, top=top).top_ids != want).sum()
+        assert int(wrong) == 0
+        for x, t in inputs:
+            _check(torch, x, t, top)
+
+
 @pytest.mark.parametrize("pad,skip", [(1, 0), (1, 1), (3, 2), (8, 8), (5, 3)])
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 def test_strides_and_alignment(pad, skip, dtype):
