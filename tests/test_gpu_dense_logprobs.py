@@ -120,6 +120,32 @@ def test_masks(v, dtype):
             _check(torch, x, t, 20)
 
 
+@pytest.mark.parametrize("n,v,dtype", [(700, 131072, "bf16"), (2, 600001, "bf16"), (200, 40000, "fp32"), (305, 60000, "fp16")])
+def test_spans_that_a_second_kernel_joins(n, v, dtype):
+    """Rows in spans that are too many, or too long, for a cluster (the only ones that need working memory)."""
+    torch = torch_cuda()
+    from paper_2504_01506_gb300 import _lib
+
+    lib = _lib.load()
+    kind = {"fp32": _lib.TYPE_FLOAT, "bf16": _lib.TYPE_BFLOAT, "fp16": _lib.TYPE_HALF}[dtype]
+    for top in (0, 20, 32):
+        assert lib.mlkv_token_logprobs_workspace(n, v, kind, top) > 0
+        _check(torch, *_logits(torch, n, v, _t(dtype), seed=top), top, scale=0.8)
+        x, t = _logits(torch, n, v, _t(dtype), seed=top + 1, pad=3, skip=1)
+        ties = torch.arange(v, device="cuda") % 7 < 2
+        rows = [  # one after another of the given, as many as there are
+            lambda r: r.fill_(-math.inf), lambda r: r[: 2 * v // 3].fill_(-math.inf), lambda r: r[v // 2:v // 2 + 1].fill_(math.nan),
+            lambda r: r[5:6].fill_(math.inf), lambda r: r.copy_(ties), lambda r: r[:-3].fill_(-math.inf), lambda r: r.fill_(2.0),
+            lambda r: r[v - 2:].fill_(math.nan)]
+        for at in range(0, len(rows), min(n, len(rows))):
+            y, ty = x.clone(), t.clone()
+            for row, change in zip(y, rows[at:at + n]):
+                change(row)
+            if n > 10:
+                ty[8], ty[9] = -1, v
+            _check(torch, y, ty, top)
+
+
 def test_masked_target():
     torch = torch_cuda()
     x, t = _logits(torch, 4, 500, torch.float32)
