@@ -24,7 +24,8 @@
  *     memory but their arguments.  The stream's device must be current.
  *   - A call that needs working memory has a function that says how many bytes;
  *     the caller gives that much device memory, 256-byte aligned, which the call
- *     uses until it is done on the stream.  (-1: the arguments are not valid.)
+ *     uses until it is done on the stream.  It goes by the device that is current.
+ *     (-1: the arguments are not valid, or there is no device.)
  *   - Errors a host check finds are returned at once (MLKV_ERR_INVALID,
  *     MLKV_ERR_UNSUPPORTED, MLKV_ERR_CUDA) and nothing is enqueued.
  *   - Results do not change from run to run: no sum's order depends on timing.

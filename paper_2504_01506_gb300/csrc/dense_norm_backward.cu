@@ -245,18 +245,38 @@ __global__ void __launch_bounds__(1024) k_norm_cols(const float* __restrict__ pa
     }
 }
 
-// Blocks whose sums of columns are kept apart: as many as run at a time.
-int64_t backward_blocks(int64_t rows, int teams, int sms, int threads) {
-    const int64_t most = (int64_t)sms * (kBackwardLanes / threads);
-    return std::max<int64_t>(1, std::min(most, (rows + teams - 1) / teams));
+// How the rows are dealt out, and the blocks whose sums of columns are kept apart:
+// as many as run at a time, or, of rows too long for registers, shares of the rows
+// that give every SM two blocks of k_norm_cols_long.
+struct BackwardShape {
+    NormShape sh;
+    int threads, teams;
+    int64_t blocks;
+};
+BackwardShape backward_shape(int64_t rows, int64_t dim, int V, int sms) {
+    BackwardShape b;
+    b.sh = norm_shape(rows, dim, V, kBackwardValues, kBackwardLanes, sms);
+    if (b.sh.lanes) {
+        b.threads = norm_team_threads(b.sh.lanes);
+        b.teams = b.threads / b.sh.lanes;
+        b.blocks = std::min<int64_t>((int64_t)sms * (kBackwardLanes / b.threads), (rows + b.teams - 1) / b.teams);
+    } else {
+        b.threads = kNormLongLanes;
+        b.teams = 1;
+        b.blocks = std::min<int64_t>(rows, (2ll * sms * 128 + dim - 1) / dim);
+    }
+    return b;
 }
-constexpr int64_t kMostBlocks = 256 * 8;  // of any device
 
 }  // namespace
 
+// (The type of x, and with it the values of a vector, is not known here: of both, what takes more.)
 extern "C" int64_t mlkv_layer_norm_backward_workspace(int64_t rows, int64_t dim) {
     if (rows < 0 || rows >= (int64_t)1 << 30 || dim < 1 || dim >= kNormMaxDim) return -1;
-    return std::min(kMostBlocks, std::max<int64_t>(rows, 1)) * 2 * dim * (int64_t)sizeof(float);
+    if (rows == 0) return 0;
+    const int sms = dense_sms();
+    if (!sms) return -1;
+    return std::max(backward_shape(rows, dim, 4, sms).blocks, backward_shape(rows, dim, 8, sms).blocks) * 2 * dim * (int64_t)sizeof(float);
 }
 
 extern "C" int mlkv_layer_norm_backward(const void* d_dy, int64_t dy_stride, int32_t dy_type, const void* d_x,
@@ -286,10 +306,10 @@ extern "C" int mlkv_layer_norm_backward(const void* d_dy, int64_t dy_stride, int
     const int V = 16 / xs;
     const bool aligned = norm_aligned(d_x, x_stride, xs, dim, V) && norm_aligned(d_dy, dy_stride, ys, dim, V) &&
                          norm_aligned(d_dx, dx_stride, xs, dim, V);
-    const NormShape sh = norm_shape(rows, dim, V, kBackwardValues, kBackwardLanes, sms);
-    const int threads = sh.lanes ? norm_team_threads(sh.lanes) : kNormLongLanes, teams = sh.lanes ? threads / sh.lanes : 1;
-    int64_t blocks = sh.lanes ? std::min(kMostBlocks, backward_blocks(rows, teams, sms, threads)) : 0;
-    if (!sh.lanes) blocks = std::max<int64_t>(1, std::min<int64_t>(rows, (2 * sms * 128 + dim - 1) / dim));
+    const BackwardShape shape = backward_shape(rows, dim, V, sms);
+    const NormShape& sh = shape.sh;
+    const int threads = shape.threads, teams = shape.teams;
+    const int64_t blocks = shape.blocks;
     const bool parts = want_cols && (blocks > 1 || !sh.lanes);
     if (!workspace_ok(d_workspace, workspace_bytes, parts ? blocks * 2 * dim * (int64_t)sizeof(float) : 0)) return MLKV_ERR_INVALID;
     a.part = parts ? static_cast<float*>(d_workspace) : nullptr;

@@ -183,3 +183,17 @@ def test_more_rows_than_blocks_of_both_passes():
     torch = torch_cuda()
     _run(torch, 60_001, 24, "fp32", "bf16", "fp32")
     _run(torch, 20_011, 333, "fp16", "fp16", "fp16")
+
+
+@pytest.mark.parametrize("rows,dim", [(1, 8), (300, 100), (65536, 2048), (2048, 8192), (5000, 16384), (700, 65536), (12, 2 ** 20 - 1), (10 ** 6, 16384)])
+def test_working_memory_of_the_gradients(rows, dim):
+    """The sums of as many blocks as run at a time (of long rows: of a few columns' shares), not of every row."""
+    torch = torch_cuda()
+    from paper_2504_01506_gb300 import _lib
+
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    most = 3 * sms if dim <= 8192 else max(2 * sms * 128 // dim, rows // 256) + 1
+    assert 0 <= _lib.load().mlkv_layer_norm_backward_workspace(rows, dim) <= min(rows, most) * 2 * dim * 4
+    if rows * dim < 2 ** 28:  # ... and it is enough
+        _run(torch, rows, dim, "bf16", "bf16", "fp32")
+        _run(torch, rows, dim, "fp32", "bf16", "fp32")
