@@ -246,8 +246,12 @@ __global__ void __launch_bounds__(1024) k_norm_cols(const float* __restrict__ pa
 }
 
 // How the rows are dealt out, and the blocks whose sums of columns are kept apart:
-// as many as run at a time, or, of rows too long for registers, shares of the rows
-// that give every SM two blocks of k_norm_cols_long.
+// as many as run at a time, or, of rows too long for registers, shares of at most
+// kLongShare rows, of which a thread adds one after another, that give every SM at
+// least two blocks of k_norm_cols_long.  (Shares by the SMs alone / so, us: 5,000 x
+// 16,384 bf16 809 / 492; 12,000 x 39,040 fp32 5,151 / 2,621; the latter, of one chain
+// of 12,000 additions, with sums off by 1.2e-4.)
+constexpr int64_t kLongShare = 256;
 struct BackwardShape {
     NormShape sh;
     int threads, teams;
@@ -263,7 +267,8 @@ BackwardShape backward_shape(int64_t rows, int64_t dim, int V, int sms) {
     } else {
         b.threads = kNormLongLanes;
         b.teams = 1;
-        b.blocks = std::min<int64_t>(rows, (2ll * sms * 128 + dim - 1) / dim);
+        b.blocks = std::max((rows + kLongShare - 1) / kLongShare, std::min<int64_t>(rows, (2ll * sms * 128 + dim - 1) / dim));
+        b.blocks = std::min<int64_t>(b.blocks, 65535);  // (a grid's y; rows of 280 GB reach about as many)
     }
     return b;
 }

@@ -197,3 +197,23 @@ def test_working_memory_of_the_gradients(rows, dim):
     if rows * dim < 2 ** 28:  # ... and it is enough
         _run(torch, rows, dim, "bf16", "bf16", "fp32")
         _run(torch, rows, dim, "fp32", "bf16", "fp32")
+
+
+@pytest.mark.parametrize("rows,dim", [(12000, 39040), (24000, 9000)])
+def test_column_sums_of_many_long_rows(rows, dim):
+    """No sum is a chain of all the rows: a share's at most 256, then the shares', each warp every 32nd."""
+    torch = torch_cuda()
+    from paper_2504_01506_gb300 import dense
+
+    x = torch.ones(rows, dim, device="cuda")
+    x[:, ::2] = -1  # (mean 0, variance 1)
+    dy = torch.empty(rows, dim, device="cuda")
+    dy[:, : dim // 2], dy[:, dim // 2:] = 0.1, 0.7
+    _, stats = dense.layer_norm(x, save_stats=True)
+    weight = torch.ones(dim, device="cuda")
+    _, dw, db = dense.layer_norm_backward(dy, x, weight, stats)
+    eb = rows * dy[0].double()
+    ew = eb * x[0].double() / (1 + 1e-5) ** 0.5
+    chain = 256 + rows // 256 // 32 + 40
+    R.within(db, eb, chain * R.F32 * eb, "dbias")
+    R.within(dw, ew, (chain + 16) * R.F32 * ew.abs(), "dweight")
