@@ -146,6 +146,9 @@ __device__ __forceinline__ float exp2_fast(float x) {
     return r;
 }
 
+// The scale of exponents of 2.  (Not infinite, whose product with 0 is not 0.)
+__device__ __forceinline__ float of_log2(float scale) { return fminf(scale * kLog2e, 3.4028234663852886e38f); }
+
 // A row's values in 16-byte pieces: the first begins at or before the row's
 // first value, on a 16-byte boundary; the values outside the row are not read.
 template <class T>
@@ -310,7 +313,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprobs(ProbArgs a
     const int span = (int)(blockIdx.x % (unsigned)a.spans);
     const RowPieces<T> row(a.x, r * a.stride, a.vocab);
     const int p0 = span * a.per_span, p1 = min(row.count, p0 + a.per_span);
-    const float c = a.scale * kLog2e;
+    const float c = of_log2(a.scale);
     const float2 c2 = make_float2(c, c);
     auto fetch = [&](int base, int stage) {
         uint4* to = ring + stage * kStep;
@@ -580,7 +583,7 @@ __global__ void __launch_bounds__(kMostThreads) k_logprobs_join(ProbArgs a) {
         select<kMostThreads>(list, count, a.top);
     }
     if (warp != 0) return;
-    const float c = a.scale * kLog2e;
+    const float c = of_log2(a.scale);
     float m = -CUDART_INF_F;
     for (int i = lane; i < a.spans; i += 32) m = max_nan(m, part[i].x);
     for (int o = 16; o; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
@@ -639,10 +642,12 @@ __global__ void __launch_bounds__(kMostThreads, 4) k_logprobs_backward(GradArgs 
     const float m = a.stats[2 * r], logs = a.stats[2 * r + 1];
     const int64_t target = a.targets[r];
     const float g = target >= 0 && a.dlogprob ? a.dlogprob[r] : 0.f, h = a.dentropy ? a.dentropy[r] : 0.f;
-    // dx = p (A + B u) with u = log2 p, and scale g more at the target
-    const float c = a.scale * kLog2e, base = m == -CUDART_INF_F ? 0.f : m;
-    float A = -a.scale * (g + (h != 0.f ? h * a.entropy[r] : 0.f));
-    const float B = -a.scale * h * kLn2, at_target = a.scale * g;
+    // dx = p (A + B u) with u = log2 p, and scale g more at the target.  A scale so large that A and B would not be
+    // finite comes last (of what is often 0 then).
+    const bool large = a.scale > 0x1p64f;
+    const float c = of_log2(a.scale), base = m == -CUDART_INF_F ? 0.f : m, by = large ? 1.f : a.scale;
+    float A = -by * (g + (h != 0.f ? h * a.entropy[r] : 0.f));
+    const float B = -by * h * kLn2, at_target = by * g;
     if (isnan(m) || m == CUDART_INF_F || target >= a.vocab) A = CUDART_NAN_F;
     const float2 minus = make_float2(-base, -base), c2 = make_float2(c, c), A2 = make_float2(A, A), B2 = make_float2(B, B),
                  l2 = make_float2(-logs * kLog2e, -logs * kLog2e);
@@ -666,6 +671,9 @@ __global__ void __launch_bounds__(kMostThreads, 4) k_logprobs_backward(GradArgs 
             for (int e = 0; e < N; ++e)
                 if (at + e == target && (e & 1 ? P::pair(q[i], e / 2).y : P::pair(q[i], e / 2).x) != -CUDART_INF_F) v[e] += at_target;
         }
+        if (large)
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[e] *= a.scale;
         if (aligned && row.whole(p)) {
             if constexpr (sizeof(T) == 4) {
                 *reinterpret_cast<float4*>(out + (int64_t)p * N) = make_float4(v[0], v[1], v[2], v[3]);

@@ -281,3 +281,29 @@ def test_offsets_past_32_bits():
     dz = dense.token_logprobs_backward(x, t, r, g)
     want, tol = R.token_logprobs_backward(x[-2:], t[-2:], 1.0, g[-2:], None)
     R.within(dz[-2:], want, tol + R.rounding(want.abs() + tol, x.dtype), "dlogits")
+
+
+@pytest.mark.parametrize("n,v", [(5, 400), (3, 70000), (200, 40000)])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_any_finite_scale(n, v, dtype):
+    """Up to the largest: all of the weight is at the largest scores, and what the others weigh does not spoil it."""
+    torch = torch_cuda()
+    from paper_2504_01506_gb300 import dense
+
+    x, _ = _logits(torch, n, v, _t(dtype), sigma=0.02)
+    t = x.float().argmax(1)
+    t[::2] = 7
+    g, h = torch.full((n,), 0.5, device="cuda"), torch.full((n,), 0.3, device="cuda")
+    for scale in (1e-40, 1e-37, 1e32, 1e37, 2e38, 2.5e38, 3.4e38):
+        r = dense.token_logprobs(x, t, top=3, scale=scale)
+        lp, ent, every, _ = R.token_logprobs(x, t, scale)
+        R.within(r.logprob, lp, 2.0 ** -17 * (1 + lp.abs()), f"logprob, {scale}")
+        R.within(r.entropy, ent, 2.0 ** -16 * (1 + ent.abs()), f"entropy, {scale}")
+        ids = R.alternatives(x, 3)
+        assert torch.equal(r.top_ids, ids)
+        want = every.gather(1, ids)
+        R.within(r.top_logprobs, want, 2.0 ** -17 * (1 + want.abs()), f"alternatives, {scale}")
+        for gg, hh in ((g, h), (g, None), (None, h)):
+            dz = dense.token_logprobs_backward(x, t, r, gg, hh, scale=scale)
+            want, tol = R.token_logprobs_backward(x, t, scale, gg, hh)
+            R.within(dz, want, tol + R.rounding(want.abs() + tol, x.dtype), f"dlogits, {scale}")
