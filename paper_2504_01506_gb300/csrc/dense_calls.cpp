@@ -95,7 +95,14 @@ struct Workspace {
     }
 };
 PyObject* pass() { Py_RETURN_NOTIMPLEMENTED; }
-bool truth(PyObject* o) { return o == Py_True || (o != Py_False && PyObject_IsTrue(o) == 1); }
+// An error that Python has been told of already.
+struct Told {};
+bool truth(PyObject* o) {
+    if (o == Py_True || o == Py_False) return o == Py_True;
+    const int r = PyObject_IsTrue(o);
+    if (r < 0) throw Told{};
+    return r != 0;
+}
 PyObject* given(const at::Tensor& t) {
     if (!t.defined()) Py_RETURN_NONE;
     return THPVariable_Wrap(t);
@@ -114,13 +121,15 @@ PyObject* tuple_of(const at::Tensor (&t)[N]) {
     return r;
 }
 void* at_of(const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
-// A C++ exception (of torch's allocator: out of memory) as a Python one.
+// A C++ exception (of torch's allocator: out of memory; of a flag without a truth) as a Python one.
 template <class F>
 PyObject* guarded(F f) {
     try {
         return f();
     } catch (const c10::OutOfMemoryError&) {
         return pass();  // the call in Python meets the same, and raises torch's error
+    } catch (const Told&) {
+        return nullptr;
     } catch (const std::exception& e) {
         PyErr_SetString(PyExc_RuntimeError, e.what());
         return nullptr;

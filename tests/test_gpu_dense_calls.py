@@ -88,3 +88,20 @@ def test_refusals_are_the_checked_ones():
             (TypeError, lambda: dense.token_logprobs(x, t.int())), (ValueError, lambda: dense.token_logprobs(x, t[:3]))):
         with pytest.raises(kind):
             call()
+
+
+def test_a_flag_that_is_neither():
+    """Something whose truth raises: what it raises, not a result."""
+    torch = torch_cuda()
+    from paper_2504_01506_gb300 import dense
+
+    x, h = torch.randn(4, 8, device="cuda"), torch.randn(4, 8, device="cuda", dtype=torch.bfloat16)
+    t, two = torch.zeros(4, dtype=torch.int64, device="cuda"), torch.ones(2)
+    r = dense.token_logprobs(x, t)
+    stats = dense.layer_norm(x, save_stats=True)[1]
+    for call in (lambda: dense.layer_norm(x, save_stats=two), lambda: dense.layer_norm_backward(x, x, None, stats, bias=two),
+                 lambda: dense.linear(h, h, save_pre=two), lambda: dense.linear_backward(h[:, :4], h, h[:4], want_dx=two),
+                 lambda: dense.linear_backward(h[:, :4], h, h[:4], bias=two), lambda: dense.linear_backward(h[:, :4], h, h[:4], want_dweight=two),
+                 lambda: dense.token_logprobs_backward(x, t, r, r.logprob, in_place=two)):
+        with pytest.raises(RuntimeError, match="ambiguous"):
+            call()
