@@ -301,7 +301,11 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, pre
 def sync(device=None):
     """Waits for the current stream; raises if a bounded wait inside a product's kernel
     ran out since the last call (its outputs are then not valid)."""
-    device = torch.device("cuda", torch.cuda.current_device() if device is None else torch.device(device).index or 0)
+    device = torch.device("cuda" if device is None else device)
+    if device.type != "cuda":
+        raise TypeError(f"device must be a CUDA device, not {device}")
+    if device.index is None:
+        device = torch.device("cuda", _current_device())
     _call(device, L.load().mlkv_dense_sync, _stream(device))
 
 

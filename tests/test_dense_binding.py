@@ -136,3 +136,16 @@ def test_argument_checks_of_the_python_face():
         dense._matrix(x, "x", None, (1, 8))
     with pytest.raises(dense.MLKVError):
         dense._workspace(-1, x.device)
+
+
+def test_sync_of_a_device_without_an_index_is_the_current_ones(monkeypatch):
+    asked = []
+    monkeypatch.setattr(dense, "_current_device", lambda: 3)
+    monkeypatch.setattr(dense.torch.cuda, "current_device", lambda: 3)
+    monkeypatch.setattr(dense, "_stream", lambda device: None)
+    monkeypatch.setattr(dense, "_call", lambda device, call, *args: asked.append(device))
+    for device in (None, "cuda", torch.device("cuda"), "cuda:1", torch.device("cuda", 2), 0):
+        dense.sync(device)
+    assert asked == [torch.device("cuda", i) for i in (3, 3, 3, 1, 2, 0)]
+    with pytest.raises(TypeError, match="CUDA"):
+        dense.sync("cpu")
