@@ -21,7 +21,8 @@
  *   - Calls are asynchronous on `stream` (a cudaStream_t; NULL = legacy default
  *     stream), allocate nothing, keep nothing between calls and may be captured
  *     into a CUDA graph.  Calls on different streams or host threads share no
- *     memory but their arguments.  The stream's device must be current.
+ *     memory but their arguments (and a device's count of waits that ran out, which
+ *     mlkv_dense_sync reads).  The stream's device must be current.
  *   - A call that needs working memory has a function that says how many bytes;
  *     the caller gives that much device memory, 256-byte aligned, which the call
  *     uses until it is done on the stream.  It goes by the device that is current.
@@ -125,9 +126,12 @@ int64_t mlkv_linear_backward_workspace(const mlkv_linear_args* args);
 int mlkv_linear(const mlkv_linear_args* args, void* stream);
 int mlkv_linear_backward(const mlkv_linear_args* args, void* stream);
 
-/* Waits for the stream and returns the sticky status of the products' kernels
- * on the current device, clearing it: MLKV_OK, or MLKV_ERR_TIMEOUT when a bounded
- * wait inside one ran out (its outputs are then not valid). */
+/* Waits for the stream.  MLKV_ERR_TIMEOUT when a bounded wait inside a product's
+ * kernel has run out since this was last told (its outputs are then not valid;
+ * the product's own call returned before), else MLKV_OK.  What is told is the
+ * current device's, of whichever stream, and it is told to whoever asks first: all
+ * that the stream held before the call is counted, and none that runs out on
+ * another stream meanwhile is lost (of one of its launches several calls may tell). */
 int mlkv_dense_sync(void* stream);
 
 /* Log probabilities of given tokens under softmax(scale * logits), row by row.

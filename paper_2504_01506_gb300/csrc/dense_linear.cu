@@ -26,7 +26,7 @@ namespace {
 constexpr int kBM = 128;      // rows (i) of a tile
 constexpr int kBK = 64;       // values along k of a stage: 128 bytes
 
-__device__ uint32_t g_status;  // MLKV_ERR_TIMEOUT: a wait ran out
+__device__ uint32_t g_timeouts;  // blocks in which a wait ran out (never set back: what has been told of is the host's)
 
 struct Epilogue {
     const void* bias;
@@ -618,7 +618,7 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR>::kThreads, 1)
     }
     if (PAIR || joined) cluster_sync();  // nothing of this block's memory is wanted by another any more
     tc_fence_after();
-    if (threadIdx.x == 0 && stop) atomicMax(&g_status, (uint32_t)MLKV_ERR_TIMEOUT);
+    if (threadIdx.x == 0 && stop) atomicAdd(&g_timeouts, 1u);
     if (warp == kMma) tmem_free<PAIR>(tmem, R::kColumns);
     if (p.beside) pdl_enter_last();  // whoever waits for this grid waits for those before it
 }
@@ -1162,11 +1162,15 @@ extern "C" int mlkv_linear_backward(const mlkv_linear_args* args, void* stream) 
 
 extern "C" int mlkv_dense_sync(void* stream) {
     MLKV_DENSE_RANGE("mlkv_dense_sync");
-    uint32_t status = 0;
-    const uint32_t none = 0;
-    if (cudaStreamSynchronize((cudaStream_t)stream) != cudaSuccess ||
-        cudaMemcpyFromSymbol(&status, g_status, sizeof(status)) != cudaSuccess)
+    constexpr int kDevices = 64;
+    static std::atomic<uint32_t> told[kDevices];  // of g_timeouts
+    int dev = 0;
+    uint32_t now = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kDevices ||
+        cudaMemcpyFromSymbolAsync(&now, g_timeouts, sizeof(now), 0, cudaMemcpyDeviceToHost, (cudaStream_t)stream) != cudaSuccess ||
+        cudaStreamSynchronize((cudaStream_t)stream) != cudaSuccess)
         return MLKV_ERR_CUDA;
-    if (status && cudaMemcpyToSymbol(g_status, &none, sizeof(none)) != cudaSuccess) return MLKV_ERR_CUDA;
-    return (int)status;
+    for (uint32_t before = told[dev].load(); (int32_t)(now - before) > 0;)
+        if (told[dev].compare_exchange_weak(before, now)) return MLKV_ERR_TIMEOUT;
+    return MLKV_OK;
 }

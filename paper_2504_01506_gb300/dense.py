@@ -243,7 +243,8 @@ def linear(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None = No
     """act(x @ weight.T + bias) + residual: x [m, k], weight [n, k], bias [n], residual
     [m, n], all of x's type; activation: "none", "relu", "gelu_tanh" or "silu".  With
     save_pre also the value before the activation, [m, n], for linear_backward (None
-    without an activation, whose gradient does not need it)."""
+    without an activation, whose gradient does not need it).  That the kernel's waits
+    were all met, and the outputs are valid, is known after sync()."""
     if (native := _native(x)) is not None:
         r = native.linear(x, weight, bias, _ACTIVATIONS.get(activation, -1), residual, save_pre)
         if r is not NotImplemented:
@@ -270,7 +271,8 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, pre
                     activation: str | None = None, bias: bool = False, want_dx: bool = True, want_dweight: bool = True):
     """Gradients (dx, dweight, dbias) of linear(x, weight, bias, activation=...), all of
     x's type; dbias is None without `bias`, the others where they are not wanted.  pre:
-    what save_pre gave (needed with an activation).  The residual's gradient is dy."""
+    what save_pre gave (needed with an activation).  The residual's gradient is dy.
+    Valid when sync() says so, as linear's."""
     if (native := _native(x)) is not None:
         r = native.linear_backward(dy, x, weight, pre, _ACTIVATIONS.get(activation, -1), bias, want_dx, want_dweight)
         if r is not NotImplemented:
@@ -300,7 +302,8 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, pre
 
 def sync(device=None):
     """Waits for the current stream; raises if a bounded wait inside a product's kernel
-    ran out since the last call (its outputs are then not valid)."""
+    ran out on the device, on any stream, since a call last raised for one (the
+    outputs of that product are then not valid)."""
     device = torch.device("cuda" if device is None else device)
     if device.type != "cuda":
         raise TypeError(f"device must be a CUDA device, not {device}")
