@@ -531,8 +531,8 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR>::kThreads, 1)
                 }
             }
             if (!ok && rank == 0) {  // given up: the copies in flight still write into shared memory
-                for (uint32_t b = n > S ? n - S : 0; b < n; ++b)
-                    for (uint32_t tries = 0; tries < 1u << 20 && !mbar_try(full + 8 * (b % S), (b / S) & 1); ++tries) {}
+                Waited waited;
+                for (uint32_t b = n > S ? n - S : 0; b < n; ++b) mbar_drain(full + 8 * (b % S), (b / S) & 1, waited);
             }
         }
     } else if (warp == kMma) {
@@ -558,7 +558,8 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR>::kThreads, 1)
             }
             if (!ok) {  // given up: products in flight still write into tensor memory
                 tc_commit<PAIR>(ended);
-                for (uint32_t tries = 0; tries < 1u << 20 && !mbar_try(ended, 0); ++tries) {}
+                Waited waited;
+                mbar_drain(ended, 0, waited);
             }
         }
     } else {

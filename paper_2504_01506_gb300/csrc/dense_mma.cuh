@@ -33,22 +33,41 @@ __device__ __forceinline__ uint64_t time_ns() {
     return t;
 }
 
+// How long a thread has waited, by what has passed between its looks at the clock:
+// of two looks, further apart only where the block was switched out meanwhile, at
+// most kLookNs.
+constexpr uint64_t kLookNs = 100000000ull;
+struct Waited {
+    uint64_t last = 0, ns = 0;
+    __device__ __forceinline__ bool over(uint64_t limit) {
+        const uint64_t now = time_ns();
+        if (last) ns += min(now - last, kLookNs);
+        last = now;
+        return ns > limit;
+    }
+};
+
 // Longest wait on a barrier.  What a wait stands for takes microseconds; one
 // that runs out sets the block's `stop`, which ends the block's other waits.
 constexpr uint64_t kWaitLimitNs = 2000000000ull;
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* stop) {
-    uint64_t since = 0;
+    Waited waited;
     for (uint32_t n = 1;; ++n) {
         if (mbar_try(bar, parity)) return true;
         if (n & 31) continue;
         if (*stop) return false;
-        const uint64_t now = time_ns();
-        if (!since) since = now;
-        if (now - since > kWaitLimitNs) {
+        if (waited.over(kWaitLimitNs)) {
             *stop = 1;
             return false;
         }
     }
+}
+
+// After giving up: waits for what is in flight all the same, for kDrainLimitNs over all that `waited` counts.
+constexpr uint64_t kDrainLimitNs = 1000000000ull;
+__device__ __forceinline__ void mbar_drain(uint32_t bar, uint32_t parity, Waited& waited) {
+    for (uint32_t n = 1; !mbar_try(bar, parity); ++n)
+        if (!(n & 31) && waited.over(kDrainLimitNs)) return;
 }
 
 // An arrival on a barrier of another block of the cluster (place_in).
