@@ -530,6 +530,8 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR>::kThreads, 1)
                         load(at + R::kA, &mb, k * kBK, col);
                 }
             }
+            // (all have been brought: until the last has been read, the products may give up)
+            if (ok && n) ok = mbar_wait(empty + 8 * ((n - 1) % S), ((n - 1) / S) & 1, &stop);
             if (!ok && rank == 0) {  // given up: the copies in flight still write into shared memory
                 Waited waited;
                 for (uint32_t b = n > S ? n - S : 0; b < n; ++b) mbar_drain(full + 8 * (b % S), (b / S) & 1, waited);
