@@ -617,7 +617,6 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR>::kThreads, 1)
         const Work w(p, first, true, mine);
         cluster_sync();
         if (warp < 4) join_columns<T, BN>(p, ring, w.i, w.j, mine);
-        __syncwarp();
     }
     if (PAIR || joined) cluster_sync();  // nothing of this block's memory is wanted by another any more
     tc_fence_after();

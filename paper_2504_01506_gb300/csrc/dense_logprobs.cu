@@ -550,7 +550,6 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprobs(ProbArgs a
             const float s = group_sum(one.s, 32), p = group_sum(one.p, 32);
             finish_row<T>(a, r, m, s, p, TOP && lane < a.top ? list[lane] : 0ull, lane);
         }
-        __syncwarp();
     }
     cluster_sync();  // (nothing of a block's memory is wanted by another any more)
 }
