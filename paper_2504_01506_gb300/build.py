@@ -8,9 +8,12 @@ contracting any other.  The dense operators are held to a tolerance, not to an
 order of operations, and may contract.
 
 Beside it _dense_calls.so, by g++: the dense operators' calls from Python
-(csrc/dense_calls.cpp), against the installed torch.
+(csrc/dense_calls.cpp), against the installed torch, and built anew with another
+torch.  Where that cannot be built (no headers of Python's or torch's), the
+library is there all the same, and dense.py makes the calls by ctypes.
 """
 import concurrent.futures as cf
+import importlib.metadata
 import importlib.util
 import os
 import shutil
@@ -24,6 +27,8 @@ ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libmlkv_gb300.so")
 CALLS = os.path.join(HERE, "_dense_calls.so")
 BUILD = os.path.join(ROOT, "_build")
+CALLS_SOURCE = "dense_calls.cpp"
+HEADERS = [os.path.join(ROOT, "include", f) for f in ("mlkv_gpu.h", "mlkv_dense.h")]
 SOURCES = ["mlkv_index.cu", "mlkv_sort.cu", "mlkv_apply.cu", "mlkv_plan.cu", "mlkv_table.cu", "mlkv_tier.cu", "mlkv_static.cu"]
 DENSE = ["dense_norm.cu", "dense_norm_backward.cu", "dense_linear.cu", "dense_logprobs.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
@@ -38,34 +43,60 @@ def nvcc() -> str:
     raise RuntimeError("nvcc not found")
 
 
-def _deps():
-    files = [os.path.join(CSRC, f) for f in os.listdir(CSRC)]
-    files += [os.path.join(ROOT, "include", f) for f in ("mlkv_gpu.h", "mlkv_dense.h")]
-    files.append(os.path.abspath(__file__))
-    return files
+def _newer(out: str, sources) -> bool:
+    """Whether `out` is there and no older than what it is made of."""
+    if not os.path.exists(out):
+        return False
+    t = os.path.getmtime(out)
+    return all(os.path.getmtime(f) <= t for f in [*sources, *HEADERS, os.path.abspath(__file__)])
+
+
+def _torch_version() -> str:
+    try:
+        return importlib.metadata.version("torch")
+    except importlib.metadata.PackageNotFoundError:
+        return ""
+
+
+def _calls_torch() -> str:
+    """The file with the version of torch that the extension module was built against."""
+    return os.path.join(BUILD, "dense_calls.torch")
+
+
+def library_up_to_date() -> bool:
+    return _newer(LIB, [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cu", ".cuh"))])
+
+
+def calls_up_to_date() -> bool:
+    if not _newer(CALLS, [os.path.join(CSRC, CALLS_SOURCE)]) or not os.path.exists(_calls_torch()):
+        return False
+    with open(_calls_torch()) as f:
+        return f.read() == _torch_version()
 
 
 def up_to_date() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(CALLS):
-        return False
-    t = min(os.path.getmtime(LIB), os.path.getmtime(CALLS))
-    return all(os.path.getmtime(f) <= t for f in _deps())
+    return library_up_to_date() and calls_up_to_date()
 
 
 def build_calls() -> str:
     """The extension module of the dense operators' calls."""
-    torch = importlib.util.find_spec("torch").submodule_search_locations[0]
+    spec = importlib.util.find_spec("torch")
+    if spec is None:
+        raise RuntimeError("torch is not installed")
+    torch = spec.submodule_search_locations[0]
     cuda = os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(nvcc()))), "include")
     include = [os.path.join(ROOT, "include"), sysconfig.get_paths()["include"], os.path.join(torch, "include"),
                os.path.join(torch, "include", "torch", "csrc", "api", "include"), cuda]
     tmp = CALLS + f".tmp{os.getpid()}"
     cmd = [shutil.which("g++") or "g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden", *(f"-I{d}" for d in include),
-           os.path.join(CSRC, "dense_calls.cpp"), "-o", tmp, f"-L{os.path.join(torch, 'lib')}",
+           os.path.join(CSRC, CALLS_SOURCE), "-o", tmp, f"-L{os.path.join(torch, 'lib')}",
            *(f"-l{n}" for n in ("torch_python", "torch", "torch_cpu", "torch_cuda", "c10", "c10_cuda"))]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
-        raise RuntimeError(f"g++ failed on dense_calls.cpp:\n{r.stderr}")
+        raise RuntimeError(f"g++ failed on {CALLS_SOURCE}:\n{r.stderr}")
     os.replace(tmp, CALLS)
+    with open(_calls_torch(), "w") as f:
+        f.write(_torch_version())
     return CALLS
 
 
@@ -74,9 +105,26 @@ def build(force: bool = False, verbose: bool = False, extra=()) -> str:
     # tuning constants for a sweep; a build with them is always forced.
     env_extra = os.environ.get("MLKV_NVCC_FLAGS", "").split()
     extra = [*extra, *env_extra]
-    if not force and not env_extra and up_to_date():
+    library = force or bool(env_extra) or not library_up_to_date()
+    calls = force or not calls_up_to_date()
+    if not library and not calls:
         return LIB
     os.makedirs(BUILD, exist_ok=True)
+    with cf.ThreadPoolExecutor(max_workers=1) as ex:
+        module = ex.submit(build_calls) if calls else None
+        if library:
+            build_library(verbose, extra)
+        try:
+            if module:
+                module.result()
+        except (RuntimeError, OSError) as e:
+            if os.path.exists(CALLS):  # (of other sources, or another torch)
+                os.remove(CALLS)
+            sys.stderr.write(f"{os.path.basename(CALLS)} cannot be built, the dense operators are called by ctypes: {e}\n")
+    return LIB
+
+
+def build_library(verbose: bool = False, extra=()) -> str:
     cc = nvcc()
 
     def compile_one(src):
@@ -90,10 +138,8 @@ def build(force: bool = False, verbose: bool = False, extra=()) -> str:
             sys.stderr.write(r.stderr)
         return obj
 
-    with cf.ThreadPoolExecutor(max_workers=len(SOURCES) + len(DENSE) + 1) as ex:
-        calls = ex.submit(build_calls)
+    with cf.ThreadPoolExecutor(max_workers=len(SOURCES) + len(DENSE)) as ex:
         objs = list(ex.map(compile_one, [*DENSE, *SOURCES]))
-        calls.result()
     tmp = LIB + f".tmp{os.getpid()}"
     r = subprocess.run([cc, *ARCH, "-shared", "-o", tmp, *objs], capture_output=True, text=True)
     if r.returncode != 0:

@@ -17,10 +17,12 @@ torch stream of its first tensor's device and runs in the CUDA library; working
 memory comes from torch's allocator for the length of the call.  This module
 only checks arguments (TypeError, ValueError) and passes pointers; where nothing
 is wrong with them and nothing has to be copied, _dense_calls does (csrc/dense_calls.cpp:
-the host's part of a call is what a small one takes).  Formulas and
+the host's part of a call is what a small one takes; without that module this one
+makes every call).  Formulas and
 the treatment of masked and invalid values: include/mlkv_dense.h.
 """
 import typing
+import warnings
 
 import torch
 
@@ -55,10 +57,13 @@ def _native(x):
         try:
             from . import _dense_calls
         except ImportError as e:
-            raise ImportError(f"the dense operators' calls are missing: build them with __graft_entry__.build() ({e})") from None
-        _dense_calls.bind(lib._name)
-        _calls = _dense_calls
-    return _calls
+            warnings.warn(f"the dense operators' extension module is missing, calls take 10 us or so longer: build it with "
+                          f"__graft_entry__.build() ({e})", RuntimeWarning, stacklevel=3)
+            _calls = ()
+        else:
+            _dense_calls.bind(lib._name)
+            _calls = _dense_calls
+    return _calls or None
 
 
 def _done(result):
