@@ -18,7 +18,8 @@ constexpr int kBackwardLanes = 512;  // threads an SM: 128 registers each
 
 // The rows' gradients, and the sums over this block's rows of dy xh and dy.  Rows
 // come through shared memory, the next one or two of each team on their way (a
-// thread reads what it copied itself).  What a lane holds beyond the row's end is a copy of its last vector, or 0, with weight 0.
+// thread reads what it copied itself).  What a lane holds beyond the row's end is a copy of its last vector, left out of
+// the sums, or, within that vector, 0.
 template <class TX, class TY, int NV, bool ALIGNED>
 __global__ void __launch_bounds__(kBackwardLanes, 1) k_norm_backward(NormArgs a) {
     pdl_enter();
@@ -93,8 +94,10 @@ __global__ void __launch_bounds__(kBackwardLanes, 1) k_norm_backward(NormArgs a)
 #pragma unroll
             for (int k = 0; k < H; ++k) {
                 const float2 d = dy[i].pair(k), xh = mul2(add2(x[i].pair(k), minus), rs), g = mul2(d, w[k]);
-                c1 = add2(c1, g);
-                c2 = fma2(g, xh, c2);
+                if (tm.lane + i * tm.L < nvec) {  // (a copy's weight of 0 does not take an infinite value out)
+                    c1 = add2(c1, g);
+                    c2 = fma2(g, xh, c2);
+                }
                 dw[i][k] = fma2(d, xh, dw[i][k]);
                 db[i][k] = add2(db[i][k], d);
             }

@@ -217,3 +217,36 @@ def test_column_sums_of_many_long_rows(rows, dim):
     chain = 256 + rows // 256 // 32 + 40
     R.within(db, eb, chain * R.F32 * eb, "dbias")
     R.within(dw, ew, (chain + 16) * R.F32 * ew.abs(), "dweight")
+
+
+@pytest.mark.parametrize("rows,dim", [(700, 100), (700, 36), (3, 100), (700, 520), (60, 1032), (700, 101), (9, 8200)])
+@pytest.mark.parametrize("types", [("fp32", "fp32"), ("fp32", "bf16"), ("bf16", "bf16")])
+def test_infinite_gradients_at_the_last_columns(rows, dim, types):
+    """A row's gradient is infinite or NaN where the formula makes it so, column by column; no other row's is."""
+    torch = torch_cuda()
+    from paper_2504_01506_gb300 import dense
+
+    gen = torch.Generator("cuda")
+    gen.manual_seed(dim)
+    x = _matrix(torch, rows, dim, _t(types[0]), gen)
+    dy = _matrix(torch, rows, dim, _t(types[1]), gen)
+    w = torch.rand(dim, generator=gen, device="cuda") + 0.5
+    _, stats = dense.layer_norm(x, w, save_stats=True, out_dtype=_t(types[1]))
+    clean = dense.layer_norm_backward(dy, x, w, stats)
+    bad = rows // 2
+    for column in (dim - 1, dim - 2):
+        for value in (float("inf"), -float("inf")):
+            d = dy.clone()
+            d[bad, column] = value
+            dx, dw, db = dense.layer_norm_backward(d, x, w, stats)
+            keep = torch.ones(rows, dtype=torch.bool, device="cuda")
+            keep[bad] = False
+            assert torch.equal(dx[keep], clean[0][keep])
+            mu, r = stats[bad, 0].double(), stats[bad, 1].double()
+            g, xh = d[bad].double() * w.double(), (x[bad].double() - mu) * r
+            want = r * (g - g.mean() - xh * (g * xh).mean())
+            assert torch.equal(dx[bad].isnan(), want.isnan()) and torch.equal(dx[bad].isposinf(), want.isposinf())
+            assert torch.equal(dx[bad].isneginf(), want.isneginf())
+            finite = torch.arange(dim, device="cuda") != column
+            assert torch.equal(dw[finite], clean[1][finite]) and torch.equal(db[finite], clean[2][finite])
+            assert db[column] == value and dw[column].isinf()
