@@ -18,8 +18,12 @@ memory comes from torch's allocator for the length of the call.  This module
 only checks arguments (TypeError, ValueError) and passes pointers; where nothing
 is wrong with them and nothing has to be copied, _dense_calls does (csrc/dense_calls.cpp:
 the host's part of a call is what a small one takes; without that module this one
-makes every call).  Formulas and
-the treatment of masked and invalid values: include/mlkv_dense.h.
+makes every call).  Formulas, the treatment of masked and invalid values, and what
+takes longer for the data's sake: include/mlkv_dense.h.
+
+Nothing here is recorded for torch's autograd, whether or not an argument requires
+a gradient: what a call returns has no history, and the gradients are what the
+*_backward calls return.
 """
 import typing
 import warnings
@@ -247,8 +251,8 @@ def linear(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None = No
            residual: torch.Tensor | None = None, save_pre: bool = False):
     """act(x @ weight.T + bias) + residual: x [m, k], weight [n, k], bias [n], residual
     [m, n], all of x's type; activation: "none", "relu", "gelu_tanh" or "silu".  With
-    save_pre also the value before the activation, [m, n], for linear_backward (None
-    without an activation, whose gradient does not need it).  That the kernel's waits
+    save_pre also the value before the activation, [m, n], rounded to x's type, for
+    linear_backward (None without an activation, whose gradient does not need it).  That the kernel's waits
     were all met, and the outputs are valid, is known after sync()."""
     if (native := _native(x)) is not None:
         r = native.linear(x, weight, bias, _ACTIVATIONS.get(activation, -1), residual, save_pre)
@@ -276,7 +280,8 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, pre
                     activation: str | None = None, bias: bool = False, want_dx: bool = True, want_dweight: bool = True):
     """Gradients (dx, dweight, dbias) of linear(x, weight, bias, activation=...), all of
     x's type; dbias is None without `bias`, the others where they are not wanted.  pre:
-    what save_pre gave (needed with an activation).  The residual's gradient is dy.
+    what save_pre gave (needed with an activation): the slopes are taken there, and dy
+    times them is rounded to x's type.  The residual's gradient is dy.
     Valid when sync() says so, as linear's."""
     if (native := _native(x)) is not None:
         r = native.linear_backward(dy, x, weight, pre, _ACTIVATIONS.get(activation, -1), bias, want_dx, want_dweight)
