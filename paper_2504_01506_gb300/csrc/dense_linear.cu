@@ -1170,7 +1170,8 @@ extern "C" int mlkv_dense_sync(void* stream) {
     static std::atomic<uint32_t> told[kDevices];  // of g_timeouts
     int dev = 0;
     uint32_t now = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kDevices ||
+    // (first the wait, which a stream that is being captured refuses: a copy would be captured)
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kDevices || cudaStreamSynchronize((cudaStream_t)stream) != cudaSuccess ||
         cudaMemcpyFromSymbolAsync(&now, g_timeouts, sizeof(now), 0, cudaMemcpyDeviceToHost, (cudaStream_t)stream) != cudaSuccess ||
         cudaStreamSynchronize((cudaStream_t)stream) != cudaSuccess)
         return MLKV_ERR_CUDA;
