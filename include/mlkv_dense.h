@@ -169,6 +169,53 @@ int mlkv_token_logprobs_backward(const void* d_logits, int64_t stride, int32_t t
                                  const float* d_stats, const float* d_dlogprob, const float* d_dentropy,
                                  void* d_dlogits, int64_t dlogits_stride, void* stream);
 
+/* The AdamW step of many tensors at once, in place.  Of every value, with t the
+ * step's number (from 1 on):
+ *     g' = grad_scale g;  m' = beta1 m + (1 - beta1) g';  v' = beta2 v + (1 - beta2) g'^2
+ *     p' = p (1 - lr weight_decay) - lr (m' / (1 - beta1^t)) / (sqrt(v' / (1 - beta2^t)) + eps)
+ * computed in 32 bits; p' is rounded to the parameter's type, and where d_copy is
+ * not null to copy_type (a 16-bit copy of fp32 weights for the products) too.
+ * state_bits 32: d_m and d_v are fp32 [n].  state_bits 8: both are e4m3 codes [n],
+ * d_m's of m and d_v's of sqrt(v), and d_scales is fp32 [2][ceil(n / 256)], the
+ * powers of two that the codes of each 256 values of m, then of sqrt(v), stand in.
+ * Codes are rounded up or down by chance, with the value as the mean: by a hash of
+ * seed, step, the tensor's place in the list and the value's in the tensor, so that
+ * the same call gives the same codes.  sqrt(v) > 0 keeps a code above 0.  A value
+ * that is not finite has the code NaN and leaves its block's others as they are.
+ * All zeros is the state before the first step.
+ * `tensors` is a host array; no tensor may overlap another, but gradients each
+ * other.  Parameters and gradients are of any element type, 0 <= n < 2^40; a tensor
+ * off 32 bytes (16-bit values: 16, codes: 8) takes several times as long.
+ * d_step (int64), d_lr and d_grad_scale (fp32): a value each on the device, read when the
+ * call runs, instead of step, lr and 1 (null), so that a captured step can be
+ * replayed; a *d_step below 1 gives NaN.  lr, weight_decay finite, eps >= 0,
+ * 0 <= beta < 1. */
+typedef struct mlkv_adamw_tensor {
+    int64_t n;
+    void* d_param;
+    const void* d_grad;
+    void* d_m;
+    void* d_v;
+    float* d_scales;
+    void* d_copy;
+    int32_t param_type;
+    int32_t grad_type;
+    int32_t copy_type;
+    int32_t reserved;
+} mlkv_adamw_tensor;
+typedef struct mlkv_adamw_args {
+    const mlkv_adamw_tensor* tensors;
+    int64_t count;
+    double lr, beta1, beta2, eps, weight_decay;
+    int64_t step;
+    const float* d_lr;
+    const int64_t* d_step;
+    const float* d_grad_scale;
+    uint32_t seed;
+    int32_t state_bits;
+} mlkv_adamw_args;
+int mlkv_adamw(const mlkv_adamw_args* args, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -67,6 +67,7 @@ EXPORTED_DENSE = [
     "mlkv_layer_norm", "mlkv_layer_norm_backward_workspace", "mlkv_layer_norm_backward", "mlkv_linear_workspace",
     "mlkv_linear_backward_workspace", "mlkv_linear", "mlkv_linear_backward", "mlkv_dense_sync",
     "mlkv_token_logprobs_workspace", "mlkv_token_logprobs", "mlkv_token_logprobs_backward",
+    "mlkv_adamw",
 ]
 
 
@@ -116,6 +117,40 @@ class LinearArgs(ctypes.Structure):
         ("workspace_bytes", ctypes.c_int64),
         ("type", ctypes.c_int32),
         ("activation", ctypes.c_int32),
+    ]
+
+
+class AdamWTensor(ctypes.Structure):
+    _fields_ = [
+        ("n", ctypes.c_int64),
+        ("d_param", ctypes.c_void_p),
+        ("d_grad", ctypes.c_void_p),
+        ("d_m", ctypes.c_void_p),
+        ("d_v", ctypes.c_void_p),
+        ("d_scales", ctypes.c_void_p),
+        ("d_copy", ctypes.c_void_p),
+        ("param_type", ctypes.c_int32),
+        ("grad_type", ctypes.c_int32),
+        ("copy_type", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+    ]
+
+
+class AdamWArgs(ctypes.Structure):
+    _fields_ = [
+        ("tensors", ctypes.POINTER(AdamWTensor)),
+        ("count", ctypes.c_int64),
+        ("lr", ctypes.c_double),
+        ("beta1", ctypes.c_double),
+        ("beta2", ctypes.c_double),
+        ("eps", ctypes.c_double),
+        ("weight_decay", ctypes.c_double),
+        ("step", ctypes.c_int64),
+        ("d_lr", ctypes.c_void_p),
+        ("d_step", ctypes.c_void_p),
+        ("d_grad_scale", ctypes.c_void_p),
+        ("seed", ctypes.c_uint32),
+        ("state_bits", ctypes.c_int32),
     ]
 
 
@@ -174,6 +209,7 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.mlkv_token_logprobs_workspace.argtypes = [i64, i64, i32, i32]
     lib.mlkv_token_logprobs.argtypes = [vp, i64, i32, i64, i64, vp, f32, i32, vp, vp, vp, vp, vp, vp, i64, vp]
     lib.mlkv_token_logprobs_backward.argtypes = [vp, i64, i32, i64, i64, vp, f32, vp, vp, vp, vp, vp, i64, vp]
+    lib.mlkv_adamw.argtypes = [ctypes.POINTER(AdamWArgs), vp]
     for name in EXPORTED_DENSE:
         getattr(lib, name).restype = i64 if name.endswith("_workspace") else i32
     for name in ("mlkv_open", "mlkv_close", "mlkv_get", "mlkv_put", "mlkv_insert", "mlkv_apply_grad",

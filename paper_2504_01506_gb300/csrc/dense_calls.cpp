@@ -17,6 +17,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <limits>
+#include <vector>
 
 #include "mlkv_dense.h"
 
@@ -33,6 +34,7 @@ struct Library {
     decltype(&mlkv_token_logprobs) token_logprobs;
     decltype(&mlkv_token_logprobs_workspace) token_logprobs_workspace;
     decltype(&mlkv_token_logprobs_backward) token_logprobs_backward;
+    decltype(&mlkv_adamw) adamw;
 } lib = {};
 
 constexpr auto kFloat = at::kFloat;
@@ -285,6 +287,99 @@ PyObject* token_logprobs_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// A list or a tuple of n objects (null: None).
+struct Items {
+    PyObject* const* at = nullptr;
+    bool read(PyObject* o, Py_ssize_t n) {
+        if (!(PyList_CheckExact(o) || PyTuple_CheckExact(o)) || PySequence_Fast_GET_SIZE(o) != n) return false;
+        at = PySequence_Fast_ITEMS(o);
+        return true;
+    }
+    bool read_or_none(PyObject* o, Py_ssize_t n) { return o == Py_None || read(o, n); }
+};
+const at::Tensor* contiguous(PyObject* o, c10::Device device) {
+    if (!THPVariable_Check(o)) return nullptr;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    return t.defined() && t.layout() == at::kStrided && t.device() == device && t.is_contiguous() ? &t : nullptr;
+}
+// A value on the device.
+template <class T>
+bool value_of(PyObject* o, c10::Device device, at::ScalarType scalar, const T** at) {
+    const at::Tensor* t = contiguous(o, device);
+    if (!t || t->scalar_type() != scalar || t->numel() != 1) return false;
+    *at = (const T*)t->data_ptr();
+    return true;
+}
+
+// params, grads, m, v, scales, copies, lr, beta1, beta2, eps, weight_decay, step, grad_scale, seed
+PyObject* adamw(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        if (n != 14 || !(PyList_CheckExact(a[0]) || PyTuple_CheckExact(a[0]))) return pass();
+        const Py_ssize_t count = PySequence_Fast_GET_SIZE(a[0]);
+        Items params, grads, m, v, scales, copies;
+        if (count < 1 || !params.read(a[0], count) || !grads.read(a[1], count) || !m.read(a[2], count) || !v.read(a[3], count) ||
+            !scales.read_or_none(a[4], count) || !copies.read_or_none(a[5], count) || !THPVariable_Check(params.at[0]))
+            return pass();
+        const at::Tensor& first = THPVariable_Unpack(params.at[0]);
+        if (!first.defined() || !first.is_cuda() || c10::cuda::current_device() != first.device().index()) return pass();
+        const c10::Device device = first.device();
+        const bool small = scales.at != nullptr;
+        const at::ScalarType state = small ? at::kFloat8_e4m3fn : kFloat;
+        static thread_local std::vector<mlkv_adamw_tensor> table;
+        table.assign(count, mlkv_adamw_tensor{});
+        for (Py_ssize_t i = 0; i < count; ++i) {
+            mlkv_adamw_tensor& t = table[i];
+            const at::Tensor *p = contiguous(params.at[i], device), *ms = contiguous(m.at[i], device), *vs = contiguous(v.at[i], device);
+            if (!p || !ms || !vs || type_of(p->scalar_type()) < 0 || ms->scalar_type() != state || vs->scalar_type() != state ||
+                ms->sizes() != p->sizes() || vs->sizes() != p->sizes())
+                return pass();
+            t.param_type = type_of(p->scalar_type());
+            if (small) {
+                const at::Tensor* s = contiguous(scales.at[i], device);
+                if (!s || s->scalar_type() != kFloat || s->dim() != 2 || s->size(0) != 2 || s->size(1) != (p->numel() + 255) / 256) return pass();
+                t.d_scales = (float*)s->data_ptr();
+            }
+            if (copies.at && copies.at[i] != Py_None) {
+                const at::Tensor* c = contiguous(copies.at[i], device);
+                if (!c || t.param_type != MLKV_TYPE_FLOAT || c->sizes() != p->sizes()) return pass();
+                t.copy_type = type_of(c->scalar_type());
+                if (t.copy_type <= MLKV_TYPE_FLOAT) return pass();
+                t.d_copy = c->data_ptr();
+            }
+            if (grads.at[i] == Py_None) continue;
+            const at::Tensor* g = contiguous(grads.at[i], device);
+            if (!g || type_of(g->scalar_type()) < 0 || g->sizes() != p->sizes()) return pass();
+            t.grad_type = type_of(g->scalar_type());
+            t.d_grad = g->data_ptr();
+            t.d_param = p->data_ptr();
+            t.d_m = ms->data_ptr();
+            t.d_v = vs->data_ptr();
+            t.n = p->numel();
+        }
+        mlkv_adamw_args g = {};
+        for (int i = 7; i < 11; ++i)
+            if (!PyFloat_CheckExact(a[i])) return pass();
+        if (!PyLong_CheckExact(a[13])) return pass();
+        const long long seed = PyLong_AsLongLong(a[13]);
+        if (seed < 0 || seed > 0xFFFFFFFFll) return PyErr_Clear(), pass();
+        if (PyFloat_CheckExact(a[6])) g.lr = PyFloat_AS_DOUBLE(a[6]);
+        else if (!value_of(a[6], device, kFloat, &g.d_lr)) return pass();
+        if (PyLong_CheckExact(a[11])) {
+            g.step = PyLong_AsLongLong(a[11]);
+            if (g.step < 1) return PyErr_Clear(), pass();
+        } else if (!value_of(a[11], device, at::kLong, &g.d_step)) {
+            return pass();
+        }
+        if (a[12] != Py_None && !value_of(a[12], device, kFloat, &g.d_grad_scale)) return pass();
+        g.tensors = table.data(); g.count = count;
+        g.beta1 = PyFloat_AS_DOUBLE(a[7]); g.beta2 = PyFloat_AS_DOUBLE(a[8]); g.eps = PyFloat_AS_DOUBLE(a[9]); g.weight_decay = PyFloat_AS_DOUBLE(a[10]);
+        g.seed = (uint32_t)seed; g.state_bits = small ? 8 : 32;
+        const int rc = lib.adamw(&g, c10::cuda::getCurrentCUDAStream(device.index()).stream());
+        if (rc != MLKV_OK) return PyLong_FromLong(rc);
+        Py_RETURN_NONE;
+    });
+}
+
 // The library's path: its calls from here on.
 PyObject* bind(PyObject*, PyObject* path) {
     const char* p = PyUnicode_AsUTF8(path);
@@ -306,6 +401,7 @@ PyObject* bind(PyObject*, PyObject* path) {
     get(found.token_logprobs, "mlkv_token_logprobs");
     get(found.token_logprobs_workspace, "mlkv_token_logprobs_workspace");
     get(found.token_logprobs_backward, "mlkv_token_logprobs_backward");
+    get(found.adamw, "mlkv_adamw");
     if (!ok) return PyErr_Format(PyExc_ImportError, "%s: not the library of these calls", p);
     lib = found;
     Py_RETURN_NONE;
@@ -313,7 +409,7 @@ PyObject* bind(PyObject*, PyObject* path) {
 
 #define CALL(f) {#f, (PyCFunction)(void (*)())(f), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {CALL(layer_norm), CALL(layer_norm_backward), CALL(linear), CALL(linear_backward), CALL(token_logprobs),
-                         CALL(token_logprobs_backward), {"bind", bind, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                         CALL(token_logprobs_backward), CALL(adamw), {"bind", bind, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_dense_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

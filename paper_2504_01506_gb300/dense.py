@@ -390,3 +390,115 @@ def token_logprobs_backward(logits: torch.Tensor, targets: torch.Tensor, result:
           targets.data_ptr(), scale, entropy.data_ptr(), stats.data_ptr(), None if g is None else g.data_ptr(),
           None if h is None else h.data_ptr(), out.data_ptr(), out_stride, _stream(device))
     return out
+
+
+# -- AdamW ------------------------------------------------------------------------------
+class AdamWState(typing.NamedTuple):
+    """What adamw keeps of every parameter: m and v, fp32 tensors of its shape; or, in 8
+    bits, the codes of m and of sqrt(v) (torch.float8_e4m3fn, of its shape), with their
+    scales, fp32 [2, ceil(n / 256)] (None in 32 bits)."""
+    m: list
+    v: list
+    scales: list | None
+
+
+_CODES = torch.float8_e4m3fn
+
+
+def adamw_state(params, bits: int = 32) -> AdamWState:
+    """The state before the first step (zeros), of 32 or 8 bits a value."""
+    if bits not in (8, 32):
+        raise ValueError(f"bits must be 8 or 32, not {bits}")
+    dtype = torch.float32 if bits == 32 else _CODES
+    zeros = lambda: [torch.zeros(p.shape, dtype=dtype, device=p.device) for p in params]  # noqa: E731
+    scales = None if bits == 32 else [torch.zeros((2, (p.numel() + 255) // 256), device=p.device) for p in params]
+    return AdamWState(zeros(), zeros(), scales)
+
+
+def _like(x, name: str, dtypes, shape, device) -> int:
+    """The address of a contiguous tensor that is written in place."""
+    if not isinstance(x, torch.Tensor) or x.dtype not in dtypes or x.device != device:
+        raise TypeError(f"{name} must be a tensor of {_names(dtypes)} on {device}")
+    if x.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}, not {list(x.shape)}")
+    if not x.is_contiguous():
+        raise TypeError(f"{name} must be contiguous")
+    return x.data_ptr()
+
+
+def _value(x, name: str, dtype, device) -> int:
+    """The address of a single value on the device."""
+    if x.dtype != dtype or x.device != device or x.numel() != 1:
+        raise TypeError(f"{name} must be a number or one value of {dtype} on {device}")
+    return x.data_ptr()
+
+
+def adamw(params, grads, state: AdamWState, step, *, lr, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01,
+          grad_scale: torch.Tensor | None = None, copies=None, seed: int = 0) -> None:
+    """One AdamW step of all `params`, in place, with `state` (adamw_state):
+
+        g = grad_scale * grad;  m = b1 m + (1 - b1) g;  v = b2 v + (1 - b2) g^2
+        p = p (1 - lr weight_decay) - lr (m / (1 - b1^step)) / (sqrt(v / (1 - b2^step)) + eps)
+
+    params: contiguous tensors of any shape, no one twice, all on one device; grads:
+    tensors of their shapes (None: that parameter stays as it is).  copies: None, or a
+    16-bit tensor (or None) for each fp32 parameter, which takes the new values rounded:
+    what the products use.  step: the step's number, from 1 on; lr: the rate; both also as a value
+    on the device (int64, fp32) that is read when the step runs, as is grad_scale (fp32;
+    a factor that clips): a step captured into a graph then goes by what they hold.
+    State in 8 bits is rounded up or down by chance: by `seed` (32 bits), step and the
+    values' places alone, so that a step can be repeated."""
+    first = params[0] if len(params) else None
+    if (native := _native(first)) is not None:
+        r = native.adamw(params, grads, state.m, state.v, state.scales, copies, lr, betas[0], betas[1], eps, weight_decay, step, grad_scale, seed)
+        if r is not NotImplemented:
+            return _done(r)
+    n = len(params)
+    for name, xs in (("grads", grads), ("state.m", state.m), ("state.v", state.v), ("state.scales", state.scales), ("copies", copies)):
+        if xs is not None and len(xs) != n or xs is None and name[:5] in ("grads", "state") and name != "state.scales":
+            raise ValueError(f"{name} must have {n} tensors, as params")
+    if not 0 <= seed < 1 << 32:
+        raise ValueError(f"seed must be 0 to 2^32 - 1, not {seed}")
+    if not n:
+        return None
+    if not isinstance(first, torch.Tensor):
+        raise TypeError("params must be tensors")
+    _on_gpu(first, "params[0]")
+    device = first.device
+    bits = 32 if state.scales is None else 8
+    table = (L.AdamWTensor * n)()
+    keep = []  # (of gradients that had to be copied)
+    for i, (p, g, t) in enumerate(zip(params, grads, table)):
+        at = _like(p, f"params[{i}]", _TYPES, getattr(p, "shape", None), device)
+        kinds = (torch.float32,) if bits == 32 else (_CODES,)
+        m, v = _like(state.m[i], f"state.m[{i}]", kinds, p.shape, device), _like(state.v[i], f"state.v[{i}]", kinds, p.shape, device)
+        scales = None if bits == 32 else _like(state.scales[i], f"state.scales[{i}]", (torch.float32,), (2, (p.numel() + 255) // 256), device)
+        copy, kind = None, 0
+        if copies is not None and copies[i] is not None:
+            if p.dtype != torch.float32:
+                raise TypeError(f"copies[{i}] of a parameter of {p.dtype}")
+            copy, kind = _like(copies[i], f"copies[{i}]", _HALVES, p.shape, device), _TYPES[copies[i].dtype]
+        if g is None:
+            continue
+        if isinstance(g, torch.Tensor) and not g.is_contiguous():
+            g = g.contiguous()
+            keep.append(g)
+        grad = _like(g, f"grads[{i}]", _TYPES, p.shape, device)
+        t.n, t.d_param, t.d_grad, t.d_m, t.d_v, t.d_scales, t.d_copy = p.numel(), at, grad, m, v, scales, copy
+        t.param_type, t.grad_type, t.copy_type = _TYPES[p.dtype], _TYPES[g.dtype], kind
+    a = L.AdamWArgs(tensors=table, count=n, beta1=betas[0], beta2=betas[1], eps=eps, weight_decay=weight_decay, seed=seed, state_bits=bits)
+    if isinstance(step, torch.Tensor):
+        a.d_step = _value(step, "step", torch.int64, device)
+    elif not 1 <= step < 1 << 63:
+        raise ValueError(f"step must be 1 or more, not {step}")
+    else:
+        a.step = step
+    if isinstance(lr, torch.Tensor):
+        a.d_lr = _value(lr, "lr", torch.float32, device)
+    else:
+        a.lr = lr
+    if grad_scale is not None:
+        if not isinstance(grad_scale, torch.Tensor):
+            raise TypeError("grad_scale must be a tensor")
+        a.d_grad_scale = _value(grad_scale, "grad_scale", torch.float32, device)
+    _call(device, L.load().mlkv_adamw, a, _stream(device))
