@@ -49,6 +49,7 @@ struct Hyper {
     const int64_t* d_step;
     const float* d_grad_scale;
     uint32_t seed, step;
+    float one;                          // 1, which the compiler does not know
 };
 template <int N> struct Batch {
     Hyper h;
@@ -154,6 +155,10 @@ __device__ __forceinline__ void widen(float2 (&x)[4], const uint32_t* w, int typ
 }
 __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 
+// a + b, each rounded by itself: an add of two products of pairs becomes one fused operation (whatever -fmad says), whose sum may lie
+// the other side of a power of two, and a code's neighbours with it.
+__device__ __forceinline__ float2 sum_of(float2 a, float2 b, float one) { return fma2(a, both(one), b); }
+
 // e4m3 codes.
 __device__ __forceinline__ float2 of_codes(uint32_t two) {
     const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, __NV_E4M3);
@@ -257,8 +262,8 @@ __global__ void __launch_bounds__(kWarps * 32) k_adamw(const __grid_constant__ B
                 v = make_float2(__uint_as_float(wv[2 * k]), __uint_as_float(wv[2 * k + 1]));
             }
             if (h.d_grad_scale) g[k] = mul2(g[k], factor);
-            m[k] = add2(mul2(m[k], both(h.b1)), mul2(g[k], both(h.c1)));
-            v = add2(mul2(v, both(h.b2)), mul2(mul2(g[k], g[k]), both(h.c2)));
+            m[k] = sum_of(mul2(m[k], both(h.b1)), mul2(g[k], both(h.c1)), h.one);
+            v = sum_of(mul2(v, both(h.b2)), mul2(mul2(g[k], g[k]), both(h.c2)), h.one);
             r[k] = make_float2(__fsqrt_rn(v.x), __fsqrt_rn(v.y));
             if constexpr (BITS == 32) {
                 wv[2 * k] = __float_as_uint(v.x);
@@ -394,7 +399,7 @@ extern "C" int mlkv_adamw(const mlkv_adamw_args* args, void* stream) {
     h.rate = (float)(a.lr / (1 - std::pow(a.beta1, t)));
     h.root = (float)(1 / std::sqrt(1 - std::pow(a.beta2, t)));
     h.d_lr = a.d_lr; h.d_step = a.d_step; h.d_grad_scale = a.d_grad_scale;
-    h.seed = a.seed; h.step = (uint32_t)a.step;
+    h.seed = a.seed; h.step = (uint32_t)a.step; h.one = 1.f;
     // The tensors' table is an argument of the launch: 1.8 KB of 24 tensors, 32 KB of 440.
     for (int64_t at = 0; at < a.count;) at += a.count - at <= 24 ? launch_batch<24>(a, h, at, (cudaStream_t)stream) : launch_batch<440>(a, h, at, (cudaStream_t)stream);
     return cudaGetLastError() == cudaSuccess ? MLKV_OK : MLKV_ERR_CUDA;

@@ -128,15 +128,15 @@ def test_codes_bit_for_bit(off):
     torch = torch_cuda()
     from paper_2504_01506_gb300 import dense
 
-    sizes = [5, 256, 700, 20_000]
-    params, grads, _, state = _network(torch, sizes, torch.float32, torch.float32, None, 8, seed=3, off=off)
+    sizes = [5, 256, 700, 500_000]  # (few bits a gradient: sums meet powers of two, where the rounding of each product tells)
+    params, grads, _, state = _network(torch, sizes, torch.float32, torch.bfloat16, None, 8, seed=3, off=off)
     f = np.float32
     for t in (1, 2, 1000):
         m0 = [(m.float().cpu().numpy() * s[0].cpu().numpy().repeat(256)[:m.numel()]) for m, s in zip(state.m, state.scales)]
         r0 = [(v.float().cpu().numpy() * s[1].cpu().numpy().repeat(256)[:v.numel()]) for v, s in zip(state.v, state.scales)]
         dense.adamw(params, grads, state, t, **HYPER, seed=0xFFFFFFFF)
         for i, n in enumerate(sizes):
-            g = grads[i].cpu().numpy()
+            g = grads[i].float().cpu().numpy()
             m1 = m0[i] * f(0.9) + g * f(1 - 0.9)
             v1 = r0[i] * r0[i] * f(0.999) + g * g * f(1 - 0.999)
             r1 = np.sqrt(v1)
