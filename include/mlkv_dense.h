@@ -130,6 +130,52 @@ int64_t mlkv_linear_backward_workspace(const mlkv_linear_args* args);
 int mlkv_linear(const mlkv_linear_args* args, void* stream);
 int mlkv_linear_backward(const mlkv_linear_args* args, void* stream);
 
+/* The gated block, and its gradients.  All matrices are of `type` (MLKV_TYPE_BFLOAT
+ * or MLKV_TYPE_HALF).
+ *   forward:   g = x w_gate^T;  u = x w_up^T;  h = act(g) u
+ *   backward:  dg = dh u act'(g);  du = dh act(g);  dx = dg w_gate + du w_up;
+ *              dw_gate = dg^T x;  dw_up = du^T x
+ * x: [m][k]; w_gate, w_up: [f][k]; h: [m][f]; gate, up: [m][f], g and u rounded to
+ * `type`: outputs of the forward pass where not null (both or neither), inputs of the
+ * backward pass.  dh: [m][f]; dx: [m][k]; dw_gate, dw_up: [f][k]; each of the three may
+ * be null (not wanted).  m, f, k >= 0, each < 2^29; k == 0 gives h = 0, m == 0 zero
+ * gradients of the weights.  h is taken of the sums before they are rounded; dg and
+ * du are rounded to `type`.  MLKV_ACT_RELU's slope is that of the rounded g, whose sign next to 0
+ * is the sum's in 32 bits. */
+typedef struct mlkv_gated_linear_args {
+    int64_t m, f, k;
+    const void* d_x;
+    int64_t x_stride;
+    const void* d_w_gate;
+    int64_t w_gate_stride;
+    const void* d_w_up;
+    int64_t w_up_stride;
+    void* d_h;
+    int64_t h_stride;
+    void* d_gate;
+    int64_t gate_stride;
+    void* d_up;
+    int64_t up_stride;
+    const void* d_dh;
+    int64_t dh_stride;
+    void* d_dx;
+    int64_t dx_stride;
+    void* d_dw_gate;
+    int64_t dw_gate_stride;
+    void* d_dw_up;
+    int64_t dw_up_stride;
+    void* d_workspace;
+    int64_t workspace_bytes;
+    int32_t type;
+    int32_t activation;
+} mlkv_gated_linear_args;
+
+/* As mlkv_linear's. */
+int64_t mlkv_gated_linear_workspace(const mlkv_gated_linear_args* args);
+int64_t mlkv_gated_linear_backward_workspace(const mlkv_gated_linear_args* args);
+int mlkv_gated_linear(const mlkv_gated_linear_args* args, void* stream);
+int mlkv_gated_linear_backward(const mlkv_gated_linear_args* args, void* stream);
+
 /* Waits for the stream.  MLKV_ERR_TIMEOUT when a bounded wait inside a product's
  * kernel has run out since this was last told (its outputs are then not valid;
  * the product's own call returned before), else MLKV_OK.  What is told is the
@@ -168,6 +214,50 @@ int mlkv_token_logprobs_backward(const void* d_logits, int64_t stride, int32_t t
                                  const int64_t* d_targets, float scale, const float* d_entropy,
                                  const float* d_stats, const float* d_dlogprob, const float* d_dentropy,
                                  void* d_dlogits, int64_t dlogits_stride, void* stream);
+
+/* The cross entropy of a linear layer over a vocabulary, whose logits are not kept,
+ * and its gradients.  x: [n][k] and weight: [vocab][k], of `type` (MLKV_TYPE_BFLOAT or
+ * MLKV_TYPE_HALF).  With z = scale x weight^T, row by row,
+ *     loss = log sum_v exp(z_v) - z_target,  d_loss: fp32 [n].
+ * d_targets: int64 [n]; a negative target is none (loss 0, no gradient); one of vocab
+ * or above gives NaN.  d_stats: fp32 [n][2], (max of x weight^T, log sum exp(scale
+ * (logit - max))): an output of the forward pass, an input of the backward pass.
+ * Backward: d_dloss, fp32 [n], gives d_dx [n][k] and d_dweight [vocab][k] of `type`,
+ * each null where not wanted.  The logits are computed again, in pieces of the vocabulary;
+ * their gradients are rounded to `type`, all times one power of two that brings the largest
+ * scale |dloss| to 2^13 .. 2^14 and is taken back in 32 bits (in fp16 a row whose
+ * gradient is far below the largest one's, by 2^20 or more, loses bits of its small probabilities).
+ * n >= 0, k >= 1, vocab >= 1, each < 2^30; scale > 0, finite.  n == 0 gives a zero dweight.
+ * Logits are never rounded to 16 bits.  One of -inf has probability 0, and a row of
+ * nothing else loss +inf; NaN or +inf among them make a row's statistics NaN.
+ * Working memory: forward 64 MB at most, or 512 bytes a row; backward 512 MB at most, or 8 KB a
+ * row, and fp32 sums of dx (up to four of each) where that takes several pieces; and copies of
+ * operands whose rows are not multiples of 16 bytes. */
+typedef struct mlkv_linear_cross_entropy_args {
+    int64_t n, k, vocab;
+    const void* d_x;
+    int64_t x_stride;
+    const void* d_weight;
+    int64_t weight_stride;
+    const int64_t* d_targets;
+    float* d_loss;
+    float* d_stats;
+    const float* d_dloss;
+    void* d_dx;
+    int64_t dx_stride;
+    void* d_dweight;
+    int64_t dweight_stride;
+    void* d_workspace;
+    int64_t workspace_bytes;
+    float scale;
+    int32_t type;
+} mlkv_linear_cross_entropy_args;
+
+/* As mlkv_linear's. */
+int64_t mlkv_linear_cross_entropy_workspace(const mlkv_linear_cross_entropy_args* args);
+int64_t mlkv_linear_cross_entropy_backward_workspace(const mlkv_linear_cross_entropy_args* args);
+int mlkv_linear_cross_entropy(const mlkv_linear_cross_entropy_args* args, void* stream);
+int mlkv_linear_cross_entropy_backward(const mlkv_linear_cross_entropy_args* args, void* stream);
 
 /* The AdamW step of many tensors at once, in place.  Of every value, with t the
  * step's number (from 1 on):

@@ -67,7 +67,9 @@ EXPORTED_DENSE = [
     "mlkv_layer_norm", "mlkv_layer_norm_backward_workspace", "mlkv_layer_norm_backward", "mlkv_linear_workspace",
     "mlkv_linear_backward_workspace", "mlkv_linear", "mlkv_linear_backward", "mlkv_dense_sync",
     "mlkv_token_logprobs_workspace", "mlkv_token_logprobs", "mlkv_token_logprobs_backward",
-    "mlkv_adamw",
+    "mlkv_gated_linear_workspace", "mlkv_gated_linear_backward_workspace", "mlkv_gated_linear", "mlkv_gated_linear_backward",
+    "mlkv_linear_cross_entropy_workspace", "mlkv_linear_cross_entropy_backward_workspace", "mlkv_linear_cross_entropy",
+    "mlkv_linear_cross_entropy_backward", "mlkv_adamw",
 ]
 
 
@@ -117,6 +119,62 @@ class LinearArgs(ctypes.Structure):
         ("workspace_bytes", ctypes.c_int64),
         ("type", ctypes.c_int32),
         ("activation", ctypes.c_int32),
+    ]
+
+
+class GatedLinearArgs(ctypes.Structure):
+    _fields_ = [
+        ("m", ctypes.c_int64),
+        ("f", ctypes.c_int64),
+        ("k", ctypes.c_int64),
+        ("d_x", ctypes.c_void_p),
+        ("x_stride", ctypes.c_int64),
+        ("d_w_gate", ctypes.c_void_p),
+        ("w_gate_stride", ctypes.c_int64),
+        ("d_w_up", ctypes.c_void_p),
+        ("w_up_stride", ctypes.c_int64),
+        ("d_h", ctypes.c_void_p),
+        ("h_stride", ctypes.c_int64),
+        ("d_gate", ctypes.c_void_p),
+        ("gate_stride", ctypes.c_int64),
+        ("d_up", ctypes.c_void_p),
+        ("up_stride", ctypes.c_int64),
+        ("d_dh", ctypes.c_void_p),
+        ("dh_stride", ctypes.c_int64),
+        ("d_dx", ctypes.c_void_p),
+        ("dx_stride", ctypes.c_int64),
+        ("d_dw_gate", ctypes.c_void_p),
+        ("dw_gate_stride", ctypes.c_int64),
+        ("d_dw_up", ctypes.c_void_p),
+        ("dw_up_stride", ctypes.c_int64),
+        ("d_workspace", ctypes.c_void_p),
+        ("workspace_bytes", ctypes.c_int64),
+        ("type", ctypes.c_int32),
+        ("activation", ctypes.c_int32),
+    ]
+
+
+class LinearCrossEntropyArgs(ctypes.Structure):
+    _fields_ = [
+        ("n", ctypes.c_int64),
+        ("k", ctypes.c_int64),
+        ("vocab", ctypes.c_int64),
+        ("d_x", ctypes.c_void_p),
+        ("x_stride", ctypes.c_int64),
+        ("d_weight", ctypes.c_void_p),
+        ("weight_stride", ctypes.c_int64),
+        ("d_targets", ctypes.c_void_p),
+        ("d_loss", ctypes.c_void_p),
+        ("d_stats", ctypes.c_void_p),
+        ("d_dloss", ctypes.c_void_p),
+        ("d_dx", ctypes.c_void_p),
+        ("dx_stride", ctypes.c_int64),
+        ("d_dweight", ctypes.c_void_p),
+        ("dweight_stride", ctypes.c_int64),
+        ("d_workspace", ctypes.c_void_p),
+        ("workspace_bytes", ctypes.c_int64),
+        ("scale", ctypes.c_float),
+        ("type", ctypes.c_int32),
     ]
 
 
@@ -209,6 +267,10 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.mlkv_token_logprobs_workspace.argtypes = [i64, i64, i32, i32]
     lib.mlkv_token_logprobs.argtypes = [vp, i64, i32, i64, i64, vp, f32, i32, vp, vp, vp, vp, vp, vp, i64, vp]
     lib.mlkv_token_logprobs_backward.argtypes = [vp, i64, i32, i64, i64, vp, f32, vp, vp, vp, vp, vp, i64, vp]
+    for name, args in (("gated_linear", GatedLinearArgs), ("linear_cross_entropy", LinearCrossEntropyArgs)):
+        for call in (name, name + "_backward"):
+            getattr(lib, f"mlkv_{call}_workspace").argtypes = [ctypes.POINTER(args)]
+            getattr(lib, f"mlkv_{call}").argtypes = [ctypes.POINTER(args), vp]
     lib.mlkv_adamw.argtypes = [ctypes.POINTER(AdamWArgs), vp]
     for name in EXPORTED_DENSE:
         getattr(lib, name).restype = i64 if name.endswith("_workspace") else i32

@@ -30,7 +30,8 @@ BUILD = os.path.join(ROOT, "_build")
 CALLS_SOURCE = "dense_calls.cpp"
 HEADERS = [os.path.join(ROOT, "include", f) for f in ("mlkv_gpu.h", "mlkv_dense.h")]
 SOURCES = ["mlkv_index.cu", "mlkv_sort.cu", "mlkv_apply.cu", "mlkv_plan.cu", "mlkv_table.cu", "mlkv_tier.cu", "mlkv_static.cu"]
-DENSE = ["dense_norm.cu", "dense_norm_backward.cu", "dense_linear.cu", "dense_logprobs.cu", "dense_adamw.cu"]
+DENSE = ["dense_norm.cu", "dense_norm_backward.cu", "dense_linear.cu", "dense_gated.cu", "dense_xent.cu",
+         "dense_logprobs.cu", "dense_adamw.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC",
          "-Xcompiler", "-ffp-contract=off", f"-I{os.path.join(ROOT, 'include')}"]

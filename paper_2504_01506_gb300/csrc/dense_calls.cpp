@@ -34,6 +34,14 @@ struct Library {
     decltype(&mlkv_token_logprobs) token_logprobs;
     decltype(&mlkv_token_logprobs_workspace) token_logprobs_workspace;
     decltype(&mlkv_token_logprobs_backward) token_logprobs_backward;
+    decltype(&mlkv_gated_linear) gated_linear;
+    decltype(&mlkv_gated_linear_workspace) gated_linear_workspace;
+    decltype(&mlkv_gated_linear_backward) gated_linear_backward;
+    decltype(&mlkv_gated_linear_backward_workspace) gated_linear_backward_workspace;
+    decltype(&mlkv_linear_cross_entropy) linear_cross_entropy;
+    decltype(&mlkv_linear_cross_entropy_workspace) linear_cross_entropy_workspace;
+    decltype(&mlkv_linear_cross_entropy_backward) linear_cross_entropy_backward;
+    decltype(&mlkv_linear_cross_entropy_backward_workspace) linear_cross_entropy_backward_workspace;
     decltype(&mlkv_adamw) adamw;
 } lib = {};
 
@@ -287,6 +295,115 @@ PyObject* token_logprobs_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// x [m][k], w_gate and w_up [f][k], all of one 16-bit type
+bool gated_operands(PyObject* xo, PyObject* go, PyObject* uo, PyObject* act, Mat& x, mlkv_gated_linear_args& g) {
+    Mat wg, wu;
+    if (!x.read(xo) || !here(x) || x.type == MLKV_TYPE_FLOAT || !wg.read(go) || wg.device != x.device || wg.type != x.type || wg.cols != x.cols ||
+        !wu.read(uo, x, wg.rows, x.cols) || wu.type != x.type)
+        return false;
+    g = mlkv_gated_linear_args{};
+    g.m = x.rows; g.f = wg.rows; g.k = x.cols;
+    g.d_x = x.p; g.x_stride = x.stride; g.d_w_gate = wg.p; g.w_gate_stride = wg.stride; g.d_w_up = wu.p; g.w_up_stride = wu.stride;
+    g.type = x.type;
+    g.activation = (int32_t)PyLong_AsLong(act);
+    return g.activation >= MLKV_ACT_NONE;
+}
+
+// x, w_gate, w_up, activation, save_pre
+PyObject* gated_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        Mat x;
+        mlkv_gated_linear_args g;
+        if (n != 5 || !gated_operands(a[0], a[1], a[2], a[3], x, g)) return pass();
+        const bool save = truth(a[4]);
+        auto out = [&] { return make(x, {g.m, g.f}, x.scalar); };
+        const at::Tensor r[3] = {out(), save ? out() : at::Tensor(), save ? out() : at::Tensor()};
+        g.d_h = r[0].data_ptr(); g.d_gate = at_of(r[1]); g.d_up = at_of(r[2]);
+        g.h_stride = g.gate_stride = g.up_stride = g.f;
+        g.workspace_bytes = lib.gated_linear_workspace(&g);
+        const Workspace ws(x, g.workspace_bytes);
+        g.d_workspace = ws.p;
+        const int rc = lib.gated_linear(&g, stream_of(x));
+        if (rc != MLKV_OK) return PyLong_FromLong(rc);
+        return save ? tuple_of(r) : given(r[0]);
+    });
+}
+
+// dh, x, w_gate, w_up, gate, up, activation, want_dx, want_dweight
+PyObject* gated_linear_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        Mat x, dh, gate, up;
+        mlkv_gated_linear_args g;
+        if (n != 9 || !gated_operands(a[1], a[2], a[3], a[6], x, g) || !dh.read(a[0], x, g.m, g.f) || dh.type != x.type || !gate.read(a[4], x, g.m, g.f) ||
+            gate.type != x.type || !up.read(a[5], x, g.m, g.f) || up.type != x.type)
+            return pass();
+        g.d_dh = dh.p; g.dh_stride = dh.stride; g.d_gate = gate.p; g.gate_stride = gate.stride; g.d_up = up.p; g.up_stride = up.stride;
+        const bool dx = truth(a[7]), dw = truth(a[8]);
+        const at::Tensor r[3] = {dx ? make(x, {g.m, g.k}, x.scalar) : at::Tensor(), dw ? make(x, {g.f, g.k}, x.scalar) : at::Tensor(),
+                                 dw ? make(x, {g.f, g.k}, x.scalar) : at::Tensor()};
+        g.d_dx = at_of(r[0]); g.d_dw_gate = at_of(r[1]); g.d_dw_up = at_of(r[2]);
+        g.dx_stride = g.dw_gate_stride = g.dw_up_stride = g.k;
+        g.workspace_bytes = lib.gated_linear_backward_workspace(&g);
+        const Workspace ws(x, g.workspace_bytes);
+        g.d_workspace = ws.p;
+        const int rc = lib.gated_linear_backward(&g, stream_of(x));
+        return rc != MLKV_OK ? PyLong_FromLong(rc) : tuple_of(r);
+    });
+}
+
+// x [n][k] and weight [vocab][k], of one 16-bit type
+bool xent_operands(PyObject* xo, PyObject* wo, PyObject* targets, PyObject* scale, Mat& x, mlkv_linear_cross_entropy_args& g) {
+    Mat w;
+    void* t;
+    if (!x.read(xo) || !here(x) || x.type == MLKV_TYPE_FLOAT || !w.read(wo) || w.device != x.device || w.type != x.type || w.cols != x.cols ||
+        w.rows < 1 || x.cols < 1 || !PyFloat_Check(scale) || !vector_of(targets, x, x.rows, at::kLong, &t))
+        return false;
+    const double s = PyFloat_AS_DOUBLE(scale);
+    if (!(s > 0 && s < std::numeric_limits<double>::infinity())) return false;
+    g = mlkv_linear_cross_entropy_args{};
+    g.n = x.rows; g.k = x.cols; g.vocab = w.rows;
+    g.d_x = x.p; g.x_stride = x.stride; g.d_weight = w.p; g.weight_stride = w.stride; g.d_targets = (const int64_t*)t;
+    g.scale = (float)s; g.type = x.type;
+    return true;
+}
+
+// x, weight, targets, scale
+PyObject* linear_cross_entropy(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        Mat x;
+        mlkv_linear_cross_entropy_args g;
+        if (n != 4 || !xent_operands(a[0], a[1], a[2], a[3], x, g)) return pass();
+        const at::Tensor r[2] = {make(x, {g.n}, kFloat), make(x, {g.n, 2}, kFloat)};
+        g.d_loss = (float*)r[0].data_ptr(); g.d_stats = (float*)r[1].data_ptr();
+        g.workspace_bytes = lib.linear_cross_entropy_workspace(&g);
+        const Workspace ws(x, g.workspace_bytes);
+        g.d_workspace = ws.p;
+        const int rc = lib.linear_cross_entropy(&g, stream_of(x));
+        return rc != MLKV_OK ? PyLong_FromLong(rc) : tuple_of(r);
+    });
+}
+
+// dloss, x, weight, targets, stats, scale, want_dx, want_dweight
+PyObject* linear_cross_entropy_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        Mat x, stats;
+        mlkv_linear_cross_entropy_args g;
+        void* d;
+        if (n != 8 || !xent_operands(a[1], a[2], a[3], a[5], x, g) || !vector_of(a[0], x, g.n, kFloat, &d) || !stats.read(a[4], x, g.n, 2) ||
+            stats.type != MLKV_TYPE_FLOAT || stats.stride != 2)
+            return pass();
+        g.d_dloss = (const float*)d; g.d_stats = (float*)stats.p;
+        const at::Tensor r[2] = {truth(a[6]) ? make(x, {g.n, g.k}, x.scalar) : at::Tensor(), truth(a[7]) ? make(x, {g.vocab, g.k}, x.scalar) : at::Tensor()};
+        g.d_dx = at_of(r[0]); g.d_dweight = at_of(r[1]);
+        g.dx_stride = g.dweight_stride = g.k;
+        g.workspace_bytes = lib.linear_cross_entropy_backward_workspace(&g);
+        const Workspace ws(x, g.workspace_bytes);
+        g.d_workspace = ws.p;
+        const int rc = lib.linear_cross_entropy_backward(&g, stream_of(x));
+        return rc != MLKV_OK ? PyLong_FromLong(rc) : tuple_of(r);
+    });
+}
+
 // A list or a tuple of n objects (null: None).
 struct Items {
     PyObject* const* at = nullptr;
@@ -401,6 +518,14 @@ PyObject* bind(PyObject*, PyObject* path) {
     get(found.token_logprobs, "mlkv_token_logprobs");
     get(found.token_logprobs_workspace, "mlkv_token_logprobs_workspace");
     get(found.token_logprobs_backward, "mlkv_token_logprobs_backward");
+    get(found.gated_linear, "mlkv_gated_linear");
+    get(found.gated_linear_workspace, "mlkv_gated_linear_workspace");
+    get(found.gated_linear_backward, "mlkv_gated_linear_backward");
+    get(found.gated_linear_backward_workspace, "mlkv_gated_linear_backward_workspace");
+    get(found.linear_cross_entropy, "mlkv_linear_cross_entropy");
+    get(found.linear_cross_entropy_workspace, "mlkv_linear_cross_entropy_workspace");
+    get(found.linear_cross_entropy_backward, "mlkv_linear_cross_entropy_backward");
+    get(found.linear_cross_entropy_backward_workspace, "mlkv_linear_cross_entropy_backward_workspace");
     get(found.adamw, "mlkv_adamw");
     if (!ok) return PyErr_Format(PyExc_ImportError, "%s: not the library of these calls", p);
     lib = found;
@@ -409,7 +534,8 @@ PyObject* bind(PyObject*, PyObject* path) {
 
 #define CALL(f) {#f, (PyCFunction)(void (*)())(f), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {CALL(layer_norm), CALL(layer_norm_backward), CALL(linear), CALL(linear_backward), CALL(token_logprobs),
-                         CALL(token_logprobs_backward), CALL(adamw), {"bind", bind, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                         CALL(token_logprobs_backward), CALL(gated_linear), CALL(gated_linear_backward), CALL(linear_cross_entropy),
+                         CALL(linear_cross_entropy_backward), CALL(adamw), {"bind", bind, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_dense_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,350 @@
+// The gated block and its gradients (mlkv_gated_linear, mlkv_gated_linear_backward).
+//
+//   forward   g = x Wg^T,  u = x Wu^T,  h = act(g) u
+//   backward  dg = dh u act'(g),  du = dh act(g)
+//             dx = dg Wg + du Wu,  dWg = dg^T x,  dWu = du^T x
+//
+// Forward is one product (dense_product.cuh): of the rows of W that a tile takes, half
+// are Wg's and half Wu's, so that an accumulator holds both factors of the tile's
+// outputs, x is read once for both, and g and u meet in registers.  dx is one product too, of twice
+// the length along k, whose second half comes from du and Wu: its sum stays in the accumulator.
+//
+// Sums are fp32; what is rounded to 16 bits is h, the saved g and u (the slopes are
+// taken there), dg, du and the gradients, once each.
+#include "dense_product.cuh"
+
+using namespace mlkv;
+
+namespace {
+
+// Four neighbouring outputs of a row.
+struct Outputs {
+    void *h, *gate, *up;
+    int64_t h_stride, gate_stride, up_stride;
+    int32_t f, act, wide;  // wide: rows of all three can be moved 16 bytes at a time
+    template <class T>
+    __device__ __forceinline__ void put_four(const float4& g4, const float4& u4, int64_t row, int64_t col) const {
+        float2 g[2] = {make_float2(g4.x, g4.y), make_float2(g4.z, g4.w)}, u[2] = {make_float2(u4.x, u4.y), make_float2(u4.z, u4.w)};
+        auto store = [&](void* m, int64_t stride, const float2 (&v)[2]) {
+            T* at = static_cast<T*>(m) + row * stride + col;
+            if (wide && col + 4 <= f) {
+                *reinterpret_cast<uint2*>(at) = make_uint2(word_of_pair<T>(v[0]), word_of_pair<T>(v[1]));
+                return;
+            }
+            const float x[4] = {v[0].x, v[0].y, v[1].x, v[1].y};
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (col + k < f) at[k] = from_float<T>(x[k]);
+        };
+        if (gate) {
+            store(gate, gate_stride, g);
+            store(up, up_stride, u);
+        }
+        by_act(act, [&](auto a) {
+            g[0] = activate<decltype(a)::value>(g[0]);
+            g[1] = activate<decltype(a)::value>(g[1]);
+        });
+        g[0] = mul2(g[0], u[0]);
+        g[1] = mul2(g[1], u[1]);
+        store(h, h_stride, g);
+    }
+};
+
+struct Gated : Outputs {
+    static constexpr int kKind = kGated;
+    CUtensorMap second, gate_map, up_map;  // of Wu, and where g and u go
+    int32_t m;
+
+    // A warp's 32 rows of a tile, 32 outputs at a time: g at `tmem`, u HALF columns on.
+    template <class T, int HALF, class W>
+    __device__ __forceinline__ bool put(const CUtensorMap* h_map, uint32_t tmem, uint8_t* corner, int r0, int c0, int blocks, int lane,
+                                        uint32_t& turn, W wait) const {
+        if (!wait()) return false;
+#pragma unroll 1
+        for (int b = 0; b < blocks && c0 + b * 32 < f; ++b) {
+            const Place q = {r0, c0 + b * 32, m, f, lane, wide && c0 + b * 32 + 32 <= f};
+            uint32_t acc[2][32];
+            __syncwarp();
+            tmem_ld32(tmem + b * 32, acc[0]);
+            tmem_ld32(tmem + HALF + b * 32, acc[1]);
+            tmem_wait_ld();
+            float2 g[16], u[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                g[k] = make_float2(__uint_as_float(acc[0][2 * k]), __uint_as_float(acc[0][2 * k + 1]));
+                u[k] = make_float2(__uint_as_float(acc[1][2 * k]), __uint_as_float(acc[1][2 * k + 1]));
+            }
+            // The halves take turns; whoever fills one waits until its last store has read it.
+            auto out = [&](const float2 (&v)[16], const CUtensorMap* map, void* to, int64_t stride) {
+                const Half s = {corner + (turn++ & 1) * kHalf};
+                if (wide && lane == 0) tma_store_read<1>();
+                __syncwarp();
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    s.piece(lane, c) = make_uint4(word_of_pair<T>(v[4 * c]), word_of_pair<T>(v[4 * c + 1]), word_of_pair<T>(v[4 * c + 2]), word_of_pair<T>(v[4 * c + 3]));
+                if (wide) fence_async();
+                __syncwarp();
+                if (!wide) put_values(s, static_cast<T*>(to), stride, q);
+                else if (lane == 0) tma_store(map, q.c0, q.r0, smem_of(s.at));
+            };
+            if (gate) {
+                out(g, &gate_map, gate, gate_stride);
+                out(u, &up_map, up, up_stride);
+            }
+            by_act(act, [&](auto a) {
+#pragma unroll
+                for (int k = 0; k < 16; ++k) g[k] = activate<decltype(a)::value>(g[k]);
+            });
+#pragma unroll
+            for (int k = 0; k < 16; ++k) g[k] = mul2(g[k], u[k]);
+            out(g, h_map, h, h_stride);
+        }
+        return true;
+    }
+
+    // Few rows: the shares of a tile of 64 rows of each weight, [row of x j][128 sums: 64 of g, 64 of u] at `at` in
+    // the shared memory of each block of the cluster, added up in order.
+    template <class T, int BN>
+    __device__ __forceinline__ void join(const Product& p, uint32_t at, int i, int j, uint32_t rank) const {
+        const int rows = kBM / 2 / p.shares / 4, columns = min(BN, p.J - j * BN);
+        for (int q = threadIdx.x; q < rows * columns; q += 128) {
+            const int c = q / rows, r = ((int)rank * rows + q % rows) * 4;
+            float4 sum[2] = {};
+            for (int s = 0; s < p.shares; ++s)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    float4 x;
+                    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                                 : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w)
+                                 : "r"(place_in(at + (c * kBM + half * (kBM / 2) + r) * 4, s))
+                                 : "memory");
+                    sum[half] = make_float4(sum[half].x + x.x, sum[half].y + x.y, sum[half].z + x.z, sum[half].w + x.w);
+                }
+            put_four<T>(sum[0], sum[1], (int64_t)j * BN + c, (int64_t)i * (kBM / 2) + r);
+        }
+    }
+};
+
+// dx's product: the second one's operands, from block `first` of k on.
+struct Two {
+    static constexpr int kKind = kTwo;
+    CUtensorMap a, b;
+    int32_t first;
+};
+
+// The shares of the tiles that are not whole, added up in a fixed order, and what the block makes of them: four
+// outputs a thread, 2^blocks_per_tile blocks a tile of 2^(wide + 2) outputs across.
+template <class T>
+__global__ void __launch_bounds__(256) k_gated_finish(const Product p, const Outputs o, int m, int blocks_per_tile, int wide) {
+    pdl_enter();
+    const int q = (int)(blockIdx.x & ((1u << blocks_per_tile) - 1)) * 256 + threadIdx.x, across = 1 << wide;  // (vectors of 4)
+    const int64_t tile = blockIdx.x >> blocks_per_tile, high = (256 << blocks_per_tile) >> wide, tiles = p.tiles_i * p.tiles_j - p.whole;
+    const int r = q >> wide, c = q & (across - 1);
+    const float4* part = reinterpret_cast<const float4*>(p.part) + (tile * high + r) * 2 * across + c;
+    float4 g = make_float4(0.f, 0.f, 0.f, 0.f), u = g;
+#pragma unroll 4
+    for (int s = 0; s < p.shares; ++s) {
+        const float4 x = part[s * tiles * high * 2 * across], y = part[s * tiles * high * 2 * across + across];
+        g = make_float4(g.x + x.x, g.y + x.y, g.z + x.z, g.w + x.w);
+        u = make_float4(u.x + y.x, u.y + y.y, u.z + y.z, u.w + y.w);
+    }
+    int i, j;
+    tile_at(p, p.whole + (int)tile, i, j);
+    const int64_t row = i * high + r, col = ((int64_t)j * across + c) * 4;
+    if (row < m && col < o.f) o.put_four<T>(g, u, row, col);
+}
+
+// dg = dh u act'(g), du = dh act(g): a thread takes 8 columns of two rows at a time.  Bound by HBM.
+struct Slopes {
+    const void *dh, *gate, *up;
+    void *dg, *du;
+    int64_t dh_stride, gate_stride, up_stride, out_stride, rows, cols, share;
+    int32_t act;
+};
+template <class T, bool ALIGNED>
+__global__ void __launch_bounds__(256, ALIGNED ? 4 : 2) k_gated_slopes(Slopes a) {
+    pdl_enter();
+    using Row = Values<T, 8, ALIGNED>;
+    constexpr int kRows = ALIGNED ? 2 : 1;  // on their way at a time
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t c = (blockIdx.x * 32ll + lane) * 8;
+    const int n = (int)min((int64_t)8, a.cols - c);
+    const int64_t r0 = blockIdx.y * a.share, r1 = min(a.rows, r0 + a.share);
+    const T *dh = static_cast<const T*>(a.dh), *gate = static_cast<const T*>(a.gate), *up = static_cast<const T*>(a.up);
+    const Span dh_span(dh, a.rows, a.dh_stride, (int)a.cols), gate_span(gate, a.rows, a.gate_stride, (int)a.cols), up_span(up, a.rows, a.up_stride, (int)a.cols);
+    if (n <= 0) return;
+    for (int64_t r = r0 + warp; r < r1; r += 8 * kRows) {
+        typename Row::Around at[kRows][3];
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            if (r + 8 * i >= r1) continue;
+            at[i][0] = Row::around(dh + (r + 8 * i) * a.dh_stride + c, dh_span);
+            at[i][1] = Row::around(gate + (r + 8 * i) * a.gate_stride + c, gate_span);
+            at[i][2] = Row::around(up + (r + 8 * i) * a.up_stride + c, up_span);
+        }
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            if (r + 8 * i >= r1) continue;
+            Row d, g, u;
+            d.settle(at[i][0], Row::place(dh + (r + 8 * i) * a.dh_stride), n);
+            g.settle(at[i][1], Row::place(gate + (r + 8 * i) * a.gate_stride), n);
+            u.settle(at[i][2], Row::place(up + (r + 8 * i) * a.up_stride), n);
+            auto both = [&](auto act) {
+                constexpr int kAct = decltype(act)::value;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const float2 x = d.pair(q), z = g.pair(q);
+                    g.set(q, mul2(mul2(x, u.pair(q)), slope<kAct>(z)));
+                    u.set(q, mul2(x, activate<kAct>(z)));
+                }
+            };
+            if (a.act == MLKV_ACT_NONE) both(Act<MLKV_ACT_NONE>{});
+            else by_act(a.act, both);
+            *reinterpret_cast<uint4*>(static_cast<T*>(a.dg) + (r + 8 * i) * a.out_stride + c) = make_uint4(g.w[0], g.w[1], g.w[2], g.w[3]);
+            *reinterpret_cast<uint4*>(static_cast<T*>(a.du) + (r + 8 * i) * a.out_stride + c) = make_uint4(u.w[0], u.w[1], u.w[2], u.w[3]);
+        }
+    }
+}
+
+// --- host ----------------------------------------------------------------------
+
+Matrix matrix_of(const void* p, int64_t stride, int64_t rows, int64_t cols) { return {static_cast<const uint16_t*>(p), stride, rows, cols}; }
+
+struct Caller : Products {
+    void forward(const mlkv_gated_linear_args& g) {
+        if (!g.m || !g.f) return;
+        Gated x = {};
+        x.h = g.d_h; x.h_stride = g.h_stride; x.gate = g.d_gate; x.gate_stride = g.gate_stride; x.up = g.d_up; x.up_stride = g.up_stride;
+        x.f = (int32_t)g.f; x.act = g.activation; x.m = (int32_t)g.m;
+        if (!g.k) {  // (the sums are 0)
+            auto clear = [&](void* to, int64_t stride) {
+                if (run && to && cudaMemset2DAsync(to, (g.m > 1 ? stride : g.f) * 2, 0, g.f * 2, g.m, st) != cudaSuccess) rc = MLKV_ERR_CUDA;
+            };
+            clear(x.h, x.h_stride);
+            clear(x.gate, x.gate_stride);
+            clear(x.up, x.up_stride);
+            return;
+        }
+        auto on16 = [](const void* p, int64_t stride) { return !p || (reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 8 == 0); };
+        x.wide = on16(x.h, x.h_stride) && on16(x.gate, x.gate_stride) && on16(x.up, x.up_stride);
+        Matrix in = matrix_of(g.d_x, g.x_stride, g.m, g.k), wg = matrix_of(g.d_w_gate, g.w_gate_stride, g.f, g.k),
+               wu = matrix_of(g.d_w_up, g.w_up_stride, g.f, g.k), none = {};
+        align(in, wg);
+        align(wu, none);
+        const Rest r = product<Gated, false, false>(in, wg, g.m, g.f, g.k, {}, false, x, {none, wu});
+        if (!run || !r.p.part) return;
+        const int across = r.bn / 2 / 4, blocks = r.high * across / 256;
+        int wide = 0, per = 0;
+        while (1 << wide < across) ++wide;
+        while (1 << per < blocks) ++per;
+        const dim3 grid((unsigned)((int64_t)(r.p.tiles_i * r.p.tiles_j - r.p.whole) * blocks));
+        const Outputs o = x;
+        launch_kernel(true, type == MLKV_TYPE_BFLOAT ? k_gated_finish<__nv_bfloat16> : k_gated_finish<__half>, grid, dim3(256), 0, st, r.p, o, (int)g.m, per, wide);
+    }
+
+    void backward(const mlkv_gated_linear_args& g) {
+        const bool any = g.m && g.f && (g.d_dx || g.d_dw_gate || g.d_dw_up);
+        Matrix dg = {}, du = {}, none = {};
+        Matrix x = matrix_of(g.d_x, g.x_stride, g.m, g.k), wg = matrix_of(g.d_w_gate, g.w_gate_stride, g.f, g.k), wu = matrix_of(g.d_w_up, g.w_up_stride, g.f, g.k);
+        if (any) {
+            Slopes s = {};
+            s.dh = g.d_dh; s.gate = g.d_gate; s.up = g.d_up;
+            s.dh_stride = g.dh_stride; s.gate_stride = g.gate_stride; s.up_stride = g.up_stride;
+            s.rows = g.m; s.cols = g.f; s.act = g.activation;
+            s.out_stride = round_up(g.f, 8);
+            s.dg = arena.take(g.m * s.out_stride * 2);
+            s.du = arena.take(g.m * s.out_stride * 2);
+            dg = matrix_of(s.dg, s.out_stride, g.m, g.f);
+            du = matrix_of(s.du, s.out_stride, g.m, g.f);
+            if (run) {
+                const bool whole = g.f % 8 == 0 && matrix_of(s.dh, s.dh_stride, 0, 0).aligned() && matrix_of(s.gate, s.gate_stride, 0, 0).aligned() &&
+                                   matrix_of(s.up, s.up_stride, 0, 0).aligned();
+                const int64_t across = (g.f + 255) / 256, wanted = std::max<int64_t>(1, std::min<int64_t>((g.m + 15) / 16, 4ll * sms / across));
+                s.share = (g.m + wanted - 1) / wanted;
+                const dim3 grid((unsigned)across, (unsigned)((g.m + s.share - 1) / s.share));
+                const bool b = type == MLKV_TYPE_BFLOAT;
+                launch_kernel(true, whole ? (b ? k_gated_slopes<__nv_bfloat16, true> : k_gated_slopes<__half, true>)
+                                          : (b ? k_gated_slopes<__nv_bfloat16, false> : k_gated_slopes<__half, false>),
+                              grid, dim3(256), 0, st, s);
+            }
+            if (g.k) {
+                align(g.d_dw_gate || g.d_dw_up ? x : none, g.d_dx ? wg : none);
+                if (g.d_dx) align(wu, none);
+            }
+        }
+        Epilogue e = {};
+        Rest rests[3] = {};
+        if (g.d_dx) {
+            e.out = g.d_dx; e.out_stride = g.dx_stride;
+            rests[0] = product<Two, false, true>(dg, wg, g.m, g.k, g.f, e, false, {}, {du, wu});
+        }
+        // The weights' blocks take the SMs that dx has no work for as its last tiles run out.
+        const bool beside = !MLKV_PDL_TRIGGER_FIRST && rc == MLKV_OK && g.d_dx && g.m && g.f && g.k;
+        if (g.d_dw_gate) {
+            e.out = g.d_dw_gate; e.out_stride = g.dw_gate_stride;
+            rests[1] = product_of_columns(*this, dg, x, g.f, g.k, g.m, e, beside);
+        }
+        if (g.d_dw_up) {
+            e.out = g.d_dw_up; e.out_stride = g.dw_up_stride;
+            rests[2] = product_of_columns(*this, du, x, g.f, g.k, g.m, e, beside);
+        }
+        for (const Rest& r : rests) finish(r);
+    }
+};
+
+bool gated_ok(const mlkv_gated_linear_args* g) {
+    if (!g || g->m < 0 || g->f < 0 || g->k < 0) return false;
+    if (std::max(g->m, std::max(g->f, g->k)) >= (int64_t)1 << 29) return false;  // (a tile's rows, of both weights, in 32 bits)
+    if (g->type != MLKV_TYPE_BFLOAT && g->type != MLKV_TYPE_HALF) return false;
+    if (g->activation < MLKV_ACT_NONE || g->activation > MLKV_ACT_SILU) return false;
+    return rows_ok(g->d_x, g->x_stride, g->m, g->k, false) && rows_ok(g->d_w_gate, g->w_gate_stride, g->f, g->k, false) &&
+           rows_ok(g->d_w_up, g->w_up_stride, g->f, g->k, false);
+}
+bool forward_ok(const mlkv_gated_linear_args* g) {
+    return gated_ok(g) && !g->d_gate == !g->d_up && rows_ok(g->d_h, g->h_stride, g->m, g->f, false) &&
+           rows_ok(g->d_gate, g->gate_stride, g->m, g->f, true) && rows_ok(g->d_up, g->up_stride, g->m, g->f, true);
+}
+bool backward_ok(const mlkv_gated_linear_args* g) {
+    return gated_ok(g) && rows_ok(g->d_dh, g->dh_stride, g->m, g->f, false) && rows_ok(g->d_gate, g->gate_stride, g->m, g->f, false) &&
+           rows_ok(g->d_up, g->up_stride, g->m, g->f, false) && rows_ok(g->d_dx, g->dx_stride, g->m, g->k, true) &&
+           rows_ok(g->d_dw_gate, g->dw_gate_stride, g->f, g->k, true) && rows_ok(g->d_dw_up, g->dw_up_stride, g->f, g->k, true);
+}
+
+int64_t working_memory(const mlkv_gated_linear_args* g, bool backward) {
+    Caller c = {{nullptr, dense_sms(), false, g->type, {nullptr}}};
+    if (!c.sms) return -1;
+    if (backward) c.backward(*g);
+    else c.forward(*g);
+    return c.rc == MLKV_OK ? c.arena.used : -2;
+}
+int run_gated(const mlkv_gated_linear_args* g, bool backward, void* stream) {
+    const int64_t need = working_memory(g, backward);
+    if (need < 0) return need == -2 ? MLKV_ERR_UNSUPPORTED : MLKV_ERR_CUDA;
+    if (!workspace_ok(g->d_workspace, g->workspace_bytes, need)) return MLKV_ERR_INVALID;
+    Caller c = {{(cudaStream_t)stream, dense_sms(), true, g->type, {static_cast<char*>(g->d_workspace)}}};
+    if (backward) c.backward(*g);
+    else c.forward(*g);
+    if (c.rc != MLKV_OK) return c.rc;
+    return cudaGetLastError() == cudaSuccess ? MLKV_OK : MLKV_ERR_CUDA;
+}
+
+}  // namespace
+
+namespace mlkv {
+cudaError_t timeouts_of_gated(uint32_t* to, cudaStream_t st) { return cudaMemcpyFromSymbolAsync(to, g_timeouts, sizeof(*to), 0, cudaMemcpyDeviceToHost, st); }
+}  // namespace mlkv
+
+extern "C" int64_t mlkv_gated_linear_workspace(const mlkv_gated_linear_args* args) {
+    return forward_ok(args) ? working_memory(args, false) : -1;
+}
+extern "C" int64_t mlkv_gated_linear_backward_workspace(const mlkv_gated_linear_args* args) {
+    return backward_ok(args) ? working_memory(args, true) : -1;
+}
+extern "C" int mlkv_gated_linear(const mlkv_gated_linear_args* args, void* stream) {
+    MLKV_DENSE_RANGE("mlkv_gated_linear");
+    return forward_ok(args) ? run_gated(args, false, stream) : MLKV_ERR_INVALID;
+}
+extern "C" int mlkv_gated_linear_backward(const mlkv_gated_linear_args* args, void* stream) {
+    MLKV_DENSE_RANGE("mlkv_gated_linear_backward");
+    return backward_ok(args) ? run_gated(args, true, stream) : MLKV_ERR_INVALID;
+}

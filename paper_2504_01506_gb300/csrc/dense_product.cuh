@@ -1,0 +1,994 @@
+// Matrix products on the tensor cores: the kernel that the linear layer, the gated
+// block and the cross entropy of a linear layer are made of, and how its launches
+// are chosen.
+//
+// All products are D[i][j] = sum_k A[i][k] B[j][k] for operands whose rows
+// in memory run along k, or along i or j (dx: W's; dW: both), which the matrix
+// unit takes as they lie.  One kernel computes them (k_product): TMA brings
+// tiles into a ring in shared memory, one thread issues tcgen05.mma into one of
+// two accumulators in tensor memory, and 4 to 16 warps take the other one out
+// through the epilogue, whose blocks leave by TMA too.  What is between the
+// accumulator and memory goes by the product's kind (X).
+#pragma once
+
+#include <cudaTypedefs.h>
+
+#include <algorithm>
+
+#include "dense_mma.cuh"
+
+namespace mlkv {
+
+constexpr int kBM = 128;      // rows (i) of a tile
+constexpr int kBK = 64;       // values along k of a stage: 128 bytes
+
+struct Epilogue {
+    const void* bias;
+    const void* residual;
+    void* pre;
+    void* out;
+    int64_t residual_stride, pre_stride, out_stride;
+    int32_t type, act;
+    int32_t wide;       // rows of out, pre and residual can be moved 16 bytes at a time
+    const float* alpha; // null: 1; else the sums are taken times *alpha, first of all
+};
+
+struct Product {
+    int32_t I, J, blocks;            // extents; 64-value blocks along k
+    int32_t tiles_i, tiles_j;
+    int32_t whole;                   // tiles that are computed whole; of the others, in shares of k, ...
+    int32_t shares, blocks_per_share;
+    float* part;                     // ... the sums: [share][tile][rows of a tile][columns of a tile]
+    int32_t joined;                  // a tile's shares are a cluster, which adds them up itself
+    int32_t injected;                // (mlkv_debug_fail) no operands are brought
+    int32_t beside;                  // needs nothing of the launch before it, which needs nothing of its outputs
+    uint32_t idesc;
+    // The operands (rows of k values), where sums near 0 are computed again (relu's): below `doubt` of the
+    // largest beside them.
+    const void *a, *b;
+    int64_t a_stride, b_stride;
+    int32_t k;
+    float doubt;
+    int32_t add;                     // the sums in `part` are added to
+    Epilogue e;
+};
+}  // namespace mlkv
+
+namespace {
+using namespace mlkv;
+
+__device__ uint32_t g_timeouts;  // blocks in which a wait ran out (never set back: what has been told of is the host's)
+
+__device__ __forceinline__ float widen(int32_t type, uint16_t v) {
+    return type == MLKV_TYPE_BFLOAT ? __uint_as_float((uint32_t)v << 16) : __half2float(__ushort_as_half(v));
+}
+__device__ __forceinline__ uint16_t narrow(int32_t type, float v) {
+    return type == MLKV_TYPE_BFLOAT ? __bfloat16_as_ushort(__float2bfloat16_rn(v)) : __half_as_ushort(__float2half_rn(v));
+}
+
+// 1 / (1 + 2^u), two at a time, to a few units of 2^-22: what follows is rounded to 16 bits.
+__device__ __forceinline__ float2 squash(float2 u) {
+    float2 e, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.x) : "f"(u.x));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.y) : "f"(u.y));
+    e = add2(e, make_float2(1.f, 1.f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.x) : "f"(e.x));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(e.y));
+    return r;
+}
+__device__ __forceinline__ float2 splat2(float x) { return make_float2(x, x); }
+__device__ __forceinline__ float at_least(float x, float least) {  // NaN stays NaN
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(least));
+    return r;
+}
+__device__ __forceinline__ float at_most(float x, float most) {
+    float r;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(most));
+    return r;
+}
+// sigmoid(z) = squash(kSilu z);  (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2 = squash(z (kGelu + kGelu3 z^2))
+constexpr float kLog2e = 1.4426950408889634f, kSilu = -kLog2e, kGeluSlope = 1.5957691216057308f, kCube = 0.044715f;
+constexpr float kGelu = -kLog2e * kGeluSlope, kGelu3 = kGelu * kCube;
+// Of two values.  (Far below 0 the value is 0, not the product of -inf and 0.)
+template <int ACT>
+__device__ __forceinline__ float2 activate(float2 z) {
+    if (ACT == MLKV_ACT_NONE) return z;
+    if (ACT == MLKV_ACT_RELU) return make_float2(at_least(z.x, 0.f), at_least(z.y, 0.f));
+    const float2 low = make_float2(at_least(z.x, -1e4f), at_least(z.y, -1e4f));
+    if (ACT == MLKV_ACT_SILU) return mul2(low, squash(mul2(low, splat2(kSilu))));
+    return mul2(low, squash(mul2(low, fma2(mul2(low, low), splat2(kGelu3), splat2(kGelu)))));
+}
+// The slope there.  (Far from 0 it is 0 or 1, not a product with an infinite factor.)
+template <int ACT>
+__device__ __forceinline__ float2 slope(float2 z) {
+    if (ACT == MLKV_ACT_NONE) return splat2(1.f);
+    if (ACT == MLKV_ACT_RELU) return make_float2(z.x > 0.f ? 1.f : z.x != z.x ? z.x : 0.f, z.y > 0.f ? 1.f : z.y != z.y ? z.y : 0.f);
+    z = make_float2(at_most(at_least(z.x, -100.f), 100.f), at_most(at_least(z.y, -100.f), 100.f));
+    const float2 one = splat2(1.f), z2 = mul2(z, z);
+    // q + z q (1 - q) u', u the argument of the sigmoid
+    const float2 q = squash(ACT == MLKV_ACT_SILU ? mul2(z, splat2(kSilu)) : mul2(z, fma2(z2, splat2(kGelu3), splat2(kGelu))));
+    const float2 rest = mul2(mul2(z, q), fma2(q, splat2(-1.f), one));
+    return ACT == MLKV_ACT_SILU ? add2(rest, q) : fma2(rest, fma2(z2, splat2(3.f * kGeluSlope * kCube), splat2(kGeluSlope)), q);
+}
+template <int N> struct Act { static constexpr int value = N; };
+template <class F>
+__device__ __forceinline__ void by_act(int32_t act, F f) {
+    if (act == MLKV_ACT_RELU) f(Act<MLKV_ACT_RELU>{});
+    else if (act == MLKV_ACT_GELU_TANH) f(Act<MLKV_ACT_GELU_TANH>{});
+    else if (act == MLKV_ACT_SILU) f(Act<MLKV_ACT_SILU>{});
+}
+
+// What becomes of the sum at (row, col) of the output.
+__device__ __forceinline__ float finish(const Epilogue& e, float v, int64_t row, int64_t col) {
+    if (e.alpha) v *= *e.alpha;
+    if (e.bias) v += widen(e.type, static_cast<const uint16_t*>(e.bias)[col]);
+    if (e.pre) static_cast<uint16_t*>(e.pre)[row * e.pre_stride + col] = narrow(e.type, v);
+    by_act(e.act, [&](auto act) { v = activate<decltype(act)::value>(splat2(v)).x; });
+    if (e.residual) v += widen(e.type, static_cast<const uint16_t*>(e.residual)[row * e.residual_stride + col]);
+    return v;
+}
+
+// A tile: groups of 8 tiles along i by all along j, so that tiles that run at the same time share operands in L2.
+__device__ __forceinline__ void tile_at(const Product& p, int t, int& i, int& j) {
+    const int group = t / (8 * p.tiles_j), first = group * 8, size = min(8, p.tiles_i - first);
+    t -= group * 8 * p.tiles_j;
+    i = first + t % size;
+    j = t / size;
+}
+// What a block does t-th: a tile, or a share of one.
+struct Work {
+    int i, j, share, k0, k1;
+    int64_t part;  // which of the tiles' shares
+    __device__ __forceinline__ Work(const Product& p, int t, bool joined, int mine) {
+        share = joined ? mine : 0;
+        part = -1;
+        if (!joined && t >= p.whole) {
+            const int rest = p.tiles_i * p.tiles_j - p.whole;
+            part = t - p.whole;
+            share = (t - p.whole) / rest;
+            t = p.whole + (t - p.whole) % rest;
+        }
+        tile_at(p, t, i, j);
+        k0 = joined || part >= 0 ? share * p.blocks_per_share : 0;
+        k1 = joined || part >= 0 ? min(p.blocks, k0 + p.blocks_per_share) : p.blocks;
+    }
+};
+
+// 16 sums of a tile whose rows run along the output's columns: this lane's
+// column i of the output, from row j0 on.  A warp writes 32 columns of a row at a time.
+template <class T>
+__device__ __forceinline__ void put_columns(const Product& p, const uint32_t (&r)[16], int64_t i, int64_t j0) {
+    const Epilogue& e = p.e;
+#pragma unroll
+    for (int q = 0; q < 16; ++q) {
+        if (j0 + q >= p.J) break;
+        static_cast<T*>(e.out)[(j0 + q) * e.out_stride + i] = from_float<T>(finish(e, __uint_as_float(r[q]), j0 + q, i));
+    }
+}
+
+// Four sums of one row of the output, from col on, through the epilogue.
+template <class T>
+__device__ __forceinline__ void put_four(const Epilogue& e, const float4& sum, int64_t row, int64_t col, int64_t cols) {
+    if (e.wide && col + 4 <= cols) {
+        float2 v[2] = {make_float2(sum.x, sum.y), make_float2(sum.z, sum.w)};
+        if (e.alpha) v[0] = mul2(v[0], splat2(*e.alpha)), v[1] = mul2(v[1], splat2(*e.alpha));
+        uint2 x = make_uint2(0, 0);
+        if (e.residual) x = *reinterpret_cast<const uint2*>(static_cast<const T*>(e.residual) + row * e.residual_stride + col);
+        if (e.bias) {
+            const T* b = static_cast<const T*>(e.bias) + col;
+            v[0] = add2(v[0], make_float2(to_float(b[0]), to_float(b[1])));
+            v[1] = add2(v[1], make_float2(to_float(b[2]), to_float(b[3])));
+        }
+        if (e.pre)
+            *reinterpret_cast<uint2*>(static_cast<T*>(e.pre) + row * e.pre_stride + col) = make_uint2(word_of_pair<T>(v[0]), word_of_pair<T>(v[1]));
+        by_act(e.act, [&](auto act) {
+            v[0] = activate<decltype(act)::value>(v[0]);
+            v[1] = activate<decltype(act)::value>(v[1]);
+        });
+        if (e.residual) {
+            v[0] = add2(v[0], pair_of_word<T>(x.x));
+            v[1] = add2(v[1], pair_of_word<T>(x.y));
+        }
+        *reinterpret_cast<uint2*>(static_cast<T*>(e.out) + row * e.out_stride + col) = make_uint2(word_of_pair<T>(v[0]), word_of_pair<T>(v[1]));
+        return;
+    }
+    const float v[4] = {sum.x, sum.y, sum.z, sum.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (col + k < cols) static_cast<T*>(e.out)[row * e.out_stride + col + k] = from_float<T>(finish(e, v[k], row, col + k));
+}
+
+// The shares of a tile whose rows run along the output's columns, [column j][128
+// rows i] of sums at `at` in the shared memory of each block of the cluster, added
+// up in order: this block's part of the rows, four of one column a thread (of 128) at a time.
+template <class T, int BN>
+__device__ __forceinline__ void join_columns(const Product& p, uint32_t at, int i, int j, uint32_t rank) {
+    const int rows = kBM / p.shares / 4, columns = min(BN, p.J - j * BN);
+    for (int q = threadIdx.x; q < rows * columns; q += 128) {
+        const int c = q / rows, r = ((int)rank * rows + q % rows) * 4;
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int s = 0; s < p.shares; ++s) {
+            float4 x;
+            asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                         : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w)
+                         : "r"(place_in(at + (c * kBM + r) * 4, s))
+                         : "memory");
+            sum = make_float4(sum.x + x.x, sum.y + x.y, sum.z + x.z, sum.w + x.w);
+        }
+        put_four<T>(p.e, sum, (int64_t)j * BN + c, (int64_t)i * kBM + r, p.I);
+    }
+}
+
+// A warp's corner of shared memory: two halves of 32 rows by 32 values (64 bytes a
+// row, 16-byte pieces in the 64-byte swizzle: piece c of a row at c ^ (row / 2 & 3)),
+// or 32 rows by 32 sums (128 bytes a row, piece c at c ^ (row & 7)).  The lane that
+// has a row writes and reads it here without bank conflicts, TMA or, for rows that
+// it does not take, the lanes side by side move it to memory and from it.
+struct Half {
+    uint8_t* at;
+    __device__ __forceinline__ uint4& piece(int row, int c) const { return *reinterpret_cast<uint4*>(at + row * 64 + ((c ^ (row >> 1 & 3)) << 4)); }
+    __device__ __forceinline__ uint16_t& value(int row, int c) const {
+        return *reinterpret_cast<uint16_t*>(at + row * 64 + (((c >> 3) ^ (row >> 1 & 3)) << 4) + (c & 7) * 2);
+    }
+};
+constexpr int kHalf = 2048, kCorner = 2 * kHalf, kBias = 128;
+
+// A block of 32 rows by 32 columns of a matrix of 16-bit values.
+struct Place {
+    int r0, c0, rows, cols, lane;  // (from r0, c0 on; of the matrix)
+    bool whole;                    // all its columns are there, and 16 bytes of a row can be moved at a time
+};
+template <class T>
+__device__ __forceinline__ void put_values(Half s, T* m, int64_t stride, const Place& q) {
+    if (q.c0 + q.lane >= q.cols) return;
+    uint16_t* at = reinterpret_cast<uint16_t*>(m) + q.r0 * stride + q.c0 + q.lane;
+    const int n = min(32, q.rows - q.r0);
+#pragma unroll 8
+    for (int r = 0; r < n; ++r, at += stride) *at = s.value(r, q.lane);
+}
+// A block of the residual: loaded ahead of its use, then put into a half.
+template <class T>
+struct Ahead {
+    uint4 v[4];
+    __device__ __forceinline__ void load(const T* m, int64_t stride, const Place& q) {
+        if (!q.whole) return;
+        const int row = q.r0 + (q.lane >> 2);
+        const T* at = m + row * stride + q.c0 + (q.lane & 3) * 8;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (row + i * 8 < q.rows) v[i] = *reinterpret_cast<const uint4*>(at + i * 8 * stride);
+    }
+    __device__ __forceinline__ void settle(Half s, const T* m, int64_t stride, const Place& q) const {
+        if (q.whole) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s.piece(i * 8 + (q.lane >> 2), q.lane & 3) = v[i];
+        } else if (q.c0 + q.lane < q.cols) {
+            const uint16_t* at = reinterpret_cast<const uint16_t*>(m) + q.r0 * stride + q.c0 + q.lane;
+            const int n = min(32, q.rows - q.r0);
+#pragma unroll 8
+            for (int r = 0; r < n; ++r, at += stride) s.value(r, q.lane) = *at;
+        }
+    }
+};
+
+// relu's slope jumps at 0, where the matrix unit's rounding (about 2^-24 of the
+// sums on the way, every 16 values of k) decides it at random: one such value moves
+// a whole row of dx.  So of a lane's 32 values the smallest, where it is that near
+// 0, is computed again by the warp, in 64 bits.  (65,536 x 416 by 512: about 90 of
+// 33.5 million.  Of sums that go out as shares, or of 64 rows or fewer, it is not:
+// they are a few million at the most.  A column alone in its block of 32 has none
+// to be small beside, and stays as it is.  A sum of exactly 0 beside others that
+// are not always comes here, so that a weight row of zeros sends every row round:
+// 304 us with one, 2,797 with one in each 32 columns, 37 without.)
+template <class T>
+__device__ __forceinline__ void doubtful(const Product& p, float2 (&v)[16], int r0, int c0, int lane) {
+    const int columns = p.J - c0;  // (the sums past the last are 0)
+    float least = INFINITY, most = 0.f;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+        least = fminf(least, fminf(2 * k < columns ? fabsf(v[k].x) : INFINITY, 2 * k + 1 < columns ? fabsf(v[k].y) : INFINITY));
+        most = fmaxf(most, fmaxf(fabsf(v[k].x), fabsf(v[k].y)));
+    }
+    uint32_t again = __ballot_sync(0xffffffffu, r0 + lane < p.I && least < most * p.doubt && most < 1e30f);
+    if (!again) return;
+    int at = 32;  // this lane's smallest (the first one)
+#pragma unroll
+    for (int k = 15; k >= 0; --k) {
+        if (fabsf(v[k].y) == least) at = 2 * k + 1;
+        if (fabsf(v[k].x) == least) at = 2 * k;
+    }
+    for (; again; again &= again - 1) {
+        const int from = __ffs(again) - 1, c = __shfl_sync(0xffffffffu, at, from), col = c0 + c;
+        if (c == 32) continue;
+        const T *a = static_cast<const T*>(p.a) + (r0 + from) * p.a_stride, *b = static_cast<const T*>(p.b) + col * p.b_stride;
+        double sum = 0;
+#pragma unroll 4
+        for (int k = lane * 8; k + 8 <= p.k; k += 256) {  // (rows that TMA takes: on 16 bytes)
+            const uint4 x = *reinterpret_cast<const uint4*>(a + k), y = *reinterpret_cast<const uint4*>(b + k);
+            auto add = [&](uint32_t u, uint32_t w) {
+                const float2 m = mul2(pair_of_word<T>(u), pair_of_word<T>(w));  // (exact)
+                sum += (double)m.x + (double)m.y;
+            };
+            add(x.x, y.x);
+            add(x.y, y.y);
+            add(x.z, y.z);
+            add(x.w, y.w);
+        }
+        if (lane < (p.k & 7)) sum += (double)to_float(a[(p.k & ~7) + lane]) * (double)to_float(b[(p.k & ~7) + lane]);
+#pragma unroll
+        for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (p.e.bias) sum += (double)to_float(static_cast<const T*>(p.e.bias)[col]);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            if (lane == from && c == 2 * k) v[k].x = (float)sum;
+            if (lane == from && c == 2 * k + 1) v[k].y = (float)sum;
+        }
+    }
+}
+
+// A warp's 32 rows of a tile's sums, from column c0 on, 32 columns at a time: out
+// of tensor memory and through the epilogue.  `wait` returns when the sums are
+// there; the residual's first block is on its way before that, each other while
+// the one before it is worked on.  `part`: where the sums of a share go as they
+// are, this warp's part of it (rows of `stride`).
+template <class T, bool DOUBT, class W>
+__device__ __forceinline__ bool put_blocks(const Product& p, const CUtensorMap* out_map, const CUtensorMap* pre_map, uint32_t tmem,
+                                           uint8_t* corner, float* bias_at, int r0, int c0, int blocks, float* part, int stride, int lane,
+                                           uint32_t& turn, W wait) {
+    const Epilogue& e = p.e;
+    const T* residual = part ? nullptr : static_cast<const T*>(e.residual);
+    const bool biased = e.bias && !part;
+    auto place = [&](int b) { return Place{r0, c0 + b * 32, p.I, p.J, lane, e.wide && c0 + b * 32 + 32 <= p.J}; };
+    auto bias_of = [&](int b) {
+        const int c = c0 + b * 32 + lane;
+        return c < p.J ? to_float(static_cast<const T*>(e.bias)[c]) : 0.f;
+    };
+    const float alpha = e.alpha ? *e.alpha : 1.f;
+    Ahead<T> ahead;
+    float bias = 0.f;
+    if (biased) bias = bias_of(0);
+    if (residual) ahead.load(residual, e.residual_stride, place(0));
+    if (!wait()) return false;
+    const bool two = e.pre || residual;  // both halves have a use of their own; else they take turns, from tile to tile
+#pragma unroll 1
+    for (int b = 0; b < blocks && c0 + b * 32 < p.J; ++b) {
+        const Place q = place(b);
+        uint32_t acc[32];
+        __syncwarp();
+        tmem_ld32(tmem + b * 32, acc);
+        if (part) {  // (a corner's 4 KB as 32 rows of 128 bytes)
+            if (b == 0) {  // what an earlier tile has left there is still on its way
+                if (e.wide && lane == 0) tma_store_read<0>();
+                __syncwarp();
+            }
+            tmem_wait_ld();
+            auto sums = [&](int row, int c) -> uint4& { return *reinterpret_cast<uint4*>(corner + row * 128 + ((c ^ (row & 7)) << 4)); };
+#pragma unroll
+            for (int c = 0; c < 8; ++c) sums(lane, c) = make_uint4(acc[4 * c], acc[4 * c + 1], acc[4 * c + 2], acc[4 * c + 3]);
+            __syncwarp();
+            float* to = part + (lane >> 3) * stride + b * 32 + (lane & 7) * 4;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                uint4 x = sums(i * 4 + (lane >> 3), lane & 7);
+                if (p.add) {
+                    const float4 y = *reinterpret_cast<const float4*>(to + i * 4 * stride);
+                    x = make_uint4(__float_as_uint(__uint_as_float(x.x) + y.x), __float_as_uint(__uint_as_float(x.y) + y.y),
+                                   __float_as_uint(__uint_as_float(x.z) + y.z), __float_as_uint(__uint_as_float(x.w) + y.w));
+                }
+                *reinterpret_cast<uint4*>(to + i * 4 * stride) = x;
+            }
+            continue;
+        }
+        if (biased) {
+            bias_at[lane] = bias;
+            if (b + 1 < blocks) bias = bias_of(b + 1);
+        }
+        __syncwarp();
+        tmem_wait_ld();
+        float2 v[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) v[k] = make_float2(__uint_as_float(acc[2 * k]), __uint_as_float(acc[2 * k + 1]));
+        if (e.alpha) {
+#pragma unroll
+            for (int k = 0; k < 16; ++k) v[k] = mul2(v[k], splat2(alpha));
+        }
+        if (biased) {
+#pragma unroll
+            for (int k = 0; k < 16; k += 2) {
+                const float4 x = reinterpret_cast<const float4*>(bias_at)[k / 2];
+                v[k] = add2(v[k], make_float2(x.x, x.y));
+                v[k + 1] = add2(v[k + 1], make_float2(x.z, x.w));
+            }
+        }
+        if (DOUBT && p.a) doubtful<T>(p, v, r0, q.c0, lane);
+        // What a half holds goes to memory; whoever fills it next waits until it has been read.
+        auto put = [&](Half s, const CUtensorMap* map, void* m, int64_t stride) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                s.piece(lane, c) = make_uint4(word_of_pair<T>(v[4 * c]), word_of_pair<T>(v[4 * c + 1]), word_of_pair<T>(v[4 * c + 2]), word_of_pair<T>(v[4 * c + 3]));
+            if (e.wide) fence_async();
+            __syncwarp();
+            if (!e.wide) put_values(s, static_cast<T*>(m), stride, q);
+            else if (lane == 0) tma_store(map, q.c0, q.r0, smem_of(s.at));
+        };
+        auto free_half = [&](bool all) {  // all stores have read theirs, or all but the last
+            if (e.wide && lane == 0) {
+                if (all) tma_store_read<0>();
+                else tma_store_read<1>();
+            }
+            __syncwarp();
+        };
+        const Half first = {corner}, second = {corner + kHalf};
+        if (e.pre) {
+            free_half(false);
+            put(first, pre_map, e.pre, e.pre_stride);
+        }
+        if (residual) {
+            free_half(!e.pre);
+            ahead.settle(second, residual, e.residual_stride, q);
+            if (b + 1 < blocks) ahead.load(residual, e.residual_stride, place(b + 1));
+        }
+        by_act(e.act, [&](auto act) {
+#pragma unroll
+            for (int k = 0; k < 16; ++k) v[k] = activate<decltype(act)::value>(v[k]);
+        });
+        if (residual) {
+            __syncwarp();
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const uint4 x = second.piece(lane, c);
+                v[4 * c] = add2(v[4 * c], pair_of_word<T>(x.x));
+                v[4 * c + 1] = add2(v[4 * c + 1], pair_of_word<T>(x.y));
+                v[4 * c + 2] = add2(v[4 * c + 2], pair_of_word<T>(x.z));
+                v[4 * c + 3] = add2(v[4 * c + 3], pair_of_word<T>(x.w));
+            }
+            __syncwarp();
+        } else {
+            free_half(false);
+        }
+        put(two || (turn++ & 1) ? second : first, out_map, e.out, e.out_stride);
+    }
+    return true;
+}
+
+// The shared memory of a block: the ring of operand tiles, and a corner and 32
+// bias values for every epilogue warp.
+// A pair of blocks has a tile of 256 rows between them, and half of its columns' operand each.
+// (WIDE: two sums an output; 16 warps have not the registers for that.)
+template <int BN, bool SWAP, bool PAIR, bool WIDE> struct Ring {
+    // Epilogue warps.  A tile's sums take 8 warps 2.8 us to take out, 16 of them 2.1 (65,536 x 512 by k = 64: 21.3 and
+    // 17.2 us): 16 where single blocks have short k, 8 where pairs have the shared memory in more stages.
+    static constexpr int kEpilogue = SWAP || BN < 128 ? 4 : BN == 128 || PAIR || WIDE ? 8 : 16;
+    static constexpr int kThreads = (kEpilogue + 2) * 32;       // ... and the TMA warp, and the MMA warp
+    static constexpr int kA = kBM * kBK * 2, kB = (PAIR ? BN / 2 : BN) * kBK * 2, kStage = kA + kB;
+    static constexpr int kCorners = SWAP ? 0 : kEpilogue * (kCorner + kBias);
+    static constexpr int kFit = (kDenseSmem - 1024 - kCorners) / kStage;
+    static constexpr int kStages = kFit < 12 ? kFit : 12;
+    static constexpr int kBytes = kStages * kStage + kCorners + 1024;  // (aligned to 1,024 within)
+    static constexpr uint32_t kColumns = 2 * BN < 32 ? 32 : 2 * BN;
+};
+
+// Kinds of products.
+constexpr int kPlain = 0, kTwo = 1, kGated = 2, kStats = 3, kProbs = 4;
+
+// Bound by the matrix unit where k is long: 16,384 x 4,096 by k = 4,096 (pairs) 284 us, 1.94 PFLOP/s, its pipe active
+// 81 to 87% of the time.  By what L2 hands to the SMs (48 KB a block of k and tile) and the epilogue's bytes where k is
+// short: 65,536 x 512 by 416, relu and pre 41 us, 189 MB of them to HBM at 4.6 TB/s.  By the weight's bytes where rows are few: one
+// row by a weight of 4,096 x 4,096 8.3 us, 4.0 TB/s.
+//
+// A_MN, B_MN: the operand's rows run along i (j), not k.  SWAP: i runs along
+// the output's columns (few rows: the weight is the operand of 128 rows a tile).
+// PAIR: two blocks on neighbouring SMs share a tile of 256 rows.  Each holds its
+// own 128 rows of A, half of B's and its rows' sums; the first issues the
+// products of both, so that B crosses each SM's shared memory half as often.
+// X: what kind of product it is, and what only that kind needs.
+template <int BN, bool A_MN, bool B_MN, bool SWAP, bool PAIR, class T, class X>
+__global__ void __launch_bounds__(Ring<BN, SWAP, PAIR, X::kKind == kGated>::kThreads, 1)
+    k_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mb,
+              const __grid_constant__ CUtensorMap out_map, const __grid_constant__ CUtensorMap pre_map, const Product p,
+              const __grid_constant__ X x) {
+    using R = Ring<BN, SWAP, PAIR, X::kKind == kGated>;
+    constexpr int S = R::kStages, kTma = R::kEpilogue, kMma = kTma + 1, kBlocks = PAIR ? 2 : 1, kCols = BN / kBlocks;
+    extern __shared__ uint8_t raw[];
+    __shared__ __align__(8) uint64_t bars[2 * S + 5];
+    __shared__ uint32_t tmem_at;
+    __shared__ volatile int stop;
+    const uint32_t ring = (smem_of(raw) + 1023u) & ~1023u;
+    const uint32_t full = smem_of(bars), empty = full + 8 * S, done = empty + 8 * S, drained = done + 16, ended = drained + 16;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = PAIR ? cluster_rank() : 0;
+    const bool joined = SWAP && p.joined;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S; ++s) {
+            mbar_init(full + 8 * s, 1);
+            mbar_init(empty + 8 * s, 1);
+        }
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(done + 8 * s, 1);
+            mbar_init(drained + 8 * s, kBlocks * R::kEpilogue);
+        }
+        mbar_init(ended, 1);
+        stop = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        tma_prefetch(&ma);
+        tma_prefetch(&mb);
+    }
+    if (warp == kMma) tmem_alloc<PAIR>(smem_of(&tmem_at), R::kColumns);
+    tc_fence_before();
+    __syncthreads();
+    if (PAIR) cluster_sync();
+    tc_fence_after();
+    const uint32_t tmem = tmem_at;
+    // Beside the product before it: by the time this is placed, that one's blocks have all seen what is before it
+    // complete, and this reads by TMA alone (L1 holds nothing of it).
+    if (p.beside) pdl_next();
+    else pdl_enter();
+
+    // joined shares: one tile a block, its share by its place in the cluster
+    const int tiles = p.tiles_i * p.tiles_j, mine = joined ? (int)cluster_rank() : 0;
+    const int total = joined ? tiles : p.whole + (tiles - p.whole) * p.shares, first = joined ? blockIdx.x / p.shares : blockIdx.x / kBlocks;
+    const int step = joined ? tiles : gridDim.x / kBlocks;
+    if (warp == kTma) {
+        if (lane == 0 && !p.injected) {
+            uint32_t n = 0;  // stages filled
+            bool ok = true;
+            for (int t = first; t < total && ok; t += step) {
+                const Work w(p, t, joined, mine);
+                const int row = (w.i * kBlocks + (int)rank) * kBM, col = w.j * BN + (int)rank * kCols;
+                for (int k = w.k0; k < w.k1; ++k, ++n) {
+                    const uint32_t s = n % S, at = ring + s * R::kStage;
+                    if (n >= S && !(ok = mbar_wait(empty + 8 * s, (n / S - 1) & 1, &stop))) break;
+                    if (rank == 0) mbar_expect(full + 8 * s, kBlocks * R::kStage);
+                    const uint32_t bar = PAIR ? place_in(full + 8 * s, 0) : full + 8 * s;
+                    auto load = [&](uint32_t to, const CUtensorMap* m, int x, int y) {
+                        if (PAIR) tma_load_pair(to, m, x, y, bar);
+                        else tma_load(to, m, x, y, bar);
+                    };
+                    if constexpr (X::kKind == kGated) {  // the tile's rows of both weights, as one operand
+                        if constexpr (SWAP) {
+                            load(at, &ma, k * kBK, w.i * (kBM / 2));
+                            load(at + R::kA / 2, &x.second, k * kBK, w.i * (kBM / 2));
+                            load(at + R::kA, &mb, k * kBK, col);
+                        } else {
+                            load(at, &ma, k * kBK, row);
+                            if constexpr (PAIR) {
+                                load(at + R::kA, rank ? &x.second : &mb, k * kBK, w.j * (BN / 2));
+                            } else {
+                                load(at + R::kA, &mb, k * kBK, w.j * (BN / 2));
+                                load(at + R::kA + R::kB / 2, &x.second, k * kBK, w.j * (BN / 2));
+                            }
+                        }
+                        continue;
+                    }
+                    const CUtensorMap *a = &ma, *bm = &mb;
+                    int along = k;
+                    if constexpr (X::kKind == kTwo)
+                        if (k >= x.first) {  // the second product's
+                            a = &x.a;
+                            bm = &x.b;
+                            along = k - x.first;
+                        }
+                    if (A_MN)
+                        for (int b = 0; b < kBM / 64; ++b) load(at + b * 8192, a, row + b * 64, along * kBK);
+                    else
+                        load(at, a, along * kBK, row);
+                    if (B_MN)
+                        for (int b = 0; b < kCols / 64; ++b) load(at + R::kA + b * 8192, bm, col + b * 64, along * kBK);
+                    else
+                        load(at + R::kA, bm, along * kBK, col);
+                }
+            }
+            // (all have been brought: until the last has been read, the products may give up)
+            if (ok && n) ok = mbar_wait(empty + 8 * ((n - 1) % S), ((n - 1) / S) & 1, &stop);
+            if (!ok && rank == 0) {  // given up: the copies in flight still write into shared memory
+                Waited waited;
+                for (uint32_t b = n > S ? n - S : 0; b < n; ++b) mbar_drain(full + 8 * (b % S), (b / S) & 1, waited);
+            }
+        }
+    } else if (warp == kMma) {
+        if (lane == 0 && rank == 0) {
+            uint32_t n = 0, u = 0;  // stages read, accumulators used
+            bool ok = true;
+            for (int t = first; t < total && ok; t += step, ++u) {
+                const Work w(p, t, joined, mine);
+                const uint32_t acc = u & 1, d = tmem + acc * BN;
+                if (u >= 2 && !(ok = mbar_wait(drained + 8 * acc, (u / 2 - 1) & 1, &stop))) break;
+                tc_fence_after();
+                for (int k = w.k0; k < w.k1; ++k, ++n) {
+                    const uint32_t s = n % S, at = ring + s * R::kStage;
+                    if (!(ok = mbar_wait(full + 8 * s, (n / S) & 1, &stop))) break;
+                    tc_fence_after();
+                    const uint64_t da = smem_desc(at, A_MN ? 8192 : 16), db = smem_desc(at + R::kA, B_MN ? 8192 : 16);
+#pragma unroll
+                    for (int q = 0; q < kBK / 16; ++q)  // 16 values along k: 32 bytes of a row, or 16 rows
+                        tc_mma<PAIR>(d, da + q * (A_MN ? 128 : 2), db + q * (B_MN ? 128 : 2), p.idesc, k > w.k0 || q > 0);
+                    tc_commit<PAIR>(empty + 8 * s);
+                }
+                if (ok) tc_commit<PAIR>(done + 8 * acc);
+            }
+            if (!ok) {  // given up: products in flight still write into tensor memory
+                tc_commit<PAIR>(ended);
+                Waited waited;
+                mbar_drain(ended, 0, waited);
+            }
+        }
+    } else {
+        uint32_t u = 0, turn = 0;
+        const uint32_t told = PAIR ? place_in(drained, 0) : drained;
+        for (int t = first; t < total; t += step, ++u) {
+            const Work w(p, t, joined, mine);
+            const uint32_t acc = u & 1, at = tmem + acc * BN + ((uint32_t)(warp & 3) << 21);
+            auto wait = [&] {
+                const bool ok = __all_sync(0xffffffffu, mbar_wait(done + 8 * acc, (u / 2) & 1, &stop));
+                tc_fence_after();
+                return ok;
+            };
+            const int in_tile = (int)rank * kBM + (warp & 3) * 32, r0 = w.i * kBlocks * kBM + in_tile;
+            if constexpr (SWAP) {
+                if (!wait()) break;
+#pragma unroll 1
+                for (int c = 0; c < BN; c += 16) {
+                    uint32_t r[16];
+                    __syncwarp();
+                    tmem_ld16(at + c, r);
+                    tmem_wait_ld();
+                    if (joined) {  // where the ring was: all of it has been read
+                        const bool any = w.k0 < w.k1;
+#pragma unroll
+                        for (int q = 0; q < 16; ++q)
+                            reinterpret_cast<uint32_t*>(raw + (ring - smem_of(raw)))[(c + q) * kBM + warp * 32 + lane] = any ? r[q] : 0u;
+                    } else if (r0 + lane < p.I) {
+                        put_columns<T>(p, r, r0 + lane, (int64_t)w.j * BN + c);
+                    }
+                }
+            } else {
+                const int cols = BN * 4 / R::kEpilogue, c = (warp >> 2) * cols;  // this warp's
+                uint8_t* corners = raw + (ring - smem_of(raw)) + S * R::kStage;
+                const int blocks = r0 < p.I ? cols / 32 : 0;
+                bool ok = true;
+                if constexpr (X::kKind == kStats) {
+                    ok = x.template put<T>(p, at + c, r0 + lane, w.j * BN + c, blocks, w.j * (R::kEpilogue / 4) + (warp >> 2), wait);
+                } else if constexpr (X::kKind == kProbs) {
+                    ok = x.template put<T>(p, &out_map, at + c, corners + warp * kCorner, r0, w.j * BN + c, blocks, lane, turn, wait);
+                } else if (X::kKind == kGated && w.part < 0) {
+                    if constexpr (X::kKind == kGated)  // (half of the columns: of each a gate's and, BN / 2 on, the other factor's sum)
+                        ok = x.template put<T, BN / 2>(&out_map, at + c / 2, corners + warp * kCorner, r0, w.j * (BN / 2) + c / 2, blocks / 2, lane, turn, wait);
+                } else {
+                float* part = w.part < 0 ? nullptr : p.part + (w.part * kBlocks * kBM + in_tile) * BN + c;
+                ok = put_blocks<T, !A_MN && !B_MN && X::kKind == kPlain>(p, &out_map, &pre_map, at + c, corners + warp * kCorner,
+                                   reinterpret_cast<float*>(corners + R::kEpilogue * kCorner + warp * kBias), r0, w.j * BN + c,
+                                   blocks, part, BN, lane, turn, wait);
+                }
+                if (!ok) break;
+            }
+            __syncwarp();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if (PAIR) mbar_arrive_in(told + 8 * acc);
+                else mbar_arrive(told + 8 * acc);
+            }
+        }
+    }
+    if (!SWAP && warp < R::kEpilogue && lane == 0) tma_store_done();
+    tc_fence_before();
+    __syncthreads();
+    if (joined) {
+        const Work w(p, first, true, mine);
+        cluster_sync();
+        if constexpr (X::kKind == kGated) {
+            if (warp < 4) x.template join<T, BN>(p, ring, w.i, w.j, mine);
+        } else if (warp < 4) {
+            join_columns<T, BN>(p, ring, w.i, w.j, mine);
+        }
+    }
+    if (PAIR || joined) cluster_sync();  // nothing of this block's memory is wanted by another any more
+    tc_fence_after();
+    if (threadIdx.x == 0 && stop) atomicAdd(&g_timeouts, 1u);
+    if (warp == kMma) tmem_free<PAIR>(tmem, R::kColumns);
+    if (p.beside) pdl_enter_last();  // whoever waits for this grid waits for those before it
+}
+}  // namespace
+
+// --- host ----------------------------------------------------------------------
+namespace mlkv {
+
+inline PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encode() {
+    static const PFN_cuTensorMapEncodeTiled_v12000 fn = [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult q = cudaDriverEntryPointSymbolNotFound;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &q) != cudaSuccess ||
+            q != cudaDriverEntryPointSuccess)
+            f = nullptr;
+        return (PFN_cuTensorMapEncodeTiled_v12000)f;
+    }();
+    return fn;
+}
+
+inline int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
+constexpr int64_t kAlign = 256;
+
+// Working memory handed out in order; with base == nullptr only counted.
+struct Arena {
+    char* base;
+    int64_t used = 0;
+    void* take(int64_t bytes) {
+        void* p = base ? base + used : nullptr;
+        used += round_up(bytes, kAlign);
+        return p;
+    }
+};
+
+struct Matrix {
+    const uint16_t* p;
+    int64_t stride, rows, cols;
+    bool aligned() const { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 8 == 0; }
+};
+
+// A second pair of operands (kTwo), or one operand (kGated: rows beside the first one's).
+struct Second {
+    Matrix a, b;
+};
+// Sums that are kept over several products: of every tile, up to `shares` of them.  bn, high: the first one's tiles.
+struct Kept {
+    float* part;
+    int32_t shares, add, bn, high;
+};
+
+// What a product leaves to another launch: shares to be added up.
+struct Rest {
+    Product p;
+    int high, bn;
+};
+
+struct Products {
+    cudaStream_t st;
+    int sms;
+    bool run;        // false: only count the working memory
+    int32_t type;
+    Arena arena;
+    int rc = MLKV_OK;
+    unsigned blocks_for(int64_t items) const { return (unsigned)std::max<int64_t>(1, std::min<int64_t>((items + 255) / 256, 16ll * sms)); }
+
+    // Two matrices as TMA takes them.
+    void align(Matrix& a, Matrix& b);
+    // The shares of a product's tiles, added up.
+    void finish_shares(const Product& p, int high, int bn);
+
+    bool encode(CUtensorMap* map, const Matrix& m, bool mn, int rows) {
+        return encode(map, m, 64, mn ? kBK : rows, CU_TENSOR_MAP_SWIZZLE_128B);
+    }
+    bool encode(CUtensorMap* map, const Matrix& m, int across, int down, CUtensorMapSwizzle swizzle) {
+        const auto fn = tensor_map_encode();
+        if (!fn) return false;
+        const cuuint64_t dims[2] = {(cuuint64_t)m.cols, (cuuint64_t)m.rows}, strides[1] = {(cuuint64_t)m.stride * 2};
+        const cuuint32_t box[2] = {(cuuint32_t)across, (cuuint32_t)down}, step[2] = {1, 1};
+        return fn(map, type == MLKV_TYPE_BFLOAT ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
+                  const_cast<uint16_t*>(m.p), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    }
+
+    template <int BN, bool A_MN, bool B_MN, bool SWAP, bool PAIR, class X>
+    void launch(const Matrix& a, const Matrix& b, const Second& more, Product p, X x) {
+        using R = Ring<BN, SWAP, PAIR, X::kKind == kGated>;
+        constexpr bool kBoth = X::kKind == kGated;  // (two matrices' rows in an operand: half of them each)
+        constexpr int kRowsA = kBoth && SWAP ? kBM / 2 : kBM, kRowsB = PAIR || (kBoth && !SWAP) ? BN / 2 : BN;
+        CUtensorMap ma, mb;
+        bool ok = encode(&ma, a, A_MN, kRowsA) && encode(&mb, b, B_MN, kRowsB);
+        if constexpr (X::kKind == kTwo) ok = ok && encode(&x.a, more.a, A_MN, kBM) && encode(&x.b, more.b, B_MN, kRowsB);
+        if constexpr (kBoth) ok = ok && encode(&x.second, SWAP ? more.a : more.b, false, SWAP ? kRowsA : kRowsB);
+        CUtensorMap out = ma, pre = ma;  // (not looked at where the epilogue does not store by TMA)
+        auto stored = [&](CUtensorMap* map, const void* m, int64_t stride, int64_t rows, int64_t cols) {
+            ok = ok && encode(map, {static_cast<const uint16_t*>(m), stride, rows, cols}, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B);
+        };
+        if constexpr (kBoth) {
+            if (!SWAP && x.wide) {
+                stored(&out, x.h, x.h_stride, p.I, x.f);
+                if (x.gate) stored(&x.gate_map, x.gate, x.gate_stride, p.I, x.f), stored(&x.up_map, x.up, x.up_stride, p.I, x.f);
+            }
+        } else if (!SWAP && X::kKind != kStats && p.e.wide) {
+            stored(&out, p.e.out, p.e.out_stride, p.I, p.J);
+            if (p.e.pre) stored(&pre, p.e.pre, p.e.pre_stride, p.I, p.J);
+        }
+        if (!ok) {
+            rc = MLKV_ERR_CUDA;
+            return;
+        }
+        p.injected = take_injected_product();
+        p.idesc = mma_desc(type == MLKV_TYPE_BFLOAT, A_MN, B_MN, PAIR ? 2 * kBM : kBM, BN);
+        const int64_t all = (int64_t)p.tiles_i * p.tiles_j, tiles = p.joined ? all * p.shares : p.whole + (all - p.whole) * p.shares;
+        auto go = [&](auto kernel) {
+            if (!dense_smem(kernel, R::kBytes)) rc = MLKV_ERR_CUDA;
+            else if (PAIR) launch_clusters(kernel, 2, 2 * std::min<int64_t>(tiles, sms / 2), R::kThreads, R::kBytes, st, ma, mb, out, pre, p, x);
+            else if (p.joined) launch_clusters(kernel, p.shares, tiles, R::kThreads, R::kBytes, st, ma, mb, out, pre, p, x);
+            else launch_kernel(true, kernel, dim3((unsigned)std::min<int64_t>(tiles, sms)), dim3(R::kThreads), R::kBytes, st, ma, mb, out, pre, p, x);
+        };
+        if (type == MLKV_TYPE_BFLOAT) go(k_product<BN, A_MN, B_MN, SWAP, PAIR, __nv_bfloat16, X>);
+        else go(k_product<BN, A_MN, B_MN, SWAP, PAIR, __half, X>);
+    }
+
+    // Whether pairs of blocks take the tiles of 256 columns: where there are enough for every pair, and k is long
+    // enough for the products to count beside the epilogue.  (Single blocks / pairs, us: 16,384 x 4,096 by k = 4,096
+    // 331 / 298; 8,192 x 1,024 by 8,192 102 / 86; 4,096 x 4,096 by 1,024 32 / 29; 65,536 x 512 by 416 37 / 42.)
+    bool pair_pays(int64_t tiles_i, int64_t tiles_j, int64_t blocks) const {
+        return blocks >= 12 && (tiles_i + 1) / 2 * tiles_j * (blocks / 12) >= sms / 2;
+    }
+
+    // The time, in us, of `rounds` of work after one another, each of a tile of bn columns (and 128 rows a block) and
+    // `blocks` blocks of k, on `busy` SMs: what a width takes besides k, once; a block of k, by its operands' latency,
+    // their bytes through L2 on all those SMs, or the matrix unit's rate.
+    static float time_of(int64_t rounds, int bn, int64_t blocks, int64_t busy, bool pair) {
+        constexpr float kLatency = 0.25f, kL2 = 15e6f;
+        const float fixed = bn == 64 ? 5.f : bn == 128 ? 6.5f : 8.5f, bytes = (float)(kBM + (pair ? bn / 2 : bn)) * kBK * 2;
+        const float block = std::max(rounds > 1 ? 0.f : kLatency, std::max((float)busy * bytes / kL2, 0.34f * bn / 256));
+        return fixed + (float)(rounds * blocks) * block;
+    }
+    // The launch that adds shares of tiles up.
+    static float time_to_finish(int64_t tiles, int64_t shares, int high, int bn) {
+        constexpr float kLaunch = 4.f, kBytes = 6e6f;
+        return kLaunch + (float)((shares + 1) * tiles * high * bn) * 4 / kBytes;
+    }
+    // Tiles (the last ones) whose k is shared out, and their shares, of at least 4 blocks: where the tiles do not fill
+    // the GPU, or its last round.  (Gradients of a 4,096 x 4,096 weight over 16,384 rows: 256 tiles on 76 pairs of SMs.)
+    struct Split { int64_t tiles, shares; float time; };
+    Split split(int64_t tiles, int high, int bn, int64_t blocks) const {
+        const bool pair = high > kBM;
+        const int64_t places = pair ? sms / 2 : sms, full = tiles / places, rest = tiles % places;
+        const int64_t busy = full ? sms : rest * (pair ? 2 : 1);
+        Split best = {0, 1, time_of(full + (rest > 0), bn, blocks, busy, pair)};
+        const float before = full ? time_of(full, bn, blocks, busy, pair) : 0.f;
+        if (!rest) return best;
+        auto look = [&](int64_t s) {
+            const int64_t rounds = (rest * s + places - 1) / places;
+            if (s < 2 || s * 4 > blocks || rounds >= s) return;
+            const float t = before + time_of(rounds, bn, (blocks + s - 1) / s, std::min(rest * s, places) * (pair ? 2 : 1), pair) + time_to_finish(rest, s, high, bn);
+            if (t < best.time) best = {rest, s, t};
+        };
+        for (int64_t s = std::min(places / rest, blocks / 4); s > 1; s /= 2) look(s);  // within a round
+        for (int64_t r = 2; r <= 4 && full; ++r) look(r * places / rest);               // the most in r short ones
+        return best;
+    }
+    // The width of single blocks' tiles, where the narrower ones fit on the GPU at once.  (Widths of 256 / 128 / 64 at
+    // their best, us: 300 x 1,000 by k = 520 9.7 / 7.8 / 7.2; 1,000 x 1,000 by 1,000 12.8 / 9.9 / 8.3; 200 x 512 by 8,192
+    // 12.3 / 10.5 / 10.3; 512 x 512 by 8,000 13.1 / 12.4 / 14.6; 4,096 x 1,000 by 776 14.6 / 16.0 / 21.0.)
+    int width(int64_t rows, int64_t cols, int64_t blocks) const {
+        int best = cols <= 64 ? 64 : cols <= 128 ? 128 : 256;
+        float least = 3e38f;
+        for (int bn = 64; bn <= 256; bn *= 2) {
+            const int64_t tiles = (rows + kBM - 1) / kBM * ((cols + bn - 1) / bn);
+            if (tiles <= sms) {
+                const float t = split(tiles, kBM, bn, blocks).time;
+                if (t < least) {
+                    least = t;
+                    best = bn;
+                }
+            }
+            if (bn >= cols) break;
+        }
+        return best;
+    }
+
+    void finish(const Rest& r) {
+        if (r.p.part) finish_shares(r.p, r.high, r.bn);
+    }
+
+    // The width of tiles that are all computed whole, by one launch.
+    int whole_width(int64_t rows, int64_t cols, int64_t blocks) const {
+        int best = 256;
+        float least = 3e38f;
+        for (int bn = 256; bn >= 64; bn /= 2) {
+            const int64_t tiles = (rows + kBM - 1) / kBM * ((cols + bn - 1) / bn), rounds = (tiles + sms - 1) / sms;
+            const float t = time_of(rounds, bn, blocks, std::min<int64_t>(tiles, sms), false);
+            if (t < least) {
+                least = t;
+                best = bn;
+            }
+        }
+        return best;
+    }
+
+    // out = epilogue(A B^T): A [rows][k], B [cols][k]; *_mn: held as [k][rows], [k][cols].
+    // kTwo: A B^T + A' B'^T, k values each.  kGated: cols of each of B and B', and what x says.  kStats, kProbs: tiles
+    // are computed whole.  kept: the sums go there as they are, all in its shares, and no epilogue is run.
+    template <class X, bool A_MN, bool B_MN>
+    Rest product(Matrix a, Matrix b, int64_t rows, int64_t cols, int64_t k, Epilogue e, bool beside = false, X x = {}, Second more = {}, Kept kept = {}) {
+        if (!rows || !cols) return {};
+        constexpr bool kWholeTiles = X::kKind == kStats || X::kKind == kProbs, kBoth = X::kKind == kGated;
+        e.type = type;
+        auto wide = [](const void* p, int64_t stride) { return !p || (reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 8 == 0); };
+        e.wide = wide(e.out, e.out_stride) && wide(e.pre, e.pre_stride) && wide(e.residual, e.residual_stride);
+        const bool swap = !A_MN && !kWholeTiles && rows <= 64 && k > 0 && !kept.shares;  // few rows: the wide operand fills the tiles' 128 rows
+        const int64_t all_cols = kBoth ? 2 * cols : cols;
+        Product p = {};
+        p.I = (int32_t)(swap ? cols : rows);
+        p.J = (int32_t)(swap ? rows : all_cols);
+        p.blocks = (int32_t)((k + kBK - 1) / kBK);
+        if constexpr (X::kKind == kTwo) {
+            x.first = p.blocks;
+            p.blocks *= 2;
+        }
+        p.e = e;
+        if (X::kKind == kPlain && !A_MN && !B_MN && !swap && e.act == MLKV_ACT_RELU) {
+            p.a = a.p; p.a_stride = a.stride; p.b = b.p; p.b_stride = b.stride;
+            p.k = (int32_t)k;
+            p.doubt = (float)p.blocks / (1 << 22);
+        }
+        const int64_t down = kBoth && swap ? (cols + 63) / 64 : ((int64_t)p.I + kBM - 1) / kBM;
+        const bool pair = kept.bn ? kept.high > kBM : !swap && all_cols > 128 && pair_pays(down, (p.J + 255) / 256, p.blocks);
+        const int bn = kept.bn ? kept.bn : swap ? (rows <= 16 ? 16 : rows <= 32 ? 32 : 64) : pair ? 256 : kWholeTiles ? whole_width(rows, cols, p.blocks) : width(rows, all_cols, p.blocks);
+        const int64_t across = (p.J + bn - 1) / bn, high = pair ? 2 * kBM : kBM, tiles = (pair ? (down + 1) / 2 : down) * across;
+        if (tiles >= (int64_t)1 << 30) {
+            rc = MLKV_ERR_UNSUPPORTED;
+            return {};
+        }
+        p.tiles_i = (int32_t)(tiles / across);
+        p.tiles_j = (int32_t)across;
+        if (kBoth) (swap ? p.I : p.J) = (int32_t)(swap ? down * kBM : across * bn);  // (whole tiles: x.f is the outputs' end)
+        p.whole = (int32_t)tiles;
+        p.shares = 1;
+        if (k == 0) {
+            p.whole = p.shares = 0;
+            if (!kBoth) finish_shares(p, (int)high, bn);
+            return {};
+        }
+        if (swap) {
+            // few rows: k in shares of at least 4 blocks, those of a tile a cluster (of 2, 4 or 8), one tile a block
+            int n = 1;
+            while (n < 8 && 2 * n <= std::min<int64_t>(sms / tiles, p.blocks / 4)) n *= 2;
+            p.shares = n;
+            p.joined = n > 1 || kBoth;
+            p.blocks_per_share = (p.blocks + n - 1) / n;  // (the last may be of nothing)
+        } else if (kept.shares) {
+            p.whole = 0;
+            p.blocks_per_share = (p.blocks + kept.shares - 1) / kept.shares;
+            p.shares = (p.blocks + p.blocks_per_share - 1) / p.blocks_per_share;
+            p.part = kept.part;
+            p.add = kept.add;
+        } else if (!kWholeTiles) {
+            const Split s = split(tiles, (int)high, bn, p.blocks);
+            if (s.shares > 1) {
+                p.whole = (int32_t)(tiles - s.tiles);
+                p.blocks_per_share = (int32_t)((p.blocks + s.shares - 1) / s.shares);
+                p.shares = (p.blocks + p.blocks_per_share - 1) / p.blocks_per_share;
+                p.part = static_cast<float*>(arena.take(s.tiles * p.shares * high * bn * 4));
+            }
+        }
+        p.beside = beside;
+        const Rest rest = {p, (int)high, bn};
+        if (!run) return rest;
+        if constexpr (!A_MN && !kWholeTiles) {
+            if (swap) {
+                const Second turned = {more.b, more.a};
+                if (bn == 16) launch<16, B_MN, false, true, false>(b, a, turned, p, x);
+                else if (bn == 32) launch<32, B_MN, false, true, false>(b, a, turned, p, x);
+                else launch<64, B_MN, false, true, false>(b, a, turned, p, x);
+            }
+        }
+        if (!swap) {
+            if (bn == 64) launch<64, A_MN, B_MN, false, false>(a, b, more, p, x);
+            else if (bn == 128) launch<128, A_MN, B_MN, false, false>(a, b, more, p, x);
+            else if (pair) launch<256, A_MN, B_MN, false, true>(a, b, more, p, x);
+            else launch<256, A_MN, B_MN, false, false>(a, b, more, p, x);
+        }
+        return rest;
+    }
+};
+
+struct Plain {
+    static constexpr int kKind = kPlain;
+};
+
+inline bool rows_ok(const void* p, int64_t stride, int64_t rows, int64_t cols, bool may_be_null) {
+    if (!p) return may_be_null || rows == 0 || cols == 0;
+    return stride >= cols && stride < (int64_t)1 << 38;  // (TMA's strides have 40 bits)
+}
+
+// Products of other operators, by dense_linear.cu's kernels: A [rows][k] times B held as [k][cols] (product_of_rows),
+// or both held along k (product_of_columns).
+Rest product_of_rows(Products& c, const Matrix& a, const Matrix& b, int64_t rows, int64_t cols, int64_t k, const Epilogue& e, const Kept& kept);
+Rest product_of_columns(Products& c, const Matrix& a, const Matrix& b, int64_t rows, int64_t cols, int64_t k, const Epilogue& e, bool beside);
+// The count of waits that ran out in the products' kernels of a file, on its way to the host.
+cudaError_t timeouts_of_gated(uint32_t* to, cudaStream_t st);
+cudaError_t timeouts_of_xent(uint32_t* to, cudaStream_t st);
+}  // namespace mlkv

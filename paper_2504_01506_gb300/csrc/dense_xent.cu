@@ -1,0 +1,385 @@
+// The cross entropy of a linear layer, without its logits (mlkv_linear_cross_entropy,
+// mlkv_linear_cross_entropy_backward).
+//
+//   forward   z = s x W^T,  loss_i = log sum_v exp(z_iv) - z_it
+//   backward  P_iv = s dl_i (exp(z_iv - lse_i) - [v = t_i]),  dx = P W,  dW = P^T x
+//
+// Forward is a product (dense_product.cuh) whose epilogue keeps of the 64 to 128 logits of
+// a row that a warp takes out their largest and the sum of exponentials against it; a second
+// kernel joins these, in a fixed order.  Backward goes over pieces of the vocabulary: a
+// piece's logits again, with P as the epilogue, then P's two products.  dx is
+// the sum over the pieces: it stays in fp32 until the last.
+//
+// P is rounded to the operands' type, times a power of two that brings the largest
+// |s dl| to 2^13 .. 2^14, which its products' epilogues take back: in fp16 a probability
+// of 1e-5 times a gradient of 1e-4 would be 0.
+#include "dense_product.cuh"
+
+using namespace mlkv;
+
+namespace {
+
+constexpr float kLog2 = 0.6931471805599453f;
+
+// Forward: the largest of the logits that a warp takes of each row, and the sum.
+struct Stats {
+    static constexpr int kKind = kStats;
+    float2* part;            // [part][rows]: (max, sum of exp(scale (z - max)))
+    float* target_logit;     // [rows]
+    const int64_t* targets;
+    float rate;              // scale / log 2
+    int32_t rows, v0;        // v0: the first column's token
+
+    template <class T, class W>
+    __device__ __forceinline__ bool put(const Product& p, uint32_t tmem, int row, int c0, int blocks, int which, W wait) const {
+        const bool mine = row < rows;
+        const int64_t target = blocks && mine ? targets[row] - v0 : -1;
+        if (!wait()) return false;
+        float most = -INFINITY, sum = 0.f;
+#pragma unroll 1
+        for (int b = 0; b < blocks && c0 + b * 32 < p.J; ++b) {
+            uint32_t acc[32];
+            __syncwarp();
+            tmem_ld32(tmem + b * 32, acc);
+            tmem_wait_ld();
+            const int at = c0 + b * 32, n = p.J - at;
+            float v[32];
+#pragma unroll
+            for (int k = 0; k < 32; ++k) v[k] = __uint_as_float(acc[k]);
+            if (n < 32) {
+#pragma unroll
+                for (int k = 0; k < 32; ++k)
+                    if (k >= n) v[k] = -INFINITY;
+            }
+            const int64_t place = target - at;
+            if (__any_sync(0xffffffffu, place >= 0 && place < 32)) {
+                float z = 0.f;
+#pragma unroll
+                for (int k = 0; k < 32; ++k)
+                    if (place == k) z = v[k];
+                if (place >= 0 && place < 32 && place < n) target_logit[row] = z;
+            }
+            float top = v[0];
+#pragma unroll
+            for (int k = 1; k < 32; ++k) top = fmaxf(top, v[k]);
+            if (top > most) {
+                sum *= exp2f((most - top) * rate);  // (of -inf: 0)
+                most = top;
+            }
+            const float from = most == -INFINITY ? 0.f : most;
+            float2 s[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                float2 d = mul2(add2(make_float2(v[2 * k], v[2 * k + 1]), splat2(-from)), splat2(rate));
+                asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(d.x));
+                asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(d.y));
+                s[k & 1] = add2(s[k & 1], d);
+            }
+            s[0] = add2(s[0], s[1]);
+            sum += s[0].x + s[0].y;
+        }
+        if (mine && blocks) part[(int64_t)which * rows + row] = make_float2(most, sum);
+        return true;
+    }
+};
+
+// Backward: what a row needs.
+struct RowOf {
+    float max, logs;  // of the logits before the scale; log2 of the sum of exponentials
+    float g;          // scale times the loss's gradient, times the power of two
+    int32_t target;
+};
+struct Probs {
+    static constexpr int kKind = kProbs;
+    const RowOf* of;
+    float rate;
+    int32_t rows, v0;
+
+    template <class T, class W>
+    __device__ __forceinline__ bool put(const Product& p, const CUtensorMap* map, uint32_t tmem, uint8_t* corner, int r0, int c0, int blocks, int lane,
+                                        uint32_t& turn, W wait) const {
+        RowOf r = {0.f, 0.f, 0.f, -1};
+        if (blocks && r0 + lane < rows) {
+            const uint4 w = *reinterpret_cast<const uint4*>(of + r0 + lane);
+            r = {__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), (int32_t)w.w};
+        }
+        if (!wait()) return false;
+#pragma unroll 1
+        for (int b = 0; b < blocks && c0 + b * 32 < p.J; ++b) {
+            const int at = c0 + b * 32;
+            uint32_t acc[32];
+            __syncwarp();
+            tmem_ld32(tmem + b * 32, acc);
+            tmem_wait_ld();
+            float2 v[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                float2 d = add2(make_float2(__uint_as_float(acc[2 * k]), __uint_as_float(acc[2 * k + 1])), splat2(-r.max));
+                d = fma2(d, splat2(rate), splat2(-r.logs));
+                asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(d.x));
+                asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(d.y));
+                v[k] = mul2(d, splat2(r.g));
+            }
+            const int place = r.target - v0 - at;
+            if (__any_sync(0xffffffffu, place >= 0 && place < 32)) {
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                    if (place == 2 * k) v[k].x -= r.g;
+                    if (place == 2 * k + 1) v[k].y -= r.g;
+                }
+            }
+            const Half s = {corner + (turn++ & 1) * kHalf};
+            if (lane == 0) tma_store_read<1>();
+            __syncwarp();
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                s.piece(lane, c) = make_uint4(word_of_pair<T>(v[4 * c]), word_of_pair<T>(v[4 * c + 1]), word_of_pair<T>(v[4 * c + 2]), word_of_pair<T>(v[4 * c + 3]));
+            fence_async();
+            __syncwarp();
+            if (lane == 0) tma_store(map, at, r0, smem_of(s.at));
+        }
+        return true;
+    }
+};
+
+// The statistics of a row out of its parts': 2^log_threads threads a row.  Of several pieces of the vocabulary each
+// adds its own to what the ones before it have left in `stats`; the last one makes the loss.
+struct Join {
+    const float2* part;
+    const float* target_logit;
+    const int64_t* targets;
+    float* loss;
+    float2* stats;
+    float scale, rate;
+    int32_t rows, parts, vocab, log_threads, first, last;
+};
+__device__ __forceinline__ float2 joined(float2 a, float2 b, float rate) {  // (max, sum), a's before b's
+    const float most = fmaxf(a.x, b.x);
+    if (most == -INFINITY) return make_float2(most, a.y + b.y);  // (0, or NaN)
+    // (equal ones apart: inf - inf)
+    return make_float2(most, a.y * (a.x == most ? 1.f : exp2f((a.x - most) * rate)) + b.y * (b.x == most ? 1.f : exp2f((b.x - most) * rate)));
+}
+__global__ void __launch_bounds__(256) k_xent_join(Join a) {
+    pdl_enter();
+    __shared__ float2 of[256];
+    const int per = 256 >> a.log_threads, row = blockIdx.x * per + threadIdx.x % per, share = threadIdx.x / per;
+    float2 s = make_float2(-INFINITY, 0.f);
+    if (row < a.rows)
+#pragma unroll 4
+        for (int q = share; q < a.parts; q += 1 << a.log_threads) s = joined(s, a.part[(int64_t)q * a.rows + row], a.rate);
+    of[threadIdx.x] = s;
+    for (int step = 1 << a.log_threads >> 1; step; step >>= 1) {
+        __syncthreads();
+        if (share < step) of[threadIdx.x] = joined(of[threadIdx.x], of[threadIdx.x + step * per], a.rate);
+    }
+    if (share || row >= a.rows) return;
+    s = of[threadIdx.x];
+    if (!a.first) s = joined(a.stats[row], s, a.rate);
+    if (!a.last) {
+        a.stats[row] = s;
+        return;
+    }
+    const float logs = logf(s.y);
+    a.stats[row] = make_float2(s.x, logs);
+    const int64_t t = a.targets[row];
+    float loss = 0.f;
+    if (t >= a.vocab) loss = NAN;
+    else if (t >= 0) {
+        const float z = a.target_logit[row];
+        loss = s.x == -INFINITY || z == -INFINITY ? (s.y != s.y ? NAN : INFINITY) : a.scale * (s.x - z) + logs;
+    }
+    a.loss[row] = loss;
+}
+
+// Rows as the backward pass takes them, and the power of two: every block looks for the largest gradient itself.
+struct Prepare {
+    const float* dloss;
+    const float2* stats;
+    const int64_t* targets;
+    RowOf* of;
+    float* back;  // what takes the power of two out of the products
+    float scale;
+    int32_t rows, vocab;
+};
+__global__ void __launch_bounds__(1024) k_xent_rows(Prepare a) {
+    pdl_enter();
+    __shared__ uint32_t most[32];
+    auto gradient = [&](int i) { return a.targets[i] < 0 ? 0.f : a.dloss[i] * a.scale; };
+    uint32_t m = 0;
+    for (int i = threadIdx.x; i < a.rows; i += 1024) {
+        const uint32_t bits = __float_as_uint(gradient(i)) & 0x7FFFFFFFu;
+        if (bits < 0x7F800000u) m = max(m, bits);
+    }
+    m = __reduce_max_sync(0xffffffffu, m);
+    if ((threadIdx.x & 31) == 0) most[threadIdx.x >> 5] = m;
+    __syncthreads();
+    m = __reduce_max_sync(0xffffffffu, most[threadIdx.x & 31]);
+    // 2^(140 - e) brings 2^(e - 127) <= |g| to 2^13; 2^-126 .. 2^126
+    const int e = min(max(140 - (int)(m >> 23), -126), 126);
+    const float up = m ? __uint_as_float((uint32_t)(e + 127) << 23) : 1.f;
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.back = m ? __uint_as_float((uint32_t)(127 - e) << 23) : 1.f;
+    for (int i = blockIdx.x * 1024 + threadIdx.x; i < a.rows; i += gridDim.x * 1024) {
+        const float2 s = a.stats[i];
+        const int64_t t = a.targets[i];
+        RowOf r = {s.x, s.y / kLog2, gradient(i) * up, t < 0 || t >= a.vocab ? -1 : (int32_t)t};
+        if (t >= a.vocab) r.g = NAN;
+        if (s.x == -INFINITY) r = {0.f, INFINITY, 0.f, -1};  // nothing to choose from
+        a.of[i] = r;
+    }
+}
+
+// --- host ----------------------------------------------------------------------
+
+Matrix matrix_of(const void* p, int64_t stride, int64_t rows, int64_t cols) { return {static_cast<const uint16_t*>(p), stride, rows, cols}; }
+
+struct Caller : Products {
+    // Forward's parts are held for as many columns as 64 MB allow, ...
+    static constexpr int64_t kPartBytes = 64 << 20;
+    // ... P for as many as 512 MB do, 4,096 at least.
+    static constexpr int64_t kProbBytes = 512 << 20;
+
+    static Matrix rows_of(const Matrix& m, int64_t from, int64_t n) { return {m.p + from * m.stride, m.stride, n, m.cols}; }
+
+    void forward(const mlkv_linear_cross_entropy_args& g) {
+        if (!g.n) return;
+        Matrix x = matrix_of(g.d_x, g.x_stride, g.n, g.k), w = matrix_of(g.d_weight, g.weight_stride, g.vocab, g.k);
+        align(x, w);
+        // (parts of 64 columns at least)
+        const int64_t most = std::max<int64_t>(4096, kPartBytes / (8 * g.n) * 64 / 4096 * 4096), piece = std::min(g.vocab, most);
+        Stats s = {};
+        s.part = static_cast<float2*>(arena.take(round_up(piece, 256) / 64 * g.n * 8));
+        s.target_logit = static_cast<float*>(arena.take(g.n * 4));
+        s.targets = g.d_targets; s.rate = g.scale * 1.4426950408889634f; s.rows = (int32_t)g.n;
+        for (int64_t v = 0; v < g.vocab && rc == MLKV_OK; v += piece) {
+            const int64_t cols = std::min(piece, g.vocab - v);
+            s.v0 = (int32_t)v;
+            const Rest r = product<Stats, false, false>(x, rows_of(w, v, cols), g.n, cols, g.k, {}, false, s);
+            if (!run) continue;
+            Join j = {};
+            j.part = s.part; j.target_logit = s.target_logit; j.targets = g.d_targets; j.loss = g.d_loss; j.stats = reinterpret_cast<float2*>(g.d_stats);
+            j.scale = g.scale; j.rate = s.rate; j.rows = (int32_t)g.n; j.vocab = (int32_t)g.vocab;
+            const int per_warp = r.bn == 256 && r.high == kBM ? 64 : r.bn == 64 ? 64 : r.bn / 2;  // (columns that an epilogue's warp takes)
+            // (a tile past the last column has no part; those of its warps that are past it say (-inf, 0))
+            j.parts = (int32_t)(r.p.tiles_j * (r.bn / per_warp));
+            j.first = v == 0; j.last = v + cols == g.vocab;
+            while (j.log_threads < 8 && (1 << j.log_threads) * 4 < j.parts && (g.n << j.log_threads) < 256ll * 4 * sms) ++j.log_threads;
+            launch_kernel(true, k_xent_join, dim3((unsigned)((g.n + (256 >> j.log_threads) - 1) / (256 >> j.log_threads))), dim3(256), 0, st, j);
+        }
+    }
+
+    void backward(const mlkv_linear_cross_entropy_args& g) {
+        auto clear = [&](void* to, int64_t stride, int64_t rows) {
+            if (run && to && rows && cudaMemset2DAsync(to, (rows > 1 ? stride : g.k) * 2, 0, g.k * 2, rows, st) != cudaSuccess) rc = MLKV_ERR_CUDA;
+        };
+        if (!g.n) return clear(g.d_dweight, g.dweight_stride, g.vocab);
+        if (!g.d_dx && !g.d_dweight) return;
+        Matrix x = matrix_of(g.d_x, g.x_stride, g.n, g.k), w = matrix_of(g.d_weight, g.weight_stride, g.vocab, g.k);
+        align(x, w);
+        RowOf* of = static_cast<RowOf*>(arena.take(g.n * sizeof(RowOf)));
+        float* back = static_cast<float*>(arena.take(4));
+        if (run) {
+            const Prepare q = {g.d_dloss, reinterpret_cast<const float2*>(g.d_stats), g.d_targets, of, back, g.scale, (int32_t)g.n, (int32_t)g.vocab};
+            launch_kernel(true, k_xent_rows, dim3((unsigned)std::min<int64_t>((g.n + 1023) / 1024, sms)), dim3(1024), 0, st, q);
+        }
+        // Pieces of equal width, whole tiles of 256 columns.
+        const int64_t most = std::max<int64_t>(4096, kProbBytes / (2 * g.n) / 256 * 256), pieces = (g.vocab + most - 1) / most;
+        const int64_t piece = pieces == 1 ? g.vocab : round_up((g.vocab + pieces - 1) / pieces, 256);
+        const int64_t stride = round_up(piece, 8);
+        uint16_t* probs = static_cast<uint16_t*>(arena.take(g.n * stride * 2));
+        Epilogue dx = {}, dw = {};
+        dx.out = g.d_dx; dx.out_stride = g.dx_stride; dx.alpha = back;
+        dw.alpha = back;
+        Kept kept = {};
+        Rest sums = {};
+        if (pieces > 1 && g.d_dx) {
+            // dx's sums, over the pieces, in shares of a piece's columns where the tiles are too few to fill the GPU
+            const int64_t tiles = (g.n + 127) / 128 * ((g.k + 255) / 256);
+            kept.shares = (int32_t)std::max<int64_t>(1, std::min<int64_t>(4, sms / tiles));
+            kept.part = static_cast<float*>(arena.take(kept.shares * ((g.n + 255) / 256) * 256 * round_up(g.k, 256) * 4));
+        }
+        // (counting: a piece's products take the most memory in the first, the widest)
+        for (int64_t v = 0; v < g.vocab && rc == MLKV_OK; v += piece) {
+            const int64_t cols = std::min(piece, g.vocab - v), mark = arena.used;
+            const Matrix wv = rows_of(w, v, cols), p = {probs, stride, g.n, cols};
+            Probs s = {of, g.scale * 1.4426950408889634f, (int32_t)g.n, (int32_t)v};
+            Epilogue e = {};
+            e.out = probs; e.out_stride = stride;
+            product<Probs, false, false>(x, wv, g.n, cols, g.k, e, false, s);
+            Rest rests[2] = {};
+            const bool beside = !MLKV_PDL_TRIGGER_FIRST && rc == MLKV_OK && g.d_dx;
+            if (g.d_dx) {
+                kept.add = v > 0;
+                rests[0] = product_of_rows(*this, p, wv, g.n, g.k, cols, dx, kept);
+                if (kept.shares) {
+                    if (v == 0) {  // (the last piece may be narrower: its tiles are the first one's)
+                        sums = rests[0];
+                        kept.bn = sums.bn;
+                        kept.high = sums.high;
+                    }
+                    rests[0] = {};
+                }
+            }
+            if (g.d_dweight) {
+                dw.out = static_cast<uint16_t*>(g.d_dweight) + v * g.dweight_stride; dw.out_stride = g.dweight_stride;
+                rests[1] = product_of_columns(*this, p, x, cols, g.k, g.n, dw, beside);
+            }
+            for (const Rest& r : rests) finish(r);
+            if (run) arena.used = mark;
+            else top = std::max(top, arena.used), arena.used = mark;
+        }
+        finish(sums);
+    }
+    int64_t top = 0;  // the most that was held at a time
+};
+
+bool xent_ok(const mlkv_linear_cross_entropy_args* g) {
+    if (!g || g->n < 0 || g->k < 1 || g->vocab < 1 || std::max(g->n, std::max(g->k, g->vocab)) >= (int64_t)1 << 30) return false;
+    if (g->type != MLKV_TYPE_BFLOAT && g->type != MLKV_TYPE_HALF) return false;
+    if (!(g->scale > 0) || !(g->scale < INFINITY)) return false;
+    if (!rows_ok(g->d_x, g->x_stride, g->n, g->k, false) || !rows_ok(g->d_weight, g->weight_stride, g->vocab, g->k, false)) return false;
+    return !g->n || (g->d_targets && g->d_stats);
+}
+bool forward_ok(const mlkv_linear_cross_entropy_args* g) { return xent_ok(g) && (!g->n || g->d_loss); }
+bool backward_ok(const mlkv_linear_cross_entropy_args* g) {
+    return xent_ok(g) && (!g->n || g->d_dloss) && rows_ok(g->d_dx, g->dx_stride, g->n, g->k, true) &&
+           rows_ok(g->d_dweight, g->dweight_stride, g->vocab, g->k, true);
+}
+
+int64_t working_memory(const mlkv_linear_cross_entropy_args* g, bool backward) {
+    Caller c = {{nullptr, dense_sms(), false, g->type, {nullptr}}};
+    if (!c.sms) return -1;
+    if (backward) c.backward(*g);
+    else c.forward(*g);
+    return c.rc == MLKV_OK ? std::max(c.arena.used, c.top) : -2;
+}
+int run_xent(const mlkv_linear_cross_entropy_args* g, bool backward, void* stream) {
+    const int64_t need = working_memory(g, backward);
+    if (need < 0) return need == -2 ? MLKV_ERR_UNSUPPORTED : MLKV_ERR_CUDA;
+    if (!workspace_ok(g->d_workspace, g->workspace_bytes, need)) return MLKV_ERR_INVALID;
+    Caller c = {{(cudaStream_t)stream, dense_sms(), true, g->type, {static_cast<char*>(g->d_workspace)}}};
+    if (backward) c.backward(*g);
+    else c.forward(*g);
+    if (c.rc != MLKV_OK) return c.rc;
+    return cudaGetLastError() == cudaSuccess ? MLKV_OK : MLKV_ERR_CUDA;
+}
+
+}  // namespace
+
+namespace mlkv {
+cudaError_t timeouts_of_xent(uint32_t* to, cudaStream_t st) { return cudaMemcpyFromSymbolAsync(to, g_timeouts, sizeof(*to), 0, cudaMemcpyDeviceToHost, st); }
+}  // namespace mlkv
+
+extern "C" int64_t mlkv_linear_cross_entropy_workspace(const mlkv_linear_cross_entropy_args* args) {
+    return forward_ok(args) ? working_memory(args, false) : -1;
+}
+extern "C" int64_t mlkv_linear_cross_entropy_backward_workspace(const mlkv_linear_cross_entropy_args* args) {
+    return backward_ok(args) ? working_memory(args, true) : -1;
+}
+extern "C" int mlkv_linear_cross_entropy(const mlkv_linear_cross_entropy_args* args, void* stream) {
+    MLKV_DENSE_RANGE("mlkv_linear_cross_entropy");
+    return forward_ok(args) ? run_xent(args, false, stream) : MLKV_ERR_INVALID;
+}
+extern "C" int mlkv_linear_cross_entropy_backward(const mlkv_linear_cross_entropy_args* args, void* stream) {
+    MLKV_DENSE_RANGE("mlkv_linear_cross_entropy_backward");
+    return backward_ok(args) ? run_xent(args, true, stream) : MLKV_ERR_INVALID;
+}

@@ -310,6 +310,72 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, pre
     return dx, dw, db
 
 
+# -- the gated block ----------------------------------------------------------------
+def _gated_args(x, w_gate, w_up, activation):
+    """(x, w_gate, w_up, their type and device, m, f, k, the call's arguments so far)"""
+    x, m, k, x_stride = _rows(x, "x", _HALVES)
+    _on_gpu(x, "x")
+    dtype, device = x.dtype, x.device
+    w_gate, f, along, gate_stride = _rows(w_gate, "w_gate", (dtype,), None, device)
+    if along != k:
+        raise ValueError(f"w_gate must be [f, {k}], not {[f, along]}")
+    w_up, _, _, up_stride = _rows(w_up, "w_up", (dtype,), (f, k), device)
+    act = _ACTIVATIONS.get(activation)
+    if act is None:
+        raise ValueError(f"activation must be one of {', '.join(filter(None, _ACTIVATIONS))}, not {activation!r}")
+    a = L.GatedLinearArgs(m, f, k, x.data_ptr(), x_stride, w_gate.data_ptr(), gate_stride, w_up.data_ptr(), up_stride)
+    a.type = _TYPES[dtype]
+    a.activation = act
+    return x, w_gate, w_up, dtype, device, m, f, k, a
+
+
+def gated_linear(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, *, activation: str | None = "silu", save_pre: bool = False):
+    """act(x @ w_gate.T) * (x @ w_up.T), in one kernel: x [m, k], w_gate and w_up [f, k],
+    of one 16-bit type; activation as linear's.  With save_pre also the two factors'
+    sums before the activation, [m, f] each, rounded to x's type, for
+    gated_linear_backward.  Valid when sync() says so, as linear's."""
+    if (native := _native(x)) is not None:
+        r = native.gated_linear(x, w_gate, w_up, _ACTIVATIONS.get(activation, -1), save_pre)
+        if r is not NotImplemented:
+            return _done(r)
+    x, w_gate, w_up, dtype, device, m, f, k, a = _gated_args(x, w_gate, w_up, activation)
+    h = _empty((m, f), dtype=dtype, device=device)
+    a.d_h, a.h_stride = h.data_ptr(), f
+    gate = up = None
+    if save_pre:
+        gate, up = _empty((m, f), dtype=dtype, device=device), _empty((m, f), dtype=dtype, device=device)
+        a.d_gate, a.gate_stride, a.d_up, a.up_stride = gate.data_ptr(), f, up.data_ptr(), f
+    lib = L.load()
+    _run_linear(lib.mlkv_gated_linear, lib.mlkv_gated_linear_workspace, a, device)
+    return (h, gate, up) if save_pre else h
+
+
+def gated_linear_backward(dh: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, gate: torch.Tensor,
+                          up: torch.Tensor, *, activation: str | None = "silu", want_dx: bool = True, want_dweight: bool = True):
+    """Gradients (dx, dw_gate, dw_up), of x's type, of gated_linear(x, w_gate, w_up,
+    activation=...) whose save_pre gave `gate` and `up`; None where they are not wanted.
+    The factors' gradients are rounded to x's type.  Valid when sync() says so, as linear's."""
+    if (native := _native(x)) is not None:
+        r = native.gated_linear_backward(dh, x, w_gate, w_up, gate, up, _ACTIVATIONS.get(activation, -1), want_dx, want_dweight)
+        if r is not NotImplemented:
+            return _done(r)
+    x, w_gate, w_up, dtype, device, m, f, k, a = _gated_args(x, w_gate, w_up, activation)
+    dh, _, _, a.dh_stride = _rows(dh, "dh", (dtype,), (m, f), device)
+    gate, _, _, a.gate_stride = _rows(gate, "gate", (dtype,), (m, f), device)
+    up, _, _, a.up_stride = _rows(up, "up", (dtype,), (m, f), device)
+    a.d_dh, a.d_gate, a.d_up = dh.data_ptr(), gate.data_ptr(), up.data_ptr()
+    dx = dwg = dwu = None
+    if want_dx:
+        dx = _empty((m, k), dtype=dtype, device=device)
+        a.d_dx, a.dx_stride = dx.data_ptr(), k
+    if want_dweight:
+        dwg, dwu = _empty((f, k), dtype=dtype, device=device), _empty((f, k), dtype=dtype, device=device)
+        a.d_dw_gate, a.dw_gate_stride, a.d_dw_up, a.dw_up_stride = dwg.data_ptr(), k, dwu.data_ptr(), k
+    lib = L.load()
+    _run_linear(lib.mlkv_gated_linear_backward, lib.mlkv_gated_linear_backward_workspace, a, device)
+    return dx, dwg, dwu
+
+
 def sync(device=None):
     """Waits for the current stream; raises if a bounded wait inside a product's kernel
     ran out on the device, on any stream, since a call last raised for one (the
@@ -390,6 +456,72 @@ def token_logprobs_backward(logits: torch.Tensor, targets: torch.Tensor, result:
           targets.data_ptr(), scale, entropy.data_ptr(), stats.data_ptr(), None if g is None else g.data_ptr(),
           None if h is None else h.data_ptr(), out.data_ptr(), out_stride, _stream(device))
     return out
+
+
+# -- the cross entropy of a linear layer ----------------------------------------------
+class LinearCrossEntropy(typing.NamedTuple):
+    """Of every row: the loss (fp32 [n]) and the statistics the backward pass takes (fp32
+    [n, 2]: the largest logit before the scale, log of the sum of exponentials against it)."""
+    loss: torch.Tensor
+    stats: torch.Tensor
+
+
+def _xent_args(x, weight, targets, scale):
+    x, n, k, x_stride = _rows(x, "x", _HALVES)
+    _on_gpu(x, "x")
+    device = x.device
+    weight, vocab, along, weight_stride = _rows(weight, "weight", (x.dtype,), None, device)
+    if along != k or vocab < 1 or k < 1:
+        raise ValueError(f"weight must be [vocab, {k}] with at least one value, not {[vocab, along]}")
+    if not 0 < scale < float("inf"):
+        raise ValueError(f"scale must be positive and finite, not {scale}")
+    targets = _vector(targets, "targets", n, device, (torch.int64,))
+    a = L.LinearCrossEntropyArgs(n, k, vocab, x.data_ptr(), x_stride, weight.data_ptr(), weight_stride, targets.data_ptr())
+    a.scale, a.type = scale, _TYPES[x.dtype]
+    return x, weight, targets, n, k, vocab, device, a
+
+
+def linear_cross_entropy(x: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, *, scale: float = 1.0) -> LinearCrossEntropy:
+    """Of every row the cross entropy of softmax(scale * x @ weight.T) with targets[i]:
+    x [n, k], weight [vocab, k] of one 16-bit type, targets int64 [n] (negative: none,
+    loss 0).  The logits are not kept, nor rounded to 16 bits.  Valid when sync() says so,
+    as linear's."""
+    if (native := _native(x)) is not None:
+        r = native.linear_cross_entropy(x, weight, targets, scale)
+        if r is not NotImplemented:
+            return LinearCrossEntropy(*_done(r))
+    x, weight, targets, n, k, vocab, device, a = _xent_args(x, weight, targets, scale)
+    loss, stats = _empty(n, dtype=torch.float32, device=device), _empty((n, 2), dtype=torch.float32, device=device)
+    a.d_loss, a.d_stats = loss.data_ptr(), stats.data_ptr()
+    lib = L.load()
+    _run_linear(lib.mlkv_linear_cross_entropy, lib.mlkv_linear_cross_entropy_workspace, a, device)
+    return LinearCrossEntropy(loss, stats)
+
+
+def linear_cross_entropy_backward(dloss: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor,
+                                  result: LinearCrossEntropy, *, scale: float = 1.0, want_dx: bool = True, want_dweight: bool = True):
+    """Gradients (dx, dweight), of x's type, from those of the losses (fp32 [n]) that
+    linear_cross_entropy of the same arguments gave in `result`; None where they are not
+    wanted.  The logits are computed again, a piece of the vocabulary at a time, and their
+    gradients rounded to x's type.  Valid when sync() says so, as linear's."""
+    if (native := _native(x)) is not None:
+        r = native.linear_cross_entropy_backward(dloss, x, weight, targets, result.stats, scale, want_dx, want_dweight)
+        if r is not NotImplemented:
+            return _done(r)
+    x, weight, targets, n, k, vocab, device, a = _xent_args(x, weight, targets, scale)
+    dloss = _vector(dloss, "dloss", n, device, (torch.float32,))
+    stats = _rows(result.stats, "result.stats", (torch.float32,), (n, 2), device)[0].contiguous()
+    a.d_dloss, a.d_stats = dloss.data_ptr(), stats.data_ptr()
+    dx = dw = None
+    if want_dx:
+        dx = _empty((n, k), dtype=x.dtype, device=device)
+        a.d_dx, a.dx_stride = dx.data_ptr(), k
+    if want_dweight:
+        dw = _empty((vocab, k), dtype=x.dtype, device=device)
+        a.d_dweight, a.dweight_stride = dw.data_ptr(), k
+    lib = L.load()
+    _run_linear(lib.mlkv_linear_cross_entropy_backward, lib.mlkv_linear_cross_entropy_backward_workspace, a, device)
+    return dx, dw
 
 
 # -- AdamW ------------------------------------------------------------------------------
