@@ -132,6 +132,14 @@ struct Two {
     int32_t first;
 };
 
+// The weights' products: the second factor's gradients and where dWu goes.
+struct Twin {
+    static constexpr int kKind = kTwin;
+    CUtensorMap a, out;
+    void* to;
+    int64_t to_stride;
+};
+
 // The shares of the tiles that are not whole, added up in a fixed order, and what the block makes of them: four
 // outputs a thread, 2^blocks_per_tile blocks a tile of 2^(wide + 2) outputs across.
 template <class T>
@@ -152,6 +160,22 @@ __global__ void __launch_bounds__(256) k_gated_finish(const Product p, const Out
     tile_at(p, p.whole + (int)tile, i, j);
     const int64_t row = i * high + r, col = ((int64_t)j * across + c) * 4;
     if (row < m && col < o.f) o.put_four<T>(g, u, row, col);
+}
+
+// The activation and its slope, with one exponential and one division of each value.
+template <int ACT>
+__device__ __forceinline__ void act_and_slope(float2 z, float2& a, float2& s) {
+    if (ACT == MLKV_ACT_NONE || ACT == MLKV_ACT_RELU) {
+        a = activate<ACT>(z);
+        s = slope<ACT>(z);
+        return;
+    }
+    // (far from 0 the sigmoid is 0 or 1 and the slope's last term 0, not a product with an infinite factor)
+    const float2 near = make_float2(at_most(at_least(z.x, -100.f), 100.f), at_most(at_least(z.y, -100.f), 100.f)), z2 = mul2(near, near);
+    const float2 q = squash(ACT == MLKV_ACT_SILU ? mul2(near, splat2(kSilu)) : mul2(near, fma2(z2, splat2(kGelu3), splat2(kGelu))));
+    const float2 rest = mul2(mul2(near, q), fma2(q, splat2(-1.f), splat2(1.f)));
+    s = ACT == MLKV_ACT_SILU ? add2(rest, q) : fma2(rest, fma2(z2, splat2(3.f * kGeluSlope * kCube), splat2(kGeluSlope)), q);
+    a = mul2(make_float2(at_least(z.x, -100.f), at_least(z.y, -100.f)), q);
 }
 
 // dg = dh u act'(g), du = dh act(g): a thread takes 8 columns of two rows at a time.  Bound by HBM.
@@ -193,9 +217,11 @@ __global__ void __launch_bounds__(256, ALIGNED ? 4 : 2) k_gated_slopes(Slopes a)
                 constexpr int kAct = decltype(act)::value;
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const float2 x = d.pair(q), z = g.pair(q);
-                    g.set(q, mul2(mul2(x, u.pair(q)), slope<kAct>(z)));
-                    u.set(q, mul2(x, activate<kAct>(z)));
+                    const float2 x = d.pair(q);
+                    float2 y, s;
+                    act_and_slope<kAct>(g.pair(q), y, s);
+                    g.set(q, mul2(mul2(x, u.pair(q)), s));
+                    u.set(q, mul2(x, y));
                 }
             };
             if (a.act == MLKV_ACT_NONE) both(Act<MLKV_ACT_NONE>{});
@@ -229,8 +255,7 @@ struct Caller : Products {
         x.wide = on16(x.h, x.h_stride) && on16(x.gate, x.gate_stride) && on16(x.up, x.up_stride);
         Matrix in = matrix_of(g.d_x, g.x_stride, g.m, g.k), wg = matrix_of(g.d_w_gate, g.w_gate_stride, g.f, g.k),
                wu = matrix_of(g.d_w_up, g.w_up_stride, g.f, g.k), none = {};
-        align(in, wg);
-        align(wu, none);
+        align(in, wg, wu);
         const Rest r = product<Gated, false, false>(in, wg, g.m, g.f, g.k, {}, false, x, {none, wu});
         if (!run || !r.p.part) return;
         const int across = r.bn / 2 / 4, blocks = r.high * across / 256;
@@ -268,25 +293,29 @@ struct Caller : Products {
                               grid, dim3(256), 0, st, s);
             }
             if (g.k) {
-                align(g.d_dw_gate || g.d_dw_up ? x : none, g.d_dx ? wg : none);
-                if (g.d_dx) align(wu, none);
+                Matrix none2 = {};
+                align(g.d_dw_gate || g.d_dw_up ? x : none, g.d_dx ? wg : none, g.d_dx ? wu : none2);
             }
         }
         Epilogue e = {};
-        Rest rests[3] = {};
+        Rest rests[2] = {};
         if (g.d_dx) {
             e.out = g.d_dx; e.out_stride = g.dx_stride;
             rests[0] = product<Two, false, true>(dg, wg, g.m, g.k, g.f, e, false, {}, {du, wu});
         }
         // The weights' blocks take the SMs that dx has no work for as its last tiles run out.
         const bool beside = !MLKV_PDL_TRIGGER_FIRST && rc == MLKV_OK && g.d_dx && g.m && g.f && g.k;
-        if (g.d_dw_gate) {
-            e.out = g.d_dw_gate; e.out_stride = g.dw_gate_stride;
+        e.out = g.d_dw_gate; e.out_stride = g.dw_gate_stride;
+        if (g.d_dw_gate && g.d_dw_up) {
+            Twin both = {};
+            both.to = g.d_dw_up;
+            both.to_stride = g.dw_up_stride;
+            rests[1] = product<Twin, true, true>(dg, x, g.f, g.k, g.m, e, beside, both, {du, none});
+        } else if (g.d_dw_gate) {
             rests[1] = product_of_columns(*this, dg, x, g.f, g.k, g.m, e, beside);
-        }
-        if (g.d_dw_up) {
+        } else if (g.d_dw_up) {
             e.out = g.d_dw_up; e.out_stride = g.dw_up_stride;
-            rests[2] = product_of_columns(*this, du, x, g.f, g.k, g.m, e, beside);
+            rests[1] = product_of_columns(*this, du, x, g.f, g.k, g.m, e, beside);
         }
         for (const Rest& r : rests) finish(r);
     }

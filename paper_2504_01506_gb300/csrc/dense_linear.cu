@@ -37,21 +37,27 @@ __global__ void __launch_bounds__(256) k_product_finish(const Product p, int blo
     const int q = (int)(blockIdx.x & ((1u << blocks_per_tile) - 1)) * kOf + mine;
     int i, j;
     tile_at(p, p.whole + (int)(blockIdx.x >> blocks_per_tile), i, j);
+    Epilogue e = p.e;
+    if (p.half && i >= p.half) {
+        i -= p.half;
+        e.out = p.out2;
+        e.out_stride = p.out2_stride;
+    }
     const int64_t row = (int64_t)i * ((kOf << blocks_per_tile) >> wide) + (q >> wide);
     const int64_t col = ((int64_t)j << (wide + 2)) + (q & ((1 << wide) - 1)) * 4;
-    if (row < p.I && col < p.J) put_four<T>(p.e, sum, row, col, p.J);
+    if (row < p.I && col < p.J) put_four<T>(e, sum, row, col, p.J);
 }
 
-// Rows whose stride or place TMA does not take (multiples of 16 bytes), laid out anew: up to two matrices at a time.
+// Rows whose stride or place TMA does not take (multiples of 16 bytes), laid out anew: up to three matrices at a time.
 // Bound by latency at the sizes met (4,099 x 777 and 1,001 x 777: 6 us, 16 MB), by HBM above.
 struct Align {
     const uint16_t* in;
     uint16_t* out;
     int64_t stride, out_stride, rows, cols;
 };
-__global__ void __launch_bounds__(256) k_align(Align a, Align b) {
+__global__ void __launch_bounds__(256) k_align(Align a, Align b, Align c) {
     pdl_enter();
-    const Align m = blockIdx.y ? b : a;
+    const Align m = blockIdx.y == 0 ? a : blockIdx.y == 1 ? b : c;
     const Span span(m.in, m.rows, m.stride, (int)m.cols);
     const int64_t per = m.out_stride / 8, step = gridDim.x * 256ll;
     for (int64_t at = blockIdx.x * 256ll + threadIdx.x; at < m.rows * per; at += step) {
@@ -283,9 +289,13 @@ int run_linear(const mlkv_linear_args* g, bool backward, void* stream) {
 
 namespace mlkv {
 void Products::align(Matrix& a, Matrix& b) {
-    Align to[2] = {};
+    Matrix none = {};
+    align(a, b, none);
+}
+void Products::align(Matrix& a, Matrix& b, Matrix& c) {
+    Align to[3] = {};
     int n = 0;
-    for (Matrix* m : {&a, &b}) {
+    for (Matrix* m : {&a, &b, &c}) {
         if (m->rows == 1) m->stride = round_up(m->cols, 8);  // (the one row's end is its end)
         if (m->aligned() || !m->rows || !m->cols) continue;
         const int64_t stride = round_up(m->cols, 8);
@@ -294,15 +304,15 @@ void Products::align(Matrix& a, Matrix& b) {
         *m = {p, stride, m->rows, m->cols};
     }
     if (!run || !n) return;
-    const int64_t vectors = std::max(to[0].rows * to[0].out_stride, to[1].rows * to[1].out_stride) / 8;
-    launch_kernel(true, k_align, dim3(blocks_for(vectors), n), dim3(256), 0, st, to[0], to[1]);
+    const int64_t vectors = std::max({to[0].rows * to[0].out_stride, to[1].rows * to[1].out_stride, to[2].rows * to[2].out_stride}) / 8;
+    launch_kernel(true, k_align, dim3(blocks_for(vectors), n), dim3(256), 0, st, to[0], to[1], to[2]);
 }
-void Products::finish_shares(const Product& p, int high, int bn) {
-    if (!run) return;
+void Products::finish_shares(const Product& p, int64_t tiles, int high, int bn) {
+    if (!run || !tiles) return;
     const int groups = p.shares >= 8 ? 4 : 1, blocks = high * bn / 1024 * groups, wide = bn == 64 ? 4 : bn == 128 ? 5 : 6;
     int per = 0;
     while (1 << per < blocks) ++per;
-    const dim3 grid((unsigned)((int64_t)(p.tiles_i * p.tiles_j - p.whole) * blocks));
+    const dim3 grid((unsigned)(tiles * blocks));
     const bool b = type == MLKV_TYPE_BFLOAT;
     const auto kernel = groups == 4 ? (b ? k_product_finish<__nv_bfloat16, 4> : k_product_finish<__half, 4>)
                                     : (b ? k_product_finish<__nv_bfloat16, 1> : k_product_finish<__half, 1>);

@@ -49,7 +49,10 @@ struct Product {
     int64_t a_stride, b_stride;
     int32_t k;
     float doubt;
-    int32_t add;                     // the sums in `part` are added to
+    int32_t kept, add;               // every tile's sums go to `part` (those of tile t < whole to place t - whole), or are added there
+    int32_t half;                    // not 0: tiles from there on along i are another matrix's, at out2
+    void* out2;
+    int64_t out2_stride;
     Epilogue e;
 };
 }  // namespace mlkv
@@ -139,19 +142,21 @@ __device__ __forceinline__ void tile_at(const Product& p, int t, int& i, int& j)
 // What a block does t-th: a tile, or a share of one.
 struct Work {
     int i, j, share, k0, k1;
-    int64_t part;  // which of the tiles' shares
+    int64_t part;  // which of the tiles' shares (kNone: none)
+    static constexpr int64_t kNone = (int64_t)1 << 62;
     __device__ __forceinline__ Work(const Product& p, int t, bool joined, int mine) {
         share = joined ? mine : 0;
-        part = -1;
-        if (!joined && t >= p.whole) {
+        part = !joined && p.kept ? t - p.whole : kNone;
+        const bool shared = !joined && t >= p.whole;
+        if (shared) {
             const int rest = p.tiles_i * p.tiles_j - p.whole;
             part = t - p.whole;
             share = (t - p.whole) / rest;
             t = p.whole + (t - p.whole) % rest;
         }
         tile_at(p, t, i, j);
-        k0 = joined || part >= 0 ? share * p.blocks_per_share : 0;
-        k1 = joined || part >= 0 ? min(p.blocks, k0 + p.blocks_per_share) : p.blocks;
+        k0 = joined || shared ? share * p.blocks_per_share : 0;
+        k1 = joined || shared ? min(p.blocks, k0 + p.blocks_per_share) : p.blocks;
     }
 };
 
@@ -335,7 +340,7 @@ __device__ __forceinline__ void doubtful(const Product& p, float2 (&v)[16], int 
 template <class T, bool DOUBT, class W>
 __device__ __forceinline__ bool put_blocks(const Product& p, const CUtensorMap* out_map, const CUtensorMap* pre_map, uint32_t tmem,
                                            uint8_t* corner, float* bias_at, int r0, int c0, int blocks, float* part, int stride, int lane,
-                                           uint32_t& turn, W wait) {
+                                           uint32_t& turn, void* to_matrix, int64_t to_stride, W wait) {
     const Epilogue& e = p.e;
     const T* residual = part ? nullptr : static_cast<const T*>(e.residual);
     const bool biased = e.bias && !part;
@@ -447,7 +452,7 @@ __device__ __forceinline__ bool put_blocks(const Product& p, const CUtensorMap* 
         } else {
             free_half(false);
         }
-        put(two || (turn++ & 1) ? second : first, out_map, e.out, e.out_stride);
+        put(two || (turn++ & 1) ? second : first, out_map, to_matrix, to_stride);
     }
     return true;
 }
@@ -463,14 +468,15 @@ template <int BN, bool SWAP, bool PAIR, bool WIDE> struct Ring {
     static constexpr int kThreads = (kEpilogue + 2) * 32;       // ... and the TMA warp, and the MMA warp
     static constexpr int kA = kBM * kBK * 2, kB = (PAIR ? BN / 2 : BN) * kBK * 2, kStage = kA + kB;
     static constexpr int kCorners = SWAP ? 0 : kEpilogue * (kCorner + kBias);
-    static constexpr int kFit = (kDenseSmem - 1024 - kCorners) / kStage;
+    // (two blocks an SM where a block's start is a large part of its time)
+    static constexpr int kFit = ((SWAP && WIDE ? kDenseSmem / 2 : kDenseSmem) - 1024 - kCorners) / kStage;
     static constexpr int kStages = kFit < 12 ? kFit : 12;
     static constexpr int kBytes = kStages * kStage + kCorners + 1024;  // (aligned to 1,024 within)
     static constexpr uint32_t kColumns = 2 * BN < 32 ? 32 : 2 * BN;
 };
 
 // Kinds of products.
-constexpr int kPlain = 0, kTwo = 1, kGated = 2, kStats = 3, kProbs = 4;
+constexpr int kPlain = 0, kTwo = 1, kTwin = 2, kGated = 3, kStats = 4, kProbs = 5;
 
 // Bound by the matrix unit where k is long: 16,384 x 4,096 by k = 4,096 (pairs) 284 us, 1.94 PFLOP/s, its pipe active
 // 81 to 87% of the time.  By what L2 hands to the SMs (48 KB a block of k and tile) and the epilogue's bytes where k is
@@ -490,6 +496,8 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR, X::kKind == kGated>::kThr
               const __grid_constant__ X x) {
     using R = Ring<BN, SWAP, PAIR, X::kKind == kGated>;
     constexpr int S = R::kStages, kTma = R::kEpilogue, kMma = kTma + 1, kBlocks = PAIR ? 2 : 1, kCols = BN / kBlocks;
+    uint32_t brought = kBlocks * R::kStage;  // bytes a stage
+    if constexpr (!PAIR && (X::kKind == kStats || X::kKind == kProbs)) brought = x.a_rows * kBK * 2 + R::kB;  // (of few rows no more than there are)
     extern __shared__ uint8_t raw[];
     __shared__ __align__(8) uint64_t bars[2 * S + 5];
     __shared__ uint32_t tmem_at;
@@ -535,11 +543,12 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR, X::kKind == kGated>::kThr
             bool ok = true;
             for (int t = first; t < total && ok; t += step) {
                 const Work w(p, t, joined, mine);
-                const int row = (w.i * kBlocks + (int)rank) * kBM, col = w.j * BN + (int)rank * kCols;
+                const bool twin = X::kKind == kTwin && w.i >= p.half;
+                const int row = ((twin ? w.i - p.half : w.i) * kBlocks + (int)rank) * kBM, col = w.j * BN + (int)rank * kCols;
                 for (int k = w.k0; k < w.k1; ++k, ++n) {
                     const uint32_t s = n % S, at = ring + s * R::kStage;
                     if (n >= S && !(ok = mbar_wait(empty + 8 * s, (n / S - 1) & 1, &stop))) break;
-                    if (rank == 0) mbar_expect(full + 8 * s, kBlocks * R::kStage);
+                    if (rank == 0) mbar_expect(full + 8 * s, brought);
                     const uint32_t bar = PAIR ? place_in(full + 8 * s, 0) : full + 8 * s;
                     auto load = [&](uint32_t to, const CUtensorMap* m, int x, int y) {
                         if (PAIR) tma_load_pair(to, m, x, y, bar);
@@ -563,6 +572,8 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR, X::kKind == kGated>::kThr
                     }
                     const CUtensorMap *a = &ma, *bm = &mb;
                     int along = k;
+                    if constexpr (X::kKind == kTwin)
+                        if (twin) a = &x.a;
                     if constexpr (X::kKind == kTwo)
                         if (k >= x.first) {  // the second product's
                             a = &x.a;
@@ -624,7 +635,8 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR, X::kKind == kGated>::kThr
                 tc_fence_after();
                 return ok;
             };
-            const int in_tile = (int)rank * kBM + (warp & 3) * 32, r0 = w.i * kBlocks * kBM + in_tile;
+            const int in_tile = (int)rank * kBM + (warp & 3) * 32;
+            const int r0 = (X::kKind == kTwin && w.i >= p.half ? w.i - p.half : w.i) * kBlocks * kBM + in_tile;
             if constexpr (SWAP) {
                 if (!wait()) break;
 #pragma unroll 1
@@ -651,14 +663,23 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR, X::kKind == kGated>::kThr
                     ok = x.template put<T>(p, at + c, r0 + lane, w.j * BN + c, blocks, w.j * (R::kEpilogue / 4) + (warp >> 2), wait);
                 } else if constexpr (X::kKind == kProbs) {
                     ok = x.template put<T>(p, &out_map, at + c, corners + warp * kCorner, r0, w.j * BN + c, blocks, lane, turn, wait);
-                } else if (X::kKind == kGated && w.part < 0) {
+                } else if (X::kKind == kGated && w.part == Work::kNone) {
                     if constexpr (X::kKind == kGated)  // (half of the columns: of each a gate's and, BN / 2 on, the other factor's sum)
                         ok = x.template put<T, BN / 2>(&out_map, at + c / 2, corners + warp * kCorner, r0, w.j * (BN / 2) + c / 2, blocks / 2, lane, turn, wait);
                 } else {
-                float* part = w.part < 0 ? nullptr : p.part + (w.part * kBlocks * kBM + in_tile) * BN + c;
-                ok = put_blocks<T, !A_MN && !B_MN && X::kKind == kPlain>(p, &out_map, &pre_map, at + c, corners + warp * kCorner,
+                float* part = w.part == Work::kNone ? nullptr : p.part + (w.part * kBlocks * kBM + in_tile) * BN + c;
+                const CUtensorMap* to = &out_map;
+                void* matrix = p.e.out;
+                int64_t stride = p.e.out_stride;
+                if constexpr (X::kKind == kTwin)
+                    if (w.i >= p.half) {
+                        to = &x.out;
+                        matrix = p.out2;
+                        stride = p.out2_stride;
+                    }
+                ok = put_blocks<T, !A_MN && !B_MN && X::kKind == kPlain>(p, to, &pre_map, at + c, corners + warp * kCorner,
                                    reinterpret_cast<float*>(corners + R::kEpilogue * kCorner + warp * kBias), r0, w.j * BN + c,
-                                   blocks, part, BN, lane, turn, wait);
+                                   blocks, part, BN, lane, turn, matrix, stride, wait);
                 }
                 if (!ok) break;
             }
@@ -730,10 +751,11 @@ struct Matrix {
 struct Second {
     Matrix a, b;
 };
-// Sums that are kept over several products: of every tile, up to `shares` of them.  bn, high: the first one's tiles.
+// Sums that are kept over several products, of equal tiles; the first one's say which are shared out (`rest`, `shares`).
 struct Kept {
+    bool on, add;
     float* part;
-    int32_t shares, add, bn, high;
+    int32_t rest, shares, bn, high;
 };
 
 // What a product leaves to another launch: shares to be added up.
@@ -751,10 +773,11 @@ struct Products {
     int rc = MLKV_OK;
     unsigned blocks_for(int64_t items) const { return (unsigned)std::max<int64_t>(1, std::min<int64_t>((items + 255) / 256, 16ll * sms)); }
 
-    // Two matrices as TMA takes them.
+    // Matrices as TMA takes them.
     void align(Matrix& a, Matrix& b);
-    // The shares of a product's tiles, added up.
-    void finish_shares(const Product& p, int high, int bn);
+    void align(Matrix& a, Matrix& b, Matrix& c);
+    // The shares of `tiles` of a product's tiles, from p.whole on, added up.
+    void finish_shares(const Product& p, int64_t tiles, int high, int bn);
 
     bool encode(CUtensorMap* map, const Matrix& m, bool mn, int rows) {
         return encode(map, m, 64, mn ? kBK : rows, CU_TENSOR_MAP_SWIZZLE_128B);
@@ -773,11 +796,14 @@ struct Products {
     void launch(const Matrix& a, const Matrix& b, const Second& more, Product p, X x) {
         using R = Ring<BN, SWAP, PAIR, X::kKind == kGated>;
         constexpr bool kBoth = X::kKind == kGated;  // (two matrices' rows in an operand: half of them each)
-        constexpr int kRowsA = kBoth && SWAP ? kBM / 2 : kBM, kRowsB = PAIR || (kBoth && !SWAP) ? BN / 2 : BN;
+        int rows_a = kBoth && SWAP ? kBM / 2 : kBM;
+        if constexpr (!PAIR && (X::kKind == kStats || X::kKind == kProbs)) rows_a = x.a_rows;
+        constexpr int kRowsB = PAIR || (kBoth && !SWAP) ? BN / 2 : BN;
         CUtensorMap ma, mb;
-        bool ok = encode(&ma, a, A_MN, kRowsA) && encode(&mb, b, B_MN, kRowsB);
+        bool ok = encode(&ma, a, A_MN, rows_a) && encode(&mb, b, B_MN, kRowsB);
         if constexpr (X::kKind == kTwo) ok = ok && encode(&x.a, more.a, A_MN, kBM) && encode(&x.b, more.b, B_MN, kRowsB);
-        if constexpr (kBoth) ok = ok && encode(&x.second, SWAP ? more.a : more.b, false, SWAP ? kRowsA : kRowsB);
+        if constexpr (kBoth) ok = ok && encode(&x.second, SWAP ? more.a : more.b, false, SWAP ? rows_a : kRowsB);
+        if constexpr (X::kKind == kTwin) ok = ok && encode(&x.a, more.a, A_MN, kBM);
         CUtensorMap out = ma, pre = ma;  // (not looked at where the epilogue does not store by TMA)
         auto stored = [&](CUtensorMap* map, const void* m, int64_t stride, int64_t rows, int64_t cols) {
             ok = ok && encode(map, {static_cast<const uint16_t*>(m), stride, rows, cols}, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B);
@@ -789,6 +815,7 @@ struct Products {
             }
         } else if (!SWAP && X::kKind != kStats && p.e.wide) {
             stored(&out, p.e.out, p.e.out_stride, p.I, p.J);
+            if constexpr (X::kKind == kTwin) stored(&x.out, p.out2, p.out2_stride, p.I, p.J);
             if (p.e.pre) stored(&pre, p.e.pre, p.e.pre_stride, p.I, p.J);
         }
         if (!ok) {
@@ -870,7 +897,14 @@ struct Products {
     }
 
     void finish(const Rest& r) {
-        if (r.p.part) finish_shares(r.p, r.high, r.bn);
+        if (!r.p.part) return;
+        finish_shares(r.p, (int64_t)r.p.tiles_i * r.p.tiles_j - r.p.whole, r.high, r.bn);
+        if (!r.p.kept || !r.p.whole) return;
+        Product p = r.p;  // the tiles that are whole: one share each
+        p.part -= (int64_t)p.whole * r.high * r.bn;
+        p.whole = 0;
+        p.shares = 1;
+        finish_shares(p, r.p.whole, r.high, r.bn);
     }
 
     // The width of tiles that are all computed whole, by one launch.
@@ -888,8 +922,12 @@ struct Products {
         return best;
     }
 
+#ifndef MLKV_GATED_ROUNDS
+#define MLKV_GATED_ROUNDS 6
+#endif
+    static constexpr int64_t kGatedRounds = MLKV_GATED_ROUNDS;
     // out = epilogue(A B^T): A [rows][k], B [cols][k]; *_mn: held as [k][rows], [k][cols].
-    // kTwo: A B^T + A' B'^T, k values each.  kGated: cols of each of B and B', and what x says.  kStats, kProbs: tiles
+    // kTwo: A B^T + A' B'^T, k values each.  kTwin: also A' B^T, of as many rows, to x.to.  kGated: cols of each of B and B', and what x says.  kStats, kProbs: tiles
     // are computed whole.  kept: the sums go there as they are, all in its shares, and no epilogue is run.
     template <class X, bool A_MN, bool B_MN>
     Rest product(Matrix a, Matrix b, int64_t rows, int64_t cols, int64_t k, Epilogue e, bool beside = false, X x = {}, Second more = {}, Kept kept = {}) {
@@ -898,7 +936,7 @@ struct Products {
         e.type = type;
         auto wide = [](const void* p, int64_t stride) { return !p || (reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 8 == 0); };
         e.wide = wide(e.out, e.out_stride) && wide(e.pre, e.pre_stride) && wide(e.residual, e.residual_stride);
-        const bool swap = !A_MN && !kWholeTiles && rows <= 64 && k > 0 && !kept.shares;  // few rows: the wide operand fills the tiles' 128 rows
+        const bool swap = !A_MN && !kWholeTiles && rows <= 64 && k > 0 && !kept.on;  // few rows: the wide operand fills the tiles' 128 rows
         const int64_t all_cols = kBoth ? 2 * cols : cols;
         Product p = {};
         p.I = (int32_t)(swap ? cols : rows);
@@ -915,36 +953,49 @@ struct Products {
             p.doubt = (float)p.blocks / (1 << 22);
         }
         const int64_t down = kBoth && swap ? (cols + 63) / 64 : ((int64_t)p.I + kBM - 1) / kBM;
-        const bool pair = kept.bn ? kept.high > kBM : !swap && all_cols > 128 && pair_pays(down, (p.J + 255) / 256, p.blocks);
-        const int bn = kept.bn ? kept.bn : swap ? (rows <= 16 ? 16 : rows <= 32 ? 32 : 64) : pair ? 256 : kWholeTiles ? whole_width(rows, cols, p.blocks) : width(rows, all_cols, p.blocks);
-        const int64_t across = (p.J + bn - 1) / bn, high = pair ? 2 * kBM : kBM, tiles = (pair ? (down + 1) / 2 : down) * across;
+        const bool pair = kept.bn ? kept.high > kBM : !swap && all_cols > 128 && (X::kKind == kPlain || down > 1) && pair_pays(down, (p.J + 255) / 256, p.blocks);
+        const int bn = kept.bn ? kept.bn : swap ? (rows <= 16 ? 16 : rows <= 32 ? 32 : 64) : pair ? 256 : kWholeTiles ? whole_width(rows, cols, p.blocks) : width(X::kKind == kTwin ? 2 * rows : rows, all_cols, p.blocks);
+        const int64_t across = (p.J + bn - 1) / bn, high = pair ? 2 * kBM : kBM, tiles = (pair ? (down + 1) / 2 : down) * across * (X::kKind == kTwin ? 2 : 1);
         if (tiles >= (int64_t)1 << 30) {
             rc = MLKV_ERR_UNSUPPORTED;
             return {};
         }
         p.tiles_i = (int32_t)(tiles / across);
         p.tiles_j = (int32_t)across;
+        if constexpr (X::kKind == kTwin) {
+            p.half = p.tiles_i / 2;
+            p.out2 = x.to;
+            p.out2_stride = x.to_stride;
+            e.wide = e.wide && wide(x.to, x.to_stride);
+            p.e = e;
+        }
+        if constexpr (kWholeTiles) x.a_rows = (int32_t)std::min<int64_t>(kBM, round_up(rows, 8));
         if (kBoth) (swap ? p.I : p.J) = (int32_t)(swap ? down * kBM : across * bn);  // (whole tiles: x.f is the outputs' end)
         p.whole = (int32_t)tiles;
         p.shares = 1;
         if (k == 0) {
             p.whole = p.shares = 0;
-            if (!kBoth) finish_shares(p, (int)high, bn);
+            if (!kBoth) finish_shares(p, tiles, (int)high, bn);
             return {};
         }
         if (swap) {
             // few rows: k in shares of at least 4 blocks, those of a tile a cluster (of 2, 4 or 8), one tile a block
             int n = 1;
             while (n < 8 && 2 * n <= std::min<int64_t>(sms / tiles, p.blocks / 4)) n *= 2;
+            // (two weights: so many blocks that the last ones to run are a small part of all, while they have 8 blocks of k)
+            while (kBoth && n < 8 && 16 * n <= p.blocks && 2 * n * tiles <= kGatedRounds * sms) n *= 2;
             p.shares = n;
             p.joined = n > 1 || kBoth;
             p.blocks_per_share = (p.blocks + n - 1) / n;  // (the last may be of nothing)
-        } else if (kept.shares) {
-            p.whole = 0;
-            p.blocks_per_share = (p.blocks + kept.shares - 1) / kept.shares;
+        } else if (kept.on) {
+            Split s = {kept.rest, kept.shares, 0.f};
+            if (!kept.bn) s = split(tiles, (int)high, bn, p.blocks);
+            p.whole = (int32_t)(tiles - (s.shares > 1 ? s.tiles : 0));
+            p.blocks_per_share = (int32_t)((p.blocks + s.shares - 1) / s.shares);
             p.shares = (p.blocks + p.blocks_per_share - 1) / p.blocks_per_share;
-            p.part = kept.part;
+            p.kept = 1;
             p.add = kept.add;
+            p.part = kept.bn ? kept.part : static_cast<float*>(arena.take((p.whole + (tiles - p.whole) * p.shares) * high * bn * 4)) + (int64_t)p.whole * high * bn;
         } else if (!kWholeTiles) {
             const Split s = split(tiles, (int)high, bn, p.blocks);
             if (s.shares > 1) {

@@ -29,6 +29,7 @@ struct Stats {
     const int64_t* targets;
     float rate;              // scale / log 2
     int32_t rows, v0;        // v0: the first column's token
+    int32_t a_rows;
 
     template <class T, class W>
     __device__ __forceinline__ bool put(const Product& p, uint32_t tmem, int row, int c0, int blocks, int which, W wait) const {
@@ -94,6 +95,7 @@ struct Probs {
     const RowOf* of;
     float rate;
     int32_t rows, v0;
+    int32_t a_rows;
 
     template <class T, class W>
     __device__ __forceinline__ bool put(const Product& p, const CUtensorMap* map, uint32_t tmem, uint8_t* corner, int r0, int c0, int blocks, int lane,
@@ -291,17 +293,13 @@ struct Caller : Products {
         dw.alpha = back;
         Kept kept = {};
         Rest sums = {};
-        if (pieces > 1 && g.d_dx) {
-            // dx's sums, over the pieces, in shares of a piece's columns where the tiles are too few to fill the GPU
-            const int64_t tiles = (g.n + 127) / 128 * ((g.k + 255) / 256);
-            kept.shares = (int32_t)std::max<int64_t>(1, std::min<int64_t>(4, sms / tiles));
-            kept.part = static_cast<float*>(arena.take(kept.shares * ((g.n + 255) / 256) * 256 * round_up(g.k, 256) * 4));
-        }
+        kept.on = pieces > 1;  // dx's sums, over the pieces
         // (counting: a piece's products take the most memory in the first, the widest)
         for (int64_t v = 0; v < g.vocab && rc == MLKV_OK; v += piece) {
-            const int64_t cols = std::min(piece, g.vocab - v), mark = arena.used;
+            const int64_t cols = std::min(piece, g.vocab - v);
+            int64_t mark = arena.used;
             const Matrix wv = rows_of(w, v, cols), p = {probs, stride, g.n, cols};
-            Probs s = {of, g.scale * 1.4426950408889634f, (int32_t)g.n, (int32_t)v};
+            Probs s = {of, g.scale * 1.4426950408889634f, (int32_t)g.n, (int32_t)v, 0};
             Epilogue e = {};
             e.out = probs; e.out_stride = stride;
             product<Probs, false, false>(x, wv, g.n, cols, g.k, e, false, s);
@@ -310,11 +308,15 @@ struct Caller : Products {
             if (g.d_dx) {
                 kept.add = v > 0;
                 rests[0] = product_of_rows(*this, p, wv, g.n, g.k, cols, dx, kept);
-                if (kept.shares) {
+                if (kept.on) {
                     if (v == 0) {  // (the last piece may be narrower: its tiles are the first one's)
                         sums = rests[0];
+                        kept.part = sums.p.part;
+                        kept.rest = sums.p.tiles_i * sums.p.tiles_j - sums.p.whole;
+                        kept.shares = sums.p.shares;
                         kept.bn = sums.bn;
                         kept.high = sums.high;
+                        mark = arena.used;
                     }
                     rests[0] = {};
                 }
