@@ -27,7 +27,7 @@ using namespace mlkv;
 namespace {
 
 constexpr int kGroup = 256;                   // values a warp takes at a time, 8 a lane: a block of codes
-constexpr int kWarps = 8, kGroupsPerWarp = 4;
+constexpr int kWarps = 8, kGroupsPerWarp = 4;  // a block's part of a tensor; of small networks a quarter of that
 constexpr int kChunk = kGroup * kWarps * kGroupsPerWarp;
 
 struct Tensor {
@@ -53,10 +53,11 @@ struct Hyper {
 };
 template <int N> struct Batch {
     Hyper h;
-    int count;
+    int count, groups;  // groups a warp
     Tensor t[N];
 };
 
+constexpr uint32_t kWeyl = 0x9E3779B9u;  // (the golden ratio's fraction, odd)
 __host__ __device__ __forceinline__ uint32_t mix(uint32_t h) {
     h ^= h >> 16;
     h *= 0x6A09E667u;  // (the fractions of the roots of 2 and 3, odd)
@@ -159,6 +160,13 @@ __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 // the other side of a power of two, and a code's neighbours with it.
 __device__ __forceinline__ float2 sum_of(float2 a, float2 b, float one) { return fma2(a, both(one), b); }
 
+// 1 / x to 2^-22 of itself: the update's last step.
+__device__ __forceinline__ float inverse(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
 // e4m3 codes.
 __device__ __forceinline__ float2 of_codes(uint32_t two) {
     const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, __NV_E4M3);
@@ -166,13 +174,17 @@ __device__ __forceinline__ float2 of_codes(uint32_t two) {
 }
 __device__ __forceinline__ uint32_t to_codes(float2 x) { return __nv_cvt_float2_to_fp8x2(x, __NV_SATFINITE, __NV_E4M3); }
 constexpr uint32_t kInfinite = 0x7F800000u;
-// Of a warp's values (none below 0 where they are roots): the largest one's bits, of those that are finite.
+__device__ __forceinline__ float max3(float a, float b, float c) {  // of the magnitudes; NaN if one is
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+// Of a warp's values: the largest one's bits, of those that are finite (odd: not all are).
 __device__ __forceinline__ uint32_t largest(const float2 (&x)[4], bool& odd) {
-    uint32_t most = 0;
+    float m = 0.f;
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-        most = max(most, max(__float_as_uint(x[k].x) & 0x7FFFFFFFu, __float_as_uint(x[k].y) & 0x7FFFFFFFu));
-    most = __reduce_max_sync(0xffffffffu, most);
+    for (int k = 0; k < 4; ++k) m = max3(m, x[k].x, x[k].y);
+    uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(m));
     odd = most >= kInfinite;
     if (!odd) return most;
     most = 0;
@@ -187,10 +199,12 @@ __device__ __forceinline__ uint32_t largest(const float2 (&x)[4], bool& odd) {
 __device__ __forceinline__ uint32_t power_of(uint32_t most) {
     return (uint32_t)max((int)(most >> 23) - 8 + ((most & 0x7FFFFFu) > 0x600000u), 1);
 }
-// x / scale, moved by up to half a code's step either way.
-__device__ __forceinline__ float moved(float q, uint32_t hash) {
-    const uint32_t step = max(__float_as_uint(q) & kInfinite, (127u - 6) << 23) - (3u << 23);
-    return fmaf(__uint_as_float(step), __uint_as_float(0x3F800000u | hash >> 9) - 1.5f, q);  // (the product is exact)
+// Two values over their scale, each moved by up to half a code's step either way: the step is 1/8 of the power of two
+// below the value, or of 2^-6, and what moves it a number from -1/2 up to 1/2 of the hash's 23 upper bits.  (Every product is exact.)
+__device__ __forceinline__ float2 moved(float2 q, uint32_t hash_x, uint32_t hash_y) {
+    const float2 power = make_float2(fmaxf(__uint_as_float(__float_as_uint(q.x) & kInfinite), 0.015625f), fmaxf(__uint_as_float(__float_as_uint(q.y) & kInfinite), 0.015625f));
+    const float2 from_1_to_2 = make_float2(__uint_as_float(__funnelshift_r(hash_x, 0x7Fu, 9)), __uint_as_float(__funnelshift_r(hash_y, 0x7Fu, 9)));
+    return fma2(power, fma2(from_1_to_2, both(0.125f), both(-0.1875f)), q);
 }
 
 template <int BITS, int N>
@@ -220,7 +234,7 @@ __global__ void __launch_bounds__(kWarps * 32) k_adamw(const __grid_constant__ B
         else to = mid;
     }
     const Tensor& t = batch.t[i];
-    const int64_t n = t.n, from = (int64_t)(blockIdx.x - t.first) * kChunk;
+    const int64_t n = t.n, from = (int64_t)(blockIdx.x - t.first) * (batch.groups * kWarps * kGroup);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t blocks = (n + kGroup - 1) / kGroup;
     const uint32_t key = BITS == 8 ? mix(mix(mix(h.seed) + step) + t.index) : 0u;
@@ -228,7 +242,7 @@ __global__ void __launch_bounds__(kWarps * 32) k_adamw(const __grid_constant__ B
     constexpr int kWords = BITS == 8 ? 2 : 8;
 
 #pragma unroll 2
-    for (int q = 0; q < kGroupsPerWarp; ++q) {
+    for (int q = 0; q < batch.groups; ++q) {
         Lane l;
         l.at = from + (q * kWarps + warp) * kGroup;
         if (l.at >= n) break;
@@ -274,7 +288,7 @@ __global__ void __launch_bounds__(kWarps * 32) k_adamw(const __grid_constant__ B
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const float2 d = fma2(r[k], both(root), both(h.eps)), up = mul2(m[k], both(-rate));
-            p[k] = fma2(p[k], both(decay), make_float2(__fdividef(up.x, d.x), __fdividef(up.y, d.y)));
+            p[k] = fma2(p[k], both(decay), mul2(up, make_float2(inverse(d.x), inverse(d.y))));
         }
         l.store(t.p, t.p_type, p);
         if (t.copy) l.store(t.copy, t.copy_type, p);
@@ -286,18 +300,23 @@ __global__ void __launch_bounds__(kWarps * 32) k_adamw(const __grid_constant__ B
             const uint32_t pm = power_of(largest(m, odd_m)), pr = power_of(largest(r, odd_r));
             const float2 im = both(__uint_as_float((254u - pm) << 23)), ir = both(__uint_as_float((254u - pr) << 23));
             float2 cm[4], cr[4];
+            uint32_t hash = key + (uint32_t)l.place(0) * kWeyl;
+            const uint32_t more = (l.wide ? 1u : 32u) * kWeyl;
+            float least = INFINITY;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                cm[k] = mul2(m[k], im);
-                cr[k] = mul2(r[k], ir);
-                auto code = [&](float& a, float& b, float root_of_v, int j) {
-                    uint32_t hash = key + (uint32_t)l.place(j) * 0x9E3779B9u;
-                    hash ^= hash >> 15;
-                    a = moved(a, hash * 0x6A09E667u);
-                    b = root_of_v == 0.f ? 0.f : fmaxf(moved(b, hash * 0xBB67AE85u), 0.001953125f);
-                };
-                code(cm[k].x, cr[k].x, r[k].x, 2 * k);
-                code(cm[k].y, cr[k].y, r[k].y, 2 * k + 1);
+                uint32_t a = hash, b = hash + more;
+                hash = b + more;
+                a ^= a >> 15;
+                b ^= b >> 15;
+                cm[k] = moved(mul2(m[k], im), a * 0x6A09E667u, b * 0x6A09E667u);
+                cr[k] = moved(mul2(r[k], ir), a * 0xBB67AE85u, b * 0xBB67AE85u);
+                cr[k] = make_float2(fmaxf(cr[k].x, 0.001953125f), fmaxf(cr[k].y, 0.001953125f));  // (the least code)
+                least = fminf(least, fminf(r[k].x, r[k].y));
+            }
+            if (least == 0.f) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) cr[k] = make_float2(r[k].x == 0.f ? 0.f : cr[k].x, r[k].y == 0.f ? 0.f : cr[k].y);
             }
             if (odd_m || odd_r) {  // a value that is not finite reads back as NaN, the block's others as they are
                 auto mark = [](float& c, float x) { if (!(fabsf(x) < INFINITY)) c = __uint_as_float(0x7FFFFFFFu); };
@@ -355,16 +374,18 @@ bool adamw_ok(const mlkv_adamw_args* a) {
 
 // A launch of up to N tensors from `at` on; how many it took.
 template <int N>
-int64_t launch_batch(const mlkv_adamw_args& a, const Hyper& h, int64_t at, cudaStream_t st) {
+int64_t launch_batch(const mlkv_adamw_args& a, const Hyper& h, int groups, int64_t at, cudaStream_t st) {
     static thread_local Batch<N> b;  // (a launch copies it)
     b.h = h;
+    b.groups = groups;
+    const int64_t chunk = (int64_t)groups * kWarps * kGroup;
     b.count = 0;
     uint32_t chunks = 0;
     const int64_t first = at;
     for (; at < a.count && b.count < N; ++at) {
         const mlkv_adamw_tensor& t = a.tensors[at];
         if (!t.n) continue;
-        const int64_t more = (t.n + kChunk - 1) / kChunk;
+        const int64_t more = (t.n + chunk - 1) / chunk;
         if (chunks + more >= (int64_t)1 << 31) break;
         auto on = [](const void* p, int64_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; };
         const bool wide = on(t.d_param, 8 * dense_type_size(t.param_type)) && on(t.d_grad, 8 * dense_type_size(t.grad_type)) &&
@@ -401,6 +422,11 @@ extern "C" int mlkv_adamw(const mlkv_adamw_args* args, void* stream) {
     h.d_lr = a.d_lr; h.d_step = a.d_step; h.d_grad_scale = a.d_grad_scale;
     h.seed = a.seed; h.step = (uint32_t)a.step; h.one = 1.f;
     // The tensors' table is an argument of the launch: 1.8 KB of 24 tensors, 32 KB of 440.
-    for (int64_t at = 0; at < a.count;) at += a.count - at <= 24 ? launch_batch<24>(a, h, at, (cudaStream_t)stream) : launch_batch<440>(a, h, at, (cudaStream_t)stream);
+    int64_t all = 0;
+    for (int64_t i = 0; i < a.count; ++i) all += a.tensors[i].n;
+    // (four blocks an SM at once: below that many whole parts, smaller ones)
+    const int groups = all < (int64_t)kChunk * 4 * dense_sms() ? 1 : kGroupsPerWarp;
+    for (int64_t at = 0; at < a.count;)
+        at += a.count - at <= 24 ? launch_batch<24>(a, h, groups, at, (cudaStream_t)stream) : launch_batch<440>(a, h, groups, at, (cudaStream_t)stream);
     return cudaGetLastError() == cudaSuccess ? MLKV_OK : MLKV_ERR_CUDA;
 }

@@ -316,10 +316,11 @@ PyObject* gated_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
         mlkv_gated_linear_args g;
         if (n != 5 || !gated_operands(a[0], a[1], a[2], a[3], x, g)) return pass();
         const bool save = truth(a[4]);
-        auto out = [&] { return make(x, {g.m, g.f}, x.scalar); };
-        const at::Tensor r[3] = {out(), save ? out() : at::Tensor(), save ? out() : at::Tensor()};
+        const int64_t wide = (g.f + 7) / 8 * 8;
+        auto saved = [&] { return !save ? at::Tensor() : wide == g.f ? make(x, {g.m, g.f}, x.scalar) : make(x, {g.m, wide}, x.scalar).narrow(1, 0, g.f); };
+        const at::Tensor r[3] = {make(x, {g.m, g.f}, x.scalar), saved(), saved()};
         g.d_h = r[0].data_ptr(); g.d_gate = at_of(r[1]); g.d_up = at_of(r[2]);
-        g.h_stride = g.gate_stride = g.up_stride = g.f;
+        g.h_stride = g.f; g.gate_stride = g.up_stride = wide;
         g.workspace_bytes = lib.gated_linear_workspace(&g);
         const Workspace ws(x, g.workspace_bytes);
         g.d_workspace = ws.p;

@@ -21,13 +21,13 @@ namespace {
 struct Outputs {
     void *h, *gate, *up;
     int64_t h_stride, gate_stride, up_stride;
-    int32_t f, act, wide;  // wide: rows of all three can be moved 16 bytes at a time
+    int32_t f, act, wide, wide_pre;  // rows of h, of gate and up can be moved 16 bytes at a time
     template <class T>
     __device__ __forceinline__ void put_four(const float4& g4, const float4& u4, int64_t row, int64_t col) const {
         float2 g[2] = {make_float2(g4.x, g4.y), make_float2(g4.z, g4.w)}, u[2] = {make_float2(u4.x, u4.y), make_float2(u4.z, u4.w)};
-        auto store = [&](void* m, int64_t stride, const float2 (&v)[2]) {
+        auto store = [&](void* m, int64_t stride, bool whole, const float2 (&v)[2]) {
             T* at = static_cast<T*>(m) + row * stride + col;
-            if (wide && col + 4 <= f) {
+            if (whole && col + 4 <= f) {
                 *reinterpret_cast<uint2*>(at) = make_uint2(word_of_pair<T>(v[0]), word_of_pair<T>(v[1]));
                 return;
             }
@@ -37,8 +37,8 @@ struct Outputs {
                 if (col + k < f) at[k] = from_float<T>(x[k]);
         };
         if (gate) {
-            store(gate, gate_stride, g);
-            store(up, up_stride, u);
+            store(gate, gate_stride, wide_pre, g);
+            store(up, up_stride, wide_pre, u);
         }
         by_act(act, [&](auto a) {
             g[0] = activate<decltype(a)::value>(g[0]);
@@ -46,7 +46,7 @@ struct Outputs {
         });
         g[0] = mul2(g[0], u[0]);
         g[1] = mul2(g[1], u[1]);
-        store(h, h_stride, g);
+        store(h, h_stride, wide, g);
     }
 };
 
@@ -60,9 +60,10 @@ struct Gated : Outputs {
     __device__ __forceinline__ bool put(const CUtensorMap* h_map, uint32_t tmem, uint8_t* corner, int r0, int c0, int blocks, int lane,
                                         uint32_t& turn, W wait) const {
         if (!wait()) return false;
+        const bool all = wide && (wide_pre || !gate);  // leave by TMA
 #pragma unroll 1
         for (int b = 0; b < blocks && c0 + b * 32 < f; ++b) {
-            const Place q = {r0, c0 + b * 32, m, f, lane, wide && c0 + b * 32 + 32 <= f};
+            const Place q = {r0, c0 + b * 32, m, f, lane, false};
             uint32_t acc[2][32];
             __syncwarp();
             tmem_ld32(tmem + b * 32, acc[0]);
@@ -75,21 +76,24 @@ struct Gated : Outputs {
                 u[k] = make_float2(__uint_as_float(acc[1][2 * k]), __uint_as_float(acc[1][2 * k + 1]));
             }
             // The halves take turns; whoever fills one waits until its last store has read it.
-            auto out = [&](const float2 (&v)[16], const CUtensorMap* map, void* to, int64_t stride) {
+            auto out = [&](const float2 (&v)[16], const CUtensorMap* map, void* to, int64_t stride, bool by_tma) {
                 const Half s = {corner + (turn++ & 1) * kHalf};
-                if (wide && lane == 0) tma_store_read<1>();
+                if (lane == 0) {
+                    if (all) tma_store_read<1>();
+                    else tma_store_read<0>();  // (of those by TMA the last may be of this half)
+                }
                 __syncwarp();
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
                     s.piece(lane, c) = make_uint4(word_of_pair<T>(v[4 * c]), word_of_pair<T>(v[4 * c + 1]), word_of_pair<T>(v[4 * c + 2]), word_of_pair<T>(v[4 * c + 3]));
-                if (wide) fence_async();
+                if (by_tma) fence_async();
                 __syncwarp();
-                if (!wide) put_values(s, static_cast<T*>(to), stride, q);
+                if (!by_tma) put_values(s, static_cast<T*>(to), stride, q);
                 else if (lane == 0) tma_store(map, q.c0, q.r0, smem_of(s.at));
             };
             if (gate) {
-                out(g, &gate_map, gate, gate_stride);
-                out(u, &up_map, up, up_stride);
+                out(g, &gate_map, gate, gate_stride, wide_pre);
+                out(u, &up_map, up, up_stride, wide_pre);
             }
             by_act(act, [&](auto a) {
 #pragma unroll
@@ -97,7 +101,7 @@ struct Gated : Outputs {
             });
 #pragma unroll
             for (int k = 0; k < 16; ++k) g[k] = mul2(g[k], u[k]);
-            out(g, h_map, h, h_stride);
+            out(g, h_map, h, h_stride, wide);
         }
         return true;
     }
@@ -178,18 +182,22 @@ __device__ __forceinline__ void act_and_slope(float2 z, float2& a, float2& s) {
     a = mul2(make_float2(at_least(z.x, -100.f), at_least(z.y, -100.f)), q);
 }
 
-// dg = dh u act'(g), du = dh act(g): a thread takes 8 columns of two rows at a time.  Bound by HBM.
+// dg = dh u act'(g), du = dh act(g): a thread takes 8 columns of a row at a time, the warps of a block
+// rows one after another.  Bound by HBM: 8,192 x 12,288 bf16, silu, 155 us, 6.5 TB/s.  (Rows of dh off 16 bytes: 12,283 columns 260 us.)
 struct Slopes {
     const void *dh, *gate, *up;
     void *dg, *du;
     int64_t dh_stride, gate_stride, up_stride, out_stride, rows, cols, share;
     int32_t act;
 };
-template <class T, bool ALIGNED>
-__global__ void __launch_bounds__(256, ALIGNED ? 4 : 2) k_gated_slopes(Slopes a) {
+// (Blocks an SM, with the next row on its way: 4 / 3 / 2 of them 171 / 155 / 180 us for 8,192 x 12,288; without, two rows at a time, 182.)
+constexpr int kSlopeBlocks = 3;
+// DH, PRE: rows of dh, of gate and up lie on 16 bytes.
+template <class T, bool DH, bool PRE, int ACT>
+__global__ void __launch_bounds__(256, kSlopeBlocks) k_gated_slopes(Slopes a) {
     pdl_enter();
-    using Row = Values<T, 8, ALIGNED>;
-    constexpr int kRows = ALIGNED ? 2 : 1;  // on their way at a time
+    using Down = Values<T, 8, DH>;
+    using Pre = Values<T, 8, PRE>;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t c = (blockIdx.x * 32ll + lane) * 8;
     const int n = (int)min((int64_t)8, a.cols - c);
@@ -197,38 +205,52 @@ __global__ void __launch_bounds__(256, ALIGNED ? 4 : 2) k_gated_slopes(Slopes a)
     const T *dh = static_cast<const T*>(a.dh), *gate = static_cast<const T*>(a.gate), *up = static_cast<const T*>(a.up);
     const Span dh_span(dh, a.rows, a.dh_stride, (int)a.cols), gate_span(gate, a.rows, a.gate_stride, (int)a.cols), up_span(up, a.rows, a.up_stride, (int)a.cols);
     if (n <= 0) return;
-    for (int64_t r = r0 + warp; r < r1; r += 8 * kRows) {
-        typename Row::Around at[kRows][3];
+    const bool whole = n == 8;  // (the last vector of a row on 16 bytes may lie past the matrix's end)
+    auto bring = [&](auto& at, const T* p, const Span& span) {
+        using V = std::remove_reference_t<decltype(at)>;
+        if constexpr (sizeof(V) == sizeof(typename Values<T, 8, true>::Around)) {
+            if (whole) at = Values<T, 8, true>::around(p, span);
+            else
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            if (r + 8 * i >= r1) continue;
-            at[i][0] = Row::around(dh + (r + 8 * i) * a.dh_stride + c, dh_span);
-            at[i][1] = Row::around(gate + (r + 8 * i) * a.gate_stride + c, gate_span);
-            at[i][2] = Row::around(up + (r + 8 * i) * a.up_stride + c, up_span);
+                for (int k = 0; k < 4; ++k) at.v[k] = Values<T, 8, true>::edge(reinterpret_cast<const uint8_t*>(p), k, span);
+        } else {
+            at = Values<T, 8, false>::around(p, span);
         }
+    };
+    struct Row {  // on its way
+        typename Down::Around down;
+        typename Pre::Around gate, up;
+    } rows[2];
+    auto load = [&](Row& to, int64_t r) {
+        if (r >= r1) return;
+        bring(to.down, dh + r * a.dh_stride + c, dh_span);
+        bring(to.gate, gate + r * a.gate_stride + c, gate_span);
+        bring(to.up, up + r * a.up_stride + c, up_span);
+    };
+    auto work = [&](const Row& from, int64_t r) {
+        if (r >= r1) return;
+        Down d;
+        Pre g, u;
+        d.settle(from.down, Down::place(dh + r * a.dh_stride), n);
+        g.settle(from.gate, Pre::place(gate + r * a.gate_stride), n);
+        u.settle(from.up, Pre::place(up + r * a.up_stride), n);
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            if (r + 8 * i >= r1) continue;
-            Row d, g, u;
-            d.settle(at[i][0], Row::place(dh + (r + 8 * i) * a.dh_stride), n);
-            g.settle(at[i][1], Row::place(gate + (r + 8 * i) * a.gate_stride), n);
-            u.settle(at[i][2], Row::place(up + (r + 8 * i) * a.up_stride), n);
-            auto both = [&](auto act) {
-                constexpr int kAct = decltype(act)::value;
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const float2 x = d.pair(q);
-                    float2 y, s;
-                    act_and_slope<kAct>(g.pair(q), y, s);
-                    g.set(q, mul2(mul2(x, u.pair(q)), s));
-                    u.set(q, mul2(x, y));
-                }
-            };
-            if (a.act == MLKV_ACT_NONE) both(Act<MLKV_ACT_NONE>{});
-            else by_act(a.act, both);
-            *reinterpret_cast<uint4*>(static_cast<T*>(a.dg) + (r + 8 * i) * a.out_stride + c) = make_uint4(g.w[0], g.w[1], g.w[2], g.w[3]);
-            *reinterpret_cast<uint4*>(static_cast<T*>(a.du) + (r + 8 * i) * a.out_stride + c) = make_uint4(u.w[0], u.w[1], u.w[2], u.w[3]);
+        for (int q = 0; q < 4; ++q) {
+            const float2 x = d.pair(q);
+            float2 y, s;
+            act_and_slope<ACT>(g.pair(q), y, s);
+            g.set(q, mul2(mul2(x, u.pair(q)), s));
+            u.set(q, mul2(x, y));
         }
+        *reinterpret_cast<uint4*>(static_cast<T*>(a.dg) + r * a.out_stride + c) = make_uint4(g.w[0], g.w[1], g.w[2], g.w[3]);
+        *reinterpret_cast<uint4*>(static_cast<T*>(a.du) + r * a.out_stride + c) = make_uint4(u.w[0], u.w[1], u.w[2], u.w[3]);
+    };
+    load(rows[0], r0 + warp);
+    for (int64_t r = r0 + warp; r < r1; r += 16) {
+        load(rows[1], r + 8);
+        work(rows[0], r);
+        load(rows[0], r + 16);
+        work(rows[1], r + 8);
     }
 }
 
@@ -252,7 +274,8 @@ struct Caller : Products {
             return;
         }
         auto on16 = [](const void* p, int64_t stride) { return !p || (reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 8 == 0); };
-        x.wide = on16(x.h, x.h_stride) && on16(x.gate, x.gate_stride) && on16(x.up, x.up_stride);
+        x.wide = on16(x.h, x.h_stride);
+        x.wide_pre = on16(x.gate, x.gate_stride) && on16(x.up, x.up_stride);
         Matrix in = matrix_of(g.d_x, g.x_stride, g.m, g.k), wg = matrix_of(g.d_w_gate, g.w_gate_stride, g.f, g.k),
                wu = matrix_of(g.d_w_up, g.w_up_stride, g.f, g.k), none = {};
         align(in, wg, wu);
@@ -282,15 +305,23 @@ struct Caller : Products {
             dg = matrix_of(s.dg, s.out_stride, g.m, g.f);
             du = matrix_of(s.du, s.out_stride, g.m, g.f);
             if (run) {
-                const bool whole = g.f % 8 == 0 && matrix_of(s.dh, s.dh_stride, 0, 0).aligned() && matrix_of(s.gate, s.gate_stride, 0, 0).aligned() &&
-                                   matrix_of(s.up, s.up_stride, 0, 0).aligned();
-                const int64_t across = (g.f + 255) / 256, wanted = std::max<int64_t>(1, std::min<int64_t>((g.m + 15) / 16, 4ll * sms / across));
+                const bool dh = matrix_of(s.dh, s.dh_stride, 0, 0).aligned();
+                const bool pre = matrix_of(s.gate, s.gate_stride, 0, 0).aligned() && matrix_of(s.up, s.up_stride, 0, 0).aligned();
+                const int64_t across = (g.f + 255) / 256, wanted = std::max<int64_t>(1, std::min<int64_t>((g.m + 15) / 16, (int64_t)kSlopeBlocks * sms / across));
                 s.share = (g.m + wanted - 1) / wanted;
                 const dim3 grid((unsigned)across, (unsigned)((g.m + s.share - 1) / s.share));
                 const bool b = type == MLKV_TYPE_BFLOAT;
-                launch_kernel(true, whole ? (b ? k_gated_slopes<__nv_bfloat16, true> : k_gated_slopes<__half, true>)
-                                          : (b ? k_gated_slopes<__nv_bfloat16, false> : k_gated_slopes<__half, false>),
-                              grid, dim3(256), 0, st, s);
+                auto go = [&](auto act) {
+                    constexpr int kAct = decltype(act)::value;
+                    auto at = [&](auto kernel) { launch_kernel(true, kernel, grid, dim3(256), 0, st, s); };
+                    if (dh && pre) at(b ? k_gated_slopes<__nv_bfloat16, true, true, kAct> : k_gated_slopes<__half, true, true, kAct>);
+                    else if (pre) at(b ? k_gated_slopes<__nv_bfloat16, false, true, kAct> : k_gated_slopes<__half, false, true, kAct>);
+                    else at(b ? k_gated_slopes<__nv_bfloat16, false, false, kAct> : k_gated_slopes<__half, false, false, kAct>);
+                };
+                if (s.act == MLKV_ACT_RELU) go(Act<MLKV_ACT_RELU>{});
+                else if (s.act == MLKV_ACT_GELU_TANH) go(Act<MLKV_ACT_GELU_TANH>{});
+                else if (s.act == MLKV_ACT_SILU) go(Act<MLKV_ACT_SILU>{});
+                else go(Act<MLKV_ACT_NONE>{});
             }
             if (g.k) {
                 Matrix none2 = {};

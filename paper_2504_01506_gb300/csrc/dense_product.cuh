@@ -809,10 +809,8 @@ struct Products {
             ok = ok && encode(map, {static_cast<const uint16_t*>(m), stride, rows, cols}, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B);
         };
         if constexpr (kBoth) {
-            if (!SWAP && x.wide) {
-                stored(&out, x.h, x.h_stride, p.I, x.f);
-                if (x.gate) stored(&x.gate_map, x.gate, x.gate_stride, p.I, x.f), stored(&x.up_map, x.up, x.up_stride, p.I, x.f);
-            }
+            if (!SWAP && x.wide) stored(&out, x.h, x.h_stride, p.I, x.f);
+            if (!SWAP && x.gate && x.wide_pre) stored(&x.gate_map, x.gate, x.gate_stride, p.I, x.f), stored(&x.up_map, x.up, x.up_stride, p.I, x.f);
         } else if (!SWAP && X::kKind != kStats && p.e.wide) {
             stored(&out, p.e.out, p.e.out_stride, p.I, p.J);
             if constexpr (X::kKind == kTwin) stored(&x.out, p.out2, p.out2_stride, p.I, p.J);

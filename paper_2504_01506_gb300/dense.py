@@ -332,7 +332,7 @@ def _gated_args(x, w_gate, w_up, activation):
 def gated_linear(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, *, activation: str | None = "silu", save_pre: bool = False):
     """act(x @ w_gate.T) * (x @ w_up.T), in one kernel: x [m, k], w_gate and w_up [f, k],
     of one 16-bit type; activation as linear's.  With save_pre also the two factors'
-    sums before the activation, [m, f] each, rounded to x's type, for
+    sums before the activation, [m, f] each (their rows on 16 bytes), rounded to x's type, for
     gated_linear_backward.  Valid when sync() says so, as linear's."""
     if (native := _native(x)) is not None:
         r = native.gated_linear(x, w_gate, w_up, _ACTIVATIONS.get(activation, -1), save_pre)
@@ -343,8 +343,9 @@ def gated_linear(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, *, a
     a.d_h, a.h_stride = h.data_ptr(), f
     gate = up = None
     if save_pre:
-        gate, up = _empty((m, f), dtype=dtype, device=device), _empty((m, f), dtype=dtype, device=device)
-        a.d_gate, a.gate_stride, a.d_up, a.up_stride = gate.data_ptr(), f, up.data_ptr(), f
+        wide = (f + 7) // 8 * 8
+        gate, up = _empty((m, wide), dtype=dtype, device=device)[:, :f], _empty((m, wide), dtype=dtype, device=device)[:, :f]
+        a.d_gate, a.gate_stride, a.d_up, a.up_stride = gate.data_ptr(), wide, up.data_ptr(), wide
     lib = L.load()
     _run_linear(lib.mlkv_gated_linear, lib.mlkv_gated_linear_workspace, a, device)
     return (h, gate, up) if save_pre else h
