@@ -18,6 +18,7 @@
 #include <algorithm>
 #include <cmath>
 #include <new>
+#include <type_traits>
 #include <vector>
 
 #include "dense_common.cuh"
@@ -27,7 +28,11 @@ using namespace mlkv;
 namespace {
 
 constexpr int kGroup = 256;                   // values a warp takes at a time, 8 a lane: a block of codes
-constexpr int kWarps = 8, kGroupsPerWarp = 4;  // a block's part of a tensor; of small networks a quarter of that
+// A block's part of a tensor: two groups a warp, of 8-bit states both on their way before the first is worked on (of small
+// networks one).  (453 million weights with 8-bit states, us: a group at a time, 8 warps a block 1,745; two at a time, 8 warps of
+// four groups 1,341, 4 of four 1,252, 16 of four 1,066, 16 of two 1,090; 24 million in 120 tensors, the last two: 70, 65.  Many
+// values side by side on their way at once are what HBM is fastest with.  32-bit states, 16 of two: 1,816 one at a time, 1,852 two.)
+constexpr int kWarps = 16, kGroupsPerWarp = 2;
 constexpr int kChunk = kGroup * kWarps * kGroupsPerWarp;
 
 struct Tensor {
@@ -39,7 +44,7 @@ struct Tensor {
     void* copy;
     uint32_t first;      // its first chunk of the launch
     uint32_t index;      // place in the caller's list
-    int16_t p_type, g_type, copy_type, wide;
+    int16_t copy_type, wide;
 };
 struct Hyper {
     float lr, b1, c1, b2, c2, eps, wd;  // c1 = 1 - b1, c2 = 1 - b2
@@ -53,7 +58,7 @@ struct Hyper {
 };
 template <int N> struct Batch {
     Hyper h;
-    int count, groups;  // groups a warp
+    int count, groups;  // groups a warp: kGroupsPerWarp or 1
     Tensor t[N];
 };
 
@@ -90,68 +95,61 @@ __device__ __forceinline__ void store_words(void* p, const uint32_t* w) {
         *static_cast<uint2*>(p) = make_uint2(w[0], w[1]);
 }
 
-// A group of 256 values, 8 a lane: as vectors one after another (wide), else a value
-// each 32, of which `n` are left.
+// A group of 256 values, 8 a lane: as vectors one after another (WIDE: all are there, on
+// 32 bytes, 16-bit values on 16, codes on 8), else a value each 32, as far as there are any.
+template <bool WIDE>
 struct Lane {
     int64_t at;  // of the group's first value
     int64_t n;   // the tensor's
     int lane;
-    bool wide;
-    __device__ __forceinline__ int64_t place(int j) const { return at + (wide ? lane * 8 + j : j * 32 + lane); }
-    template <class T>
-    __device__ __forceinline__ void load(uint32_t* w, const void* p) const {
-        constexpr int W = 2 * sizeof(T);
-        const T* q = static_cast<const T*>(p);
-        if (wide) {
-            load_words<W>(w, q + at + lane * 8);
-            return;
+    __device__ __forceinline__ int64_t place(int j) const { return at + (WIDE ? lane * 8 + j : j * 32 + lane); }
+    template <class U>  // an integer as wide as a value
+    __device__ __forceinline__ void read(uint32_t (&w)[2 * sizeof(U)], const void* p) const {
+        const U* q = static_cast<const U*>(p);
+        if constexpr (WIDE) {
+            load_words<2 * sizeof(U)>(w, q + at + lane * 8);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2 * (int)sizeof(U); ++i) w[i] = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (place(j) < n) w[j * sizeof(U) / 4] |= (uint32_t)q[place(j)] << (j * sizeof(U) % 4 * 8);
         }
+    }
+    template <class U>
+    __device__ __forceinline__ void write(void* p, const uint32_t (&w)[2 * sizeof(U)]) const {
+        U* q = static_cast<U*>(p);
+        if constexpr (WIDE) {
+            store_words<2 * sizeof(U)>(q + at + lane * 8, w);
+        } else {
 #pragma unroll
-        for (int i = 0; i < W; ++i) w[i] = 0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (place(j) < n) w[j * sizeof(T) / 4] |= (uint32_t)q[place(j)] << (j * sizeof(T) % 4 * 8);
+            for (int j = 0; j < 8; ++j)
+                if (place(j) < n) q[place(j)] = (U)(w[j * sizeof(U) / 4] >> (j * sizeof(U) % 4 * 8));
+        }
     }
     template <class T>
-    __device__ __forceinline__ void store(void* p, const uint32_t* w) const {
-        constexpr int W = 2 * sizeof(T);
-        T* q = static_cast<T*>(p);
-        if (wide) {
-            store_words<W>(q + at + lane * 8, w);
-            return;
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (place(j) < n) q[place(j)] = (T)(w[j * sizeof(T) / 4] >> (j * sizeof(T) % 4 * 8));
-    }
-    // of an element type known at run time (w: 8 words)
-    __device__ __forceinline__ void load(uint32_t* w, const void* p, int type) const {
-        if (type == MLKV_TYPE_FLOAT) load<uint32_t>(w, p);
-        else load<uint16_t>(w, p);
-    }
-    __device__ __forceinline__ void store(void* p, int type, const float2 (&x)[4]) const {
-        uint32_t w[8];
-        if (type == MLKV_TYPE_FLOAT) {
+    __device__ __forceinline__ void put(void* p, const float2 (&x)[4]) const {
+        if constexpr (sizeof(T) == 4) {
+            uint32_t w[8];
 #pragma unroll
             for (int k = 0; k < 4; ++k) w[2 * k] = __float_as_uint(x[k].x), w[2 * k + 1] = __float_as_uint(x[k].y);
-            store<uint32_t>(p, w);
-            return;
-        }
+            write<uint32_t>(p, w);
+        } else {
+            uint32_t w[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) w[k] = type == MLKV_TYPE_BFLOAT ? word_of_pair<__nv_bfloat16>(x[k]) : word_of_pair<__half>(x[k]);
-        store<uint16_t>(p, w);
+            for (int k = 0; k < 4; ++k) w[k] = word_of_pair<T>(x[k]);
+            write<uint16_t>(p, w);
+        }
     }
 };
-__device__ __forceinline__ void widen(float2 (&x)[4], const uint32_t* w, int type) {
-    if (type == MLKV_TYPE_FLOAT) {
+template <class T> struct As { using type = uint16_t; };
+template <> struct As<float> { using type = uint32_t; };
+template <class T>
+__device__ __forceinline__ void widen(float2 (&x)[4], const uint32_t (&w)[2 * sizeof(T)]) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) x[k] = make_float2(__uint_as_float(w[2 * k]), __uint_as_float(w[2 * k + 1]));
-    } else if (type == MLKV_TYPE_BFLOAT) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) x[k] = pair_of_word<__nv_bfloat16>(w[k]);
-    } else {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) x[k] = pair_of_word<__half>(w[k]);
+    for (int k = 0; k < 4; ++k) {
+        if constexpr (sizeof(T) == 4) x[k] = make_float2(__uint_as_float(w[2 * k]), __uint_as_float(w[2 * k + 1]));
+        else x[k] = pair_of_word<T>(w[k]);
     }
 }
 __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
@@ -207,12 +205,129 @@ __device__ __forceinline__ float2 moved(float2 q, uint32_t hash_x, uint32_t hash
     return fma2(power, fma2(from_1_to_2, both(0.125f), both(-0.1875f)), q);
 }
 
-template <int BITS, int N>
-__global__ void __launch_bounds__(kWarps * 32) k_adamw(const __grid_constant__ Batch<N> batch) {
+// What a step multiplies by.
+struct Rates {
+    float decay, rate, root;
+    float2 factor;
+    uint32_t key;
+};
+// A group of 256 values, read by a warp.
+template <int BITS, class P, class G>
+struct Group {
+    using State = std::conditional_t<BITS == 8, uint8_t, uint32_t>;
+    uint32_t wp[2 * sizeof(P)], wg[2 * sizeof(G)], wm[2 * sizeof(State)], wv[2 * sizeof(State)];
+    float sm, sr;
+    template <bool WIDE>
+    __device__ __forceinline__ void load(const Tensor& t, int64_t at, int lane) {
+        const Lane<WIDE> l = {at, t.n, lane};
+        l.template read<typename As<P>::type>(wp, t.p);
+        l.template read<typename As<G>::type>(wg, t.g);
+        l.template read<State>(wm, t.m);
+        l.template read<State>(wv, t.v);
+        if constexpr (BITS == 8) {
+            sm = t.scales[at / kGroup];
+            sr = t.scales[at / kGroup + (t.n + kGroup - 1) / kGroup];
+        }
+    }
+};
+// Its step.
+template <int BITS, class P, class G, bool WIDE>
+__device__ __forceinline__ void step_group(Group<BITS, P, G>& of, const Tensor& t, const Hyper& h, const Rates& s, int64_t at, int lane) {
+    const Lane<WIDE> l = {at, t.n, lane};
+    using State = typename Group<BITS, P, G>::State;
+    auto &wp = of.wp;
+    auto &wg = of.wg;
+    auto &wm = of.wm;
+    auto &wv = of.wv;
+    const float2 sm = both(of.sm), sr = both(of.sr);
+    float2 p[4], g[4], m[4], r[4];
+    widen<G>(g, wg);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        float2 v;
+        if constexpr (BITS == 8) {
+            m[k] = mul2(of_codes(wm[k / 2] >> (k % 2 * 16) & 0xFFFFu), sm);
+            r[k] = mul2(of_codes(wv[k / 2] >> (k % 2 * 16) & 0xFFFFu), sr);
+            v = mul2(r[k], r[k]);
+        } else {
+            m[k] = make_float2(__uint_as_float(wm[2 * k]), __uint_as_float(wm[2 * k + 1]));
+            v = make_float2(__uint_as_float(wv[2 * k]), __uint_as_float(wv[2 * k + 1]));
+        }
+        if (h.d_grad_scale) g[k] = mul2(g[k], s.factor);
+        m[k] = sum_of(mul2(m[k], both(h.b1)), mul2(g[k], both(h.c1)), h.one);
+        v = sum_of(mul2(v, both(h.b2)), mul2(mul2(g[k], g[k]), both(h.c2)), h.one);
+        r[k] = make_float2(__fsqrt_rn(v.x), __fsqrt_rn(v.y));
+        if constexpr (BITS == 32) {
+            wv[2 * k] = __float_as_uint(v.x);
+            wv[2 * k + 1] = __float_as_uint(v.y);
+        }
+    }
+    widen<P>(p, wp);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const float2 d = fma2(r[k], both(s.root), both(h.eps)), up = mul2(m[k], both(-s.rate));
+        p[k] = fma2(p[k], both(s.decay), mul2(up, make_float2(inverse(d.x), inverse(d.y))));
+    }
+    l.template put<P>(t.p, p);
+    if (t.copy) {
+        if (t.copy_type == MLKV_TYPE_BFLOAT) l.template put<__nv_bfloat16>(t.copy, p);
+        else l.template put<__half>(t.copy, p);
+    }
+    if constexpr (BITS == 32) {
+        l.template put<float>(t.m, m);
+        l.template write<uint32_t>(t.v, wv);
+    } else {
+        bool odd_m, odd_r;
+        const uint32_t pm = power_of(largest(m, odd_m)), pr = power_of(largest(r, odd_r));
+        const float2 im = both(__uint_as_float((254u - pm) << 23)), ir = both(__uint_as_float((254u - pr) << 23));
+        float2 cm[4], cr[4];
+        uint32_t hash = s.key + (uint32_t)l.place(0) * kWeyl;
+        constexpr uint32_t more = (WIDE ? 1u : 32u) * kWeyl;
+        float least = INFINITY;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            uint32_t a = hash + 2 * k * more, b = hash + (2 * k + 1) * more;
+            a ^= a >> 15;
+            b ^= b >> 15;
+            cm[k] = moved(mul2(m[k], im), a * 0x6A09E667u, b * 0x6A09E667u);
+            cr[k] = moved(mul2(r[k], ir), a * 0xBB67AE85u, b * 0xBB67AE85u);
+            cr[k] = make_float2(fmaxf(cr[k].x, 0.001953125f), fmaxf(cr[k].y, 0.001953125f));  // (the least code)
+            least = fminf(least, fminf(r[k].x, r[k].y));
+        }
+        if (least == 0.f) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) cr[k] = make_float2(r[k].x == 0.f ? 0.f : cr[k].x, r[k].y == 0.f ? 0.f : cr[k].y);
+        }
+        if (odd_m || odd_r) {  // a value that is not finite reads back as NaN, the block's others as they are
+            auto mark = [](float& c, float x) { if (!(fabsf(x) < INFINITY)) c = __uint_as_float(0x7FFFFFFFu); };
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                mark(cm[k].x, m[k].x);
+                mark(cm[k].y, m[k].y);
+                mark(cr[k].x, r[k].x);
+                mark(cr[k].y, r[k].y);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            wm[k] = to_codes(cm[2 * k]) | to_codes(cm[2 * k + 1]) << 16;
+            wv[k] = to_codes(cr[2 * k]) | to_codes(cr[2 * k + 1]) << 16;
+        }
+        l.template write<uint8_t>(t.m, wm);
+        l.template write<uint8_t>(t.v, wv);
+        if (lane == 0) {
+            t.scales[at / kGroup] = __uint_as_float(pm << 23);
+            t.scales[at / kGroup + (t.n + kGroup - 1) / kGroup] = __uint_as_float(pr << 23);
+        }
+    }
+}
+
+template <int BITS, class P, class G, int N>
+__global__ void __launch_bounds__(kWarps * 32, 2) k_adamw(const __grid_constant__ Batch<N> batch) {
     pdl_enter();
     __shared__ float by_step[3];
     const Hyper& h = batch.h;
-    float decay = h.decay, rate = h.rate, root = h.root;
+    Rates s = {h.decay, h.rate, h.root, both(1.f), 0};
     uint32_t step = h.step;
     if (h.d_step || h.d_lr) {
         if (h.d_step) step = (uint32_t)*h.d_step;
@@ -223,122 +338,38 @@ __global__ void __launch_bounds__(kWarps * 32) k_adamw(const __grid_constant__ B
             by_step[2] = 1.f / sqrtf(-expm1f(t * h.log_b2));
         }
         __syncthreads();
-        decay = by_step[0];
-        rate = by_step[1];
-        root = by_step[2];
+        s.decay = by_step[0];
+        s.rate = by_step[1];
+        s.root = by_step[2];
     }
-    int i = 0;  // the tensor of this chunk
+    int i = 0;  // the tensor of this part
     for (int to = batch.count; to - i > 1;) {
         const int mid = (i + to) >> 1;
         if (batch.t[mid].first <= blockIdx.x) i = mid;
         else to = mid;
     }
     const Tensor& t = batch.t[i];
-    const int64_t n = t.n, from = (int64_t)(blockIdx.x - t.first) * (batch.groups * kWarps * kGroup);
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t blocks = (n + kGroup - 1) / kGroup;
-    const uint32_t key = BITS == 8 ? mix(mix(mix(h.seed) + step) + t.index) : 0u;
-    const float2 factor = both(h.d_grad_scale ? *h.d_grad_scale : 1.f);
-    constexpr int kWords = BITS == 8 ? 2 : 8;
-
-#pragma unroll 2
-    for (int q = 0; q < batch.groups; ++q) {
-        Lane l;
-        l.at = from + (q * kWarps + warp) * kGroup;
-        if (l.at >= n) break;
-        l.n = n;
-        l.lane = lane;
-        l.wide = t.wide && l.at + kGroup <= n;
-        uint32_t wp[8], wg[8], wm[kWords], wv[kWords];
-        l.load(wp, t.p, t.p_type);
-        l.load(wg, t.g, t.g_type);
-        float2 sm = both(0.f), sr = both(0.f);
-        if constexpr (BITS == 8) {
-            l.load<uint8_t>(wm, t.m);
-            l.load<uint8_t>(wv, t.v);
-            sm = both(t.scales[l.at / kGroup]);
-            sr = both(t.scales[blocks + l.at / kGroup]);
+    if (h.d_grad_scale) s.factor = both(*h.d_grad_scale);
+    if (BITS == 8) s.key = mix(mix(mix(h.seed) + step) + t.index);
+    const int lane = threadIdx.x & 31;
+    int64_t at = ((int64_t)(blockIdx.x - t.first) * (batch.groups * kWarps) + (threadIdx.x >> 5)) * kGroup;
+    constexpr int kStep = kWarps * kGroup;
+    Group<BITS, P, G> one, two;
+    if (BITS == 8 && t.wide && batch.groups == 2 && at + kStep + kGroup <= t.n) {
+        one.template load<true>(t, at, lane);
+        two.template load<true>(t, at + kStep, lane);
+        step_group<BITS, P, G, true>(one, t, h, s, at, lane);
+        step_group<BITS, P, G, true>(two, t, h, s, at + kStep, lane);
+        return;
+    }
+#pragma unroll 1
+    for (int q = 0; q < batch.groups && at < t.n; ++q, at += kStep) {
+        if (t.wide && at + kGroup <= t.n) {
+            one.template load<true>(t, at, lane);
+            step_group<BITS, P, G, true>(one, t, h, s, at, lane);
         } else {
-            l.load<uint32_t>(wm, t.m);
-            l.load<uint32_t>(wv, t.v);
-        }
-        float2 p[4], g[4], m[4], r[4];
-        widen(g, wg, t.g_type);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            float2 v;
-            if constexpr (BITS == 8) {
-                m[k] = mul2(of_codes(wm[k / 2] >> (k % 2 * 16) & 0xFFFFu), sm);
-                r[k] = mul2(of_codes(wv[k / 2] >> (k % 2 * 16) & 0xFFFFu), sr);
-                v = mul2(r[k], r[k]);
-            } else {
-                m[k] = make_float2(__uint_as_float(wm[2 * k]), __uint_as_float(wm[2 * k + 1]));
-                v = make_float2(__uint_as_float(wv[2 * k]), __uint_as_float(wv[2 * k + 1]));
-            }
-            if (h.d_grad_scale) g[k] = mul2(g[k], factor);
-            m[k] = sum_of(mul2(m[k], both(h.b1)), mul2(g[k], both(h.c1)), h.one);
-            v = sum_of(mul2(v, both(h.b2)), mul2(mul2(g[k], g[k]), both(h.c2)), h.one);
-            r[k] = make_float2(__fsqrt_rn(v.x), __fsqrt_rn(v.y));
-            if constexpr (BITS == 32) {
-                wv[2 * k] = __float_as_uint(v.x);
-                wv[2 * k + 1] = __float_as_uint(v.y);
-            }
-        }
-        widen(p, wp, t.p_type);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const float2 d = fma2(r[k], both(root), both(h.eps)), up = mul2(m[k], both(-rate));
-            p[k] = fma2(p[k], both(decay), mul2(up, make_float2(inverse(d.x), inverse(d.y))));
-        }
-        l.store(t.p, t.p_type, p);
-        if (t.copy) l.store(t.copy, t.copy_type, p);
-        if constexpr (BITS == 32) {
-            l.store(t.m, MLKV_TYPE_FLOAT, m);
-            l.store<uint32_t>(t.v, wv);
-        } else {
-            bool odd_m, odd_r;
-            const uint32_t pm = power_of(largest(m, odd_m)), pr = power_of(largest(r, odd_r));
-            const float2 im = both(__uint_as_float((254u - pm) << 23)), ir = both(__uint_as_float((254u - pr) << 23));
-            float2 cm[4], cr[4];
-            uint32_t hash = key + (uint32_t)l.place(0) * kWeyl;
-            const uint32_t more = (l.wide ? 1u : 32u) * kWeyl;
-            float least = INFINITY;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                uint32_t a = hash, b = hash + more;
-                hash = b + more;
-                a ^= a >> 15;
-                b ^= b >> 15;
-                cm[k] = moved(mul2(m[k], im), a * 0x6A09E667u, b * 0x6A09E667u);
-                cr[k] = moved(mul2(r[k], ir), a * 0xBB67AE85u, b * 0xBB67AE85u);
-                cr[k] = make_float2(fmaxf(cr[k].x, 0.001953125f), fmaxf(cr[k].y, 0.001953125f));  // (the least code)
-                least = fminf(least, fminf(r[k].x, r[k].y));
-            }
-            if (least == 0.f) {
-#pragma unroll
-                for (int k = 0; k < 4; ++k) cr[k] = make_float2(r[k].x == 0.f ? 0.f : cr[k].x, r[k].y == 0.f ? 0.f : cr[k].y);
-            }
-            if (odd_m || odd_r) {  // a value that is not finite reads back as NaN, the block's others as they are
-                auto mark = [](float& c, float x) { if (!(fabsf(x) < INFINITY)) c = __uint_as_float(0x7FFFFFFFu); };
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    mark(cm[k].x, m[k].x);
-                    mark(cm[k].y, m[k].y);
-                    mark(cr[k].x, r[k].x);
-                    mark(cr[k].y, r[k].y);
-                }
-            }
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                wm[k] = to_codes(cm[2 * k]) | to_codes(cm[2 * k + 1]) << 16;
-                wv[k] = to_codes(cr[2 * k]) | to_codes(cr[2 * k + 1]) << 16;
-            }
-            l.store<uint8_t>(t.m, wm);
-            l.store<uint8_t>(t.v, wv);
-            if (lane == 0) {
-                t.scales[l.at / kGroup] = __uint_as_float(pm << 23);
-                t.scales[blocks + l.at / kGroup] = __uint_as_float(pr << 23);
-            }
+            one.template load<false>(t, at, lane);
+            step_group<BITS, P, G, false>(one, t, h, s, at, lane);
         }
     }
 }
@@ -372,33 +403,43 @@ bool adamw_ok(const mlkv_adamw_args* a) {
     return true;
 }
 
-// A launch of up to N tensors from `at` on; how many it took.
-template <int N>
-int64_t launch_batch(const mlkv_adamw_args& a, const Hyper& h, int groups, int64_t at, cudaStream_t st) {
+// A launch of up to N of the tensors of these types, from `at` on; where it ended.
+template <int N, class P, class G>
+int64_t launch_batch(const mlkv_adamw_args& a, const Hyper& h, int groups, int p_type, int g_type, int64_t at, cudaStream_t st) {
     static thread_local Batch<N> b;  // (a launch copies it)
     b.h = h;
     b.groups = groups;
     const int64_t chunk = (int64_t)groups * kWarps * kGroup;
     b.count = 0;
     uint32_t chunks = 0;
-    const int64_t first = at;
     for (; at < a.count && b.count < N; ++at) {
         const mlkv_adamw_tensor& t = a.tensors[at];
-        if (!t.n) continue;
+        if (!t.n || t.param_type != p_type || t.grad_type != g_type) continue;
         const int64_t more = (t.n + chunk - 1) / chunk;
         if (chunks + more >= (int64_t)1 << 31) break;
         auto on = [](const void* p, int64_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; };
-        const bool wide = on(t.d_param, 8 * dense_type_size(t.param_type)) && on(t.d_grad, 8 * dense_type_size(t.grad_type)) &&
-                          on(t.d_m, a.state_bits) && on(t.d_v, a.state_bits) && (!t.d_copy || on(t.d_copy, 16));
-        b.t[b.count++] = {t.n, t.d_param, t.d_grad, t.d_m, t.d_v, t.d_scales, t.d_copy, chunks, (uint32_t)at,
-                          (int16_t)t.param_type, (int16_t)t.grad_type, (int16_t)t.copy_type, (int16_t)wide};
+        const bool wide = on(t.d_param, 8 * sizeof(P)) && on(t.d_grad, 8 * sizeof(G)) && on(t.d_m, a.state_bits) && on(t.d_v, a.state_bits) &&
+                          (!t.d_copy || on(t.d_copy, 16));
+        b.t[b.count++] = {t.n, t.d_param, t.d_grad, t.d_m, t.d_v, t.d_scales, t.d_copy, chunks, (uint32_t)at, (int16_t)t.copy_type, (int16_t)wide};
         chunks += (uint32_t)more;
     }
     if (b.count) {
-        if (a.state_bits == 32) launch_kernel(true, k_adamw<32, N>, dim3(chunks), dim3(kWarps * 32), 0, st, b);
-        else launch_kernel(true, k_adamw<8, N>, dim3(chunks), dim3(kWarps * 32), 0, st, b);
+        if (a.state_bits == 32) launch_kernel(true, k_adamw<32, P, G, N>, dim3(chunks), dim3(kWarps * 32), 0, st, b);
+        else launch_kernel(true, k_adamw<8, P, G, N>, dim3(chunks), dim3(kWarps * 32), 0, st, b);
     }
-    return at - first;
+    return at;
+}
+template <class P, class G>
+void launch_type(const mlkv_adamw_args& a, const Hyper& h, int groups, int p_type, int g_type, int64_t count, cudaStream_t st) {
+    // The tensors' table is an argument of the launch: 1.7 KB of 24 tensors, 32 KB of 440.
+    for (int64_t at = 0; at < a.count;)
+        at = count <= 24 ? launch_batch<24, P, G>(a, h, groups, p_type, g_type, at, st) : launch_batch<440, P, G>(a, h, groups, p_type, g_type, at, st);
+}
+template <class F>
+void with_type(int type, F f) {
+    if (type == MLKV_TYPE_FLOAT) f(float{});
+    else if (type == MLKV_TYPE_BFLOAT) f(__nv_bfloat16{});
+    else f(__half{});
 }
 
 }  // namespace
@@ -421,12 +462,18 @@ extern "C" int mlkv_adamw(const mlkv_adamw_args* args, void* stream) {
     h.root = (float)(1 / std::sqrt(1 - std::pow(a.beta2, t)));
     h.d_lr = a.d_lr; h.d_step = a.d_step; h.d_grad_scale = a.d_grad_scale;
     h.seed = a.seed; h.step = (uint32_t)a.step; h.one = 1.f;
-    // The tensors' table is an argument of the launch: 1.8 KB of 24 tensors, 32 KB of 440.
-    int64_t all = 0;
-    for (int64_t i = 0; i < a.count; ++i) all += a.tensors[i].n;
-    // (four blocks an SM at once: below that many whole parts, smaller ones)
-    const int groups = all < (int64_t)kChunk * 4 * dense_sms() ? 1 : kGroupsPerWarp;
-    for (int64_t at = 0; at < a.count;)
-        at += a.count - at <= 24 ? launch_batch<24>(a, h, groups, at, (cudaStream_t)stream) : launch_batch<440>(a, h, groups, at, (cudaStream_t)stream);
+    int64_t all = 0, of[9] = {};  // values; tensors of each pair of types
+    for (int64_t i = 0; i < a.count; ++i) {
+        const mlkv_adamw_tensor& t = a.tensors[i];
+        all += t.n;
+        if (t.n) ++of[t.param_type * 3 + t.grad_type];
+    }
+    // (two blocks an SM at once: below that many whole parts, smaller ones)
+    const int groups = all < (int64_t)kChunk * 2 * dense_sms() ? 1 : kGroupsPerWarp;
+    for (int k = 0; k < 9; ++k)
+        if (of[k])
+            with_type(k / 3, [&](auto p) {
+                with_type(k % 3, [&](auto g) { launch_type<decltype(p), decltype(g)>(a, h, groups, k / 3, k % 3, of[k], (cudaStream_t)stream); });
+            });
     return cudaGetLastError() == cudaSuccess ? MLKV_OK : MLKV_ERR_CUDA;
 }

@@ -457,26 +457,27 @@ __device__ __forceinline__ bool put_blocks(const Product& p, const CUtensorMap* 
     return true;
 }
 
+// Kinds of products.
+constexpr int kPlain = 0, kTwo = 1, kTwin = 2, kGated = 3, kStats = 4, kProbs = 5;
+
 // The shared memory of a block: the ring of operand tiles, and a corner and 32
 // bias values for every epilogue warp.
 // A pair of blocks has a tile of 256 rows between them, and half of its columns' operand each.
-// (WIDE: two sums an output; 16 warps have not the registers for that.)
-template <int BN, bool SWAP, bool PAIR, bool WIDE> struct Ring {
+template <int BN, bool SWAP, bool PAIR, int KIND> struct Ring {
+    static constexpr bool WIDE = KIND == kGated;  // (two sums an output: 16 warps have not the registers for that)
+
     // Epilogue warps.  A tile's sums take 8 warps 2.8 us to take out, 16 of them 2.1 (65,536 x 512 by k = 64: 21.3 and
     // 17.2 us): 16 where single blocks have short k, 8 where pairs have the shared memory in more stages.
     static constexpr int kEpilogue = SWAP || BN < 128 ? 4 : BN == 128 || PAIR || WIDE ? 8 : 16;
     static constexpr int kThreads = (kEpilogue + 2) * 32;       // ... and the TMA warp, and the MMA warp
-    static constexpr int kA = kBM * kBK * 2, kB = (PAIR ? BN / 2 : BN) * kBK * 2, kStage = kA + kB;
-    static constexpr int kCorners = SWAP ? 0 : kEpilogue * (kCorner + kBias);
+    static constexpr int kA = kBM * kBK * 2, kB = (PAIR ? BN / 2 : BN) * kBK * 2;
+    static constexpr int kStage = kA + kB, kCorners = SWAP || KIND == kStats ? 0 : kEpilogue * (kCorner + kBias);
     // (two blocks an SM where a block's start is a large part of its time)
     static constexpr int kFit = ((SWAP && WIDE ? kDenseSmem / 2 : kDenseSmem) - 1024 - kCorners) / kStage;
     static constexpr int kStages = kFit < 12 ? kFit : 12;
     static constexpr int kBytes = kStages * kStage + kCorners + 1024;  // (aligned to 1,024 within)
     static constexpr uint32_t kColumns = 2 * BN < 32 ? 32 : 2 * BN;
 };
-
-// Kinds of products.
-constexpr int kPlain = 0, kTwo = 1, kTwin = 2, kGated = 3, kStats = 4, kProbs = 5;
 
 // Bound by the matrix unit where k is long: 16,384 x 4,096 by k = 4,096 (pairs) 284 us, 1.94 PFLOP/s, its pipe active
 // 81 to 87% of the time.  By what L2 hands to the SMs (48 KB a block of k and tile) and the epilogue's bytes where k is
@@ -490,11 +491,11 @@ constexpr int kPlain = 0, kTwo = 1, kTwin = 2, kGated = 3, kStats = 4, kProbs = 
 // products of both, so that B crosses each SM's shared memory half as often.
 // X: what kind of product it is, and what only that kind needs.
 template <int BN, bool A_MN, bool B_MN, bool SWAP, bool PAIR, class T, class X>
-__global__ void __launch_bounds__(Ring<BN, SWAP, PAIR, X::kKind == kGated>::kThreads, 1)
+__global__ void __launch_bounds__(Ring<BN, SWAP, PAIR, X::kKind>::kThreads, 1)
     k_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mb,
               const __grid_constant__ CUtensorMap out_map, const __grid_constant__ CUtensorMap pre_map, const Product p,
               const __grid_constant__ X x) {
-    using R = Ring<BN, SWAP, PAIR, X::kKind == kGated>;
+    using R = Ring<BN, SWAP, PAIR, X::kKind>;
     constexpr int S = R::kStages, kTma = R::kEpilogue, kMma = kTma + 1, kBlocks = PAIR ? 2 : 1, kCols = BN / kBlocks;
     uint32_t brought = kBlocks * R::kStage;  // bytes a stage
     if constexpr (!PAIR && (X::kKind == kStats || X::kKind == kProbs)) brought = x.a_rows * kBK * 2 + R::kB;  // (of few rows no more than there are)
@@ -794,7 +795,7 @@ struct Products {
 
     template <int BN, bool A_MN, bool B_MN, bool SWAP, bool PAIR, class X>
     void launch(const Matrix& a, const Matrix& b, const Second& more, Product p, X x) {
-        using R = Ring<BN, SWAP, PAIR, X::kKind == kGated>;
+        using R = Ring<BN, SWAP, PAIR, X::kKind>;
         constexpr bool kBoth = X::kKind == kGated;  // (two matrices' rows in an operand: half of them each)
         int rows_a = kBoth && SWAP ? kBM / 2 : kBM;
         if constexpr (!PAIR && (X::kKind == kStats || X::kKind == kProbs)) rows_a = x.a_rows;
@@ -877,11 +878,11 @@ struct Products {
     // The width of single blocks' tiles, where the narrower ones fit on the GPU at once.  (Widths of 256 / 128 / 64 at
     // their best, us: 300 x 1,000 by k = 520 9.7 / 7.8 / 7.2; 1,000 x 1,000 by 1,000 12.8 / 9.9 / 8.3; 200 x 512 by 8,192
     // 12.3 / 10.5 / 10.3; 512 x 512 by 8,000 13.1 / 12.4 / 14.6; 4,096 x 1,000 by 776 14.6 / 16.0 / 21.0.)
-    int width(int64_t rows, int64_t cols, int64_t blocks) const {
+    int width(int64_t rows, int64_t cols, int64_t blocks, float* time = nullptr, int times = 1) const {
         int best = cols <= 64 ? 64 : cols <= 128 ? 128 : 256;
         float least = 3e38f;
         for (int bn = 64; bn <= 256; bn *= 2) {
-            const int64_t tiles = (rows + kBM - 1) / kBM * ((cols + bn - 1) / bn);
+            const int64_t tiles = (rows + kBM - 1) / kBM * ((cols + bn - 1) / bn) * times;
             if (tiles <= sms) {
                 const float t = split(tiles, kBM, bn, blocks).time;
                 if (t < least) {
@@ -891,7 +892,14 @@ struct Products {
             }
             if (bn >= cols) break;
         }
+        if (time) *time = least;
         return best;
+    }
+    // Whether pairs of blocks are faster than single ones by the same account (`times` such products at once).
+    bool pair_is_faster(int64_t down, int64_t cols, int64_t blocks, int times) const {
+        float single;
+        width(down * kBM, cols, blocks, &single, times);
+        return split((down + 1) / 2 * ((cols + 255) / 256) * times, 2 * kBM, 256, blocks).time < single;
     }
 
     void finish(const Rest& r) {
@@ -905,13 +913,18 @@ struct Products {
         finish_shares(p, r.p.whole, r.high, r.bn);
     }
 
-    // The width of tiles that are all computed whole, by one launch.
+    // The width of tiles that are all computed whole, by one launch.  Of up to 128 rows all operands' bytes come to the SMs at
+    // kFew a microsecond, whichever they are.  (Widths of 128 / 256, us: 1 row by 131,072 x 2,048 89 / 92, 16 by 65,536 x 2,048 56 / 52,
+    // 100 by 65,536 x 1,024 40 / 31.  64 columns: 136, 72, 41.)
     int whole_width(int64_t rows, int64_t cols, int64_t blocks) const {
+        constexpr float kFew = 7.5e6f;
+        const int64_t down = (rows + kBM - 1) / kBM;
         int best = 256;
         float least = 3e38f;
-        for (int bn = 256; bn >= 64; bn /= 2) {
-            const int64_t tiles = (rows + kBM - 1) / kBM * ((cols + bn - 1) / bn), rounds = (tiles + sms - 1) / sms;
-            const float t = time_of(rounds, bn, blocks, std::min<int64_t>(tiles, sms), false);
+        for (int bn = 256; bn >= (down > 1 ? 64 : 128); bn /= 2) {
+            const int64_t tiles = down * ((cols + bn - 1) / bn), rounds = (tiles + sms - 1) / sms, busy = std::min<int64_t>(tiles, sms);
+            const float t = down > 1 ? time_of(rounds, bn, blocks, busy, false)
+                                     : (float)(rounds * blocks) * std::max((float)(busy * (round_up(rows, 8) + bn)) * kBK * 2 / kFew, 0.34f * bn / 256);
             if (t < least) {
                 least = t;
                 best = bn;
@@ -920,10 +933,6 @@ struct Products {
         return best;
     }
 
-#ifndef MLKV_GATED_ROUNDS
-#define MLKV_GATED_ROUNDS 6
-#endif
-    static constexpr int64_t kGatedRounds = MLKV_GATED_ROUNDS;
     // out = epilogue(A B^T): A [rows][k], B [cols][k]; *_mn: held as [k][rows], [k][cols].
     // kTwo: A B^T + A' B'^T, k values each.  kTwin: also A' B^T, of as many rows, to x.to.  kGated: cols of each of B and B', and what x says.  kStats, kProbs: tiles
     // are computed whole.  kept: the sums go there as they are, all in its shares, and no epilogue is run.
@@ -951,8 +960,9 @@ struct Products {
             p.doubt = (float)p.blocks / (1 << 22);
         }
         const int64_t down = kBoth && swap ? (cols + 63) / 64 : ((int64_t)p.I + kBM - 1) / kBM;
-        const bool pair = kept.bn ? kept.high > kBM : !swap && all_cols > 128 && (X::kKind == kPlain || down > 1) && pair_pays(down, (p.J + 255) / 256, p.blocks);
-        const int bn = kept.bn ? kept.bn : swap ? (rows <= 16 ? 16 : rows <= 32 ? 32 : 64) : pair ? 256 : kWholeTiles ? whole_width(rows, cols, p.blocks) : width(X::kKind == kTwin ? 2 * rows : rows, all_cols, p.blocks);
+        const bool pair = kept.bn ? kept.high > kBM : !swap && all_cols > 128 && (X::kKind == kPlain || down > 1) && pair_pays(down, (p.J + 255) / 256, p.blocks) &&
+                          (X::kKind != kTwin || pair_is_faster(down, cols, p.blocks, 2));
+        const int bn = kept.bn ? kept.bn : swap ? (rows <= 16 ? 16 : rows <= 32 ? 32 : 64) : pair ? 256 : kWholeTiles ? whole_width(rows, cols, p.blocks) : width(rows, all_cols, p.blocks, nullptr, X::kKind == kTwin ? 2 : 1);
         const int64_t across = (p.J + bn - 1) / bn, high = pair ? 2 * kBM : kBM, tiles = (pair ? (down + 1) / 2 : down) * across * (X::kKind == kTwin ? 2 : 1);
         if (tiles >= (int64_t)1 << 30) {
             rc = MLKV_ERR_UNSUPPORTED;
@@ -977,11 +987,11 @@ struct Products {
             return {};
         }
         if (swap) {
-            // few rows: k in shares of at least 4 blocks, those of a tile a cluster (of 2, 4 or 8), one tile a block
+            // few rows: k in shares of at least 4 blocks, those of a tile a cluster (of 2, 4 or 8), one tile a block; of two
+            // weights two blocks an SM.  (One row, us, with as many shares as blocks fit once / twice / four times: 4,096 to
+            // 4,096 15.6 / 14.7 / 18.8; 2,048 to 8,192 15.7 / 14.7 / 18.5; 4,096 to 12,288, one share, 38.5, two 39.5, four 41.)
             int n = 1;
-            while (n < 8 && 2 * n <= std::min<int64_t>(sms / tiles, p.blocks / 4)) n *= 2;
-            // (two weights: so many blocks that the last ones to run are a small part of all, while they have 8 blocks of k)
-            while (kBoth && n < 8 && 16 * n <= p.blocks && 2 * n * tiles <= kGatedRounds * sms) n *= 2;
+            while (n < 8 && 2 * n <= std::min<int64_t>((kBoth ? 2 : 1) * sms / tiles, p.blocks / 4)) n *= 2;
             p.shares = n;
             p.joined = n > 1 || kBoth;
             p.blocks_per_share = (p.blocks + n - 1) / n;  // (the last may be of nothing)
