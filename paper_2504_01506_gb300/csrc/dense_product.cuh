@@ -471,7 +471,7 @@ template <int BN, bool SWAP, bool PAIR, int KIND> struct Ring {
     static constexpr int kEpilogue = SWAP || BN < 128 ? 4 : BN == 128 || PAIR || WIDE ? 8 : 16;
     static constexpr int kThreads = (kEpilogue + 2) * 32;       // ... and the TMA warp, and the MMA warp
     static constexpr int kA = kBM * kBK * 2, kB = (PAIR ? BN / 2 : BN) * kBK * 2;
-    static constexpr int kStage = kA + kB, kCorners = SWAP || KIND == kStats ? 0 : kEpilogue * (kCorner + kBias);
+    static constexpr int kStage = kA + kB, kCorners = SWAP || KIND == kStats ? 0 : kEpilogue * (KIND == kProbs ? kHalf : kCorner + kBias);
     // (two blocks an SM where a block's start is a large part of its time)
     static constexpr int kFit = ((SWAP && WIDE ? kDenseSmem / 2 : kDenseSmem) - 1024 - kCorners) / kStage;
     static constexpr int kStages = kFit < 12 ? kFit : 12;
@@ -663,7 +663,7 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR, X::kKind>::kThreads, 1)
                 if constexpr (X::kKind == kStats) {
                     ok = x.template put<T>(p, at + c, r0 + lane, w.j * BN + c, blocks, w.j * (R::kEpilogue / 4) + (warp >> 2), wait);
                 } else if constexpr (X::kKind == kProbs) {
-                    ok = x.template put<T>(p, &out_map, at + c, corners + warp * kCorner, r0, w.j * BN + c, blocks, lane, turn, wait);
+                    ok = x.template put<T>(p, &out_map, at + c, corners + warp * kHalf, r0, w.j * BN + c, blocks, lane, turn, wait);
                 } else if (X::kKind == kGated && w.part == Work::kNone) {
                     if constexpr (X::kKind == kGated)  // (half of the columns: of each a gate's and, BN / 2 on, the other factor's sum)
                         ok = x.template put<T, BN / 2>(&out_map, at + c / 2, corners + warp * kCorner, r0, w.j * (BN / 2) + c / 2, blocks / 2, lane, turn, wait);

@@ -130,8 +130,8 @@ struct Probs {
                     if (place == 2 * k + 1) v[k].y -= r.g;
                 }
             }
-            const Half s = {corner + (turn++ & 1) * kHalf};
-            if (lane == 0) tma_store_read<1>();
+            const Half s = {corner};
+            if (lane == 0) tma_store_read<0>();
             __syncwarp();
 #pragma unroll
             for (int c = 0; c < 4; ++c)
