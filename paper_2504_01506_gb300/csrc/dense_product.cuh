@@ -475,7 +475,12 @@ template <int BN, bool SWAP, bool PAIR, int KIND> struct Ring {
     // (two blocks an SM where a block's start is a large part of its time)
     static constexpr int kFit = ((SWAP && WIDE ? kDenseSmem / 2 : kDenseSmem) - 1024 - kCorners) / kStage;
     static constexpr int kStages = kFit < 12 ? kFit : 12;
-    static constexpr int kBytes = kStages * kStage + kCorners + 1024;  // (aligned to 1,024 within)
+    // (Aligned to 1,024 within.)  A pair asks for so much that no other block fits beside its blocks: with 209 or 225 KB they
+    // came to SMs on which blocks of the kernel before were just ending, and once in some thousand launches
+    // tcgen05.alloc for both (cta_group::2) then never returned.  An SM has 228 KB, of which each block takes 1 KB more.
+    static constexpr int kBytes = PAIR ? kDenseSmem : kStages * kStage + kCorners + 1024;
+    static_assert(kStages * kStage + kCorners + 1024 <= kBytes, "room for the ring");
+    static_assert(!PAIR || kBytes + 8 * (2 * kStages + 5) + 1024 + 1024 > 228 << 10, "a pair's blocks are alone on their SMs");
     static constexpr uint32_t kColumns = 2 * BN < 32 ? 32 : 2 * BN;
 };
 

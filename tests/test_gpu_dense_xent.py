@@ -273,6 +273,23 @@ def test_refusals():
             call()
 
 
+def test_many_steps_in_a_row():
+    """Pairs of blocks behind small kernels, again and again, with nothing that waits between them."""
+    torch = torch_cuda()
+    from paper_2504_01506_gb300 import dense
+
+    x, w, t, d = _inputs(torch, 2051, 777, 5001, torch.bfloat16)
+    r = dense.linear_cross_entropy(x, w, t)
+    want = dense.linear_cross_entropy_backward(d, x, w, t, r)
+    for _ in range(20):
+        for _ in range(200):
+            r = dense.linear_cross_entropy(x, w, t)
+            got = dense.linear_cross_entropy_backward(d, x, w, t, r)
+        dense.sync()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+
+
 def test_waits_run_out_and_are_told():
     torch = torch_cuda()
     from paper_2504_01506_gb300 import MLKVError, _lib, dense
