@@ -6,8 +6,9 @@
  * application (arXiv 2504.01506, Section 2.1: N(w_nn; E(w_emb; x)); Figure 2,
  * lines 10-16).  These calls are that part's operators: the layer norm of
  * looked-up rows, the matrix product with bias, activation and residual, the
- * log probabilities of given tokens with their entropy and the likeliest
- * alternatives, and the gradients of all three.
+ * gated block, the log probabilities of given tokens with their entropy and the
+ * likeliest alternatives, the cross entropy of a linear layer that keeps no logits,
+ * the gradients of all five, and the AdamW step of the dense weights.
  *
  * Conventions shared by every call (as mlkv_gpu.h's where it has them)
  *   - Pointers named d_* are DEVICE pointers owned by the caller.  Buffers must
@@ -48,7 +49,7 @@ extern "C" {
 #define MLKV_TYPE_BFLOAT 1 /* bfloat16 */
 #define MLKV_TYPE_HALF 2   /* IEEE fp16 */
 
-/* Activations of mlkv_linear. */
+/* Activations of mlkv_linear and mlkv_gated_linear. */
 #define MLKV_ACT_NONE 0
 #define MLKV_ACT_RELU 1
 #define MLKV_ACT_GELU_TANH 2 /* z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2 */
@@ -177,7 +178,7 @@ int mlkv_gated_linear(const mlkv_gated_linear_args* args, void* stream);
 int mlkv_gated_linear_backward(const mlkv_gated_linear_args* args, void* stream);
 
 /* Waits for the stream.  MLKV_ERR_TIMEOUT when a bounded wait inside a product's
- * kernel has run out since this was last told (its outputs are then not valid;
+ * kernel (the linear layer's, the gated block's, the cross entropy's) has run out since this was last told (its outputs are then not valid;
  * the product's own call returned before), else MLKV_OK.  What is told is the
  * current device's, of whichever stream, and it is told to whoever asks first: all
  * that the stream held before the call is counted, and none that runs out on

@@ -10,7 +10,13 @@
 // the length along k, whose second half comes from du and Wu: its sum stays in the accumulator.
 //
 // Sums are fp32; what is rounded to 16 bits is h, the saved g and u (the slopes are
-// taken there), dg, du and the gradients, once each.
+// taken there), dg, du and the gradients, once each.  (So the gradients are off by 1.8 times what rounding them alone
+// would be; g and u in 32 bits would be twice the memory that a training step keeps of the block.)
+//
+// 8,192 rows, 4,096 to 12,288 bf16, silu: forward 870 us (1.90 PFLOP/s, 87% of the time in the matrix unit's pipe), slopes 147
+// (6.8 TB/s), dx 874, both weights' 912 + 21 of shares; in a row the power cap sets the rate, 3,160 for all.  One row: 37.3 us for
+// 201 MB (5.4 TB/s): the 40 SMs with two of the 192 tiles' blocks end last.  4,099 rows, 777 to 1,001, a step: 85 us, of
+// which rows off 16 bytes cost 13 and whole tiles of 256 for 4,099 rows and 777 columns about 20.
 #include "dense_product.cuh"
 
 using namespace mlkv;

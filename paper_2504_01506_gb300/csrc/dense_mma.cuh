@@ -1,5 +1,5 @@
 // Matrix products on the tensor cores: the PTX of TMA, mbarriers and tcgen05
-// that dense_linear.cu's kernel is made of.
+// that the products' kernel (dense_product.cuh) is made of.
 #pragma once
 
 #include <cuda.h>

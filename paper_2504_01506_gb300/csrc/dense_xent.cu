@@ -13,6 +13,11 @@
 // P is rounded to the operands' type, times a power of two that brings the largest
 // |s dl| to 2^13 .. 2^14, which its products' epilogues take back: in fp16 a probability
 // of 1e-5 times a gradient of 1e-4 would be 0.
+//
+// Bound by the matrix unit, under the power cap, where rows are many: 8,192 x 2,048 over 131,072 bf16, forward and
+// backward 10.6 ms, 1.66 PFLOP/s (two pieces forward, 1,120 us each, 1.97 PFLOP/s by itself; four backward, of 582 for P, 597 for
+// dx and 580 for dW).  By the weight's bytes where they are few: one row by 131,072 x 2,048 87 us, 6.2 TB/s.  By whole tiles and L2 between: 2,051
+// x 777 over 50,001 615 us, where 2,048 x 768 over 50,176 takes 407; copies of the weight, whose rows are off 16 bytes, are 54 of it.
 #include "dense_product.cuh"
 
 using namespace mlkv;

@@ -10,6 +10,10 @@ and the apply of its gradients (MLKV, Section 2.1: N(w_nn; E(w_emb; x)); Figure 
     dx, dg, db = layer_norm_backward(dy, rows, g, stats)
     store.apply_grad(keys, dx)
 
+Beside these the gated block (gated_linear), the cross entropy of a linear layer
+without its logits (linear_cross_entropy), with their gradients, and the AdamW step of
+the dense weights (adamw), which is in place.
+
 Matrices are 2-d CUDA tensors of torch.float32, torch.bfloat16 or torch.float16
 (the products: the last two) with any row stride; one whose rows are not
 contiguous, or overlap, is copied first.  Every call is enqueued on the current
