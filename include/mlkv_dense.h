@@ -225,10 +225,11 @@ int mlkv_token_logprobs_backward(const void* d_logits, int64_t stride, int32_t t
  * (logit - max))): an output of the forward pass, an input of the backward pass.
  * Backward: d_dloss, fp32 [n], gives d_dx [n][k] and d_dweight [vocab][k] of `type`,
  * each null where not wanted.  The logits are computed again, in pieces of the vocabulary;
- * their gradients are rounded to `type`, all times one power of two that brings the largest
- * scale |dloss| to 2^13 .. 2^14 and is taken back in 32 bits (in fp16 a row whose
- * gradient is far below the largest one's, by 2^20 or more, loses bits of its small probabilities).
- * n >= 0, k >= 1, vocab >= 1, each < 2^30; scale > 0, finite.  n == 0 gives a zero dweight.
+ * their gradients are rounded to `type`, all times what makes the largest scale |dloss|
+ * 2^14, which is taken back in 32 bits (losses that all count alike lose nothing by their
+ * gradient's rounding; in fp16 a row whose gradient is far below the largest one's, by 2^20 or
+ * more, loses bits of its small probabilities).
+ * n >= 0, k >= 1, vocab >= 1, each < 2^30; 0 < scale < 2^127.  n == 0 gives a zero dweight.
  * Logits are never rounded to 16 bits.  One of -inf has probability 0, and a row of
  * nothing else loss +inf; NaN or +inf among them make a row's statistics NaN.
  * Working memory: forward 64 MB at most, or 512 bytes a row; backward 512 MB at most, or 8 KB a
@@ -274,8 +275,8 @@ int mlkv_linear_cross_entropy_backward(const mlkv_linear_cross_entropy_args* arg
  * the same call gives the same codes.  sqrt(v) > 0 keeps a code above 0.  A value
  * that is not finite has the code NaN and leaves its block's others as they are.
  * All zeros is the state before the first step.
- * `tensors` is a host array; no tensor may overlap another, but gradients each
- * other.  Parameters and gradients are of any element type, 0 <= n < 2^40; a tensor
+ * `tensors` is a host array; what is written may overlap nothing else (what is written
+ * twice is refused), gradients may overlap each other.  Parameters and gradients are of any element type, 0 <= n < 2^40; a tensor
  * off 32 bytes (16-bit values: 16, codes: 8) takes several times as long.
  * d_step (int64), d_lr and d_grad_scale (fp32): a value each on the device, read when the
  * call runs, instead of step, lr and 1 (null), so that a captured step can be

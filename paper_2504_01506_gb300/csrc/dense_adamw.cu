@@ -387,17 +387,25 @@ bool adamw_ok(const mlkv_adamw_args* a) {
         if (!t.d_param || !t.d_grad || !t.d_m || !t.d_v || (a->state_bits == 8 && !t.d_scales)) return false;
         if (t.d_copy && (t.copy_type < MLKV_TYPE_BFLOAT || t.copy_type > MLKV_TYPE_HALF)) return false;
     }
-    // No parameter twice: two blocks would step it at the same time.
+    // Nothing that is written twice: two blocks would step it at the same time.
     struct Range { uintptr_t from, to; };
     static thread_local std::vector<Range> ranges;
     ranges.clear();
+    auto take = [&](const void* p, int64_t bytes) {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+        if (p) ranges.push_back({at, at + (uintptr_t)bytes});
+    };
+    const int64_t state = a->state_bits / 8;
     for (int64_t i = 0; i < a->count; ++i) {
         const mlkv_adamw_tensor& t = a->tensors[i];
-        const uintptr_t p = reinterpret_cast<uintptr_t>(t.d_param);
-        if (t.n) ranges.push_back({p, p + t.n * dense_type_size(t.param_type)});
+        if (!t.n) continue;
+        take(t.d_param, t.n * dense_type_size(t.param_type));
+        take(t.d_m, t.n * state);
+        take(t.d_v, t.n * state);
+        take(t.d_copy, t.n * 2);
+        if (a->state_bits == 8) take(t.d_scales, (t.n + kGroup - 1) / kGroup * 8);
     }
-    auto below = [](const Range& x, const Range& y) { return x.from < y.from; };
-    if (!std::is_sorted(ranges.begin(), ranges.end(), below)) std::sort(ranges.begin(), ranges.end(), below);
+    std::sort(ranges.begin(), ranges.end(), [](const Range& x, const Range& y) { return x.from < y.from; });
     for (size_t i = 1; i < ranges.size(); ++i)
         if (ranges[i].from < ranges[i - 1].to) return false;
     return true;

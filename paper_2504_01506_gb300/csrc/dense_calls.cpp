@@ -360,7 +360,7 @@ bool xent_operands(PyObject* xo, PyObject* wo, PyObject* targets, PyObject* scal
         w.rows < 1 || x.cols < 1 || !PyFloat_Check(scale) || !vector_of(targets, x, x.rows, at::kLong, &t))
         return false;
     const double s = PyFloat_AS_DOUBLE(scale);
-    if (!(s > 0 && s < std::numeric_limits<double>::infinity())) return false;
+    if (!(s > 0 && s < 0x1p127)) return false;
     g = mlkv_linear_cross_entropy_args{};
     g.n = x.rows; g.k = x.cols; g.vocab = w.rows;
     g.d_x = x.p; g.x_stride = x.stride; g.d_weight = w.p; g.weight_stride = w.stride; g.d_targets = (const int64_t*)t;

@@ -10,9 +10,10 @@
 // piece's logits again, with P as the epilogue, then P's two products.  dx is
 // the sum over the pieces: it stays in fp32 until the last.
 //
-// P is rounded to the operands' type, times a power of two that brings the largest
-// |s dl| to 2^13 .. 2^14, which its products' epilogues take back: in fp16 a probability
-// of 1e-5 times a gradient of 1e-4 would be 0.
+// P is rounded to the operands' type, times what makes the largest |s dl| 2^14, which its
+// products' epilogues take back: in fp16 a probability of 1e-5 times a gradient of 1e-4
+// would be 0, and of losses that all count alike (a mean's 1 / n) every target's place is
+// then 2^14 (p - 1), where 1 / n rounded to 8 bits would be off by up to 2^-8 in all of them alike.
 //
 // Bound by the matrix unit, under the power cap, where rows are many: 8,192 x 2,048 over 131,072 bf16, forward and
 // backward 10.6 ms, 1.66 PFLOP/s (two pieces forward, 1,120 us each, 1.97 PFLOP/s by itself; four backward, of 582 for P, 597 for
@@ -92,7 +93,7 @@ struct Stats {
 // Backward: what a row needs.
 struct RowOf {
     float max, logs;  // of the logits before the scale; log2 of the sum of exponentials
-    float g;          // scale times the loss's gradient, times the power of two
+    float g;          // scale times the loss's gradient, of the largest one 2^14
     int32_t target;
 };
 struct Probs {
@@ -198,13 +199,13 @@ __global__ void __launch_bounds__(256) k_xent_join(Join a) {
     a.loss[row] = loss;
 }
 
-// Rows as the backward pass takes them, and the power of two: every block looks for the largest gradient itself.
+// Rows as the backward pass takes them, and the largest gradient, for which every block looks itself.
 struct Prepare {
     const float* dloss;
     const float2* stats;
     const int64_t* targets;
     RowOf* of;
-    float* back;  // what takes the power of two out of the products
+    float* back;  // what the products are to be multiplied by
     float scale;
     int32_t rows, vocab;
 };
@@ -221,14 +222,12 @@ __global__ void __launch_bounds__(1024) k_xent_rows(Prepare a) {
     if ((threadIdx.x & 31) == 0) most[threadIdx.x >> 5] = m;
     __syncthreads();
     m = __reduce_max_sync(0xffffffffu, most[threadIdx.x & 31]);
-    // 2^(140 - e) brings 2^(e - 127) <= |g| to 2^13; 2^-126 .. 2^126
-    const int e = min(max(140 - (int)(m >> 23), -126), 126);
-    const float up = m ? __uint_as_float((uint32_t)(e + 127) << 23) : 1.f;
-    if (blockIdx.x == 0 && threadIdx.x == 0) *a.back = m ? __uint_as_float((uint32_t)(127 - e) << 23) : 1.f;
+    const float most_of_all = __uint_as_float(m);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.back = m ? most_of_all * 0x1p-14f : 1.f;
     for (int i = blockIdx.x * 1024 + threadIdx.x; i < a.rows; i += gridDim.x * 1024) {
         const float2 s = a.stats[i];
         const int64_t t = a.targets[i];
-        RowOf r = {s.x, s.y / kLog2, gradient(i) * up, t < 0 || t >= a.vocab ? -1 : (int32_t)t};
+        RowOf r = {s.x, s.y / kLog2, m ? gradient(i) / most_of_all * 0x1p14f : gradient(i), t < 0 || t >= a.vocab ? -1 : (int32_t)t};
         if (t >= a.vocab) r.g = NAN;
         if (s.x == -INFINITY) r = {0.f, INFINITY, 0.f, -1};  // nothing to choose from
         a.of[i] = r;
@@ -342,7 +341,7 @@ struct Caller : Products {
 bool xent_ok(const mlkv_linear_cross_entropy_args* g) {
     if (!g || g->n < 0 || g->k < 1 || g->vocab < 1 || std::max(g->n, std::max(g->k, g->vocab)) >= (int64_t)1 << 30) return false;
     if (g->type != MLKV_TYPE_BFLOAT && g->type != MLKV_TYPE_HALF) return false;
-    if (!(g->scale > 0) || !(g->scale < INFINITY)) return false;
+    if (!(g->scale > 0) || !(g->scale < 0x1p127f)) return false;  // (times 1 / log 2 it is finite)
     if (!rows_ok(g->d_x, g->x_stride, g->n, g->k, false) || !rows_ok(g->d_weight, g->weight_stride, g->vocab, g->k, false)) return false;
     return !g->n || (g->d_targets && g->d_stats);
 }

@@ -478,8 +478,8 @@ def _xent_args(x, weight, targets, scale):
     weight, vocab, along, weight_stride = _rows(weight, "weight", (x.dtype,), None, device)
     if along != k or vocab < 1 or k < 1:
         raise ValueError(f"weight must be [vocab, {k}] with at least one value, not {[vocab, along]}")
-    if not 0 < scale < float("inf"):
-        raise ValueError(f"scale must be positive and finite, not {scale}")
+    if not 0 < scale < 2.0 ** 127:
+        raise ValueError(f"scale must be positive and below 2^127, not {scale}")
     targets = _vector(targets, "targets", n, device, (torch.int64,))
     a = L.LinearCrossEntropyArgs(n, k, vocab, x.data_ptr(), x_stride, weight.data_ptr(), weight_stride, targets.data_ptr())
     a.scale, a.type = scale, _TYPES[x.dtype]
@@ -577,7 +577,8 @@ def adamw(params, grads, state: AdamWState, step, *, lr, betas=(0.9, 0.999), eps
         g = grad_scale * grad;  m = b1 m + (1 - b1) g;  v = b2 v + (1 - b2) g^2
         p = p (1 - lr weight_decay) - lr (m / (1 - b1^step)) / (sqrt(v / (1 - b2^step)) + eps)
 
-    params: contiguous tensors of any shape, no one twice, all on one device; grads:
+    params: contiguous tensors of any shape, all on one device (what is written may not
+    overlap); grads:
     tensors of their shapes (None: that parameter stays as it is).  copies: None, or a
     16-bit tensor (or None) for each fp32 parameter, which takes the new values rounded:
     what the products use.  step: the step's number, from 1 on; lr: the rate; both also as a value

@@ -57,7 +57,7 @@ def test_gated_linear_refusals(lib):
 def test_linear_cross_entropy_refusals(lib):
     good = dict(n=4, k=8, vocab=16, d_x=P, x_stride=8, d_weight=P, weight_stride=8, d_targets=P, d_loss=P, d_stats=P, scale=1.0, type=_lib.TYPE_HALF)
     bads = (dict(n=-1), dict(k=0), dict(vocab=0), dict(n=2 ** 30), dict(vocab=2 ** 30), dict(type=_lib.TYPE_FLOAT), dict(scale=0.0), dict(scale=-1.0),
-            dict(scale=math.inf), dict(scale=math.nan), dict(d_x=None), dict(x_stride=7), dict(d_weight=None), dict(weight_stride=7), dict(d_targets=None),
+            dict(scale=math.inf), dict(scale=2.0 ** 127), dict(scale=math.nan), dict(d_x=None), dict(x_stride=7), dict(d_weight=None), dict(weight_stride=7), dict(d_targets=None),
             dict(d_stats=None))
     for bad in (*bads, dict(d_loss=None)):
         a = _lib.LinearCrossEntropyArgs(**{**good, **bad})
@@ -76,7 +76,7 @@ def _adamw(tensors, **over):
 
 
 def test_adamw_refusals(lib):
-    one = dict(n=8, d_param=P, d_grad=P, d_m=P, d_v=P)
+    one = dict(n=8, d_param=P, d_grad=P, d_m=2 * P, d_v=3 * P)
     t = lambda **over: _lib.AdamWTensor(**{**one, **over})  # noqa: E731
     for bad in (dict(n=-1), dict(n=2 ** 40), dict(d_param=None), dict(d_grad=None), dict(d_m=None), dict(d_v=None), dict(param_type=3), dict(grad_type=-1),
                 dict(d_copy=P, copy_type=_lib.TYPE_FLOAT), dict(d_copy=P, copy_type=3)):
@@ -84,9 +84,14 @@ def test_adamw_refusals(lib):
     for bad in (dict(state_bits=16), dict(state_bits=8), dict(count=-1), dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=math.nan), dict(eps=-1.0), dict(eps=math.inf),
                 dict(weight_decay=math.nan), dict(lr=math.inf), dict(step=0)):
         assert lib.mlkv_adamw(_adamw([t()], **bad), None) == _lib.ERR_INVALID, bad
-    # a parameter twice, or a part of it
-    for other in (t(), t(d_param=P + 28), t(d_param=P - 4)):
-        assert lib.mlkv_adamw(_adamw([t(), other]), None) == _lib.ERR_INVALID
+    # a parameter twice, or a part of it; a state twice; one tensor as both
+    apart = dict(d_param=5 * P, d_m=6 * P, d_v=7 * P)
+    for other in (dict(d_param=P), dict(d_param=P + 28), dict(d_param=P - 4), dict(d_m=2 * P), dict(d_v=3 * P + 4), dict(d_v=2 * P), dict(d_m=5 * P),
+                  dict(d_copy=P, copy_type=_lib.TYPE_BFLOAT)):
+        assert lib.mlkv_adamw(_adamw([t(), t(**{**apart, **other})]), None) == _lib.ERR_INVALID, other
+    assert lib.mlkv_adamw(_adamw([t(d_v=2 * P)]), None) == _lib.ERR_INVALID
+    small = dict(d_scales=8 * P)
+    assert lib.mlkv_adamw(_adamw([t(**small), t(**apart, **small)], state_bits=8), None) == _lib.ERR_INVALID
     assert lib.mlkv_adamw(None, None) == _lib.ERR_INVALID
 
 

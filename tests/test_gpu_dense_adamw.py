@@ -348,6 +348,8 @@ def test_refusals():
             (MLKVError, lambda: dense.adamw([p], [p], st, 1, lr=math.nan)),
             (MLKVError, lambda: dense.adamw([p, p], [p, p], dense.adamw_state([p, p]), 1, **ok)),
             (MLKVError, lambda: dense.adamw([p, p[4:]], [p, p[4:]], dense.adamw_state([p, p[4:]]), 1, **ok)),
+            (MLKVError, lambda: dense.adamw([p], [p], dense.AdamWState(st.m, st.m, None), 1, **ok)),
+            (MLKVError, lambda: dense.adamw([p, p.clone()], [p, p], dense.AdamWState(st.m * 2, [p.clone(), p.clone()], None), 1, **ok)),
             (TypeError, lambda: dense.adamw([p], [p], st, 1, copies=[p], **ok)), (TypeError, lambda: dense.adamw([p.half()], [p], st, 1, copies=[p.half()], **ok)),
             (ValueError, lambda: dense.adamw([p], [p], st, 1, copies=[], **ok)), (TypeError, lambda: dense.adamw([p], [p], dense.AdamWState(s8.m, s8.v, None), 1, **ok)),
             (TypeError, lambda: dense.adamw([p], [p], dense.AdamWState(st.m, st.v, s8.scales), 1, **ok)),

@@ -73,8 +73,21 @@ def test_sharp_and_flat_rows():
     _check(torch, 200, 64, 700, torch.float16, sigma=0.0)
 
 
+def test_losses_that_count_alike():
+    """A gradient that 8 bits cannot hold, the same for all rows: what is off is the outputs' own rounding (2^-8 at most, 0.0017 of the
+    norm: values spread over a binade), not the gradient's (2^-8 too, in every place alike)."""
+    torch = torch_cuda()
+    from paper_2504_01506_gb300 import dense
+
+    x, w, t, _ = _inputs(torch, 600, 96, 3000, torch.bfloat16, sigma=0.5)
+    d = torch.full((600,), 1 + 2.0 ** -8 - 2.0 ** -14, device="cuda")
+    r = dense.linear_cross_entropy(x, w, t)
+    for got, (want, _) in zip(dense.linear_cross_entropy_backward(d, x, w, t, r), ref.xent_backward(d, x, w, t, 1.0, torch.bfloat16)):
+        assert float((got.double() - want).norm()) <= 0.002 * float(want.norm())
+
+
 def test_small_gradients_in_half_precision():
-    """Of a mean over many rows without a loss scale: P would be 0 in fp16, were it not for the power of two; dx itself is given times 2^14 back."""
+    """Of a mean over many rows without a loss scale: P would be 0 in fp16, were it not held in units of the largest gradient."""
     torch = torch_cuda()
     from paper_2504_01506_gb300 import dense
 
@@ -85,6 +98,22 @@ def test_small_gradients_in_half_precision():
     for a, b in zip(big, small):
         # the same P, and so the same sums, 2^-10 times: but for the last rounding, in fp16's smallest steps
         assert bool(((a.float() * 2.0 ** -10 - b.float()).abs() <= 2.0 ** -25 + 2.0 ** -10 * 2.0 ** -11 * a.float().abs()).all())
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -100, 1.7e38])
+def test_scales_next_to_their_ends(scale):
+    """All logits as one, and none but the largest."""
+    torch = torch_cuda()
+    from paper_2504_01506_gb300 import dense
+
+    x, w, t, d = _inputs(torch, 40, 32, 300, torch.bfloat16)
+    z = x.float() @ w.float().T
+    t = z.argmax(1)
+    r = dense.linear_cross_entropy(x, w, t, scale=scale)
+    want = math.log(300) if scale < 1 else 0.0
+    assert float((r.loss - want).abs().max()) <= 1e-5
+    dx, dw = dense.linear_cross_entropy_backward(d * 1e-30, x, w, t, r, scale=scale)
+    assert bool(dx.isfinite().all()) and bool(dw.isfinite().all())
 
 
 def test_targets_that_are_none_or_not_there():
