@@ -14,8 +14,8 @@
 // would be; g and u in 32 bits would be twice the memory that a training step keeps of the block.)
 //
 // 8,192 rows, 4,096 to 12,288 bf16, silu: forward 870 us (1.90 PFLOP/s, 87% of the time in the matrix unit's pipe), slopes 147
-// (6.8 TB/s), dx 874, both weights' 912 + 21 of shares; in a row the power cap sets the rate, 3,160 for all.  One row: 37.3 us for
-// 201 MB (5.4 TB/s): the 40 SMs with two of the 192 tiles' blocks end last.  4,099 rows, 777 to 1,001, a step: 85 us, of
+// (6.8 TB/s), dx 874, both weights' 912 + 21 of shares; in a row the power cap sets the rate, 3,160 for all.  One row: 34.9 us for
+// 201 MB (5.8 TB/s).  4,099 rows, 777 to 1,001, a step: 85 us, of
 // which rows off 16 bytes cost 13 and whole tiles of 256 for 4,099 rows and 777 columns about 20.
 #include "dense_product.cuh"
 
@@ -23,24 +23,24 @@ using namespace mlkv;
 
 namespace {
 
-// Four neighbouring outputs of a row.
+// Four neighbouring outputs of a row, those before `end`.
 struct Outputs {
     void *h, *gate, *up;
     int64_t h_stride, gate_stride, up_stride;
     int32_t f, act, wide, wide_pre;  // rows of h, of gate and up can be moved 16 bytes at a time
     template <class T>
-    __device__ __forceinline__ void put_four(const float4& g4, const float4& u4, int64_t row, int64_t col) const {
+    __device__ __forceinline__ void put_four(const float4& g4, const float4& u4, int64_t row, int64_t col, int64_t end) const {
         float2 g[2] = {make_float2(g4.x, g4.y), make_float2(g4.z, g4.w)}, u[2] = {make_float2(u4.x, u4.y), make_float2(u4.z, u4.w)};
         auto store = [&](void* m, int64_t stride, bool whole, const float2 (&v)[2]) {
             T* at = static_cast<T*>(m) + row * stride + col;
-            if (whole && col + 4 <= f) {
+            if (whole && col + 4 <= end && !(col & 3)) {
                 *reinterpret_cast<uint2*>(at) = make_uint2(word_of_pair<T>(v[0]), word_of_pair<T>(v[1]));
                 return;
             }
             const float x[4] = {v[0].x, v[0].y, v[1].x, v[1].y};
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                if (col + k < f) at[k] = from_float<T>(x[k]);
+                if (col + k < end) at[k] = from_float<T>(x[k]);
         };
         if (gate) {
             store(gate, gate_stride, wide_pre, g);
@@ -60,6 +60,7 @@ struct Gated : Outputs {
     static constexpr int kKind = kGated;
     CUtensorMap second, gate_map, up_map;  // of Wu, and where g and u go
     int32_t m;
+    int32_t rows_each;  // few rows: of each weight, a tile's
 
     // A warp's 32 rows of a tile, 32 outputs at a time: g at `tmem`, u HALF columns on.
     template <class T, int HALF, class W>
@@ -116,9 +117,11 @@ struct Gated : Outputs {
     // the shared memory of each block of the cluster, added up in order.
     template <class T, int BN>
     __device__ __forceinline__ void join(const Product& p, uint32_t at, int i, int j, uint32_t rank) const {
-        const int rows = kBM / 2 / p.shares / 4, columns = min(BN, p.J - j * BN);
-        for (int q = threadIdx.x; q < rows * columns; q += 128) {
-            const int c = q / rows, r = ((int)rank * rows + q % rows) * 4;
+        // (a block of the cluster has its part of the rows, in fours)
+        const int fours = (rows_each + 3) / 4, mine = (fours + p.shares - 1) / p.shares, columns = min(BN, p.J - j * BN);
+        for (int q = threadIdx.x; q < mine * columns; q += 128) {
+            const int c = q / mine, r = ((int)rank * mine + q % mine) * 4;
+            if (r >= rows_each) continue;
             float4 sum[2] = {};
             for (int s = 0; s < p.shares; ++s)
 #pragma unroll
@@ -130,7 +133,7 @@ struct Gated : Outputs {
                                  : "memory");
                     sum[half] = make_float4(sum[half].x + x.x, sum[half].y + x.y, sum[half].z + x.z, sum[half].w + x.w);
                 }
-            put_four<T>(sum[0], sum[1], (int64_t)j * BN + c, (int64_t)i * (kBM / 2) + r);
+            put_four<T>(sum[0], sum[1], (int64_t)j * BN + c, (int64_t)i * rows_each + r, min((int64_t)f, (int64_t)(i + 1) * rows_each));
         }
     }
 };
@@ -169,7 +172,7 @@ __global__ void __launch_bounds__(256) k_gated_finish(const Product p, const Out
     int i, j;
     tile_at(p, p.whole + (int)tile, i, j);
     const int64_t row = i * high + r, col = ((int64_t)j * across + c) * 4;
-    if (row < m && col < o.f) o.put_four<T>(g, u, row, col);
+    if (row < m && col < o.f) o.put_four<T>(g, u, row, col, o.f);
 }
 
 // The activation and its slope, with one exponential and one division of each value.

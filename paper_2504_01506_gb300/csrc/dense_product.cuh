@@ -503,6 +503,7 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR, X::kKind>::kThreads, 1)
     using R = Ring<BN, SWAP, PAIR, X::kKind>;
     constexpr int S = R::kStages, kTma = R::kEpilogue, kMma = kTma + 1, kBlocks = PAIR ? 2 : 1, kCols = BN / kBlocks;
     uint32_t brought = kBlocks * R::kStage;  // bytes a stage
+    if constexpr (X::kKind == kGated && SWAP) brought = 2 * x.rows_each * kBK * 2 + R::kB;
     if constexpr (!PAIR && (X::kKind == kStats || X::kKind == kProbs)) brought = x.a_rows * kBK * 2 + R::kB;  // (of few rows no more than there are)
     extern __shared__ uint8_t raw[];
     __shared__ __align__(8) uint64_t bars[2 * S + 5];
@@ -562,8 +563,8 @@ __global__ void __launch_bounds__(Ring<BN, SWAP, PAIR, X::kKind>::kThreads, 1)
                     };
                     if constexpr (X::kKind == kGated) {  // the tile's rows of both weights, as one operand
                         if constexpr (SWAP) {
-                            load(at, &ma, k * kBK, w.i * (kBM / 2));
-                            load(at + R::kA / 2, &x.second, k * kBK, w.i * (kBM / 2));
+                            load(at, &ma, k * kBK, w.i * x.rows_each);
+                            load(at + R::kA / 2, &x.second, k * kBK, w.i * x.rows_each);
                             load(at + R::kA, &mb, k * kBK, col);
                         } else {
                             load(at, &ma, k * kBK, row);
@@ -802,7 +803,8 @@ struct Products {
     void launch(const Matrix& a, const Matrix& b, const Second& more, Product p, X x) {
         using R = Ring<BN, SWAP, PAIR, X::kKind>;
         constexpr bool kBoth = X::kKind == kGated;  // (two matrices' rows in an operand: half of them each)
-        int rows_a = kBoth && SWAP ? kBM / 2 : kBM;
+        int rows_a = kBM;
+        if constexpr (kBoth && SWAP) rows_a = x.rows_each;
         if constexpr (!PAIR && (X::kKind == kStats || X::kKind == kProbs)) rows_a = x.a_rows;
         constexpr int kRowsB = PAIR || (kBoth && !SWAP) ? BN / 2 : BN;
         CUtensorMap ma, mb;
@@ -964,7 +966,25 @@ struct Products {
             p.k = (int32_t)k;
             p.doubt = (float)p.blocks / (1 << 22);
         }
-        const int64_t down = kBoth && swap ? (cols + 63) / 64 : ((int64_t)p.I + kBM - 1) / kBM;
+        int64_t down = ((int64_t)p.I + kBM - 1) / kBM;
+        // few rows: k in shares of at least 4 blocks, those of a tile a cluster (of 2, 4 or 8), one tile a block; of two weights two
+        // blocks an SM.
+        int few_shares = 1;
+        auto share_out = [&](int64_t tiles, int64_t places) {
+            while (few_shares < 8 && 2 * few_shares <= std::min<int64_t>(places / tiles, p.blocks / 4)) few_shares *= 2;
+        };
+        if constexpr (kBoth) {
+            x.rows_each = kBM / 2;
+            if (swap) {
+                // So many of each weight's rows a tile, 16 to 64, that the blocks are whole rounds of two an SM.  (One row, us, tiles
+                // of 64 / so: 4,096 to 12,288 37.3 / 34.9, to 10,240 35.6 / 30.6.  Of shares of k, whose clusters of 4 and 8 do not
+                // fill the SMs that way: 4,096 to 4,096 15.0 / 21.8, 8,192 to 1,024 10.6 / 18.0.)
+                share_out((cols + 63) / 64, 2 * sms);
+                const int64_t places = 2ll * sms, rounds = (cols + 64 * places - 1) / (64 * places);
+                if (few_shares == 1) x.rows_each = (int32_t)std::max<int64_t>(16, (cols + places * rounds - 1) / (places * rounds));
+                down = (cols + x.rows_each - 1) / x.rows_each;
+            }
+        }
         const bool pair = kept.bn ? kept.high > kBM : !swap && all_cols > 128 && (X::kKind == kPlain || down > 1) && pair_pays(down, (p.J + 255) / 256, p.blocks) &&
                           (X::kKind != kTwin || pair_is_faster(down, cols, p.blocks, 2));
         const int bn = kept.bn ? kept.bn : swap ? (rows <= 16 ? 16 : rows <= 32 ? 32 : 64) : pair ? 256 : kWholeTiles ? whole_width(rows, cols, p.blocks) : width(rows, all_cols, p.blocks, nullptr, X::kKind == kTwin ? 2 : 1);
@@ -992,11 +1012,8 @@ struct Products {
             return {};
         }
         if (swap) {
-            // few rows: k in shares of at least 4 blocks, those of a tile a cluster (of 2, 4 or 8), one tile a block; of two
-            // weights two blocks an SM.  (One row, us, with as many shares as blocks fit once / twice / four times: 4,096 to
-            // 4,096 15.6 / 14.7 / 18.8; 2,048 to 8,192 15.7 / 14.7 / 18.5; 4,096 to 12,288, one share, 38.5, two 39.5, four 41.)
-            int n = 1;
-            while (n < 8 && 2 * n <= std::min<int64_t>((kBoth ? 2 : 1) * sms / tiles, p.blocks / 4)) n *= 2;
+            if (!kBoth) share_out(tiles, sms);
+            const int n = few_shares;
             p.shares = n;
             p.joined = n > 1 || kBoth;
             p.blocks_per_share = (p.blocks + n - 1) / n;  // (the last may be of nothing)

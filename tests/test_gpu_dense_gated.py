@@ -51,7 +51,7 @@ def test_activations_and_types(m, k, f, dtype, name):
 # pairs of blocks; sizes off 8, off tiles, of one.
 SIZES = [(1, 4096, 512), (2, 1000, 1024), (16, 72, 40), (33, 777, 1001), (64, 2048, 96), (64, 64, 10_000), (65, 64, 64), (100, 4096, 40),
          (128, 8192, 64), (129, 1024, 33), (300, 520, 1000), (1000, 64, 24), (515, 77, 1001), (4096, 128, 1000), (2048, 768, 1280),
-         (2050, 776, 1300), (1, 1, 1), (3, 7, 5), (70, 1, 1), (200, 8, 300)]
+         (2050, 776, 1300), (1, 1, 1), (3, 7, 5), (70, 1, 1), (200, 8, 300), (1, 256, 12_288), (17, 72, 9_729), (33, 40, 20_003)]
 
 
 @pytest.mark.parametrize("m,k,f", SIZES)
