@@ -96,20 +96,59 @@ struct RowOf {
     float g;          // scale times the loss's gradient, of the largest one 2^14
     int32_t target;
 };
+// Out of what: every block looks for the largest gradient itself.
+struct Rows {
+    const float* dloss;
+    const float2* stats;
+    const int64_t* targets;
+    float* back;  // what the products are to be multiplied by
+    float scale;
+    int32_t rows, vocab;
+
+    __device__ __forceinline__ float gradient(int i) const { return targets[i] < 0 ? 0.f : dloss[i] * scale; }
+    // The largest one's bits, of those that are finite, of every `step`th row: a warp's.
+    __device__ __forceinline__ uint32_t largest(int from, int step) const {
+        uint32_t m = 0;
+#pragma unroll 4
+        for (int i = from; i < rows; i += step) {
+            const uint32_t bits = __float_as_uint(gradient(i)) & 0x7FFFFFFFu;
+            if (bits < 0x7F800000u) m = max(m, bits);
+        }
+        return __reduce_max_sync(0xffffffffu, m);
+    }
+    __device__ __forceinline__ float unit(uint32_t m) const { return m ? __uint_as_float(m) * 0x1p-14f : 1.f; }
+    __device__ __forceinline__ RowOf row(int i, uint32_t m) const {
+        const float2 s = stats[i];
+        const int64_t t = targets[i];
+        const float g = gradient(i);
+        RowOf r = {s.x, s.y / kLog2, m ? g / __uint_as_float(m) * 0x1p14f : g, t < 0 || t >= vocab ? -1 : (int32_t)t};
+        if (t >= vocab) r.g = NAN;
+        if (s.x == -INFINITY) r = {0.f, INFINITY, 0.f, -1};  // nothing to choose from
+        return r;
+    }
+};
 struct Probs {
     static constexpr int kKind = kProbs;
-    const RowOf* of;
+    const RowOf* of;  // null: few rows, of which every warp makes its own (a launch less: of 14 us for 64 x 128 over 5,000, 2)
+    Rows from;
     float rate;
     int32_t rows, v0;
     int32_t a_rows;
 
     template <class T, class W>
     __device__ __forceinline__ bool put(const Product& p, const CUtensorMap* map, uint32_t tmem, uint8_t* corner, int r0, int c0, int blocks, int lane,
-                                        uint32_t& turn, W wait) const {
+                                        uint32_t& known, W wait) const {
         RowOf r = {0.f, 0.f, 0.f, -1};
-        if (blocks && r0 + lane < rows) {
-            const uint4 w = *reinterpret_cast<const uint4*>(of + r0 + lane);
-            r = {__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), (int32_t)w.w};
+        if (of) {
+            if (blocks && r0 + lane < rows) {
+                const uint4 w = *reinterpret_cast<const uint4*>(of + r0 + lane);
+                r = {__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), (int32_t)w.w};
+            }
+        } else if (blocks) {  // (known: the largest gradient, from the first tile on)
+            if (!known) known = 1u << 31 | from.largest(lane, 32);
+            const uint32_t m = known & 0x7FFFFFFFu;
+            if (r0 + lane < rows) r = from.row(r0 + lane, m);
+            if (!r0 && !c0 && !v0 && !lane) *from.back = from.unit(m);
         }
         if (!wait()) return false;
 #pragma unroll 1
@@ -199,39 +238,16 @@ __global__ void __launch_bounds__(256) k_xent_join(Join a) {
     a.loss[row] = loss;
 }
 
-// Rows as the backward pass takes them, and the largest gradient, for which every block looks itself.
-struct Prepare {
-    const float* dloss;
-    const float2* stats;
-    const int64_t* targets;
-    RowOf* of;
-    float* back;  // what the products are to be multiplied by
-    float scale;
-    int32_t rows, vocab;
-};
-__global__ void __launch_bounds__(1024) k_xent_rows(Prepare a) {
+// Rows as Probs takes them, where they are many.
+__global__ void __launch_bounds__(1024) k_xent_rows(Rows a, RowOf* of) {
     pdl_enter();
     __shared__ uint32_t most[32];
-    auto gradient = [&](int i) { return a.targets[i] < 0 ? 0.f : a.dloss[i] * a.scale; };
-    uint32_t m = 0;
-    for (int i = threadIdx.x; i < a.rows; i += 1024) {
-        const uint32_t bits = __float_as_uint(gradient(i)) & 0x7FFFFFFFu;
-        if (bits < 0x7F800000u) m = max(m, bits);
-    }
-    m = __reduce_max_sync(0xffffffffu, m);
+    uint32_t m = a.largest(threadIdx.x, 1024);
     if ((threadIdx.x & 31) == 0) most[threadIdx.x >> 5] = m;
     __syncthreads();
     m = __reduce_max_sync(0xffffffffu, most[threadIdx.x & 31]);
-    const float most_of_all = __uint_as_float(m);
-    if (blockIdx.x == 0 && threadIdx.x == 0) *a.back = m ? most_of_all * 0x1p-14f : 1.f;
-    for (int i = blockIdx.x * 1024 + threadIdx.x; i < a.rows; i += gridDim.x * 1024) {
-        const float2 s = a.stats[i];
-        const int64_t t = a.targets[i];
-        RowOf r = {s.x, s.y / kLog2, m ? gradient(i) / most_of_all * 0x1p14f : gradient(i), t < 0 || t >= a.vocab ? -1 : (int32_t)t};
-        if (t >= a.vocab) r.g = NAN;
-        if (s.x == -INFINITY) r = {0.f, INFINITY, 0.f, -1};  // nothing to choose from
-        a.of[i] = r;
-    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.back = a.unit(m);
+    for (int i = blockIdx.x * 1024 + threadIdx.x; i < a.rows; i += gridDim.x * 1024) of[i] = a.row(i, m);
 }
 
 // --- host ----------------------------------------------------------------------
@@ -243,6 +259,7 @@ struct Caller : Products {
     static constexpr int64_t kPartBytes = 64 << 20;
     // ... P for as many as 512 MB do, 4,096 at least.
     static constexpr int64_t kProbBytes = 512 << 20;
+    static constexpr int64_t kFewRows = 1024;
 
     static Matrix rows_of(const Matrix& m, int64_t from, int64_t n) { return {m.p + from * m.stride, m.stride, n, m.cols}; }
 
@@ -281,12 +298,11 @@ struct Caller : Products {
         if (!g.d_dx && !g.d_dweight) return;
         Matrix x = matrix_of(g.d_x, g.x_stride, g.n, g.k), w = matrix_of(g.d_weight, g.weight_stride, g.vocab, g.k);
         align(x, w);
-        RowOf* of = static_cast<RowOf*>(arena.take(g.n * sizeof(RowOf)));
+        const bool few = g.n <= kFewRows;
+        RowOf* of = few ? nullptr : static_cast<RowOf*>(arena.take(g.n * sizeof(RowOf)));
         float* back = static_cast<float*>(arena.take(4));
-        if (run) {
-            const Prepare q = {g.d_dloss, reinterpret_cast<const float2*>(g.d_stats), g.d_targets, of, back, g.scale, (int32_t)g.n, (int32_t)g.vocab};
-            launch_kernel(true, k_xent_rows, dim3((unsigned)std::min<int64_t>((g.n + 1023) / 1024, sms)), dim3(1024), 0, st, q);
-        }
+        const Rows from = {g.d_dloss, reinterpret_cast<const float2*>(g.d_stats), g.d_targets, back, g.scale, (int32_t)g.n, (int32_t)g.vocab};
+        if (run && !few) launch_kernel(true, k_xent_rows, dim3((unsigned)std::min<int64_t>((g.n + 1023) / 1024, sms)), dim3(1024), 0, st, from, of);
         // Pieces of equal width, whole tiles of 256 columns.
         const int64_t most = std::max<int64_t>(4096, kProbBytes / (2 * g.n) / 256 * 256), pieces = (g.vocab + most - 1) / most;
         const int64_t piece = pieces == 1 ? g.vocab : round_up((g.vocab + pieces - 1) / pieces, 256);
@@ -303,7 +319,7 @@ struct Caller : Products {
             const int64_t cols = std::min(piece, g.vocab - v);
             int64_t mark = arena.used;
             const Matrix wv = rows_of(w, v, cols), p = {probs, stride, g.n, cols};
-            Probs s = {of, g.scale * 1.4426950408889634f, (int32_t)g.n, (int32_t)v, 0};
+            Probs s = {of, from, g.scale * 1.4426950408889634f, (int32_t)g.n, (int32_t)v, 0};
             Epilogue e = {};
             e.out = probs; e.out_stride = stride;
             product<Probs, false, false>(x, wv, g.n, cols, g.k, e, false, s);
