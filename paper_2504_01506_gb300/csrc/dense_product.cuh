@@ -457,7 +457,8 @@ __device__ __forceinline__ bool put_blocks(const Product& p, const CUtensorMap* 
     return true;
 }
 
-// Kinds of products.
+// Kinds of products: the linear layer's; two products summed in the accumulator; two products of one operand; the gated
+// block's (two weights' rows a tile); the cross entropy's statistics, and its gradients of the logits.
 constexpr int kPlain = 0, kTwo = 1, kTwin = 2, kGated = 3, kStats = 4, kProbs = 5;
 
 // The shared memory of a block: the ring of operand tiles, and a corner and 32
