@@ -17,7 +17,7 @@
 //
 // Bound by the matrix unit, under the power cap, where rows are many: 8,192 x 2,048 over 131,072 bf16, forward and
 // backward 10.6 ms, 1.66 PFLOP/s (two pieces forward, 1,120 us each, 1.97 PFLOP/s by itself; four backward, of 582 for P, 597 for
-// dx and 580 for dW).  By the weight's bytes where they are few: one row by 131,072 x 2,048 87 us, 6.2 TB/s.  By whole tiles and L2 between: 2,051
+// dx and 580 for dW).  By the weight's bytes where they are few: one row by 131,072 x 2,048 85 us, 6.3 TB/s.  By whole tiles and L2 between: 2,051
 // x 777 over 50,001 615 us, where 2,048 x 768 over 50,176 takes 407; copies of the weight, whose rows are off 16 bytes, are 54 of it.
 #include "dense_product.cuh"
 
@@ -211,9 +211,15 @@ __global__ void __launch_bounds__(256) k_xent_join(Join a) {
     __shared__ float2 of[256];
     const int per = 256 >> a.log_threads, row = blockIdx.x * per + threadIdx.x % per, share = threadIdx.x / per;
     float2 s = make_float2(-INFINITY, 0.f);
+    const int step_of = 1 << a.log_threads;
     if (row < a.rows)
-#pragma unroll 4
-        for (int q = share; q < a.parts; q += 1 << a.log_threads) s = joined(s, a.part[(int64_t)q * a.rows + row], a.rate);
+        for (int q = share; q < a.parts; q += 4 * step_of) {  // four at a time, whose exponentials do not wait for one another
+            float2 v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                v[k] = q + k * step_of < a.parts ? a.part[(int64_t)(q + k * step_of) * a.rows + row] : make_float2(-INFINITY, 0.f);
+            s = joined(s, joined(joined(v[0], v[1], a.rate), joined(v[2], v[3], a.rate), a.rate), a.rate);
+        }
     of[threadIdx.x] = s;
     for (int step = 1 << a.log_threads >> 1; step; step >>= 1) {
         __syncthreads();
